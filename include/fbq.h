@@ -321,6 +321,118 @@ fbq_status fbq_train_step(const fbq_desc *d, const void *W, const void *H16, flo
                           void *Bt16_out, float *grad_At, float *grad_Bt, float *loss, void *workspace,
                           size_t workspace_bytes, fbq_stream stream);
 
+/*
+ * Key/value cache and attention: what a decoder needs between the linears of q, k, v and o.
+ *
+ * The cache is a pool of pages; a row of the table lists the pages of one sequence.  Everything a step reads or changes lies on the device, so that a captured
+ * graph of a decode step keeps working while sequences grow, come and go.
+ *   pool     [layers][pages][2 (K, V)][kv_heads][page_size][head_dim], fp16 or bf16: a page of one layer is one contiguous piece, and so are the keys, or
+ *            the values, of one head in it
+ *   table    [rows][max_pages] page numbers, -1 where a row has no page;  token j of row b lies in page table[b][j / page_size], place j % page_size
+ *   lengths  [rows] tokens a row holds;  0 and no pages: an empty row
+ *   refs     [pages] rows that hold a page; 0: free
+ * A page that several rows hold is full: fork copies a partial last page, so nothing is ever appended to a page that two rows hold.
+ *
+ * The kernels bound whatever they read from these arrays: a page number outside the pool is not followed (append writes nothing there; attention reads
+ * zeros there), a length counts as at most max_pages * page_size and at least 0, row numbers outside the table are skipped.
+ */
+enum { FBQ_F16 = 0, FBQ_BF16 = 1 };
+
+typedef struct {
+    int32_t layers;     /* 1..4096 */
+    int32_t pages;      /* 1..2^22 */
+    int32_t page_size;  /* tokens: 16, 32, 64, 128 or 256 */
+    int32_t kv_heads;   /* 1..1024 */
+    int32_t head_dim;   /* 16..256, multiple of 8 */
+    int32_t type;       /* FBQ_F16 or FBQ_BF16 */
+} fbq_cache_desc;
+
+typedef struct {
+    fbq_cache_desc desc;
+    int32_t rows;       /* 1..65536 */
+    int32_t max_pages;  /* entries a row of the table has; max_pages * page_size <= 2^24, and (rows + 1) * kv_heads * (max_pages * page_size / 32 + 1) < 2^30 */
+    void *pool;         /* device, 16-byte aligned like the other tensors of this header */
+    int32_t *table;     /* device, these three 4-byte aligned (so that a part of the rows can be passed as a cache) */
+    int32_t *lengths;
+    int32_t *refs;
+} fbq_cache;
+
+/* Validates a descriptor: FBQ_OK, FBQ_ERR_NULL, FBQ_ERR_SHAPE (out of the ranges above), FBQ_ERR_UNSUPPORTED (page_size or type not listed). */
+fbq_status fbq_check_cache(const fbq_cache_desc *d);
+
+/* Bytes of the pool, 0 for an invalid descriptor; of the device scratch that fbq_cache_fork of n pairs and fbq_cache_compact (n = 0) need. */
+size_t fbq_cache_bytes(const fbq_cache_desc *d);
+size_t fbq_cache_workspace_bytes(const fbq_cache_desc *d, int n);
+
+/*
+ * fbq_cache_reserve - pages for count[b] more tokens of each row b (device [rows], negative counts as 0).  Free pages are given lowest number first, in the order of
+ * the rows.  start[b] (device [rows]) = the length before, lengths[b] += count[b]; a row for which pages do not suffice - its own and all before it in this call taken
+ * together - or whose table row is too short gets nothing, keeps its length, and start[b] = -1.
+ *   info device, one int32 or NULL: how many pages were lacking (0: none)
+ */
+fbq_status fbq_cache_reserve(const fbq_cache *c, const int32_t *count, int32_t *start, int32_t *info, fbq_stream stream);
+
+/*
+ * fbq_cache_append - writes new keys and values of one layer into their pages: token i of row b goes to position start[b] + i; nothing where start[b] < 0.
+ *   T tokens; q_start device [rows + 1]: row b's are q_start[b] .. q_start[b + 1] - 1, in ascending order; NULL: T == rows, one token a row
+ *   k, v device [T][kv_heads][head_dim], rows k_stride and v_stride elements apart (multiples of 8, at least kv_heads * head_dim)
+ */
+fbq_status fbq_cache_append(const fbq_cache *c, int layer, int T, const int32_t *q_start, const int32_t *start, const void *k, int64_t k_stride,
+                            const void *v, int64_t v_stride, fbq_stream stream);
+
+/* fbq_cache_free - empties n rows (device int32 list, each at most once): their pages' refs go down by one, their table entries to -1, their lengths to 0. */
+fbq_status fbq_cache_free(const fbq_cache *c, int n, const int32_t *rows, fbq_stream stream);
+
+/*
+ * fbq_cache_fork - n pairs: row child[i] (empty before the call, at most once in the list) becomes a second holder of what row parent[i] holds.  Full pages are shared;
+ * a partial last page is copied, in all layers, to a free page (lowest first, in the order of the pairs).  A pair is skipped, and its child stays empty, when the
+ * pages do not suffice, a row number is outside the table, or the child is not empty.
+ *   info device, two int32 or NULL: pages lacking, pairs skipped;  workspace device, fbq_cache_workspace_bytes(&c->desc, n)
+ */
+fbq_status fbq_cache_fork(const fbq_cache *c, int n, const int32_t *parent, const int32_t *child, int32_t *info, void *workspace, size_t workspace_bytes,
+                          fbq_stream stream);
+
+/* fbq_cache_copy - n pairs: page dst[i] = page src[i], in all layers.  No page that one pair writes may appear in another; a pair with a number outside the pool is skipped. */
+fbq_status fbq_cache_copy(const fbq_cache *c, int n, const int32_t *src, const int32_t *dst, fbq_stream stream);
+
+/*
+ * fbq_cache_compact - moves the pages that are in use to the low end of the pool, in all layers: with n of them, those numbered n and up go, in ascending
+ * order, to the free ones below n.  table_out [rows][max_pages] and refs_out [pages] are c->table and c->refs after the move; they may be c's own (in place).
+ * Pages are only written where they were free: with tensors of their own the old table stays valid until pages are given out again.
+ *   info device, two int32 or NULL: n, pages moved;  workspace device, fbq_cache_workspace_bytes(&c->desc, 0)
+ */
+fbq_status fbq_cache_compact(const fbq_cache *c, int32_t *table_out, int32_t *refs_out, int32_t *info, void *workspace, size_t workspace_bytes, fbq_stream stream);
+
+/*
+ * fbq_attention - for query token i of the n_b that row b has in this call, head h, with the row's L = lengths[b] tokens (the new ones among them, appended before):
+ *     out = sum_j p_j v_j / sum_j p_j,   p_j = exp(scale q . k_j),   over the tokens j < L - n_b + i + 1     (causal; k, v of head h / (heads / kv_heads))
+ * and lse = ln sum_j p_j.  A query token that sees nothing gets 0 and -infinity.  Sums, maxima and exponentials are in fp32; p_j is rounded to the cache's type
+ * as an operand of the matrix cores, out once at the end.
+ *   T query tokens in all; q_start device [rows + 1], ascending: row b's are q_start[b] .. q_start[b + 1] - 1; NULL: T == rows, one a row.  max_q: at least the most that a
+ *            row has (1 with NULL; a row's tokens past it are left alone, and so are tokens past q_start[rows])
+ *   q, out   device [T][heads][head_dim] of the cache's type, rows q_stride and out_stride elements apart (multiples of 8, at least heads * head_dim)
+ *   lse      device [T][heads] fp32, or NULL
+ *   shared   device list of n_shared pages, or NULL and 0: the first n_shared entries of EVERY row's table are these.  They are read once for all rows together
+ *            where few query tokens come with each row; the result is that of the call without, other last bits aside.
+ *   workspace fbq_attention_workspace_bytes() of the same call (pointers are not looked at); contents do not matter.  Calls that may run concurrently must not share one.
+ */
+typedef struct {
+    fbq_cache cache;    /* refs is not used */
+    int32_t layer, heads, T, max_q;
+    const int32_t *q_start;
+    const void *q;
+    int64_t q_stride;
+    void *out;
+    int64_t out_stride;
+    float *lse;
+    const int32_t *shared;
+    int32_t n_shared;
+    float scale;
+} fbq_attention_call;
+
+size_t fbq_attention_workspace_bytes(const fbq_attention_call *a);
+fbq_status fbq_attention(const fbq_attention_call *a, void *workspace, size_t workspace_bytes, fbq_stream stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,225 @@
+"""Binding of the key/value cache and the attention over it (include/fbq.h): argument marshalling only.
+
+A `Cache` is a pool of pages and, on the device like it, the table that says which pages hold which row's tokens:
+
+    pool    [layers, pages, 2 (K, V), kv_heads, page_size, head_dim]   fp16 or bf16
+    table   [rows, max_pages] int32, -1: none        lengths [rows] int32        refs [pages] int32
+
+`cache_reserve` gives rows pages for new tokens, `cache_append` writes a layer's keys and values there, `attention` reads them; `cache_fork`, `cache_free`,
+`cache_copy` and `cache_compact` move whole sequences and pages about.  Nothing here waits for the device or asks it anything, so all of it can be captured
+in a graph; what could not be served stands in the `info` tensors.
+"""
+from __future__ import annotations
+
+import ctypes
+from dataclasses import dataclass, field
+from typing import Optional
+
+from . import fbq
+from .fbq import FbqError, _check, _dev_ptr, _stream  # noqa: F401
+
+
+class _CCacheDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("layers", "pages", "page_size", "kv_heads", "head_dim", "type")]
+
+
+class _CCache(ctypes.Structure):
+    _fields_ = [("desc", _CCacheDesc), ("rows", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("pool", ctypes.c_void_p), ("table", ctypes.c_void_p),
+                ("lengths", ctypes.c_void_p), ("refs", ctypes.c_void_p)]
+
+
+class _CAttentionCall(ctypes.Structure):
+    _fields_ = [("cache", _CCache), ("layer", ctypes.c_int32), ("heads", ctypes.c_int32), ("T", ctypes.c_int32), ("max_q", ctypes.c_int32),
+                ("q_start", ctypes.c_void_p), ("q", ctypes.c_void_p), ("q_stride", ctypes.c_int64), ("out", ctypes.c_void_p), ("out_stride", ctypes.c_int64),
+                ("lse", ctypes.c_void_p), ("shared", ctypes.c_void_p), ("n_shared", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+def declare(lib) -> None:
+    """Argument types of the entry points (called once, when the library is loaded)."""
+    vp, sz, i32, i64 = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int, ctypes.c_int64
+    dp, cp, ap = ctypes.POINTER(_CCacheDesc), ctypes.POINTER(_CCache), ctypes.POINTER(_CAttentionCall)
+    for name, res, args in (("fbq_check_cache", i32, [dp]), ("fbq_cache_bytes", sz, [dp]), ("fbq_cache_workspace_bytes", sz, [dp, i32]),
+                            ("fbq_cache_reserve", i32, [cp, vp, vp, vp, vp]), ("fbq_cache_append", i32, [cp, i32, i32, vp, vp, vp, i64, vp, i64, vp]),
+                            ("fbq_cache_free", i32, [cp, i32, vp, vp]), ("fbq_cache_fork", i32, [cp, i32, vp, vp, vp, vp, sz, vp]),
+                            ("fbq_cache_copy", i32, [cp, i32, vp, vp, vp]), ("fbq_cache_compact", i32, [cp, vp, vp, vp, vp, sz, vp]),
+                            ("fbq_attention_workspace_bytes", sz, [ap]), ("fbq_attention", i32, [ap, vp, sz, vp])):
+        f = getattr(lib, name)
+        f.restype, f.argtypes = res, args
+
+
+def _types():
+    import torch
+    return {torch.float16: 0, torch.bfloat16: 1}
+
+
+def _ints(t, what: str, n: Optional[int] = None):
+    """Pointer of a device int32 tensor (None: NULL)."""
+    if t is None:
+        return None
+    import torch
+    if t.dtype != torch.int32 or (n is not None and t.numel() != n):
+        raise ValueError(f"{what}: expected int32" + ("" if n is None else f", {n} of them"))
+    return _dev_ptr(t)
+
+
+@dataclass
+class Cache:
+    """A cache made of tensors that the caller keeps (see `cache_create`); `rows(a, b)` is the same cache with rows a .. b - 1 alone."""
+    pool: "object"
+    table: "object"
+    lengths: "object"
+    refs: "object"
+    _c: "object" = field(init=False, repr=False, compare=False)
+
+    def __post_init__(self):
+        types = _types()
+        if self.pool.dim() != 6 or self.pool.shape[2] != 2 or self.pool.dtype not in types:
+            raise ValueError("pool: expected [layers, pages, 2, kv_heads, page_size, head_dim], float16 or bfloat16")
+        if self.table.dim() != 2:
+            raise ValueError("table: expected [rows, max_pages]")
+        layers, pages, _, kv_heads, page, dim = self.pool.shape
+        rows, width = self.table.shape
+        d = _CCacheDesc(layers, pages, page, kv_heads, dim, types[self.pool.dtype])
+        self._c = _CCache(d, rows, width, _dev_ptr(self.pool), _ints(self.table, "table"), _ints(self.lengths, "lengths", rows), _ints(self.refs, "refs", pages))
+        _check(int(fbq.load().fbq_check_cache(ctypes.byref(d))), "Cache")
+
+    @property
+    def heads(self) -> int:
+        return int(self.pool.shape[3])
+
+    @property
+    def head_dim(self) -> int:
+        return int(self.pool.shape[5])
+
+    @property
+    def page_size(self) -> int:
+        return int(self.pool.shape[4])
+
+    def rows(self, first: int, end: int) -> "Cache":
+        return Cache(self.pool, self.table[first:end], self.lengths[first:end], self.refs)
+
+
+def cache_create(layers: int, pages: int, page_size: int, kv_heads: int, head_dim: int, rows: int, max_pages: int, dtype=None, device="cuda") -> Cache:
+    """An empty cache: `rows` sequences of up to max_pages * page_size tokens, out of `pages` pages in all.  dtype: torch.float16 (default) or torch.bfloat16."""
+    import torch
+    i32 = lambda v, *shape: torch.full(shape, v, dtype=torch.int32, device=device)
+    pool = torch.empty((layers, pages, 2, kv_heads, page_size, head_dim), dtype=dtype or torch.float16, device=device)
+    return Cache(pool, i32(-1, rows, max_pages), i32(0, rows), i32(0, pages))
+
+
+def cache_reserve(cache: Cache, count, start=None, info=None, stream=None):
+    """fbq_cache_reserve: pages for count[b] more tokens of each row -> start [rows], where they begin (-1: no pages left for this row)."""
+    if start is None:
+        import torch
+        start = torch.empty_like(cache.lengths)
+    rows = cache._c.rows
+    _check(fbq.load().fbq_cache_reserve(ctypes.byref(cache._c), _ints(count, "count", rows), _ints(start, "start", rows), _ints(info, "info"), _stream(stream)),
+           "fbq_cache_reserve")
+    return start
+
+
+def _tokens(cache: Cache, t, what: str, heads: Optional[int] = None):
+    """(pointer, elements between rows, tokens) of a [T, heads, head_dim] tensor of the cache's type whose rows may lie further apart."""
+    if t.dim() != 3 or t.dtype != cache.pool.dtype or t.shape[2] != cache.head_dim or (heads is not None and t.shape[1] != heads):
+        raise ValueError(f"{what}: expected [T, heads, head_dim] of the cache's type")
+    if t.stride(2) != 1 or t.stride(1) != t.shape[2]:
+        raise ValueError(f"{what}: a token's heads have to lie in one piece")
+    if not t.is_cuda:
+        raise ValueError("expected a device tensor")
+    T = int(t.shape[0])
+    return t.data_ptr(), (t.stride(0) if T > 1 else t.shape[1] * t.shape[2]), T
+
+
+def cache_append(cache: Cache, layer: int, k, v, start, q_start=None, stream=None) -> None:
+    """fbq_cache_append: k, v [T, kv_heads, head_dim] of one layer into the pages of their rows, from position start[b] on (see cache_reserve).
+    q_start [rows + 1]: the rows' tokens in k and v; None: one token a row."""
+    kp, ks, T = _tokens(cache, k, "k", cache.heads)
+    vp, vs, Tv = _tokens(cache, v, "v", cache.heads)
+    if T != Tv:
+        raise ValueError("k and v: as many tokens")
+    rows = cache._c.rows
+    _check(fbq.load().fbq_cache_append(ctypes.byref(cache._c), int(layer), T, _ints(q_start, "q_start", rows + 1), _ints(start, "start", rows), kp, ks, vp, vs,
+                                       _stream(stream)), "fbq_cache_append")
+
+
+def cache_free(cache: Cache, rows, stream=None) -> None:
+    """fbq_cache_free: empties the rows of an int32 list."""
+    _check(fbq.load().fbq_cache_free(ctypes.byref(cache._c), rows.numel(), _ints(rows, "rows"), _stream(stream)), "fbq_cache_free")
+
+
+def _room(cache: Cache, n: int):
+    import torch
+    return torch.empty(fbq.load().fbq_cache_workspace_bytes(ctypes.byref(cache._c.desc), n), dtype=torch.uint8, device=cache.pool.device)
+
+
+def _size(workspace) -> int:
+    return 0 if workspace is None else workspace.numel() * workspace.element_size()
+
+
+def cache_fork(cache: Cache, parent, child, info=None, workspace=None, stream=None) -> None:
+    """fbq_cache_fork: row child[i] becomes a second holder of what row parent[i] holds.  info: int32 [2], pages lacking and pairs skipped."""
+    n = parent.numel()
+    if workspace is None:
+        workspace = _room(cache, n)
+    _check(fbq.load().fbq_cache_fork(ctypes.byref(cache._c), n, _ints(parent, "parent"), _ints(child, "child", n), _ints(info, "info"), _dev_ptr(workspace),
+                                     _size(workspace), _stream(stream)), "fbq_cache_fork")
+
+
+def cache_copy(cache: Cache, src, dst, stream=None) -> None:
+    """fbq_cache_copy: page dst[i] = page src[i] in all layers (int32 lists)."""
+    n = src.numel()
+    _check(fbq.load().fbq_cache_copy(ctypes.byref(cache._c), n, _ints(src, "src"), _ints(dst, "dst", n), _stream(stream)), "fbq_cache_copy")
+
+
+def cache_compact(cache: Cache, out: Optional[Cache] = None, info=None, workspace=None, stream=None) -> Cache:
+    """fbq_cache_compact: live pages to the low end of the pool.  out: a Cache of the same pool whose table and refs take the new ones (None: in place).
+    info: int32 [2], pages in use and pages moved."""
+    out = cache if out is None else out
+    if out.table.shape != cache.table.shape or out.refs.shape != cache.refs.shape:
+        raise ValueError("out: a cache of the same shape")
+    if workspace is None:
+        workspace = _room(cache, 0)
+    _check(fbq.load().fbq_cache_compact(ctypes.byref(cache._c), out._c.table, out._c.refs, _ints(info, "info"), _dev_ptr(workspace), _size(workspace),
+                                        _stream(stream)), "fbq_cache_compact")
+    return out
+
+
+def _call(cache: Cache, layer: int, q, q_start, max_q: int, shared, scale, out, lse) -> _CAttentionCall:
+    qp, qs, T = _tokens(cache, q, "q")
+    heads = int(q.shape[1])
+    op, os_ = (None, heads * cache.head_dim) if out is None else _tokens(cache, out, "out", heads)[:2]
+    if out is not None and out.shape[0] != T:
+        raise ValueError("out: expected q's shape")
+    if lse is not None:
+        import torch
+        if lse.dtype != torch.float32 or tuple(lse.shape) != (T, heads):
+            raise ValueError("lse: expected float32 [T, heads]")
+    return _CAttentionCall(cache._c, int(layer), heads, T, int(max_q), _ints(q_start, "q_start", cache._c.rows + 1), qp, qs, op, os_, _dev_ptr(lse),
+                           _ints(shared, "shared"), 0 if shared is None else shared.numel(), cache.head_dim ** -0.5 if scale is None else float(scale))
+
+
+def attention_workspace(cache: Cache, q, q_start=None, max_q: int = 1, shared=None):
+    """A workspace for attention() calls with queries, rows and shared pages like these.  A T that differs, max_q and the number of shared pages change its size."""
+    import torch
+    if q_start is None and max_q > 1:                         # (only its presence counts)
+        q_start = torch.empty(cache._c.rows + 1, dtype=torch.int32, device=q.device)
+    c = _call(cache, 0, q, q_start, max_q, shared, None, None, None)
+    return torch.empty(max(16, fbq.load().fbq_attention_workspace_bytes(ctypes.byref(c))), dtype=torch.uint8, device=q.device)
+
+
+def attention(cache: Cache, layer: int, q, q_start=None, max_q: int = 1, shared=None, scale=None, out=None, lse=None, workspace=None, stream=None):
+    """fbq_attention: q [T, heads, head_dim], the newest tokens of the rows, over all the rows hold, causal -> out [T, heads, head_dim].
+
+    q_start [rows + 1]: the rows' tokens in q, at most max_q a row; None: one token a row.  shared: the pages that all rows' tables begin with, read once
+    for all rows.  scale: head_dim ** -0.5 by default.  lse: float32 [T, heads], takes the logarithm of the softmax's sums.
+    """
+    if out is None or workspace is None:
+        import torch
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    c = _call(cache, layer, q, q_start, max_q, shared, scale, out, lse)
+    lib = fbq.load()
+    if workspace is None:
+        workspace = torch.empty(max(16, lib.fbq_attention_workspace_bytes(ctypes.byref(c))), dtype=torch.uint8, device=q.device)
+    _check(lib.fbq_attention(ctypes.byref(c), _dev_ptr(workspace), _size(workspace), _stream(stream)), "fbq_attention")
+    return out

@@ -1,0 +1,118 @@
+// Attention over the paged cache: what its kernels share (device code, launch arguments).
+//
+// Two kernels read keys and values.  fbq_attend_few.hip: up to 16 query rows of one key/value head (query tokens times the heads that share it) against its
+// tokens, registers only.  fbq_attend_many.hip: 128 rows a block, key and value tiles in LDS.  Both can leave partial results - sum of p v, its maximum
+// exponent, sum of p - for fbq_attend_join_kernel (fbq_attention.hip), which adds them up in a fixed order.
+#ifndef FBQ_ATTEND_H
+#define FBQ_ATTEND_H
+
+#include "fbq_cache.h"
+#include "fbq_internal.h"
+
+namespace fbq {
+
+typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
+typedef __bf16 bfloat8_t __attribute__((ext_vector_type(8)));
+typedef float float4_t __attribute__((ext_vector_type(4)));
+typedef float float16_t __attribute__((ext_vector_type(16)));
+typedef uint32_t word2_t __attribute__((ext_vector_type(2)));
+typedef uint32_t word4_t __attribute__((ext_vector_type(4)));
+
+constexpr int kFewRows = 16;             // query rows of the few-row kernel
+constexpr int kFewTile = 32;             // its keys a step of a wave
+constexpr int kFewWaves = 4;             // waves a block; each works alone
+constexpr int kManyRows = 128;           // query rows of a block of the many-row kernel
+constexpr int kManyTile = 64;            // keys a step
+constexpr float kNoScore = -3.0e38f;     // running maximum before any score (finite, so that differences with it are)
+
+// A set of partial results: o [n][D], {maximum, sum} [n]; the maximum is an exponent of two.
+struct Partials {
+    float *o;
+    float2 *ml;
+};
+
+struct AttendArgs {
+    const unsigned char *kv;             // the layer's pages
+    const int32_t *table, *lengths, *q_start, *shared;
+    const uint16_t *q;
+    uint16_t *out;
+    float *lse;
+    long page_bytes, q_stride, out_stride;
+    int pages, log_ps, max_pages, rows, kv_heads, group, D, T, max_q, heads;
+    int n_shared;                        // tokens read through `shared` for all rows together; a row's own tokens start there
+    float scale;                         // times log2 e: scores are exponents of two
+    // few-row kernel: `workers` waves; the partial results of pieces of items, two a worker ([workers][2][slot_rows]); those of whole items where something else
+    // has to be added ([T heads]), null: out is written
+    int workers, slot_rows;
+    bool shared_here;                    // the shared tokens are items of this kernel's own, for the rows of all sequences together
+    Partials piece, whole, whole_shared;
+    // many-row kernel: `splits` of the keys, partial results [splits][T heads] (null: out is written)
+    int splits, shared_splits;
+    Partials part, part_shared;
+};
+
+// The two types: operands of the matrix cores, and two floats rounded to a word of them (to nearest, ties to even).
+struct TypeF16 {
+    typedef half8_t operand;
+    static __device__ __forceinline__ float4_t mfma(word4_t a, word4_t b, float4_t c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8_t, a), __builtin_bit_cast(half8_t, b), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ float16_t mfma(word4_t a, word4_t b, float16_t c)
+    {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8_t, a), __builtin_bit_cast(half8_t, b), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ uint32_t pack(float x, float y)
+    {
+        typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
+        return __builtin_bit_cast(uint32_t, half2_t{(_Float16)x, (_Float16)y});
+    }
+    static __device__ __forceinline__ uint16_t one(float x) { return __builtin_bit_cast(uint16_t, (_Float16)x); }
+};
+struct TypeBf16 {
+    typedef bfloat8_t operand;
+    static __device__ __forceinline__ float4_t mfma(word4_t a, word4_t b, float4_t c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bfloat8_t, a), __builtin_bit_cast(bfloat8_t, b), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ float16_t mfma(word4_t a, word4_t b, float16_t c)
+    {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bfloat8_t, a), __builtin_bit_cast(bfloat8_t, b), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ uint32_t pack(float x, float y)
+    {
+        typedef __bf16 bf2_t __attribute__((ext_vector_type(2)));
+        return __builtin_bit_cast(uint32_t, bf2_t{(__bf16)x, (__bf16)y});
+    }
+    static __device__ __forceinline__ uint16_t one(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
+};
+
+// Query tokens of a row: the first one and how many (whatever q_start holds, inside [0, T) and at most max_q).
+__device__ __forceinline__ int2 queries_of(const AttendArgs &a, int b)
+{
+    if (!a.q_start) return make_int2(b, 1);
+    const int q0 = min(max(a.q_start[b], 0), a.T), q1 = min(max(a.q_start[b + 1], q0), a.T);
+    return make_int2(q0, min(q1 - q0, a.max_q));
+}
+
+__device__ __forceinline__ int row_tokens(const AttendArgs &a, int b) { return tokens_of(a.lengths[b], a.max_pages << a.log_ps); }
+
+// Steps of a row's own tokens in the few-row kernel; none if it has no query tokens.
+__device__ __forceinline__ int few_steps(const AttendArgs &a, int b)
+{
+    const int steps = (max(row_tokens(a, b) - a.n_shared, 0) + kFewTile - 1) / kFewTile;
+    return a.q_start && queries_of(a, b).y == 0 ? 0 : steps;
+}
+
+// How many steps each worker takes, from all there are: the last ones may have none.
+__device__ __forceinline__ int few_share(const AttendArgs &a, int steps) { return max(1, (steps + a.workers - 1) / a.workers); }
+
+// A value that is the same in all lanes, as one the compiler knows to be.
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
+hipError_t launch_attend_few(const AttendArgs &a, int type, hipStream_t stream);
+hipError_t launch_attend_many(const AttendArgs &a, int type, bool shared, hipStream_t stream);   // shared: the shared tokens for all rows, else the rows' own
+
+}  // namespace fbq
+
+#endif

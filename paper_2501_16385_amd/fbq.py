@@ -22,7 +22,9 @@ _linear_address = 0
 EXPORTED_SYMBOLS = ["fbq_status_string", "fbq_check_desc", "fbq_packed_bytes", "fbq_workspace_bytes", "fbq_pack",
                     "fbq_linear", "fbq_linear_static", "fbq_linear_unfused", "fbq_linear_group", "fbq_linear_group_mix", "fbq_silu_mul", "fbq_reconstruct", "fbq_unpack_codes", "fbq_quantize_feedback",
                     "fbq_train_workspace_bytes", "fbq_gram", "fbq_train_step", "fbq_test_set_spin_limit",
-                    "fbq_measure_read_stream"]
+                    "fbq_measure_read_stream",
+                    "fbq_check_cache", "fbq_cache_bytes", "fbq_cache_workspace_bytes", "fbq_cache_reserve", "fbq_cache_append", "fbq_cache_free", "fbq_cache_fork",
+                    "fbq_cache_copy", "fbq_cache_compact", "fbq_attention_workspace_bytes", "fbq_attention"]
 
 
 class FbqError(RuntimeError):
@@ -116,6 +118,8 @@ def load() -> ctypes.CDLL:
         lib.fbq_gram.argtypes = [dp, i32, vp, f32, vp, vp, sz, vp]
         lib.fbq_train_step.restype = i32
         lib.fbq_train_step.argtypes = [dp, vp, vp, f32, vp, vp, f32] + [vp] * 9 + [sz, vp]
+        from . import cache
+        cache.declare(lib)
         global _call_linear, _linear_address
         _call_linear, _linear_address = _fbq_call.linear, ctypes.cast(lib.fbq_linear, vp).value
         _lib = lib
