@@ -24,6 +24,9 @@ constexpr int kFewWaves = 4;             // waves a block; each works alone
 constexpr int kManyRows = 128;           // query rows of a block of the many-row kernel
 constexpr int kManyTile = 64;            // keys a step
 constexpr float kNoScore = -3.0e38f;     // running maximum before any score (finite, so that differences with it are)
+// The maximum that exponents are relative to follows the scores' only when they pass it by this much: rescaling what was summed is then rare.  Probabilities reach
+// 2^8 instead of 1, far from what fp16 holds, and rounding is relative.
+constexpr float kSlack = 8.0f;
 
 // A set of partial results: o [n][D], {maximum, sum} [n]; the maximum is an exponent of two.
 struct Partials {
@@ -40,7 +43,8 @@ struct AttendArgs {
     long page_bytes, q_stride, out_stride;
     int pages, log_ps, max_pages, rows, kv_heads, group, D, T, max_q, heads;
     int n_shared;                        // tokens read through `shared` for all rows together; a row's own tokens start there
-    float scale;                         // times log2 e: scores are exponents of two
+    float scale;                         // > 0, times log2 e: scores are exponents of two.  The sign of the call's scale, and a scale of zero, are taken into the queries:
+    uint32_t q_and, q_xor;               // their words & q_and ^ q_xor
     // few-row kernel: `workers` waves; the partial results of pieces of items, two a worker ([workers][2][slot_rows]); those of whole items where something else
     // has to be added ([T heads]), null: out is written
     int workers, slot_rows;
@@ -109,6 +113,29 @@ __device__ __forceinline__ int few_share(const AttendArgs &a, int steps) { retur
 
 // A value that is the same in all lanes, as one the compiler knows to be.
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
+// The page list that a wave goes along: 64 entries a register, the next 64 under way.
+struct PageList {
+    const int32_t *list;
+    int count, base, ids, next;
+    __device__ __forceinline__ int load(int at) const { return list[min(at, count - 1)]; }
+    __device__ __forceinline__ void begin(const int32_t *l, int n, int first)
+    {
+        list = l; count = n; base = first;
+        const int lane = threadIdx.x & 63;
+        ids = load(base + lane);
+        next = load(base + 64 + lane);
+    }
+    __device__ __forceinline__ int at(int index)              // index: the same in all lanes, never going back, at most 64 further than the last
+    {
+        if (index - base >= 64) {
+            ids = next;
+            base += 64;
+            next = load(base + 64 + (threadIdx.x & 63));
+        }
+        return __builtin_amdgcn_readlane(ids, index - base);
+    }
+};
 
 hipError_t launch_attend_few(const AttendArgs &a, int type, hipStream_t stream);
 hipError_t launch_attend_many(const AttendArgs &a, int type, bool shared, hipStream_t stream);   // shared: the shared tokens for all rows, else the rows' own

@@ -19,29 +19,6 @@ namespace fbq {
 
 constexpr int kNowhere = 1 << 30;             // an offset behind every descriptor's end: loads answer zero
 
-// The page list of an item: 64 entries a register, the next 64 under way.
-struct PageList {
-    const int32_t *list;
-    int count, base, ids, next;
-    __device__ __forceinline__ int load(int at) const { return list[min(at, count - 1)]; }
-    __device__ __forceinline__ void begin(const int32_t *l, int n, int first)
-    {
-        list = l; count = n; base = first;
-        const int lane = threadIdx.x & 63;
-        ids = load(base + lane);
-        next = load(base + 64 + lane);
-    }
-    __device__ __forceinline__ int at(int index)              // index: the same in all lanes, never going back, at most 64 further than the last
-    {
-        if (index - base >= 64) {
-            ids = next;
-            base += 64;
-            next = load(base + 64 + (threadIdx.x & 63));
-        }
-        return __builtin_amdgcn_readlane(ids, index - base);
-    }
-};
-
 template <int DP>
 struct Step {
     static constexpr int kV = DP == 256 ? 2 : 1;              // 16-byte loads of a lane's features of one value row (DP 64: one of 8 bytes)
@@ -140,7 +117,7 @@ __global__ __launch_bounds__(64 * kFewWaves, DP == 256 ? 1 : 2) void fbq_attend_
         for (int s = 0; s < DP / 32; ++s) {
             const int d = 32 * s + 8 * grp;
             qf[s] = word4_t{0, 0, 0, 0};
-            if (t >= 0 && d < D) qf[s] = *reinterpret_cast<const word4_t *>(a.q + t * a.q_stride + head * D + d);
+            if (t >= 0 && d < D) qf[s] = (*reinterpret_cast<const word4_t *>(a.q + t * a.q_stride + head * D + d) & a.q_and) ^ a.q_xor;
         }
 
         const int key0 = (is_shared ? 0 : a.n_shared) + step * kFewTile;
@@ -182,7 +159,6 @@ __global__ __launch_bounds__(64 * kFewWaves, DP == 256 ? 1 : 2) void fbq_attend_
                 z[half] = float4_t{0, 0, 0, 0};
 #pragma unroll
                 for (int y = 0; y < DP / 32; ++y) z[half] = TY::mfma(x.k[half][y], qf[y], z[half]);
-                z[half] *= a.scale;
             }
             const int key = key0 + s * kFewTile;
             if (key + kFewTile > least) {
@@ -195,7 +171,8 @@ __global__ __launch_bounds__(64 * kFewWaves, DP == 256 ? 1 : 2) void fbq_attend_
             float top = fmaxf(fmaxf(fmaxf(z[0][0], z[0][1]), fmaxf(z[0][2], z[0][3])), fmaxf(fmaxf(z[1][0], z[1][1]), fmaxf(z[1][2], z[1][3])));
             top = fmaxf(top, __shfl_xor(top, 16));
             top = fmaxf(top, __shfl_xor(top, 32));
-            if (__ballot(top > m)) {
+            top *= a.scale;
+            if (__ballot(top > m + kSlack)) {
                 const float to = fmaxf(top, m), by = __builtin_amdgcn_exp2f(m - to);
                 l *= by;
 #pragma unroll
@@ -207,7 +184,7 @@ __global__ __launch_bounds__(64 * kFewWaves, DP == 256 ? 1 : 2) void fbq_attend_
             for (int half = 0; half < 2; ++half) {
 #pragma unroll
                 for (int y = 0; y < 4; ++y) {
-                    z[half][y] = __builtin_amdgcn_exp2f(z[half][y] - m);
+                    z[half][y] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[half][y], a.scale, -m));
                     l += z[half][y];
                 }
                 p[2 * half] = TY::pack(z[half][0], z[half][1]);

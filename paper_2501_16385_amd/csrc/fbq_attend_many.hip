@@ -26,12 +26,25 @@ __device__ __forceinline__ word2_t read_turned4(const unsigned char *at)
     return __builtin_bit_cast(word2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_four_t *)(__attribute__((address_space(3))) const void *)at));
 }
 
+// Tiles of a row's queries.
+__device__ __forceinline__ int tiles_of(const AttendArgs &a, int b) { return (queries_of(a, b).y * a.group + kManyRows - 1) / kManyRows; }
+
+// f(0), f(1) .. f(N - 1), each with its number as a constant
+template <int N, class F>
+__device__ __forceinline__ void each(F f)
+{
+    if constexpr (N > 0) {
+        each<N - 1>(f);
+        f(std::integral_constant<int, N - 1>());
+    }
+}
+
 template <class TY, int DP>
 __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void fbq_attend_many_kernel(const AttendArgs a, const bool shared)
 {
-    constexpr int kPieces = DP / 8, kRowBytes = DP * 2, kTileBytes = kManyTile * kRowBytes;
+    constexpr int kPieces = DP == 96 ? 16 : DP / 8, kRowBytes = kPieces * 16, kTileBytes = kManyTile * kRowBytes;   // (96: rows as long as 128's, so that they fold over the banks)
     constexpr int kRowsACopy = 64 / kPieces, kCopies = 16 / kRowsACopy;       // a wave copies 16 keys and 16 values a step
-    __shared__ __attribute__((aligned(1024))) unsigned char lds[2][2][kTileBytes];
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[2][2][kTileBytes];    // keys, values; two steps each
 
     const int lane = threadIdx.x & 63, col = lane & 31, grp = lane >> 5, wave = uniform(threadIdx.x >> 6);
     const int D = a.D, ps1 = (1 << a.log_ps) - 1;
@@ -47,20 +60,29 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void fbq_attend_many_kernel
             q0 = b;
             nq = 1;
         } else {
+            int all = 0;
+            for (int x = lane; x < a.rows; x += 64) all += tiles_of(a, x);
+#pragma unroll
+            for (int o = 32; o; o >>= 1) all += __shfl_xor(all, o);
+            all = uniform(all);
+            if (tile >= all) return;                          // the grid has a block for the most tiles there could be
+            // Blocks that are all on the GPU at once share CUs two by two, the first with the one half the grid on: the second half goes from short to long.
+            const int half = (all + 1) / 2;
+            if (tile >= half && (long)all * a.kv_heads * splits <= 512) tile = all - 1 - (tile - half);
             int before = 0, base = 0, mine, sum;
             while (true) {
-                mine = base + lane < a.rows ? (queries_of(a, base + lane).y * a.group + kManyRows - 1) / kManyRows : 0;
+                mine = base + lane < a.rows ? tiles_of(a, base + lane) : 0;
                 sum = mine;
 #pragma unroll
                 for (int o = 1; o < 64; o <<= 1) {
                     const int x = __shfl_up(sum, o);
                     if (lane >= o) sum += x;
                 }
-                const int all = uniform(__shfl(sum, 63));
-                if (tile < before + all) break;
-                before += all;
+                const int some = uniform(__shfl(sum, 63));
+                if (tile < before + some) break;
+                before += some;
                 base += 64;
-                if (base >= a.rows) return;                   // the grid has a block for the most tiles there could be
+                if (base >= a.rows) return;                   // (not unless q_start changes under the call)
             }
             const int at = __builtin_ctzll(__ballot(before + sum > tile));
             b = base + at;
@@ -109,7 +131,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void fbq_attend_many_kernel
     for (int s = 0; s < DP / 16; ++s) {
         const int d = 16 * s + 8 * grp;
         qf[s] = word4_t{0, 0, 0, 0};
-        if (t >= 0 && d < D) qf[s] = *reinterpret_cast<const word4_t *>(a.q + t * a.q_stride + head * D + d);
+        if (t >= 0 && d < D) qf[s] = (*reinterpret_cast<const word4_t *>(a.q + t * a.q_stride + head * D + d) & a.q_and) ^ a.q_xor;
     }
 
     // where this lane's pieces of a copy come from: rows 16 wave .. of a step
@@ -122,18 +144,17 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void fbq_attend_many_kernel
     }
     const int32_t *const list = shared ? a.shared : a.table + (long)b * a.max_pages;
     const int entries = shared ? a.n_shared >> a.log_ps : a.max_pages;
-    auto copy = [&](int step, int buf) __attribute__((always_inline)) {
+    // 16 keys, or values, a wave
+    PageList pages;
+    auto page_of = [&](int step) __attribute__((always_inline)) { return pages.at((key0 + step * kManyTile + 16 * wave) >> a.log_ps); };
+    auto copy = [&](int step, int page, bool values) __attribute__((always_inline)) {
         const int key = key0 + step * kManyTile + 16 * wave;
-        int valid = min(max(limit - key, 0), 16);
-        const int id = uniform(list[min(key >> a.log_ps, entries - 1)]);
-        if ((unsigned)id >= (unsigned)a.pages) valid = 0;
-        const unsigned char *const at = a.kv + (valid ? id : 0) * a.page_bytes + (((long)h << a.log_ps) + (key & ps1)) * D * 2;
-        const __amdgpu_buffer_rsrc_t kb = buffer_of(at, valid * D * 2), vb = buffer_of(at + (a.page_bytes >> 1), valid * D * 2);
-        const uint32_t to = lds_offset(&lds[buf][0][16 * wave * kRowBytes]);
+        const int valid = (unsigned)page < (unsigned)a.pages ? min(max(limit - key, 0), 16) : 0;
+        const unsigned char *const at = a.kv + (valid ? page : 0) * a.page_bytes + (values ? a.page_bytes >> 1 : 0) + (((long)h << a.log_ps) + (key & ps1)) * D * 2;
+        const __amdgpu_buffer_rsrc_t from = buffer_of(at, valid * D * 2);
+        const uint32_t to = lds_offset(&lds[values][step & 1][16 * wave * kRowBytes]);
 #pragma unroll
-        for (int c = 0; c < kCopies; ++c) copy16_to_lds(kb, k_off[c], 0, to + c * 1024);
-#pragma unroll
-        for (int c = 0; c < kCopies; ++c) copy16_to_lds(vb, v_off[c], 0, to + kTileBytes + c * 1024);
+        for (int c = 0; c < kCopies; ++c) copy16_to_lds(from, values ? v_off[c] : k_off[c], 0, to + c * 1024);
     };
 
     // reads: a key's piece s of DP / 16 pairs, and a value's column block dblk of 32
@@ -148,68 +169,114 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void fbq_attend_many_kernel
         for (int y = 0; y < 16; ++y) o[x][y] = 0;
     float m = kNoScore, l = 0;
 
-    if (s0 < s1) copy(s0, 0);
-    for (int s = s0; s < s1; ++s) {
-        const int buf = (s - s0) & 1;
-        if (s + 1 < s1) {
-            copy(s + 1, buf ^ 1);
-            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * kCopies) : "memory");
-        } else {
-            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    // A step is a row of slots with one matrix product each, first the next step's scores (kScores products, the two halves of its keys in turn), then this step's P V (kValues,
+    // 16 keys at a time).  Every slot asks LDS for the operand of the one kAhead slots on, and carries a share of the step's other work, which the compiler is kept from
+    // moving: exponentials of pair k of probabilities (in time for its product), and towards the end the maximum of the next step's scores.
+    constexpr int kScores = DP / 8, kValues = DP / 8, kAhead = 4, kLate = 12;
+    word4_t ring[kAhead];
+    auto fetch = [&](int i, int step) __attribute__((always_inline)) {        // operand of slot i of the step `step`
+        if (i < kScores) {
+            const int half = i & 1, x = i >> 1;
+            ring[i % kAhead] = *reinterpret_cast<const word4_t *>(lds[0][(step + 1) & 1] + k_at + ((k_piece ^ (2 * x)) << 4) + 32 * half * kRowBytes);
+        } else if (i < kScores + kValues) {
+            const int j = (i - kScores) / (DP / 32), d = (i - kScores) % (DP / 32);
+            const unsigned char *const at = lds[1][step & 1] + v_at + ((v_piece ^ (4 * d)) << 4) + 16 * j * kRowBytes;
+            const word2_t lo = read_turned4(at), hi = read_turned4(at + 8 * kRowBytes);
+            ring[i % kAhead] = word4_t{lo[0], lo[1], hi[0], hi[1]};
+        }
+    };
+    int page = 0;                                             // of the keys copied last
+    float top = -INFINITY;                                    // of this lane's scores of the step that is next
+    auto work = [&](float16_t (&z)[2], float16_t (&ahead)[2], int s) __attribute__((always_inline)) {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");   // what was asked for a step ago is there, what a step ago was read is free
+        if (s + 1 < s1) copy(s + 1, page, true);
+        if (s + 2 < s1) {
+            page = page_of(s + 2);
+            copy(s + 2, page, false);
         }
         const int key = key0 + s * kManyTile;
-        if (key < most) {
-            const unsigned char *const kt = lds[buf][0], *const vt = lds[buf][1];
-            float16_t z[2];
+        if (key >= most) return;
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-#pragma unroll
-                for (int y = 0; y < 16; ++y) z[half][y] = 0;
-#pragma unroll
-                for (int x = 0; x < DP / 16; ++x) {
-                    const word4_t kf = *reinterpret_cast<const word4_t *>(kt + k_at + ((k_piece ^ (2 * x)) << 4) + 32 * half * kRowBytes);
-                    z[half] = TY::mfma(kf, qf[x], z[half]);
-                }
-                z[half] *= a.scale;
-            }
-            if (key + kManyTile > least) {
-#pragma unroll
-                for (int half = 0; half < 2; ++half)
-#pragma unroll
-                    for (int y = 0; y < 16; ++y)
-                        if (key + 32 * half + 8 * (y >> 2) + 4 * grp + (y & 3) >= sees) z[half][y] = -INFINITY;
-            }
-            float top = fmaxf(z[0][0], z[1][0]);
-#pragma unroll
-            for (int y = 1; y < 16; ++y) top = fmaxf(top, fmaxf(z[0][y], z[1][y]));
-            top = fmaxf(top, __shfl_xor(top, 32));
-            if (__ballot(top > m)) {
-                const float to = fmaxf(top, m), by = __builtin_amdgcn_exp2f(m - to);
-                l *= by;
-#pragma unroll
-                for (int x = 0; x < DP / 32; ++x) o[x] *= by;
-                m = to;
-            }
+        for (int i = 0; i < kAhead; ++i) fetch(i, s);         // (past the last step: of whatever lies there, its scores are not used)
+        if (key + kManyTile > least) {
+            top = -INFINITY;
 #pragma unroll
             for (int half = 0; half < 2; ++half)
 #pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    word4_t p;
-#pragma unroll
-                    for (int y = 0; y < 4; ++y) {
-                        const float p0 = __builtin_amdgcn_exp2f(z[half][8 * x + 2 * y] - m), p1 = __builtin_amdgcn_exp2f(z[half][8 * x + 2 * y + 1] - m);
-                        l += p0 + p1;
-                        p[y] = TY::pack(p0, p1);
-                    }
-#pragma unroll
-                    for (int d = 0; d < DP / 32; ++d) {
-                        const unsigned char *const at = vt + v_at + ((v_piece ^ (4 * d)) << 4) + (32 * half + 16 * x) * kRowBytes;
-                        const word2_t lo = read_turned4(at), hi = read_turned4(at + 8 * kRowBytes);
-                        o[d] = TY::mfma(word4_t{lo[0], lo[1], hi[0], hi[1]}, p, o[d]);
-                    }
+                for (int y = 0; y < 16; ++y) {
+                    if (key + 32 * half + 8 * (y >> 2) + 4 * grp + (y & 3) >= sees) z[half][y] = -INFINITY;
+                    top = fmaxf(top, z[half][y]);
                 }
         }
-        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");       // all have read: the other buffer's successor may be copied over this one
+        const float high = fmaxf(top, __shfl_xor(top, 32)) * a.scale;
+        if (__ballot(high > m + kSlack)) {
+            const float to = fmaxf(high, m), by = __builtin_amdgcn_exp2f(m - to);
+            l *= by;
+#pragma unroll
+            for (int x = 0; x < DP / 32; ++x) o[x] *= by;
+            m = to;
+        }
+        word4_t p[4];
+        auto pair = [&](int k) __attribute__((always_inline)) {
+            const int half = k >> 3, y = 2 * (k & 7);
+            const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[half][y], a.scale, -m)), p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[half][y + 1], a.scale, -m));
+            l += p0 + p1;
+            p[k >> 2][k & 3] = TY::pack(p0, p1);
+        };
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int y = 0; y < 16; ++y) ahead[half][y] = 0;
+        each<kScores + kValues>([&](auto slot) __attribute__((always_inline)) {
+            constexpr int i = decltype(slot)::value;
+            __builtin_amdgcn_sched_barrier(0);
+            const word4_t f = ring[i % kAhead];
+            if constexpr (i < kScores) {
+                ahead[i & 1] = TY::mfma(f, qf[i >> 1], ahead[i & 1]);
+#pragma unroll
+                for (int k = 0; k < kLate; ++k)
+                    if (k * kScores / kLate == i) pair(k);
+            } else {
+                constexpr int x = i - kScores, j = x / (DP / 32), d = x % (DP / 32);
+                o[d] = TY::mfma(f, p[j], o[d]);
+#pragma unroll
+                for (int k = kLate; k < 16; ++k)
+                    if ((k - kLate) * (kValues / 2) / (16 - kLate) == x) pair(k);
+#pragma unroll
+                for (int y = 0; y < 16; ++y)
+                    if (kValues / 2 + y * (kValues / 2) / 16 == x) top = y == 0 ? fmaxf(ahead[0][0], ahead[1][0]) : fmaxf(fmaxf(top, ahead[0][y]), ahead[1][y]);
+            }
+            fetch(i + kAhead, s);
+        });
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    // Keys are a step ahead of values: while step s is worked on, keys s + 1 and values s are read, keys s + 2 and values s + 1 copied.
+    float16_t z0[2], z1[2];
+    if (s0 < s1) {
+        pages.begin(list, entries, (key0 + s0 * kManyTile + 16 * wave) >> a.log_ps);
+        page = page_of(s0);
+        copy(s0, page, false);
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        copy(s0, page, true);
+        if (s0 + 1 < s1) {
+            page = page_of(s0 + 1);
+            copy(s0 + 1, page, false);
+        }
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int y = 0; y < 16; ++y) z0[half][y] = 0;
+#pragma unroll
+        for (int i = 0; i < kScores; ++i) {
+            fetch(i, s0 - 1);
+            z0[i & 1] = TY::mfma(ring[i % kAhead], qf[i >> 1], z0[i & 1]);
+        }
+#pragma unroll
+        for (int y = 0; y < 16; ++y) top = fmaxf(fmaxf(top, z0[0][y]), z0[1][y]);
+    }
+    for (int s = s0; s < s1; s += 2) {
+        work(z0, z1, s);
+        if (s + 1 < s1) work(z1, z0, s + 1);
     }
     l += __shfl_xor(l, 32);
 
@@ -249,6 +316,7 @@ static hipError_t launch_many(const AttendArgs &a, bool shared, hipStream_t stre
     if (!shared) tiles = a.q_start ? std::min((long)a.T * ((a.group + kManyRows - 1) / kManyRows), tiles + a.rows) : (long)a.rows * ((a.group + kManyRows - 1) / kManyRows);
     const dim3 grid(a.kv_heads, (unsigned)tiles, shared ? a.shared_splits : a.splits), block(256);
     if (a.D <= 64) hipLaunchKernelGGL((fbq_attend_many_kernel<TY, 64>), grid, block, 0, stream, a, shared);
+    else if (a.D <= 96) hipLaunchKernelGGL((fbq_attend_many_kernel<TY, 96>), grid, block, 0, stream, a, shared);
     else if (a.D <= 128) hipLaunchKernelGGL((fbq_attend_many_kernel<TY, 128>), grid, block, 0, stream, a, shared);
     else hipLaunchKernelGGL((fbq_attend_many_kernel<TY, 256>), grid, block, 0, stream, a, shared);
     return hipGetLastError();

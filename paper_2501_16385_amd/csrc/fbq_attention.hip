@@ -3,18 +3,23 @@
 
 namespace fbq {
 
-constexpr int kJoinWaves = 4;
+constexpr int kJoinThreads = 256;
 
-// out = sum over the partial results of a query row, one block a row; in the order of their numbers, so that equal calls give equal bits.  A row's own part is either
-// whole (written by its one piece: nothing left to do unless shared tokens come with it), or cut into the pieces of the waves w0 .. w1 of the few-row kernel, or
-// into the splits of the many-row kernel.
-template <class TY>
-__global__ __launch_bounds__(64 * kJoinWaves) void fbq_attend_join_kernel(const AttendArgs a, const bool few)
+// The partial results of one query row, added up in the order of their numbers, so that equal calls give equal bits:  out = sum_p o_p 2^(m_p - m) / sum_p l_p 2^(m_p - m),
+// m the largest m_p.  A part whose sum l is 0 saw nothing and has no o.  Bound by the latency of a chain of three loads (where the parts lie, their m and l, their o),
+// so the loads of each link are issued together.
+
+// Few-row kernel: a block a row.  The row's own part is either whole (written by its one piece: nothing left to do unless shared tokens come with it) or cut into
+// the pieces of the workers w0 .. w1.  All parts' m and l first, then LANES lanes a part, four features each.  us, 64 heads of 8 x 256 pieces 71.6 with a wave going through
+// its parts one after the other.
+template <class TY, int LANES>
+__global__ __launch_bounds__(kJoinThreads) void fbq_join_pieces_kernel(const AttendArgs a)
 {
-    __shared__ int sums[2][kJoinWaves];
-    __shared__ float2 wave_ml[kJoinWaves];
-    __shared__ float wave_o[kJoinWaves][256];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    constexpr int kWaves = kJoinThreads / 64, kGroups = kJoinThreads / LANES;
+    __shared__ float wave_value[2][kWaves];
+    __shared__ float weight[kJoinThreads];
+    __shared__ float4_t group_o[kGroups][LANES];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int t = blockIdx.x / a.heads, head = blockIdx.x - t * a.heads, h = head / a.group, j = head - h * a.group;
     const int b = a.q_start ? row_of_token(a.q_start, a.rows, t) : t;
     if (b < 0) return;
@@ -22,91 +27,140 @@ __global__ __launch_bounds__(64 * kJoinWaves) void fbq_attend_join_kernel(const 
     const int i = t - q.x;
     if (i >= q.y) return;
 
-    const long row = (long)t * a.heads + head, rows = (long)a.T * a.heads;
-    int share = 1, own0 = 0, own1 = 0, shared0 = 0, shared1 = 0;              // few: the item's steps in the line
-    if (few) {
-        int before = 0, all = 0;
-        for (int x = threadIdx.x; x < a.rows; x += 64 * kJoinWaves) {
-            const int steps = few_steps(a, x);
-            all += steps;
-            before += x < b ? steps : 0;
-        }
-#pragma unroll
-        for (int o = 32; o; o >>= 1) {
-            all += __shfl_xor(all, o);
-            before += __shfl_xor(before, o);
-        }
-        if (lane == 0) {
-            sums[0][wave] = all;
-            sums[1][wave] = before;
-        }
-        __syncthreads();
-        all = before = 0;
-        for (int w = 0; w < kJoinWaves; ++w) {
-            all += sums[0][w];
-            before += sums[1][w];
-        }
-        const int shared_steps = a.shared_here ? (a.n_shared + kFewTile - 1) / kFewTile : 0, steps = few_steps(a, b);
-        share = few_share(a, (all + shared_steps) * a.kv_heads);
-        own0 = (shared_steps + before) * a.kv_heads + h * steps;
-        own1 = own0 + steps;
-        shared0 = h * shared_steps;
-        shared1 = shared0 + shared_steps;
+    int before = 0, all = 0;                                  // steps of the rows before b, of all rows
+    for (int x = lane; x < a.rows; x += 64) {
+        const int steps = few_steps(a, x);
+        all += steps;
+        before += x < b ? steps : 0;
     }
-    const bool one_own = few && own1 > own0 && own0 / share == (own1 - 1) / share;
+#pragma unroll
+    for (int o = 32; o; o >>= 1) {
+        all += __shfl_xor(all, o);
+        before += __shfl_xor(before, o);
+    }
+    const int shared_steps = a.shared_here ? (a.n_shared + kFewTile - 1) / kFewTile : 0, steps = few_steps(a, b);
+    const int share = few_share(a, (all + shared_steps) * a.kv_heads);
+    const int own0 = (shared_steps + before) * a.kv_heads + h * steps, own1 = own0 + steps, shared0 = h * shared_steps, shared1 = shared0 + shared_steps;
+    const bool one_own = own1 > own0 && own0 / share == (own1 - 1) / share;
     if (one_own && !a.whole.o) return;                        // written by its piece
-    const int n_own = !few ? a.splits : own1 == own0 ? 0 : (own1 - 1) / share - own0 / share + 1;
-    const int n_shared = a.shared_here ? (shared1 - 1) / share - shared0 / share + 1 : a.part_shared.o ? a.shared_splits : 0;
-    const auto piece = [&](int u0, int x, int r) {            // the x-th piece of the item that begins with step u0, its row r
-        const int w = u0 / share + x;
-        return ((long)w * 2 + ((long)w * share < u0 ? 1 : 0)) * a.slot_rows + r;
+    const int n_own = own1 == own0 ? 0 : (own1 - 1) / share - own0 / share + 1;
+    const int n_shared = a.shared_here ? (shared1 - 1) / share - shared0 / share + 1 : a.part_shared.o ? a.shared_splits : 0, n = n_shared + n_own;
+    const long row = (long)t * a.heads + head, rows = (long)a.T * a.heads;
+    const auto part = [&](int p, long *at) {                  // the set that part p lies in, and where
+        const auto piece = [&](int u0, int x, int r) {        // the x-th piece of the item that begins with step u0, its row r
+            const int w = u0 / share + x;
+            return ((long)w * 2 + ((long)w * share < u0 ? 1 : 0)) * a.slot_rows + r;
+        };
+        if (p < n_shared) {
+            if (!a.shared_here) return *at = p * rows + row, a.part_shared;
+            if (n_shared == 1) return *at = row, a.whole_shared;
+            return *at = piece(shared0, p, t * a.group + j), a.piece;
+        }
+        if (one_own) return *at = row, a.whole;
+        return *at = piece(own0, p - n_shared, i * a.group + j), a.piece;
     };
 
-    float m = kNoScore, l = 0, acc[4] = {0, 0, 0, 0};
-    for (int p = wave; p < n_shared + n_own; p += kJoinWaves) {
-        Partials from;
+    float m = kNoScore;
+    for (int p = tid; p < n; p += kJoinThreads) {
         long at;
-        if (p < n_shared) {
-            if (!a.shared_here) from = a.part_shared, at = p * rows + row;
-            else if (n_shared == 1) from = a.whole_shared, at = row;
-            else from = a.piece, at = piece(shared0, p, t * a.group + j);
-        } else {
-            const int x = p - n_shared;
-            if (!few) from = a.part, at = x * rows + row;
-            else if (one_own) from = a.whole, at = row;
-            else from = a.piece, at = piece(own0, x, i * a.group + j);
-        }
-        const float2 ml = from.ml[at];
-        if (ml.y == 0) continue;
-        const float to = fmaxf(m, ml.x), by = __builtin_amdgcn_exp2f(m - to), times = __builtin_amdgcn_exp2f(ml.x - to);
-        m = to;
-        l = l * by + ml.y * times;
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-            if (lane + 64 * k < a.D) acc[k] = acc[k] * by + from.o[at * a.D + lane + 64 * k] * times;
+        const Partials from = part(p, &at);
+        m = fmaxf(m, from.ml[at].x);
     }
-    if (lane == 0) wave_ml[wave] = make_float2(m, l);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) wave_o[wave][lane + 64 * k] = acc[k];
+    for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+    if (lane == 0) wave_value[0][wave] = m;
     __syncthreads();
-    float top = kNoScore, sum = 0, o = 0;
-    for (int w = 0; w < kJoinWaves; ++w) top = fmaxf(top, wave_ml[w].x);
-    const int d = threadIdx.x;
-    for (int w = 0; w < kJoinWaves; ++w) {
-        const float by = __builtin_amdgcn_exp2f(wave_ml[w].x - top);
-        sum += wave_ml[w].y * by;
-        o += wave_o[w][d] * by;
+    for (int w = 0; w < kWaves; ++w) m = fmaxf(m, wave_value[0][w]);
+
+    float l = 0;
+    float4_t o{0, 0, 0, 0};
+    const int group = tid / LANES, d = (tid % LANES) * 4;
+    for (int p0 = 0; p0 < n; p0 += kJoinThreads) {
+        __syncthreads();
+        if (p0 + tid < n) {
+            long at;
+            const Partials from = part(p0 + tid, &at);
+            const float2 ml = from.ml[at];
+            const float by = __builtin_amdgcn_exp2f(ml.x - m);
+            if (ml.y != 0) l += ml.y * by;                    // (not a number counts)
+            weight[tid] = ml.y == 0 ? -1.0f : by;
+        }
+        __syncthreads();
+        const int end = min(n - p0, kJoinThreads);
+#pragma unroll 4
+        for (int p = group; p < end; p += kGroups) {
+            const float by = weight[p];
+            if (by == -1.0f || d >= a.D) continue;
+            long at;
+            const Partials from = part(p0 + p, &at);
+            o += *reinterpret_cast<const float4_t *>(from.o + at * a.D + d) * by;
+        }
     }
-    if (d < a.D) a.out[t * a.out_stride + head * a.D + d] = TY::one(sum == 0 ? 0.0f : o / sum);
-    if (a.lse && d == 0) a.lse[row] = sum == 0 ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+#pragma unroll
+    for (int x = 32; x; x >>= 1) l += __shfl_xor(l, x);
+    if (lane == 0) wave_value[1][wave] = l;
+    group_o[group][tid % LANES] = o;
+    __syncthreads();
+    if (tid >= LANES || d >= a.D) return;
+    l = 0;
+    for (int w = 0; w < kWaves; ++w) l += wave_value[1][w];
+    o = group_o[0][tid];
+    for (int g = 1; g < kGroups; ++g) o += group_o[g][tid];
+    o *= l == 0 ? 0.0f : 1.0f / l;
+    *reinterpret_cast<word2_t *>(a.out + t * a.out_stride + head * a.D + d) = word2_t{TY::pack(o[0], o[1]), TY::pack(o[2], o[3])};
+    if (a.lse && tid == 0) a.lse[row] = l == 0 ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
-static hipError_t launch_join(const AttendArgs &a, int type, bool few, hipStream_t stream)
+// Many-row kernel: LANES lanes a row, four features each, its splits one behind the other.
+template <class TY, int LANES>
+__global__ __launch_bounds__(kJoinThreads) void fbq_join_splits_kernel(const AttendArgs a)
 {
-    const dim3 grid((unsigned)((long)a.T * a.heads)), block(64 * kJoinWaves);
-    if (type == FBQ_F16) hipLaunchKernelGGL(fbq_attend_join_kernel<TypeF16>, grid, block, 0, stream, a, few);
-    else hipLaunchKernelGGL(fbq_attend_join_kernel<TypeBf16>, grid, block, 0, stream, a, few);
+    const long rows = (long)a.T * a.heads, row = (long)blockIdx.x * (kJoinThreads / LANES) + threadIdx.x / LANES;
+    const int d = (threadIdx.x % LANES) * 4;
+    if (row >= rows || d >= a.D) return;
+    const int t = (int)(row / a.heads);
+    if (a.q_start) {                                          // a token of no row: nothing was written for it
+        const int b = row_of_token(a.q_start, a.rows, t);
+        if (b < 0 || t - a.q_start[b] >= a.max_q) return;
+    }
+    const int n_shared = a.part_shared.o ? a.shared_splits : 0, n = n_shared + a.splits;
+    const auto part = [&](int p, long *at) { return p < n_shared ? (*at = p * rows + row, a.part_shared) : (*at = (p - n_shared) * rows + row, a.part); };
+    float m = kNoScore, l = 0;
+#pragma unroll 4
+    for (int p = 0; p < n; ++p) {
+        long at;
+        const Partials from = part(p, &at);
+        m = fmaxf(m, from.ml[at].x);
+    }
+    float4_t o{0, 0, 0, 0};
+#pragma unroll 4
+    for (int p = 0; p < n; ++p) {
+        long at;
+        const Partials from = part(p, &at);
+        const float2 ml = from.ml[at];
+        if (ml.y == 0) continue;
+        const float by = __builtin_amdgcn_exp2f(ml.x - m);
+        l += ml.y * by;
+        o += *reinterpret_cast<const float4_t *>(from.o + at * a.D + d) * by;
+    }
+    o *= l == 0 ? 0.0f : 1.0f / l;
+    *reinterpret_cast<word2_t *>(a.out + t * a.out_stride + (row - (long)t * a.heads) * a.D + d) = word2_t{TY::pack(o[0], o[1]), TY::pack(o[2], o[3])};
+    if (a.lse && d == 0) a.lse[row] = l == 0 ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+}
+
+template <class TY, int LANES>
+static hipError_t launch_join(const AttendArgs &a, bool few, hipStream_t stream)
+{
+    const long rows = (long)a.T * a.heads, a_block = kJoinThreads / LANES;
+    if (few) hipLaunchKernelGGL((fbq_join_pieces_kernel<TY, LANES>), dim3((unsigned)rows), dim3(kJoinThreads), 0, stream, a);
+    else hipLaunchKernelGGL((fbq_join_splits_kernel<TY, LANES>), dim3((unsigned)((rows + a_block - 1) / a_block)), dim3(kJoinThreads), 0, stream, a);
     return hipGetLastError();
+}
+
+template <class TY>
+static hipError_t launch_join(const AttendArgs &a, bool few, hipStream_t stream)
+{
+    return a.D <= 64 ? launch_join<TY, 16>(a, few, stream) : a.D <= 128 ? launch_join<TY, 32>(a, few, stream) : launch_join<TY, 64>(a, few, stream);
 }
 
 struct AttendPlan {
@@ -127,7 +181,9 @@ static AttendPlan attend_plan(const fbq_attention_call &c, void *workspace)
     a.page_bytes = cache.page_bytes; a.q_stride = c.q_stride; a.out_stride = c.out_stride;
     a.pages = cache.pages; a.log_ps = cache.log_ps; a.max_pages = cache.max_pages; a.rows = cache.rows; a.kv_heads = cache.kv_heads; a.D = cache.D;
     a.heads = c.heads; a.group = c.heads / a.kv_heads; a.T = c.T; a.max_q = c.q_start ? c.max_q : 1;
-    a.scale = c.scale * 1.4426950408889634f;
+    a.scale = c.scale == 0 ? 1.0f : std::fabs(c.scale) * 1.4426950408889634f;
+    a.q_and = c.scale == 0 ? 0u : 0xffffffffu;
+    a.q_xor = c.scale < 0 ? 0x80008000u : 0u;
 
     const long row_queries = (long)a.max_q * a.group, all_queries = (long)a.T * a.group;   // of one key/value head
     p.few = row_queries <= kFewRows;
@@ -142,8 +198,8 @@ static AttendPlan attend_plan(const fbq_attention_call &c, void *workspace)
         to->ml = (float2 *)((char *)workspace + at);
         at += ((size_t)n * 8 + 255) / 256 * 256;
     };
-    const auto splits_of = [](long blocks, long tokens) {     // so that the GPU, two blocks a CU, is filled, with 256 keys or more each
-        return (int)std::max(1L, std::min({(512 + blocks - 1) / blocks, (tokens + 255) / 256, 32L}));
+    const auto splits_of = [](long blocks, long tokens) {     // so that the GPU, two blocks a CU, is about filled, with 256 keys or more each
+        return (int)std::max(1L, std::min({(512 + blocks / 2) / blocks, (tokens + 255) / 256, 32L}));
     };
     if (a.n_shared) {
         a.shared_here = p.few && all_queries <= kFewRows;
@@ -220,6 +276,6 @@ extern "C" fbq_status fbq_attention(const fbq_attention_call *c, void *workspace
     hipError_t e = hipSuccess;
     if (p.shared_many) e = launch_attend_many(p.a, type, true, s);
     if (e == hipSuccess) e = p.few ? launch_attend_few(p.a, type, s) : launch_attend_many(p.a, type, false, s);
-    if (e == hipSuccess && p.join) e = launch_join(p.a, type, p.few, s);
+    if (e == hipSuccess && p.join) e = type == FBQ_F16 ? launch_join<TypeF16>(p.a, p.few, s) : launch_join<TypeBf16>(p.a, p.few, s);
     return e == hipSuccess ? FBQ_OK : FBQ_ERR_HIP;
 }
