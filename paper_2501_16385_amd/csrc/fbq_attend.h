@@ -101,12 +101,13 @@ __device__ __forceinline__ int2 queries_of(const AttendArgs &a, int b)
 
 __device__ __forceinline__ int row_tokens(const AttendArgs &a, int b) { return tokens_of(a.lengths[b], a.max_pages << a.log_ps); }
 
-// Steps of a row's own tokens in the few-row kernel; none if it has no query tokens.
-__device__ __forceinline__ int few_steps(const AttendArgs &a, int b)
+// Steps of a row's own tokens in the few-row kernel, of which it has `tokens` with the shared ones; none if it has no query tokens.
+__device__ __forceinline__ int few_steps(const AttendArgs &a, int b, int tokens)
 {
-    const int steps = (max(row_tokens(a, b) - a.n_shared, 0) + kFewTile - 1) / kFewTile;
+    const int steps = (max(tokens - a.n_shared, 0) + kFewTile - 1) / kFewTile;
     return a.q_start && queries_of(a, b).y == 0 ? 0 : steps;
 }
+__device__ __forceinline__ int few_steps(const AttendArgs &a, int b) { return few_steps(a, b, row_tokens(a, b)); }
 
 // How many steps each worker takes, from all there are: the last ones may have none.
 __device__ __forceinline__ int few_share(const AttendArgs &a, int steps) { return max(1, (steps + a.workers - 1) / a.workers); }

@@ -15,7 +15,7 @@ constexpr int kJoinThreads = 256;
 template <class TY, int LANES>
 __global__ __launch_bounds__(kJoinThreads) void fbq_join_pieces_kernel(const AttendArgs a)
 {
-    constexpr int kWaves = kJoinThreads / 64, kGroups = kJoinThreads / LANES;
+    constexpr int kWaves = kJoinThreads / 64, kGroups = kJoinThreads / LANES, kAtOnce = 8;
     __shared__ float wave_value[2][kWaves];
     __shared__ float weight[kJoinThreads];
     __shared__ float4_t group_o[kGroups][LANES];
@@ -46,18 +46,18 @@ __global__ __launch_bounds__(kJoinThreads) void fbq_join_pieces_kernel(const Att
     const int n_own = own1 == own0 ? 0 : (own1 - 1) / share - own0 / share + 1;
     const int n_shared = a.shared_here ? (shared1 - 1) / share - shared0 / share + 1 : a.part_shared.o ? a.shared_splits : 0, n = n_shared + n_own;
     const long row = (long)t * a.heads + head, rows = (long)a.T * a.heads;
-    const auto part = [&](int p, long *at) {                  // the set that part p lies in, and where
-        const auto piece = [&](int u0, int x, int r) {        // the x-th piece of the item that begins with step u0, its row r
-            const int w = u0 / share + x;
-            return ((long)w * 2 + ((long)w * share < u0 ? 1 : 0)) * a.slot_rows + r;
-        };
+    // where part p of the n lies: parts of one list are equally far apart but for the first of an item, which may be in a worker's other place
+    const int own_w = own0 / share, shared_w = shared0 / share;
+    const auto part = [&](int p, long *at) {
         if (p < n_shared) {
             if (!a.shared_here) return *at = p * rows + row, a.part_shared;
             if (n_shared == 1) return *at = row, a.whole_shared;
-            return *at = piece(shared0, p, t * a.group + j), a.piece;
+            const int w = shared_w + p;
+            return *at = ((long)w * 2 + ((long)w * share < shared0 ? 1 : 0)) * a.slot_rows + t * a.group + j, a.piece;
         }
         if (one_own) return *at = row, a.whole;
-        return *at = piece(own0, p - n_shared, i * a.group + j), a.piece;
+        const int w = own_w + p - n_shared;
+        return *at = ((long)w * 2 + ((long)w * share < own0 ? 1 : 0)) * a.slot_rows + i * a.group + j, a.piece;
     };
 
     float m = kNoScore;
@@ -87,13 +87,19 @@ __global__ __launch_bounds__(kJoinThreads) void fbq_join_pieces_kernel(const Att
         }
         __syncthreads();
         const int end = min(n - p0, kJoinThreads);
-#pragma unroll 4
-        for (int p = group; p < end; p += kGroups) {
-            const float by = weight[p];
-            if (by == -1.0f || d >= a.D) continue;
-            long at;
-            const Partials from = part(p0 + p, &at);
-            o += *reinterpret_cast<const float4_t *>(from.o + at * a.D + d) * by;
+        for (int g0 = group; g0 < end; g0 += kGroups * kAtOnce) {
+            float4_t v[kAtOnce];
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) {               // (past the end the last one again)
+                long at;
+                const Partials from = part(p0 + min(g0 + k * kGroups, end - 1), &at);
+                v[k] = *reinterpret_cast<const float4_t *>(from.o + at * a.D + min(d, a.D - 4));
+            }
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) {
+                const float by = g0 + k * kGroups < end ? weight[g0 + k * kGroups] : -1.0f;
+                if (by != -1.0f) o += v[k] * by;
+            }
         }
     }
 #pragma unroll
