@@ -48,6 +48,7 @@ struct AttendArgs {
     // few-row kernel: `workers` waves; the partial results of pieces of items, two a worker ([workers][2][slot_rows]); those of whole items where something else
     // has to be added ([T heads]), null: out is written
     int workers, slot_rows;
+    bool direct;                         // an item a worker, no partial results
     bool shared_here;                    // the shared tokens are items of this kernel's own, for the rows of all sequences together
     Partials piece, whole, whole_shared;
     // many-row kernel: `splits` of the keys, partial results [splits][T heads] (null: out is written)
@@ -114,6 +115,18 @@ __device__ __forceinline__ int few_share(const AttendArgs &a, int steps) { retur
 
 // A value that is the same in all lanes, as one the compiler knows to be.
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
+// The larger of x and the x of the lane 16, or 32, further round in pairs of rows of 16, or 32.
+__device__ __forceinline__ float larger_of_16(float x)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+    return fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
+}
+__device__ __forceinline__ float larger_of_32(float x)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+    return fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
+}
 
 // The page list that a wave goes along: 64 entries a register, the next 64 under way.
 struct PageList {

@@ -29,6 +29,16 @@ struct Step {
     word4_t v[2][4][kV];
 };
 
+// A piece of an item: what its loads and its rows need, both for the piece worked on and the one behind it.
+template <int DP>
+struct Piece {
+    int b, h, step, steps, limit;                             // table row (-1: the shared tokens), head, its first step of the item's `steps`, tokens of the item
+    int n, key0;                                              // steps of its own, its first key
+    PageList pages;
+    int t, head, sees;                                        // this lane's query row: token (-1: none), head, how many tokens it sees
+    word4_t q[DP / 32];
+};
+
 template <class TY, int DP>
 __global__ __launch_bounds__(64 * kFewWaves, DP == 256 ? 1 : 2) void fbq_attend_few_kernel(const AttendArgs a)
 {
@@ -37,46 +47,111 @@ __global__ __launch_bounds__(64 * kFewWaves, DP == 256 ? 1 : 2) void fbq_attend_
     const int worker = uniform(blockIdx.x * kFewWaves + (threadIdx.x >> 6));
     const int D = a.D, ps1 = (1 << a.log_ps) - 1;
 
-    int own = 0;
-    for (int b = lane; b < a.rows; b += 64) own += few_steps(a, b);
-#pragma unroll
-    for (int o = 32; o; o >>= 1) own += __shfl_xor(own, o);
-    const int shared_steps = a.shared_here ? (a.n_shared + kFewTile - 1) / kFewTile : 0;
-    const int total = uniform(own + shared_steps) * a.kv_heads;
-    const int share = few_share(a, total);
-    int u = min(worker, total) * share;                       // (worker * share within an int)
-    const int end = min(total, u + share);
-    if (u >= end) return;
-
-    int b = -1, h, step, steps, limit = a.n_shared;           // the item that u lies in, its tokens; b -1: the shared ones
-    if (u < shared_steps * a.kv_heads) {
-        steps = shared_steps;
-        h = u / steps;
-        step = u - h * steps;
+    Piece<DP> cur, behind;
+    int u = 0, end = 0;
+    if (a.direct) {                                           // an item a worker
+        cur.b = worker / a.kv_heads;
+        if (cur.b >= a.rows) return;
+        cur.h = worker - cur.b * a.kv_heads;
+        cur.limit = uniform(row_tokens(a, cur.b));
+        cur.steps = uniform(few_steps(a, cur.b, cur.limit));
+        cur.step = 0;
+        cur.n = cur.steps;
     } else {
-        int rest = u - shared_steps * a.kv_heads, before = 0, base = 0, tokens, mine, sum;
-        while (true) {
-            tokens = base + lane < a.rows ? row_tokens(a, base + lane) : 0;
-            mine = base + lane < a.rows ? few_steps(a, base + lane, tokens) : 0;
-            sum = mine;
+        int own = 0;
+        for (int b = lane; b < a.rows; b += 64) own += few_steps(a, b);
 #pragma unroll
-            for (int o = 1; o < 64; o <<= 1) {
-                const int x = __shfl_up(sum, o);
-                if (lane >= o) sum += x;
+        for (int o = 32; o; o >>= 1) own += __shfl_xor(own, o);
+        const int shared_steps = a.shared_here ? (a.n_shared + kFewTile - 1) / kFewTile : 0;
+        const int total = uniform(own + shared_steps) * a.kv_heads;
+        const int share = few_share(a, total);
+        u = min(worker, total) * share;                       // (worker * share within an int)
+        end = min(total, u + share);
+        if (u >= end) return;
+        if (u < shared_steps * a.kv_heads) {
+            cur.b = -1;
+            cur.limit = a.n_shared;
+            cur.steps = shared_steps;
+            cur.h = u / cur.steps;
+            cur.step = u - cur.h * cur.steps;
+        } else {
+            int rest = u - shared_steps * a.kv_heads, before = 0, base = 0, tokens, mine, sum;
+            while (true) {
+                tokens = base + lane < a.rows ? row_tokens(a, base + lane) : 0;
+                mine = base + lane < a.rows ? few_steps(a, base + lane, tokens) : 0;
+                sum = mine;
+#pragma unroll
+                for (int o = 1; o < 64; o <<= 1) {
+                    const int x = __shfl_up(sum, o);
+                    if (lane >= o) sum += x;
+                }
+                const int some = __builtin_amdgcn_readlane(sum, 63);
+                if ((long)rest < (long)(before + some) * a.kv_heads) break;
+                before += some;
+                base += 64;
+                if (base >= a.rows) return;                   // (not unless lengths change under the call)
             }
-            if ((long)rest < (long)(before + uniform(__shfl(sum, 63))) * a.kv_heads) break;
-            before += uniform(__shfl(sum, 63));
-            base += 64;
-            if (base >= a.rows) return;                       // (not unless lengths change under the call)
+            const int at = __builtin_ctzll(__ballot((long)(before + sum) * a.kv_heads > rest));
+            cur.b = base + at;
+            cur.steps = __builtin_amdgcn_readlane(mine, at);
+            cur.limit = __builtin_amdgcn_readlane(tokens, at);
+            rest -= (before + __builtin_amdgcn_readlane(sum, at) - cur.steps) * a.kv_heads;
+            cur.h = rest / cur.steps;
+            cur.step = rest - cur.h * cur.steps;
         }
-        const int at = __builtin_ctzll(__ballot((long)(before + sum) * a.kv_heads > rest));
-        b = base + at;
-        steps = __builtin_amdgcn_readlane(mine, at);
-        limit = __builtin_amdgcn_readlane(tokens, at);
-        rest -= (before + __builtin_amdgcn_readlane(sum, at) - steps) * a.kv_heads;
-        h = rest / steps;
-        step = rest - h * steps;
+        cur.n = min(end - u, cur.steps - cur.step);
+        u += cur.n;
     }
+
+    // the item behind `x`, which ends with it; false: there is none
+    auto follow = [&](const Piece<DP> &x, Piece<DP> &to) __attribute__((always_inline)) {
+        if (u >= end) return false;
+        to.b = x.b; to.h = x.h + 1; to.steps = x.steps; to.limit = x.limit; to.step = 0;
+        if (to.h == a.kv_heads) {
+            to.h = 0;
+            do {
+                if (++to.b >= a.rows) return false;           // (not unless lengths change under the call)
+                to.limit = uniform(row_tokens(a, to.b));
+                to.steps = uniform(few_steps(a, to.b, to.limit));
+            } while (to.steps == 0);
+        }
+        to.n = min(end - u, to.steps);
+        u += to.n;
+        return true;
+    };
+    auto prepare = [&](Piece<DP> &x) __attribute__((always_inline)) {
+        const bool is_shared = x.b < 0;
+        x.key0 = (is_shared ? 0 : a.n_shared) + x.step * kFewTile;
+        x.pages.begin(is_shared ? a.shared : a.table + (long)x.b * a.max_pages, is_shared ? a.n_shared >> a.log_ps : a.max_pages, x.key0 >> a.log_ps);
+        const int i = col / a.group;
+        x.head = x.h * a.group + col - i * a.group;
+        x.t = -1;
+        x.sees = 0;
+        if (is_shared) {
+            if (i < a.T) {
+                const int row = a.q_start ? row_of_token(a.q_start, a.rows, i) : i;
+                if (row >= 0) {
+                    const int2 q = queries_of(a, row);
+                    if (i - q.x < q.y) {
+                        x.t = i;
+                        x.sees = min(row_tokens(a, row) - q.y + i - q.x + 1, x.limit);
+                    }
+                }
+            }
+        } else {
+            const int2 q = queries_of(a, x.b);
+            if (i < q.y) {
+                x.t = q.x + i;
+                x.sees = x.limit - q.y + i + 1;
+            }
+        }
+#pragma unroll
+        for (int s = 0; s < DP / 32; ++s) {
+            const int d = 32 * s + 8 * grp;
+            x.q[s] = word4_t{0, 0, 0, 0};
+            if (x.t >= 0 && d < D) x.q[s] = (*reinterpret_cast<const word4_t *>(a.q + x.t * a.q_stride + x.head * D + d) & a.q_and) ^ a.q_xor;
+        }
+    };
 
     // offsets of this lane's loads from a half step's first key, or value
     int k_off[DP / 32], v_off[4];
@@ -84,194 +159,163 @@ __global__ __launch_bounds__(64 * kFewWaves, DP == 256 ? 1 : 2) void fbq_attend_
     for (int s = 0; s < DP / 32; ++s) k_off[s] = 32 * s + 8 * grp < D ? (col * D + 32 * s + 8 * grp) * 2 : kNowhere;
 #pragma unroll
     for (int e = 0; e < 4; ++e) v_off[e] = J * col < D ? ((4 * grp + e) * D + J * col) * 2 : kNowhere;
-
-    bool first = true;
-    while (u < end) {
-        const int n = min(end - u, steps - step);
-        const bool is_shared = b < 0;
-
-        const int key0 = (is_shared ? 0 : a.n_shared) + step * kFewTile;
-        PageList pages;
-        pages.begin(is_shared ? a.shared : a.table + (long)b * a.max_pages, is_shared ? a.n_shared >> a.log_ps : a.max_pages, key0 >> a.log_ps);
-
-        // this lane's query row (column `col`): token, head, how many tokens it sees
-        int t = -1, sees = 0;
-        const int i = col / a.group, head = h * a.group + col - i * a.group;
-        if (is_shared) {
-            if (i < a.T) {
-                const int row = a.q_start ? row_of_token(a.q_start, a.rows, i) : i;
-                if (row >= 0) {
-                    const int2 q = queries_of(a, row);
-                    if (i - q.x < q.y) {
-                        t = i;
-                        sees = min(row_tokens(a, row) - q.y + i - q.x + 1, limit);
-                    }
+    auto load = [&](Step<DP> &to, Piece<DP> &x, int s) __attribute__((always_inline)) {
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const int key = x.key0 + s * kFewTile + 16 * half;
+            int valid = min(max(x.limit - key, 0), 16);
+            const int id = valid ? x.pages.at(key >> a.log_ps) : 0;
+            if ((unsigned)id >= (unsigned)a.pages) valid = 0;
+            const unsigned char *const at = a.kv + (valid ? id : 0) * a.page_bytes + (((long)x.h << a.log_ps) + (key & ps1)) * D * 2;
+            const __amdgpu_buffer_rsrc_t kb = buffer_of(at, valid * D * 2), vb = buffer_of(at + (a.page_bytes >> 1), valid * D * 2);
+#pragma unroll
+            for (int c = 0; c < DP / 32; ++c) to.k[half][c] = __builtin_amdgcn_raw_buffer_load_b128(kb, k_off[c], 0, kOnce);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (DP == 64) {
+                    const word2_t w = __builtin_amdgcn_raw_buffer_load_b64(vb, v_off[e], 0, kOnce);
+                    to.v[half][e][0] = word4_t{w[0], w[1], 0, 0};
+                } else {
+#pragma unroll
+                    for (int c = 0; c < Step<DP>::kV; ++c) to.v[half][e][c] = __builtin_amdgcn_raw_buffer_load_b128(vb, v_off[e] + 16 * c, 0, kOnce);
                 }
             }
-        } else {
-            const int2 q = queries_of(a, b);
-            if (i < q.y) {
-                t = q.x + i;
-                sees = limit - q.y + i + 1;
-            }
         }
-        word4_t qf[DP / 32];
-#pragma unroll
-        for (int s = 0; s < DP / 32; ++s) {
-            const int d = 32 * s + 8 * grp;
-            qf[s] = word4_t{0, 0, 0, 0};
-            if (t >= 0 && d < D) qf[s] = (*reinterpret_cast<const word4_t *>(a.q + t * a.q_stride + head * D + d) & a.q_and) ^ a.q_xor;
-        }
+    };
 
-        auto load = [&](Step<DP> &to, int s) __attribute__((always_inline)) {   // step s of the piece; none past its end
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                const int key = key0 + s * kFewTile + 16 * half;
-                int valid = s < n ? min(max(limit - key, 0), 16) : 0;
-                const int id = valid ? pages.at(key >> a.log_ps) : 0;
-                if ((unsigned)id >= (unsigned)a.pages) valid = 0;
-                const unsigned char *const at = a.kv + (valid ? id : 0) * a.page_bytes + (((long)h << a.log_ps) + (key & ps1)) * D * 2;
-                const __amdgpu_buffer_rsrc_t kb = buffer_of(at, valid * D * 2), vb = buffer_of(at + (a.page_bytes >> 1), valid * D * 2);
-#pragma unroll
-                for (int x = 0; x < DP / 32; ++x) to.k[half][x] = __builtin_amdgcn_raw_buffer_load_b128(kb, k_off[x], 0, kOnce);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if (DP == 64) {
-                        const word2_t w = __builtin_amdgcn_raw_buffer_load_b64(vb, v_off[e], 0, kOnce);
-                        to.v[half][e][0] = word4_t{w[0], w[1], 0, 0};
-                    } else {
-#pragma unroll
-                        for (int x = 0; x < Step<DP>::kV; ++x) to.v[half][e][x] = __builtin_amdgcn_raw_buffer_load_b128(vb, v_off[e] + 16 * x, 0, kOnce);
-                    }
-                }
-            }
-        };
-
-        float4_t o[J];
+    float4_t o[J];
+    float m, l;
+    int least;                                                // what every row of the piece sees
+    auto begin = [&]() __attribute__((always_inline)) {
 #pragma unroll
         for (int j = 0; j < J; ++j) o[j] = float4_t{0, 0, 0, 0};
-        float m = kNoScore, l = 0;
-        int least;                                            // what every row sees
-        auto compute = [&](const Step<DP> &x, int s) __attribute__((always_inline)) {
-            float4_t z[2];
+        m = kNoScore;
+        l = 0;
+        least = cur.t >= 0 ? cur.sees : cur.limit;
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                z[half] = float4_t{0, 0, 0, 0};
-#pragma unroll
-                for (int y = 0; y < DP / 32; ++y) z[half] = TY::mfma(x.k[half][y], qf[y], z[half]);
-            }
-            const int key = key0 + s * kFewTile;
-            if (key + kFewTile > least) {
-#pragma unroll
-                for (int half = 0; half < 2; ++half)
-#pragma unroll
-                    for (int y = 0; y < 4; ++y)
-                        if (key + 16 * half + 4 * grp + y >= sees) z[half][y] = -INFINITY;
-            }
-            float top = fmaxf(fmaxf(fmaxf(z[0][0], z[0][1]), fmaxf(z[0][2], z[0][3])), fmaxf(fmaxf(z[1][0], z[1][1]), fmaxf(z[1][2], z[1][3])));
-            top = fmaxf(top, __shfl_xor(top, 16));
-            top = fmaxf(top, __shfl_xor(top, 32));
-            top *= a.scale;
-            if (__ballot(top > m + kSlack)) {
-                const float to = fmaxf(top, m), by = __builtin_amdgcn_exp2f(m - to);
-                l *= by;
-#pragma unroll
-                for (int j = 0; j < J; ++j) o[j] *= by;
-                m = to;
-            }
-            word4_t p;
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-#pragma unroll
-                for (int y = 0; y < 4; ++y) {
-                    z[half][y] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[half][y], a.scale, -m));
-                    l += z[half][y];
-                }
-                p[2 * half] = TY::pack(z[half][0], z[half][1]);
-                p[2 * half + 1] = TY::pack(z[half][2], z[half][3]);
-            }
-#pragma unroll
-            for (int j = 0; j < J; ++j) {
-                word4_t vt;
-#pragma unroll
-                for (int y = 0; y < 4; ++y) {                 // two keys of feature j
-                    const uint32_t lo = x.v[y >> 1][2 * (y & 1)][j >> 3][(j & 7) >> 1], hi = x.v[y >> 1][2 * (y & 1) + 1][j >> 3][(j & 7) >> 1];
-                    vt[y] = __builtin_amdgcn_perm(hi, lo, j & 1 ? 0x07060302u : 0x05040100u);
-                }
-                o[j] = TY::mfma(vt, p, o[j]);
-            }
-        };
-
-        Step<DP> x0, x1;
-        load(x0, 0);
-        least = t >= 0 ? sees : limit;
-#pragma unroll
-        for (int o = 8; o; o >>= 1) least = min(least, __shfl_xor(least, o));
+        for (int x = 8; x; x >>= 1) least = min(least, __shfl_xor(least, x));
         least = uniform(least);
-        for (int s = 0; s < n; s += 2) {
-            load(x1, s + 1);
-            compute(x0, s);
-            if (s + 1 < n) {
-                load(x0, s + 2);
-                compute(x1, s + 1);
-            }
+    };
+    auto compute = [&](const Step<DP> &x, int s) __attribute__((always_inline)) {
+        float4_t z[2];
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            z[half] = float4_t{0, 0, 0, 0};
+#pragma unroll
+            for (int y = 0; y < DP / 32; ++y) z[half] = TY::mfma(x.k[half][y], cur.q[y], z[half]);
         }
+        const int key = cur.key0 + s * kFewTile;
+        if (key + kFewTile > least) {
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+                for (int y = 0; y < 4; ++y)
+                    if (key + 16 * half + 4 * grp + y >= cur.sees) z[half][y] = -INFINITY;
+        }
+        float top = fmaxf(fmaxf(fmaxf(z[0][0], z[0][1]), fmaxf(z[0][2], z[0][3])), fmaxf(fmaxf(z[1][0], z[1][1]), fmaxf(z[1][2], z[1][3])));
+        top = larger_of_16(top);
+        top = larger_of_32(top) * a.scale;
+        if (__ballot(top > m + kSlack)) {
+            const float to = fmaxf(top, m), by = __builtin_amdgcn_exp2f(m - to);
+            l *= by;
+#pragma unroll
+            for (int j = 0; j < J; ++j) o[j] *= by;
+            m = to;
+        }
+        word4_t p;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                z[half][y] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[half][y], a.scale, -m));
+                l += z[half][y];
+            }
+            p[2 * half] = TY::pack(z[half][0], z[half][1]);
+            p[2 * half + 1] = TY::pack(z[half][2], z[half][3]);
+        }
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            word4_t vt;
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {                     // two keys of feature j
+                const uint32_t lo = x.v[y >> 1][2 * (y & 1)][j >> 3][(j & 7) >> 1], hi = x.v[y >> 1][2 * (y & 1) + 1][j >> 3][(j & 7) >> 1];
+                vt[y] = __builtin_amdgcn_perm(hi, lo, j & 1 ? 0x07060302u : 0x05040100u);
+            }
+            o[j] = TY::mfma(vt, p, o[j]);
+        }
+    };
+    bool first = true;
+    auto finish = [&]() __attribute__((always_inline)) {
         l += __shfl_xor(l, 16);
         l += __shfl_xor(l, 32);
-
-        if (t >= 0) {
-            const bool whole = n == steps;
-            const Partials to = whole ? (is_shared ? a.whole_shared : a.whole) : a.piece;
-            const int d0 = 4 * J * grp;
-            if (whole && !to.o) {
-                const float by = l == 0 ? 0.0f : 1.0f / l;
-                uint16_t *const at = a.out + t * a.out_stride + head * D + d0;
+        if (cur.t < 0) return;
+        const bool whole = cur.n == cur.steps;
+        const Partials to = whole ? (cur.b < 0 ? a.whole_shared : a.whole) : a.piece;
+        const int d0 = 4 * J * grp;
+        if (whole && !to.o) {
+            const float by = l == 0 ? 0.0f : 1.0f / l;
+            uint16_t *const at = a.out + cur.t * a.out_stride + cur.head * D + d0;
 #pragma unroll
-                for (int c = 0; c < J / 2; ++c) {             // eight features: elements 8 c .. of o[j][i] in the order J i + j
-                    word4_t w;
+            for (int c = 0; c < J / 2; ++c) {                 // eight features: elements 8 c .. of o[j][i] in the order J i + j
+                word4_t w;
 #pragma unroll
-                    for (int y = 0; y < 4; ++y) {
-                        const int e = 8 * c + 2 * y;
-                        w[y] = TY::pack(o[e % J][e / J] * by, o[(e + 1) % J][(e + 1) / J] * by);
-                    }
-                    if (d0 + 8 * c < D) *reinterpret_cast<word4_t *>(at + 8 * c) = w;
+                for (int y = 0; y < 4; ++y) {
+                    const int e = 8 * c + 2 * y;
+                    w[y] = TY::pack(o[e % J][e / J] * by, o[(e + 1) % J][(e + 1) / J] * by);
                 }
-                if (a.lse && grp == 0) a.lse[(long)t * a.heads + head] = l == 0 ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
-            } else {
-                const long r = whole ? (long)t * a.heads + head : ((long)worker * 2 + (first ? 0 : 1)) * a.slot_rows + col;
-                float *const at = to.o + r * D + d0;
-#pragma unroll
-                for (int c = 0; c < J; ++c) {
-                    float4_t w;
-#pragma unroll
-                    for (int y = 0; y < 4; ++y) w[y] = o[(4 * c + y) % J][(4 * c + y) / J];
-                    if (d0 + 4 * c < D) *reinterpret_cast<float4_t *>(at + 4 * c) = w;
-                }
-                if (grp == 0) to.ml[r] = make_float2(m, l);
+                if (d0 + 8 * c < D) *reinterpret_cast<word4_t *>(at + 8 * c) = w;
             }
+            if (a.lse && grp == 0) a.lse[(long)cur.t * a.heads + cur.head] = l == 0 ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+        } else {
+            const long r = whole ? (long)cur.t * a.heads + cur.head : ((long)worker * 2 + (first ? 0 : 1)) * a.slot_rows + col;
+            float *const at = to.o + r * D + d0;
+#pragma unroll
+            for (int c = 0; c < J; ++c) {
+                float4_t w;
+#pragma unroll
+                for (int y = 0; y < 4; ++y) w[y] = o[(4 * c + y) % J][(4 * c + y) / J];
+                if (d0 + 4 * c < D) *reinterpret_cast<float4_t *>(at + 4 * c) = w;
+            }
+            if (grp == 0) to.ml[r] = make_float2(m, l);
         }
+    };
 
-        first = false;
-        u += n;
-        step += n;
-        if (u < end && step == steps) {                       // (u < end: some item with steps follows)
-            step = 0;
-            if (++h == a.kv_heads) {
-                h = 0;
-                do {
-                    if (++b >= a.rows) return;
-                    limit = uniform(row_tokens(a, b));
-                    steps = uniform(few_steps(a, b, limit));
-                } while (steps == 0);
-            }
-        }
+    // A step's loads go out before the step before it is worked on, those of a piece's first step too: page list and queries of the piece behind come while the one
+    // before runs.
+    prepare(cur);
+    if (cur.n == 0) {                                         // (an item a worker, and this one has no tokens)
+        begin();
+        finish();
+        return;
     }
+    bool more = follow(cur, behind);
+    if (more) prepare(behind);
+    Step<DP> x0, x1;
+    load(x0, cur, 0);
+    begin();
+    int s = 0;
+    auto turn = [&](const Step<DP> &now, Step<DP> &next) __attribute__((always_inline)) {
+        if (s + 1 < cur.n) load(next, cur, s + 1);
+        else if (more) load(next, behind, 0);
+        compute(now, s);
+        if (++s < cur.n) return false;
+        finish();
+        if (!more) return true;
+        first = false;
+        cur = behind;
+        s = 0;
+        more = follow(cur, behind);
+        if (more) prepare(behind);
+        begin();
+        return false;
+    };
+    while (!turn(x0, x1) && !turn(x1, x0)) {}
 }
 
 template <class TY>
 static hipError_t launch_few(const AttendArgs &a, hipStream_t stream)
 {
-    const dim3 grid(a.workers / kFewWaves), block(64 * kFewWaves);
+    const dim3 grid(((a.direct ? a.rows * a.kv_heads : a.workers) + kFewWaves - 1) / kFewWaves), block(64 * kFewWaves);
     if (a.D <= 64) hipLaunchKernelGGL((fbq_attend_few_kernel<TY, 64>), grid, block, 0, stream, a);
     else if (a.D <= 128) hipLaunchKernelGGL((fbq_attend_few_kernel<TY, 128>), grid, block, 0, stream, a);
     else hipLaunchKernelGGL((fbq_attend_few_kernel<TY, 256>), grid, block, 0, stream, a);

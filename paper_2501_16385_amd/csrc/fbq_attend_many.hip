@@ -208,7 +208,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void fbq_attend_many_kernel
                     top = fmaxf(top, z[half][y]);
                 }
         }
-        const float high = fmaxf(top, __shfl_xor(top, 32)) * a.scale;
+        const float high = larger_of_32(top) * a.scale;
         if (__ballot(high > m + kSlack)) {
             const float to = fmaxf(high, m), by = __builtin_amdgcn_exp2f(m - to);
             l *= by;

@@ -169,6 +169,9 @@ static hipError_t launch_join(const AttendArgs &a, bool few, hipStream_t stream)
     return a.D <= 64 ? launch_join<TY, 16>(a, few, stream) : a.D <= 128 ? launch_join<TY, 32>(a, few, stream) : launch_join<TY, 64>(a, few, stream);
 }
 
+// Few-row kernel: where a row of the table has room for no more tokens than this, a wave takes an item whole and there is nothing to join.
+constexpr long kDirectTokens = 256;
+
 struct AttendPlan {
     AttendArgs a;
     bool few, shared_many, join;
@@ -217,7 +220,9 @@ static AttendPlan attend_plan(const fbq_attention_call &c, void *workspace)
             room(&a.whole_shared, results);
         }
     }
-    if (p.few) {
+    if (p.few && !a.n_shared && own_tokens <= kDirectTokens) {
+        a.direct = true;
+    } else if (p.few) {
         const long steps = ((own_tokens + kFewTile - 1) / kFewTile * a.rows + (a.shared_here ? a.n_shared / kFewTile + 1 : 0)) * a.kv_heads;
         a.workers = (int)std::min(a.D > 128 ? 1024L : 2048L, (steps + kFewWaves - 1) / kFewWaves * kFewWaves);
         a.workers = std::max(a.workers, kFewWaves);
