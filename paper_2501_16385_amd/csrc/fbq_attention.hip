@@ -5,21 +5,19 @@ namespace fbq {
 
 constexpr int kJoinThreads = 256;
 
-// The partial results of one query row, added up in the order of their numbers, so that equal calls give equal bits:  out = sum_p o_p 2^(m_p - m) / sum_p l_p 2^(m_p - m),
-// m the largest m_p.  A part whose sum l is 0 saw nothing and has no o.  Bound by the latency of a chain of three loads (where the parts lie, their m and l, their o),
-// so the loads of each link are issued together.
+// The partial results of one query row, added up in an order that depends on their number alone, so that equal calls give equal bits:
+//     out = sum_p o_p 2^(m_p - m) / sum_p l_p 2^(m_p - m),   m the largest m_p.   A part whose sum l is 0 saw nothing and has no o.
+// Bound by the latency of a chain of loads - where the parts lie, then their m, l and o at once - so as many as possible are under way together.
 
-// Few-row kernel: a block a row.  The row's own part is either whole (written by its one piece: nothing left to do unless shared tokens come with it) or cut into
-// the pieces of the workers w0 .. w1.  All parts' m and l first, then LANES lanes a part, four features each.  us, 64 heads of 8 x 256 pieces 71.6 with a wave going through
-// its parts one after the other.
-template <class TY, int LANES>
-__global__ __launch_bounds__(kJoinThreads) void fbq_join_pieces_kernel(const AttendArgs a)
+// Few-row kernel: a block a row, LANES lanes a part, four features each.  The row's own part is either whole (written by its one piece: nothing left to do unless
+// shared tokens come with it) or cut into the pieces of the workers w0 .. w1.  THREADS: 256, or a wave where there are rows enough to fill the GPU with.
+template <class TY, int LANES, int THREADS>
+__global__ __launch_bounds__(THREADS) void fbq_join_pieces_kernel(const AttendArgs a)
 {
-    constexpr int kWaves = kJoinThreads / 64, kGroups = kJoinThreads / LANES, kAtOnce = 8;
-    __shared__ float wave_value[2][kWaves];
-    __shared__ float weight[kJoinThreads];
+    constexpr int kGroups = THREADS / LANES, kAtOnce = 8;
+    __shared__ float2 group_ml[kGroups];
     __shared__ float4_t group_o[kGroups][LANES];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63;
     const int t = blockIdx.x / a.heads, head = blockIdx.x - t * a.heads, h = head / a.group, j = head - h * a.group;
     const int b = a.q_start ? row_of_token(a.q_start, a.rows, t) : t;
     if (b < 0) return;
@@ -60,58 +58,49 @@ __global__ __launch_bounds__(kJoinThreads) void fbq_join_pieces_kernel(const Att
         return *at = ((long)w * 2 + ((long)w * share < own0 ? 1 : 0)) * a.slot_rows + i * a.group + j, a.piece;
     };
 
-    float m = kNoScore;
-    for (int p = tid; p < n; p += kJoinThreads) {
-        long at;
-        const Partials from = part(p, &at);
-        m = fmaxf(m, from.ml[at].x);
-    }
-#pragma unroll
-    for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-    if (lane == 0) wave_value[0][wave] = m;
-    __syncthreads();
-    for (int w = 0; w < kWaves; ++w) m = fmaxf(m, wave_value[0][w]);
-
-    float l = 0;
+    float m = kNoScore, l = 0;
     float4_t o{0, 0, 0, 0};
     const int group = tid / LANES, d = (tid % LANES) * 4;
-    for (int p0 = 0; p0 < n; p0 += kJoinThreads) {
-        __syncthreads();
-        if (p0 + tid < n) {
+    for (int p0 = group; p0 < n; p0 += kGroups * kAtOnce) {
+        float2 ml[kAtOnce];
+        float4_t v[kAtOnce];
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {                   // (past the end the last one again, without weight)
             long at;
-            const Partials from = part(p0 + tid, &at);
-            const float2 ml = from.ml[at];
-            const float by = __builtin_amdgcn_exp2f(ml.x - m);
-            if (ml.y != 0) l += ml.y * by;                    // (not a number counts)
-            weight[tid] = ml.y == 0 ? -1.0f : by;
+            const Partials from = part(min(p0 + k * kGroups, n - 1), &at);
+            ml[k] = from.ml[at];
+            v[k] = *reinterpret_cast<const float4_t *>(from.o + at * a.D + min(d, a.D - 4));
+            if (p0 + k * kGroups >= n) ml[k] = make_float2(kNoScore, 0.0f);
         }
-        __syncthreads();
-        const int end = min(n - p0, kJoinThreads);
-        for (int g0 = group; g0 < end; g0 += kGroups * kAtOnce) {
-            float4_t v[kAtOnce];
+        float to = m;
 #pragma unroll
-            for (int k = 0; k < kAtOnce; ++k) {               // (past the end the last one again)
-                long at;
-                const Partials from = part(p0 + min(g0 + k * kGroups, end - 1), &at);
-                v[k] = *reinterpret_cast<const float4_t *>(from.o + at * a.D + min(d, a.D - 4));
-            }
+        for (int k = 0; k < kAtOnce; ++k) to = fmaxf(to, ml[k].x);
+        const float by = __builtin_amdgcn_exp2f(m - to);
+        m = to;
+        l *= by;
+        o *= by;
 #pragma unroll
-            for (int k = 0; k < kAtOnce; ++k) {
-                const float by = g0 + k * kGroups < end ? weight[g0 + k * kGroups] : -1.0f;
-                if (by != -1.0f) o += v[k] * by;
+        for (int k = 0; k < kAtOnce; ++k) {
+            const float times = __builtin_amdgcn_exp2f(ml[k].x - m);
+            if (ml[k].y != 0) {                               // (not a number counts)
+                l += ml[k].y * times;
+                o += v[k] * times;
             }
         }
     }
-#pragma unroll
-    for (int x = 32; x; x >>= 1) l += __shfl_xor(l, x);
-    if (lane == 0) wave_value[1][wave] = l;
     group_o[group][tid % LANES] = o;
+    if (tid % LANES == 0) group_ml[group] = make_float2(m, l);
     __syncthreads();
     if (tid >= LANES || d >= a.D) return;
+    m = kNoScore;
+    for (int g = 0; g < kGroups; ++g) m = fmaxf(m, group_ml[g].x);
     l = 0;
-    for (int w = 0; w < kWaves; ++w) l += wave_value[1][w];
-    o = group_o[0][tid];
-    for (int g = 1; g < kGroups; ++g) o += group_o[g][tid];
+    o = float4_t{0, 0, 0, 0};
+    for (int g = 0; g < kGroups; ++g) {
+        const float times = __builtin_amdgcn_exp2f(group_ml[g].x - m);
+        l += group_ml[g].y * times;
+        o += group_o[g][tid] * times;
+    }
     o *= l == 0 ? 0.0f : 1.0f / l;
     *reinterpret_cast<word2_t *>(a.out + t * a.out_stride + head * a.D + d) = word2_t{TY::pack(o[0], o[1]), TY::pack(o[2], o[3])};
     if (a.lse && tid == 0) a.lse[row] = l == 0 ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
@@ -158,7 +147,8 @@ template <class TY, int LANES>
 static hipError_t launch_join(const AttendArgs &a, bool few, hipStream_t stream)
 {
     const long rows = (long)a.T * a.heads, a_block = kJoinThreads / LANES;
-    if (few) hipLaunchKernelGGL((fbq_join_pieces_kernel<TY, LANES>), dim3((unsigned)rows), dim3(kJoinThreads), 0, stream, a);
+    if (few && rows >= 2048) hipLaunchKernelGGL((fbq_join_pieces_kernel<TY, LANES, 64>), dim3((unsigned)rows), dim3(64), 0, stream, a);
+    else if (few) hipLaunchKernelGGL((fbq_join_pieces_kernel<TY, LANES, kJoinThreads>), dim3((unsigned)rows), dim3(kJoinThreads), 0, stream, a);
     else hipLaunchKernelGGL((fbq_join_splits_kernel<TY, LANES>), dim3((unsigned)((rows + a_block - 1) / a_block)), dim3(kJoinThreads), 0, stream, a);
     return hipGetLastError();
 }
