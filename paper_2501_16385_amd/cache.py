@@ -34,6 +34,10 @@ class _CAttentionCall(ctypes.Structure):
                 ("lse", ctypes.c_void_p), ("shared", ctypes.c_void_p), ("n_shared", ctypes.c_int32), ("scale", ctypes.c_float)]
 
 
+_call = None                    # the compiled calls' module and the addresses of what they call, once the library is loaded
+_int32 = _float32 = _types = None
+
+
 def declare(lib) -> None:
     """Argument types of the entry points (called once, when the library is loaded)."""
     vp, sz, i32, i64 = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int, ctypes.c_int64
@@ -45,19 +49,18 @@ def declare(lib) -> None:
                             ("fbq_attention_workspace_bytes", sz, [ap]), ("fbq_attention", i32, [ap, vp, sz, vp])):
         f = getattr(lib, name)
         f.restype, f.argtypes = res, args
-
-
-def _types():
+    global _call, _int32, _float32, _types
     import torch
-    return {torch.float16: 0, torch.bfloat16: 1}
+    from . import _fbq_call
+    _int32, _float32, _types = torch.int32, torch.float32, {torch.float16: 0, torch.bfloat16: 1}
+    _call = (_fbq_call, *(ctypes.cast(getattr(lib, n), vp).value for n in ("fbq_attention", "fbq_cache_append")))
 
 
 def _ints(t, what: str, n: Optional[int] = None):
     """Pointer of a device int32 tensor (None: NULL)."""
     if t is None:
         return None
-    import torch
-    if t.dtype != torch.int32 or (n is not None and t.numel() != n):
+    if t.dtype != _int32 or (n is not None and t.numel() != n):
         raise ValueError(f"{what}: expected int32" + ("" if n is None else f", {n} of them"))
     return _dev_ptr(t)
 
@@ -70,18 +73,20 @@ class Cache:
     lengths: "object"
     refs: "object"
     _c: "object" = field(init=False, repr=False, compare=False)
+    _at: int = field(init=False, repr=False, compare=False)
 
     def __post_init__(self):
-        types = _types()
-        if self.pool.dim() != 6 or self.pool.shape[2] != 2 or self.pool.dtype not in types:
+        lib = fbq.load()
+        if self.pool.dim() != 6 or self.pool.shape[2] != 2 or self.pool.dtype not in _types:
             raise ValueError("pool: expected [layers, pages, 2, kv_heads, page_size, head_dim], float16 or bfloat16")
         if self.table.dim() != 2:
             raise ValueError("table: expected [rows, max_pages]")
         layers, pages, _, kv_heads, page, dim = self.pool.shape
         rows, width = self.table.shape
-        d = _CCacheDesc(layers, pages, page, kv_heads, dim, types[self.pool.dtype])
+        d = _CCacheDesc(layers, pages, page, kv_heads, dim, _types[self.pool.dtype])
         self._c = _CCache(d, rows, width, _dev_ptr(self.pool), _ints(self.table, "table"), _ints(self.lengths, "lengths", rows), _ints(self.refs, "refs", pages))
-        _check(int(fbq.load().fbq_check_cache(ctypes.byref(d))), "Cache")
+        _check(lib.fbq_check_cache(ctypes.byref(d)), "Cache")
+        self._at = ctypes.addressof(self._c)
 
     @property
     def heads(self) -> int:
@@ -110,10 +115,9 @@ def cache_create(layers: int, pages: int, page_size: int, kv_heads: int, head_di
 def cache_reserve(cache: Cache, count, start=None, info=None, stream=None):
     """fbq_cache_reserve: pages for count[b] more tokens of each row -> start [rows], where they begin (-1: no pages left for this row)."""
     if start is None:
-        import torch
-        start = torch.empty_like(cache.lengths)
+        start = cache.lengths.new_empty(cache.lengths.shape)
     rows = cache._c.rows
-    _check(fbq.load().fbq_cache_reserve(ctypes.byref(cache._c), _ints(count, "count", rows), _ints(start, "start", rows), _ints(info, "info"), _stream(stream)),
+    _check(fbq.load().fbq_cache_reserve(cache._c, _ints(count, "count", rows), _ints(start, "start", rows), _ints(info, "info"), _stream(stream)),
            "fbq_cache_reserve")
     return start
 
@@ -133,18 +137,21 @@ def _tokens(cache: Cache, t, what: str, heads: Optional[int] = None):
 def cache_append(cache: Cache, layer: int, k, v, start, q_start=None, stream=None) -> None:
     """fbq_cache_append: k, v [T, kv_heads, head_dim] of one layer into the pages of their rows, from position start[b] on (see cache_reserve).
     q_start [rows + 1]: the rows' tokens in k and v; None: one token a row."""
+    rc = _call[0].append(_call[2], cache._at, cache.pool.dtype, _int32, layer, k, v, start, q_start, _stream(stream))
+    if rc is not None:                                        # (None: something is not as it should be; below it is named)
+        return _check(rc, "fbq_cache_append")
     kp, ks, T = _tokens(cache, k, "k", cache.heads)
     vp, vs, Tv = _tokens(cache, v, "v", cache.heads)
     if T != Tv:
         raise ValueError("k and v: as many tokens")
     rows = cache._c.rows
-    _check(fbq.load().fbq_cache_append(ctypes.byref(cache._c), int(layer), T, _ints(q_start, "q_start", rows + 1), _ints(start, "start", rows), kp, ks, vp, vs,
+    _check(fbq.load().fbq_cache_append(cache._c, int(layer), T, _ints(q_start, "q_start", rows + 1), _ints(start, "start", rows), kp, ks, vp, vs,
                                        _stream(stream)), "fbq_cache_append")
 
 
 def cache_free(cache: Cache, rows, stream=None) -> None:
     """fbq_cache_free: empties the rows of an int32 list."""
-    _check(fbq.load().fbq_cache_free(ctypes.byref(cache._c), rows.numel(), _ints(rows, "rows"), _stream(stream)), "fbq_cache_free")
+    _check(fbq.load().fbq_cache_free(cache._c, rows.numel(), _ints(rows, "rows"), _stream(stream)), "fbq_cache_free")
 
 
 def _room(cache: Cache, n: int):
@@ -161,14 +168,14 @@ def cache_fork(cache: Cache, parent, child, info=None, workspace=None, stream=No
     n = parent.numel()
     if workspace is None:
         workspace = _room(cache, n)
-    _check(fbq.load().fbq_cache_fork(ctypes.byref(cache._c), n, _ints(parent, "parent"), _ints(child, "child", n), _ints(info, "info"), _dev_ptr(workspace),
+    _check(fbq.load().fbq_cache_fork(cache._c, n, _ints(parent, "parent"), _ints(child, "child", n), _ints(info, "info"), _dev_ptr(workspace),
                                      _size(workspace), _stream(stream)), "fbq_cache_fork")
 
 
 def cache_copy(cache: Cache, src, dst, stream=None) -> None:
     """fbq_cache_copy: page dst[i] = page src[i] in all layers (int32 lists)."""
     n = src.numel()
-    _check(fbq.load().fbq_cache_copy(ctypes.byref(cache._c), n, _ints(src, "src"), _ints(dst, "dst", n), _stream(stream)), "fbq_cache_copy")
+    _check(fbq.load().fbq_cache_copy(cache._c, n, _ints(src, "src"), _ints(dst, "dst", n), _stream(stream)), "fbq_cache_copy")
 
 
 def cache_compact(cache: Cache, out: Optional[Cache] = None, info=None, workspace=None, stream=None) -> Cache:
@@ -179,20 +186,19 @@ def cache_compact(cache: Cache, out: Optional[Cache] = None, info=None, workspac
         raise ValueError("out: a cache of the same shape")
     if workspace is None:
         workspace = _room(cache, 0)
-    _check(fbq.load().fbq_cache_compact(ctypes.byref(cache._c), out._c.table, out._c.refs, _ints(info, "info"), _dev_ptr(workspace), _size(workspace),
+    _check(fbq.load().fbq_cache_compact(cache._c, out._c.table, out._c.refs, _ints(info, "info"), _dev_ptr(workspace), _size(workspace),
                                         _stream(stream)), "fbq_cache_compact")
     return out
 
 
-def _call(cache: Cache, layer: int, q, q_start, max_q: int, shared, scale, out, lse) -> _CAttentionCall:
+def _arguments(cache: Cache, layer: int, q, q_start, max_q: int, shared, scale, out, lse) -> _CAttentionCall:
     qp, qs, T = _tokens(cache, q, "q")
     heads = int(q.shape[1])
     op, os_ = (None, heads * cache.head_dim) if out is None else _tokens(cache, out, "out", heads)[:2]
     if out is not None and out.shape[0] != T:
         raise ValueError("out: expected q's shape")
     if lse is not None:
-        import torch
-        if lse.dtype != torch.float32 or tuple(lse.shape) != (T, heads):
+        if lse.dtype != _float32 or tuple(lse.shape) != (T, heads):
             raise ValueError("lse: expected float32 [T, heads]")
     return _CAttentionCall(cache._c, int(layer), heads, T, int(max_q), _ints(q_start, "q_start", cache._c.rows + 1), qp, qs, op, os_, _dev_ptr(lse),
                            _ints(shared, "shared"), 0 if shared is None else shared.numel(), cache.head_dim ** -0.5 if scale is None else float(scale))
@@ -203,7 +209,7 @@ def attention_workspace(cache: Cache, q, q_start=None, max_q: int = 1, shared=No
     import torch
     if q_start is None and max_q > 1:                         # (only its presence counts)
         q_start = torch.empty(cache._c.rows + 1, dtype=torch.int32, device=q.device)
-    c = _call(cache, 0, q, q_start, max_q, shared, None, None, None)
+    c = _arguments(cache, 0, q, q_start, max_q, shared, None, None, None)
     return torch.empty(max(16, fbq.load().fbq_attention_workspace_bytes(ctypes.byref(c))), dtype=torch.uint8, device=q.device)
 
 
@@ -217,7 +223,14 @@ def attention(cache: Cache, layer: int, q, q_start=None, max_q: int = 1, shared=
         import torch
         if out is None:
             out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    c = _call(cache, layer, q, q_start, max_q, shared, scale, out, lse)
+    scale = cache.head_dim ** -0.5 if scale is None else float(scale)
+    if workspace is not None:
+        # one row of 33 tokens, us a call: CALL_BEFORE by way of ctypes' argument objects, CALL_AFTER this way
+        rc = _call[0].attention(_call[1], cache._at, cache.pool.dtype, _int32, _float32, layer, q, q_start, max_q, shared, scale, out, lse, workspace, _stream(stream))
+        if rc is not None:
+            _check(rc, "fbq_attention")
+            return out
+    c = _arguments(cache, layer, q, q_start, max_q, shared, scale, out, lse)
     lib = fbq.load()
     if workspace is None:
         workspace = torch.empty(max(16, lib.fbq_attention_workspace_bytes(ctypes.byref(c))), dtype=torch.uint8, device=q.device)

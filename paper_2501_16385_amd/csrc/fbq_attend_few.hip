@@ -60,10 +60,9 @@ __global__ __launch_bounds__(64 * kFewWaves, DP == 256 ? 1 : 2) void fbq_attend_
     } else {
         int own = 0;
         for (int b = lane; b < a.rows; b += 64) own += few_steps(a, b);
-#pragma unroll
-        for (int o = 32; o; o >>= 1) own += __shfl_xor(own, o);
+        own = __builtin_amdgcn_readlane(wave_scan(own), 63);
         const int shared_steps = a.shared_here ? (a.n_shared + kFewTile - 1) / kFewTile : 0;
-        const int total = uniform(own + shared_steps) * a.kv_heads;
+        const int total = (own + shared_steps) * a.kv_heads;
         const int share = few_share(a, total);
         u = min(worker, total) * share;                       // (worker * share within an int)
         end = min(total, u + share);
@@ -79,12 +78,7 @@ __global__ __launch_bounds__(64 * kFewWaves, DP == 256 ? 1 : 2) void fbq_attend_
             while (true) {
                 tokens = base + lane < a.rows ? row_tokens(a, base + lane) : 0;
                 mine = base + lane < a.rows ? few_steps(a, base + lane, tokens) : 0;
-                sum = mine;
-#pragma unroll
-                for (int o = 1; o < 64; o <<= 1) {
-                    const int x = __shfl_up(sum, o);
-                    if (lane >= o) sum += x;
-                }
+                sum = wave_scan(mine);
                 const int some = __builtin_amdgcn_readlane(sum, 63);
                 if ((long)rest < (long)(before + some) * a.kv_heads) break;
                 before += some;

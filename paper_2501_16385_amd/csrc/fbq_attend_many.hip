@@ -62,9 +62,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void fbq_attend_many_kernel
         } else {
             int all = 0;
             for (int x = lane; x < a.rows; x += 64) all += tiles_of(a, x);
-#pragma unroll
-            for (int o = 32; o; o >>= 1) all += __shfl_xor(all, o);
-            all = uniform(all);
+            all = __builtin_amdgcn_readlane(wave_scan(all), 63);
             if (tile >= all) return;                          // the grid has a block for the most tiles there could be
             // Blocks that are all on the GPU at once share CUs two by two, the first with the one half the grid on: the second half goes from short to long.
             const int half = (all + 1) / 2;
@@ -72,13 +70,8 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void fbq_attend_many_kernel
             int before = 0, base = 0, mine, sum;
             while (true) {
                 mine = base + lane < a.rows ? tiles_of(a, base + lane) : 0;
-                sum = mine;
-#pragma unroll
-                for (int o = 1; o < 64; o <<= 1) {
-                    const int x = __shfl_up(sum, o);
-                    if (lane >= o) sum += x;
-                }
-                const int some = uniform(__shfl(sum, 63));
+                sum = wave_scan(mine);
+                const int some = __builtin_amdgcn_readlane(sum, 63);
                 if (tile < before + some) break;
                 before += some;
                 base += 64;

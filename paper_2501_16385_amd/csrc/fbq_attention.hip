@@ -31,11 +31,8 @@ __global__ __launch_bounds__(THREADS) void fbq_join_pieces_kernel(const AttendAr
         all += steps;
         before += x < b ? steps : 0;
     }
-#pragma unroll
-    for (int o = 32; o; o >>= 1) {
-        all += __shfl_xor(all, o);
-        before += __shfl_xor(before, o);
-    }
+    all = __builtin_amdgcn_readlane(wave_scan(all), 63);
+    before = __builtin_amdgcn_readlane(wave_scan(before), 63);
     const int shared_steps = a.shared_here ? (a.n_shared + kFewTile - 1) / kFewTile : 0, steps = few_steps(a, b);
     const int share = few_share(a, (all + shared_steps) * a.kv_heads);
     const int own0 = (shared_steps + before) * a.kv_heads + h * steps, own1 = own0 + steps, shared0 = h * shared_steps, shared1 = shared0 + shared_steps;

@@ -35,6 +35,18 @@ fbq_status check_cache(const fbq_cache *c, bool refs);
 
 inline bool aligned(const void *p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
 
+// Sum over this lane and those before it in the wave; the last lane has all.  (Six additions of neighbours' registers; by way of LDS each would wait for it.)
+__device__ __forceinline__ int wave_scan(int x)
+{
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);   // within 16 lanes, by 1, 2, 4, 8
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);   // lane 15's to the second 16 of each 32
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);   // lane 31's to the second 32
+    return x;
+}
+
 // How many of its tokens a row is taken to have, whatever its length says.
 __device__ __forceinline__ int tokens_of(int length, int max_tokens) { return min(max(length, 0), max_tokens); }
 

@@ -18,27 +18,17 @@ constexpr int kCopyBytes = kCopyThreads * kCopyPieces * 16;   // 16 KiB a block
 
 static int chunks_of(long page_bytes) { return (int)((page_bytes + kCopyBytes - 1) / kCopyBytes); }
 
-// Sum over the block and of the threads before this one; `scratch` kPlanThreads / 64 + 1 words.  All threads call it.
+// Sum over the block and of the threads before this one; `scratch` a word a wave.  All threads call it.
 __device__ __forceinline__ int block_scan(int v, int *scratch, int *total)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int s = v;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const int u = __shfl_up(s, o);
-        if (lane >= o) s += u;
-    }
+    constexpr int kWaves = kPlanThreads / 64;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, s = wave_scan(v);
     __syncthreads();                                          // (scratch may still be read from the scan before)
     if (lane == 63) scratch[wave] = s;
     __syncthreads();
-    int before = 0, all = 0;
-    for (int w = 0; w < kPlanThreads / 64; ++w) {
-        const int x = scratch[w];
-        before += w < wave ? x : 0;
-        all += x;
-    }
-    *total = all;
-    return before + s - v;
+    const int mine = lane < kWaves ? scratch[lane] : 0, sums = wave_scan(mine);
+    *total = __builtin_amdgcn_readlane(sums, 63);
+    return __builtin_amdgcn_readlane(sums - mine, __builtin_amdgcn_readfirstlane(wave)) + s - v;
 }
 
 __device__ __forceinline__ void copy_chunk(const unsigned char *src, unsigned char *dst, long page_bytes, int chunk)
@@ -53,56 +43,68 @@ __device__ __forceinline__ void copy_chunk(const unsigned char *src, unsigned ch
         if (at + i * (kCopyThreads * 16) < page_bytes) *reinterpret_cast<word4_t *>(dst + at + i * (kCopyThreads * 16)) = v[i];
 }
 
+// The free ones of this thread's pages of the chunk that begins with page p0, a bit each.
+__device__ __forceinline__ unsigned free_pages_of(const CacheArgs &c, int p0)
+{
+    unsigned is_free = 0;
+#pragma unroll
+    for (int k = 0; k < kRefsPerThread; ++k) {
+        const int p = p0 + threadIdx.x * kRefsPerThread + k;
+        is_free |= (p < c.pages && c.refs[p] == 0 ? 1u : 0u) << k;
+    }
+    return is_free;
+}
+
 // Deals out free pages, lowest first, to askers 0 .. n-1 that want need(i) each; who does not fit among the free ones together with all before it gets none.
-// give(i, k, page): asker i's k-th page;  done(i, served) once for every asker, after all need() calls and before any give().  Returns the pages lacking.
+// give(i, k, page): asker i's k-th page;  done(i, served) once for every asker, after its need() calls and before any give().  Returns the pages lacking.
+// A chain of loads and scans in one block: the first chunk's reference counts are asked for before anything else, since they mostly suffice.
 template <class Need, class Give, class Done>
 __device__ __forceinline__ int deal_pages(const CacheArgs &c, int n, Need need, Give give, Done done)
 {
     __shared__ int scratch[kPlanThreads / 64];
     __shared__ int first[kPlanThreads];
     const int tid = threadIdx.x;
-    long wanted = 0;
-    for (int i0 = 0; i0 < n; i0 += kPlanThreads) {
-        int all;
-        block_scan(i0 + tid < n ? need(i0 + tid) : 0, scratch, &all);
-        wanted += all;
+    const unsigned free0 = free_pages_of(c, 0);
+    int mine = tid < n ? need(tid) : 0, all, before = block_scan(mine, scratch, &all);
+    long wanted = all;
+    for (int i0 = kPlanThreads; i0 < n; i0 += kPlanThreads) {
+        int some;
+        block_scan(i0 + tid < n ? need(i0 + tid) : 0, scratch, &some);
+        wanted += some;
     }
     long free_pages = 0;                                      // found; counted on only while fewer than wanted
-    for (int p0 = 0; p0 < c.pages && free_pages < wanted; p0 += kRefsChunk) {
-        int mine = 0, all;
-#pragma unroll
-        for (int k = 0; k < kRefsPerThread; ++k) {
-            const int p = p0 + tid * kRefsPerThread + k;
-            mine += p < c.pages && c.refs[p] == 0;
+    int rank_of0 = 0, found0 = 0;
+    if (wanted > 0) {
+        rank_of0 = block_scan(__popc(free0), scratch, &found0);
+        free_pages = found0;
+        for (int p0 = kRefsChunk; p0 < c.pages && free_pages < wanted; p0 += kRefsChunk) {
+            int some;
+            block_scan(__popc(free_pages_of(c, p0)), scratch, &some);
+            free_pages += some;
         }
-        block_scan(mine, scratch, &all);
-        free_pages += all;
     }
     long dealt = 0;
     int p0 = 0;                                               // pages before this chunk are all taken
     for (int i0 = 0; i0 < n; i0 += kPlanThreads) {
-        const int i = i0 + tid, mine = i < n ? need(i) : 0;
-        int all;
-        const int before = block_scan(mine, scratch, &all);
+        const int i = i0 + tid;
+        if (i0) {
+            mine = i < n ? need(i) : 0;
+            before = block_scan(mine, scratch, &all);
+        }
         const bool served = mine == 0 || dealt + before + mine <= free_pages;
+        int give_total = all;                                        // who is served comes first: their ranks are `first`'s
+        if (wanted > free_pages) block_scan(served ? mine : 0, scratch, &give_total);
         first[tid] = before;
-        int give_total;
-        block_scan(served ? mine : 0, scratch, &give_total);         // (those served come first: their ranks are `first`'s)
         if (i < n) done(i, served);
+        __syncthreads();
         int rank0 = 0;
         while (rank0 < give_total && p0 < c.pages) {
-            bool is_free[kRefsPerThread];
-            int count = 0, found;
+            const bool again = i0 > 0 || p0 > 0;                     // (the first chunk, before anything was dealt from it, is known)
+            const unsigned is_free = again ? free_pages_of(c, p0) : free0;
+            int found = found0, rank = rank0 + (again ? block_scan(__popc(is_free), scratch, &found) : rank_of0);   // (its barriers lie between reads of refs and writes)
 #pragma unroll
             for (int k = 0; k < kRefsPerThread; ++k) {
-                const int p = p0 + tid * kRefsPerThread + k;
-                is_free[k] = p < c.pages && c.refs[p] == 0;
-                count += is_free[k];
-            }
-            int rank = rank0 + block_scan(count, scratch, &found);   // (its barriers are behind the reads of refs, in front of the writes)
-#pragma unroll
-            for (int k = 0; k < kRefsPerThread; ++k) {
-                if (!is_free[k]) continue;
+                if (!(is_free >> k & 1)) continue;
                 if (rank < give_total) {
                     int lo = 0, hi = min(kPlanThreads, n - i0);      // the last asker with first[lo] <= rank
                     while (hi - lo > 1) {
@@ -271,33 +273,8 @@ __global__ __launch_bounds__(kPlanThreads) void fbq_compact_plan_kernel(CacheArg
     __shared__ int scratch[kPlanThreads / 64];
     const int tid = threadIdx.x;
     int live = 0, before = 0;                                 // pages in use in all, and below this chunk
-    for (int i0 = 0; i0 < w.chunks; i0 += kPlanThreads) {
-        const int x = i0 + tid < w.chunks ? w.chunk[i0 + tid] : 0;
-        int all, below;
-        block_scan(x, scratch, &all);
-        block_scan(i0 + tid < (int)blockIdx.x ? x : 0, scratch, &below);
-        live += all;
-        before += below;
-    }
-    // pages in use below n: whole chunks, and the part of the one that n lies in
-    const int cut = live / kRefsChunk;
-    int low = 0;
-    for (int i0 = 0; i0 < cut; i0 += kPlanThreads) {
-        int all;
-        block_scan(i0 + tid < cut ? w.chunk[i0 + tid] : 0, scratch, &all);
-        low += all;
-    }
-    int mine = 0, all;
-#pragma unroll
-    for (int k = 0; k < kRefsPerThread; ++k) {
-        const int p = cut * kRefsChunk + tid * kRefsPerThread + k;
-        mine += p < live && p < c.pages && c.refs[p] > 0;
-    }
-    block_scan(mine, scratch, &all);
-    low += all;
     bool used[kRefsPerThread];
-    int refs[kRefsPerThread];
-    mine = 0;
+    int refs[kRefsPerThread], mine = 0, all;
 #pragma unroll
     for (int k = 0; k < kRefsPerThread; ++k) {
         const int p = blockIdx.x * kRefsChunk + tid * kRefsPerThread + k;
@@ -305,7 +282,33 @@ __global__ __launch_bounds__(kPlanThreads) void fbq_compact_plan_kernel(CacheArg
         used[k] = refs[k] > 0;
         mine += used[k];
     }
-    int at = before + block_scan(mine, scratch, &all);        // pages in use below this thread's
+    int at = block_scan(mine, scratch, &live);                // pages in use below this thread's, in this chunk
+    if (w.chunks > 1) live = 0;
+    for (int i0 = 0; w.chunks > 1 && i0 < w.chunks; i0 += kPlanThreads) {
+        const int x = i0 + tid < w.chunks ? w.chunk[i0 + tid] : 0;
+        int all, below;
+        block_scan(x, scratch, &all);
+        block_scan(i0 + tid < (int)blockIdx.x ? x : 0, scratch, &below);
+        live += all;
+        before += below;
+    }
+    // pages in use below n: whole chunks, and the part of the one that n lies in (a single chunk has not been counted: all of it is the part)
+    const int cut = w.chunks > 1 ? live / kRefsChunk : 0;
+    int low = 0;
+    for (int i0 = 0; i0 < cut; i0 += kPlanThreads) {
+        int all;
+        block_scan(i0 + tid < cut ? w.chunk[i0 + tid] : 0, scratch, &all);
+        low += all;
+    }
+    mine = 0;
+#pragma unroll
+    for (int k = 0; k < kRefsPerThread; ++k) {
+        const int p = cut * kRefsChunk + tid * kRefsPerThread + k;
+        mine += p < live && p < c.pages && c.refs[p] > 0;
+    }
+    block_scan(mine, scratch, &all);
+    low += all;
+    at += before;                                             // ... of all
 #pragma unroll
     for (int k = 0; k < kRefsPerThread; ++k) {
         const int p = blockIdx.x * kRefsChunk + tid * kRefsPerThread + k;
@@ -494,7 +497,7 @@ extern "C" fbq_status fbq_cache_compact(const fbq_cache *c, int32_t *table_out, 
     const int chunks = chunks_of(a.page_bytes);
     const int table_blocks = (int)std::min<long>(256, (std::max((long)a.rows * a.max_pages, (long)a.pages) + kCopyThreads * 4 - 1) / (kCopyThreads * 4));
     const long most = (long)(a.pages / 2) * a.layers * chunks;
-    hipLaunchKernelGGL(fbq_count_pages_kernel, dim3(w.chunks), dim3(kPlanThreads), 0, (hipStream_t)stream, a, w);
+    if (w.chunks > 1) hipLaunchKernelGGL(fbq_count_pages_kernel, dim3(w.chunks), dim3(kPlanThreads), 0, (hipStream_t)stream, a, w);
     hipLaunchKernelGGL(fbq_compact_plan_kernel, dim3(w.chunks), dim3(kPlanThreads), 0, (hipStream_t)stream, a, w, refs_out, info);
     hipLaunchKernelGGL(fbq_compact_kernel, dim3(table_blocks + (unsigned)std::min<long>(2048, most)), dim3(kCopyThreads), 0, (hipStream_t)stream, a, w, table_out,
                        refs_out, table_blocks, chunks);

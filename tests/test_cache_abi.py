@@ -64,9 +64,11 @@ def test_sizes():
     assert lib.fbq_cache_bytes(ctypes.byref(d)) == 2 * 8 * 2 * 2 * 16 * 64 * 2
     assert lib.fbq_cache_workspace_bytes(ctypes.byref(d), 5) >= 5 * 8 and lib.fbq_cache_workspace_bytes(ctypes.byref(d), 0) >= 3 * 8 * 4
     assert lib.fbq_cache_workspace_bytes(ctypes.byref(d), -1) == 0
-    assert lib.fbq_attention_workspace_bytes(ctypes.byref(call())) > 0 and lib.fbq_attention_workspace_bytes(None) == 0
-    bare = call(cache(pool=None, table=None, lengths=None, refs=None), q=None, out=None)
-    assert lib.fbq_attention_workspace_bytes(ctypes.byref(bare)) == lib.fbq_attention_workspace_bytes(ctypes.byref(call()))   # pointers are not looked at
+    assert lib.fbq_attention_workspace_bytes(ctypes.byref(call())) == 0          # rows of at most 96 tokens: nothing to join
+    wide = call(cache(max_pages=64))
+    assert lib.fbq_attention_workspace_bytes(ctypes.byref(wide)) > 0 and lib.fbq_attention_workspace_bytes(None) == 0
+    bare = call(cache(max_pages=64, pool=None, table=None, lengths=None, refs=None), q=None, out=None)
+    assert lib.fbq_attention_workspace_bytes(ctypes.byref(bare)) == lib.fbq_attention_workspace_bytes(ctypes.byref(wide))     # pointers are not looked at
 
 
 def test_page_operations():
@@ -94,16 +96,16 @@ def test_page_operations():
 
 def test_attention():
     lib = fbq.load()
-    go = lambda ws=OK, size=1 << 40, **over: lib.fbq_attention(ctypes.byref(call(**over)), ws, size, None)
+    go = lambda ws=OK, size=1 << 40, **over: lib.fbq_attention(ctypes.byref(call(cache(max_pages=64), **over)), ws, size, None)
     assert lib.fbq_attention(None, OK, 1 << 40, None) == 1
     for bad in (dict(layer=2), dict(layer=-1), dict(heads=0), dict(heads=3), dict(T=0), dict(T=3), dict(max_q=2), dict(max_q=0), dict(q_start=OK, T=9, max_q=10), dict(n_shared=-1),
-                dict(n_shared=7, shared=OK), dict(q_stride=248), dict(out_stride=255), dict(q_stride=260)):
+                dict(n_shared=65, shared=OK), dict(q_stride=248), dict(out_stride=255), dict(q_stride=260)):
         assert go(**bad) == 2, bad
-        assert lib.fbq_attention_workspace_bytes(ctypes.byref(call(**bad))) == 0, bad
+        assert lib.fbq_attention_workspace_bytes(ctypes.byref(call(cache(max_pages=64), **bad))) == 0, bad
     assert go(heads=16384, q_stride=1 << 20, out_stride=1 << 20) == go(q_start=OK, T=(1 << 20) + 1, max_q=5) == go(q_stride=1 << 33) == 3
     assert go(q=None) == go(out=None) == go(n_shared=2) == go(ws=None) == 1
     assert go(q=ODD8) == go(out=ODD8) == go(lse=ODD2) == go(q_start=ODD2, T=8, max_q=3) == go(shared=ODD2, n_shared=1) == go(ws=ODD8) == 4
-    assert go(size=lib.fbq_attention_workspace_bytes(ctypes.byref(call())) - 1) == 5
+    assert go(size=lib.fbq_attention_workspace_bytes(ctypes.byref(call(cache(max_pages=64)))) - 1) == 5
 
 
 def test_the_binding_refuses_tensors_that_are_not_as_they_should_be():

@@ -250,6 +250,15 @@ def test_compact(layers, pages, page, heads, D, in_place):
     p.compact(in_place)
 
 
+@pytest.mark.parametrize("pages", [4096, 8192])
+def test_compact_of_a_pool_in_use_to_the_last_page(pages):
+    p = Pair(1, pages, 16, 1, 16, 4, pages)
+    p.reserve([16 * pages // 2, 16 * pages // 2, 0, 0])
+    p.compact(True)
+    p.free([0])
+    p.compact(False)
+
+
 def test_copy_pages():
     import paper_2501_16385_amd as fbq
     cache = fbq.cache_create(3, 20, 64, 3, 80, 1, 1)
