@@ -51,7 +51,7 @@ struct AttendArgs {
     bool direct;                         // an item a worker, no partial results
     bool shared_here;                    // the shared tokens are items of this kernel's own, for the rows of all sequences together
     Partials piece, whole, whole_shared;
-    // many-row kernel: `splits` of the keys, partial results [splits][T heads] (null: out is written)
+    // many-row kernel: at most `splits` pieces of a tile's keys, partial results [splits][T heads] (null: out is written); shared_splits of the shared tokens
     int splits, shared_splits;
     Partials part, part_shared;
 };
@@ -112,6 +112,38 @@ __device__ __forceinline__ int few_steps(const AttendArgs &a, int b) { return fe
 
 // How many steps each worker takes, from all there are: the last ones may have none.
 __device__ __forceinline__ int few_share(const AttendArgs &a, int steps) { return max(1, (steps + a.workers - 1) / a.workers); }
+
+// Many-row kernel: tiles of a row's queries; keys that a tile's last query sees; steps to there.
+__device__ __forceinline__ int many_tiles(const AttendArgs &a, int queries) { return (queries * a.group + kManyRows - 1) / kManyRows; }
+__device__ __forceinline__ int many_limit(const AttendArgs &a, int tokens, int queries, int tile)
+{
+    return max(0, min(tokens, tokens - queries + min(queries - 1, ((tile + 1) * kManyRows - 1) / a.group) + 1));
+}
+__device__ __forceinline__ int many_steps(const AttendArgs &a, int limit) { return (max(limit - a.n_shared, 0) + kManyTile - 1) / kManyTile; }
+
+// How many steps a piece of a tile has at most.  A piece more writes and reads 128 rows of partial results again, as dear as about six steps, and pieces that do not all fit
+// the GPU at once wait for each other: so tiles are cut into as many as there is room for, the average tile and a little taken, and where there is none, those twice as long.
+// (61 tiles of 8 heads and about 100 steps, cut in two where that was above an even share: 243 us; uncut 160.)  The whole wave calls it.
+__host__ __device__ __forceinline__ constexpr int many_blocks(int D) { return D > 128 ? 256 : 512; }
+__device__ __forceinline__ int many_share(const AttendArgs &a)
+{
+    float steps = 0, tiles = 0;
+    for (int b = threadIdx.x & 63; b < a.rows; b += 64) {
+        const int n = queries_of(a, b).y, of_row = many_tiles(a, n), tokens = row_tokens(a, b);
+        if (of_row) steps += 0.5f * of_row * (many_steps(a, many_limit(a, tokens, n, 0)) + many_steps(a, tokens));
+        tiles += of_row;
+    }
+#pragma unroll
+    for (int o = 32; o; o >>= 1) {
+        steps += __shfl_xor(steps, o);
+        tiles += __shfl_xor(tiles, o);
+    }
+    const float mean = steps / fmaxf(tiles, 1.0f);
+    const int fit = (int)(many_blocks(a.D) / (fmaxf(tiles, 1.0f) * a.kv_heads));
+    return __builtin_amdgcn_readfirstlane(fit >= 2 ? max(4, (int)ceilf(1.2f * mean / fit)) : (int)(2 * mean) + 6);
+}
+// Pieces of a tile of so many steps.
+__device__ __forceinline__ int many_pieces(const AttendArgs &a, int steps, int share) { return max(1, min(a.splits, (steps + share - 1) / share)); }
 
 // A value that is the same in all lanes, as one the compiler knows to be.
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }

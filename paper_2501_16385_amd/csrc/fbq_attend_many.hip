@@ -26,9 +26,6 @@ __device__ __forceinline__ word2_t read_turned4(const unsigned char *at)
     return __builtin_bit_cast(word2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_four_t *)(__attribute__((address_space(3))) const void *)at));
 }
 
-// Tiles of a row's queries.
-__device__ __forceinline__ int tiles_of(const AttendArgs &a, int b) { return (queries_of(a, b).y * a.group + kManyRows - 1) / kManyRows; }
-
 // f(0), f(1) .. f(N - 1), each with its number as a constant
 template <int N, class F>
 __device__ __forceinline__ void each(F f)
@@ -48,44 +45,61 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void fbq_attend_many_kernel
 
     const int lane = threadIdx.x & 63, col = lane & 31, grp = lane >> 5, wave = uniform(threadIdx.x >> 6);
     const int D = a.D, ps1 = (1 << a.log_ps) - 1;
-    const int h = blockIdx.x, split = blockIdx.z, splits = shared ? a.shared_splits : a.splits;
+    const int h = blockIdx.x;
 
-    // the row of the table and the tile of its query rows (for the shared tokens all query tokens are one row's)
-    int b = 0, q0 = 0, nq = a.T, limit = a.n_shared, tile = blockIdx.y;
+    // the row of the table, the tile of its query rows and the piece of the tile's keys (for the shared tokens all query tokens are one row's)
+    int b = 0, q0 = 0, nq = a.T, limit = a.n_shared, tile = blockIdx.y, split = blockIdx.z, splits = a.shared_splits, tokens_of_row = 0;
     if (!shared) {
-        if (!a.q_start) {
-            const int per = (a.group + kManyRows - 1) / kManyRows;
-            b = tile / per;
-            tile -= b * per;
-            q0 = b;
-            nq = 1;
+        const int share = a.splits == 1 ? 1 << 30 : many_share(a);
+        int queries, tokens, tiles, pieces, count, longest;   // of the table row that is this lane's
+        const auto look = [&](int row) {
+            queries = row < a.rows ? queries_of(a, row).y : 0;
+            tokens = row < a.rows ? row_tokens(a, row) : 0;
+            tiles = many_tiles(a, queries);
+            pieces = many_pieces(a, many_steps(a, tokens), share);
+            count = tiles * pieces;
+            longest = (many_steps(a, tokens) + pieces - 1) / pieces;
+        };
+        int all = 0;
+        for (int base = 0; base < a.rows; base += 64) {
+            look(base + lane);
+            all += __builtin_amdgcn_readlane(wave_scan(count), 63);
+        }
+        int index = blockIdx.y;
+        if (index >= all) return;                             // the grid has a block for the most there could be
+        // Long pieces first: the rows by their longest piece where a wave knows them all, the tiles of a row from its last to its first.  Blocks that are all on the GPU at once
+        // share CUs two by two, the first with the one half the grid on: then the second half goes from short to long.
+        const int half = (all + 1) / 2;
+        if (index >= half && (long)all * a.kv_heads <= many_blocks(D)) index = all - 1 - (index - half);
+        int offset = 0, base = 0;
+        if (a.rows <= 64) {
+            for (int x = 0; x < a.rows; ++x) {
+                const int other = __builtin_amdgcn_readlane(longest, x);
+                if (other > longest || (other == longest && x < lane)) offset += __builtin_amdgcn_readlane(count, x);
+            }
         } else {
-            int all = 0;
-            for (int x = lane; x < a.rows; x += 64) all += tiles_of(a, x);
-            all = __builtin_amdgcn_readlane(wave_scan(all), 63);
-            if (tile >= all) return;                          // the grid has a block for the most tiles there could be
-            // Blocks that are all on the GPU at once share CUs two by two, the first with the one half the grid on: the second half goes from short to long.
-            const int half = (all + 1) / 2;
-            if (tile >= half && (long)all * a.kv_heads * splits <= 512) tile = all - 1 - (tile - half);
-            int before = 0, base = 0, mine, sum;
+            int before = 0;
             while (true) {
-                mine = base + lane < a.rows ? tiles_of(a, base + lane) : 0;
-                sum = wave_scan(mine);
-                const int some = __builtin_amdgcn_readlane(sum, 63);
-                if (tile < before + some) break;
+                look(base + lane);
+                const int sum = wave_scan(count), some = __builtin_amdgcn_readlane(sum, 63);
+                offset = before + sum - count;
+                if (index < before + some) break;
                 before += some;
                 base += 64;
-                if (base >= a.rows) return;                   // (not unless q_start changes under the call)
+                if (base >= a.rows) return;                   // (not unless the rows change under the call)
             }
-            const int at = __builtin_ctzll(__ballot(before + sum > tile));
-            b = base + at;
-            const int tiles = __builtin_amdgcn_readlane(mine, at);
-            tile = tiles - 1 - (tile - (before + __builtin_amdgcn_readlane(sum, at) - tiles));
-            const int2 q = queries_of(a, b);
-            q0 = uniform(q.x);
-            nq = uniform(q.y);
         }
-        limit = uniform(row_tokens(a, b));
+        const int at = __builtin_ctzll(__ballot(count > 0 && offset <= index && index < offset + count));
+        b = base + at;
+        const int rest = index - __builtin_amdgcn_readlane(offset, at), row_pieces = __builtin_amdgcn_readlane(pieces, at);
+        tile = __builtin_amdgcn_readlane(tiles, at) - 1 - rest / row_pieces;
+        split = rest % row_pieces;
+        nq = __builtin_amdgcn_readlane(queries, at);
+        q0 = uniform(queries_of(a, b).x);
+        tokens_of_row = __builtin_amdgcn_readlane(tokens, at);
+        limit = many_limit(a, tokens_of_row, nq, tile);
+        splits = many_pieces(a, many_steps(a, limit), share);
+        if (split >= splits) return;
     }
 
     // this lane's query row: token, head, how many tokens it sees
@@ -103,7 +117,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void fbq_attend_many_kernel
             }
         } else {
             t = q0 + i;
-            sees = limit - nq + i + 1;
+            sees = tokens_of_row - nq + i + 1;
         }
     }
     int least = t >= 0 ? sees : limit, most = t >= 0 ? sees : 0;              // of the wave's rows
@@ -114,9 +128,8 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void fbq_attend_many_kernel
     }
     least = uniform(least);
     most = uniform(most);
-    if (!shared) limit = max(0, min(limit, limit - nq + min(nq - 1, ((tile + 1) * kManyRows - 1) / a.group) + 1));   // what the block's last row sees
-
-    const int key0 = shared ? 0 : a.n_shared, all_steps = (max(limit - key0, 0) + kManyTile - 1) / kManyTile, per = (all_steps + splits - 1) / splits;
+    const int key0 = shared ? 0 : a.n_shared, all_steps = shared ? (limit + kManyTile - 1) / kManyTile : many_steps(a, limit);
+    const int per = (all_steps + splits - 1) / splits;
     const int s0 = min(split * per, all_steps), s1 = min(s0 + per, all_steps);
 
     word4_t qf[DP / 16];
@@ -276,7 +289,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void fbq_attend_many_kernel
     if (t < 0) return;
     const Partials to = shared ? a.part_shared : a.part;
     const long row = (long)t * a.heads + head;
-    if (!to.o) {
+    if (!shared && splits == 1 && !a.part_shared.o) {
         const float by = l == 0 ? 0.0f : 1.0f / l;
         uint16_t *const at = a.out + t * a.out_stride + head * D;
 #pragma unroll
@@ -304,10 +317,10 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void fbq_attend_many_kernel
 template <class TY>
 static hipError_t launch_many(const AttendArgs &a, bool shared, hipStream_t stream)
 {
-    const long rows = (long)a.T * a.group;
+    const long rows = (long)a.T * a.group, per = (a.group + kManyRows - 1) / kManyRows;
     long tiles = (rows + kManyRows - 1) / kManyRows;          // ragged rows: each may have one more, begun
-    if (!shared) tiles = a.q_start ? std::min((long)a.T * ((a.group + kManyRows - 1) / kManyRows), tiles + a.rows) : (long)a.rows * ((a.group + kManyRows - 1) / kManyRows);
-    const dim3 grid(a.kv_heads, (unsigned)tiles, shared ? a.shared_splits : a.splits), block(256);
+    if (!shared) tiles = (a.q_start ? std::min(a.T * per, tiles + a.rows) : a.rows * per) * a.splits;
+    const dim3 grid(a.kv_heads, (unsigned)tiles, shared ? a.shared_splits : 1), block(256);
     if (a.D <= 64) hipLaunchKernelGGL((fbq_attend_many_kernel<TY, 64>), grid, block, 0, stream, a, shared);
     else if (a.D <= 96) hipLaunchKernelGGL((fbq_attend_many_kernel<TY, 96>), grid, block, 0, stream, a, shared);
     else if (a.D <= 128) hipLaunchKernelGGL((fbq_attend_many_kernel<TY, 128>), grid, block, 0, stream, a, shared);

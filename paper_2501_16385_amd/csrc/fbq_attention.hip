@@ -103,41 +103,52 @@ __global__ __launch_bounds__(THREADS) void fbq_join_pieces_kernel(const AttendAr
     if (a.lse && tid == 0) a.lse[row] = l == 0 ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
-// Many-row kernel: LANES lanes a row, four features each, its splits one behind the other.
+// Many-row kernel: LANES lanes a row, four features each, its pieces one behind the other.  No more blocks than the GPU holds: what is cut they work out once, and in most
+// calls of many rows it is nothing.
+constexpr int kJoinBlocks = 2048;
 template <class TY, int LANES>
 __global__ __launch_bounds__(kJoinThreads) void fbq_join_splits_kernel(const AttendArgs a)
 {
-    const long rows = (long)a.T * a.heads, row = (long)blockIdx.x * (kJoinThreads / LANES) + threadIdx.x / LANES;
+    const int share = a.splits == 1 ? 1 << 30 : many_share(a), n_shared = a.part_shared.o ? a.shared_splits : 0;
+    if (!n_shared) {
+        int longest = 0;                                      // steps of any row's last tile
+        for (int b = threadIdx.x & 63; b < a.rows; b += 64) longest = max(longest, queries_of(a, b).y ? many_steps(a, row_tokens(a, b)) : 0);
+        if (__ballot(longest > share) == 0) return;
+    }
+    const long rows = (long)a.T * a.heads;
     const int d = (threadIdx.x % LANES) * 4;
-    if (row >= rows || d >= a.D) return;
-    const int t = (int)(row / a.heads);
-    if (a.q_start) {                                          // a token of no row: nothing was written for it
-        const int b = row_of_token(a.q_start, a.rows, t);
-        if (b < 0 || t - a.q_start[b] >= a.max_q) return;
-    }
-    const int n_shared = a.part_shared.o ? a.shared_splits : 0, n = n_shared + a.splits;
-    const auto part = [&](int p, long *at) { return p < n_shared ? (*at = p * rows + row, a.part_shared) : (*at = (p - n_shared) * rows + row, a.part); };
-    float m = kNoScore, l = 0;
+    if (d >= a.D) return;
+    for (long row = (long)blockIdx.x * (kJoinThreads / LANES) + threadIdx.x / LANES; row < rows; row += (long)gridDim.x * (kJoinThreads / LANES)) {
+        const int t = (int)(row / a.heads), b = a.q_start ? row_of_token(a.q_start, a.rows, t) : t;
+        if (b < 0) continue;                                  // a token of no row
+        const int2 q = queries_of(a, b);
+        if (t - q.x >= q.y) continue;
+        const int head = (int)(row - (long)t * a.heads), tile = ((t - q.x) * a.group + head % a.group) / kManyRows;
+        const int n = n_shared + many_pieces(a, many_steps(a, many_limit(a, row_tokens(a, b), q.y, tile)), share);
+        if (n == 1) continue;                                 // written by its one piece
+        const auto part = [&](int p, long *at) { return p < n_shared ? (*at = p * rows + row, a.part_shared) : (*at = (p - n_shared) * rows + row, a.part); };
+        float m = kNoScore, l = 0;
 #pragma unroll 4
-    for (int p = 0; p < n; ++p) {
-        long at;
-        const Partials from = part(p, &at);
-        m = fmaxf(m, from.ml[at].x);
-    }
-    float4_t o{0, 0, 0, 0};
+        for (int p = 0; p < n; ++p) {
+            long at;
+            const Partials from = part(p, &at);
+            m = fmaxf(m, from.ml[at].x);
+        }
+        float4_t o{0, 0, 0, 0};
 #pragma unroll 4
-    for (int p = 0; p < n; ++p) {
-        long at;
-        const Partials from = part(p, &at);
-        const float2 ml = from.ml[at];
-        if (ml.y == 0) continue;
-        const float by = __builtin_amdgcn_exp2f(ml.x - m);
-        l += ml.y * by;
-        o += *reinterpret_cast<const float4_t *>(from.o + at * a.D + d) * by;
+        for (int p = 0; p < n; ++p) {
+            long at;
+            const Partials from = part(p, &at);
+            const float2 ml = from.ml[at];
+            if (ml.y == 0) continue;
+            const float by = __builtin_amdgcn_exp2f(ml.x - m);
+            l += ml.y * by;
+            o += *reinterpret_cast<const float4_t *>(from.o + at * a.D + d) * by;
+        }
+        o *= l == 0 ? 0.0f : 1.0f / l;
+        *reinterpret_cast<word2_t *>(a.out + t * a.out_stride + head * a.D + d) = word2_t{TY::pack(o[0], o[1]), TY::pack(o[2], o[3])};
+        if (a.lse && d == 0) a.lse[row] = l == 0 ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
     }
-    o *= l == 0 ? 0.0f : 1.0f / l;
-    *reinterpret_cast<word2_t *>(a.out + t * a.out_stride + (row - (long)t * a.heads) * a.D + d) = word2_t{TY::pack(o[0], o[1]), TY::pack(o[2], o[3])};
-    if (a.lse && d == 0) a.lse[row] = l == 0 ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
 template <class TY, int LANES>
@@ -146,7 +157,7 @@ static hipError_t launch_join(const AttendArgs &a, bool few, hipStream_t stream)
     const long rows = (long)a.T * a.heads, a_block = kJoinThreads / LANES;
     if (few && rows >= 2048) hipLaunchKernelGGL((fbq_join_pieces_kernel<TY, LANES, 64>), dim3((unsigned)rows), dim3(64), 0, stream, a);
     else if (few) hipLaunchKernelGGL((fbq_join_pieces_kernel<TY, LANES, kJoinThreads>), dim3((unsigned)rows), dim3(kJoinThreads), 0, stream, a);
-    else hipLaunchKernelGGL((fbq_join_splits_kernel<TY, LANES>), dim3((unsigned)((rows + a_block - 1) / a_block)), dim3(kJoinThreads), 0, stream, a);
+    else hipLaunchKernelGGL((fbq_join_splits_kernel<TY, LANES>), dim3((unsigned)std::min<long>(kJoinBlocks, (rows + a_block - 1) / a_block)), dim3(kJoinThreads), 0, stream, a);
     return hipGetLastError();
 }
 
@@ -194,8 +205,9 @@ static AttendPlan attend_plan(const fbq_attention_call &c, void *workspace)
         to->ml = (float2 *)((char *)workspace + at);
         at += ((size_t)n * 8 + 255) / 256 * 256;
     };
-    const auto splits_of = [](long blocks, long tokens) {     // so that the GPU, two blocks a CU, is about filled, with 256 keys or more each
-        return (int)std::max(1L, std::min({(512 + blocks / 2) / blocks, (tokens + 255) / 256, 32L}));
+    const long room_for = many_blocks(a.D);
+    const auto splits_of = [=](long blocks, long tokens) {     // so that the GPU is about filled, with 256 keys or more each
+        return (int)std::max(1L, std::min({(room_for + blocks / 2) / blocks, (tokens + 255) / 256, 32L}));
     };
     if (a.n_shared) {
         a.shared_here = p.few && all_queries <= kFewRows;
@@ -220,7 +232,7 @@ static AttendPlan attend_plan(const fbq_attention_call &c, void *workspace)
     } else {
         const long per_row = (a.group + kManyRows - 1) / kManyRows;
         const long tiles = a.q_start ? (all_queries + kManyRows - 1) / kManyRows : a.rows * per_row;
-        a.splits = splits_of(tiles * a.kv_heads, own_tokens);
+        a.splits = (int)std::max(1L, std::min({(2 * room_for - 1) / (tiles * a.kv_heads), (own_tokens + 255) / 256, 32L, 65535 / (tiles + a.rows)}));
         p.join = a.splits > 1 || a.n_shared;
         if (p.join) room(&a.part, a.splits * results);
     }
@@ -245,7 +257,7 @@ static fbq_status check_attention(const fbq_attention_call *c, bool pointers)
     const int64_t row = (int64_t)c->heads * d.head_dim;
     if (c->q_stride < row || c->out_stride < row || c->q_stride % 8 || c->out_stride % 8) return FBQ_ERR_SHAPE;
     if (c->heads > 8192 || c->T > (1 << 20) || c->q_stride > (1L << 32) || c->out_stride > (1L << 32)) return FBQ_ERR_UNSUPPORTED;
-    if ((int64_t)c->T * c->heads > (1L << 30) || ((int64_t)c->T * (c->heads / d.kv_heads)) / kManyRows + c->cache.rows > 65535) return FBQ_ERR_UNSUPPORTED;
+    if ((int64_t)c->T * c->heads > (1L << 30) || ((int64_t)c->T * (c->heads / d.kv_heads)) / kManyRows + c->cache.rows > 32767) return FBQ_ERR_UNSUPPORTED;
     if (!pointers) return FBQ_OK;
     if (!c->q || !c->out || (c->n_shared && !c->shared)) return FBQ_ERR_NULL;
     if (!aligned(c->q, 16) || !aligned(c->out, 16) || !aligned(c->lse, 4) || !aligned(c->q_start, 4) || !aligned(c->shared, 4)) return FBQ_ERR_ALIGN;
