@@ -9,10 +9,10 @@ constexpr int kJoinThreads = 256;
 //     out = sum_p o_p 2^(m_p - m) / sum_p l_p 2^(m_p - m),   m the largest m_p.   A part whose sum l is 0 saw nothing and has no o.
 // Bound by the latency of a chain of loads - where the parts lie, then their m, l and o at once - so as many as possible are under way together.
 
-// Few-row kernel: a block a row, LANES lanes a part, four features each.  The row's own part is either whole (written by its one piece: nothing left to do unless
-// shared tokens come with it) or cut into the pieces of the workers w0 .. w1.  THREADS: 256, or a wave where there are rows enough to fill the GPU with.
+// A block a row, LANES lanes a part, four features each.  The row's own part is either whole (written by its one piece: nothing left to do unless shared tokens come with it)
+// or cut into the pieces of the few-row kernel's workers w0 .. w1, or of the many-row kernel.  THREADS: 256, or a wave where there are rows enough to fill the GPU with.
 template <class TY, int LANES, int THREADS>
-__global__ __launch_bounds__(THREADS) void fbq_join_pieces_kernel(const AttendArgs a)
+__global__ __launch_bounds__(THREADS) void fbq_join_pieces_kernel(const AttendArgs a, const bool few)
 {
     constexpr int kGroups = THREADS / LANES, kAtOnce = 8;
     __shared__ float2 group_ml[kGroups];
@@ -25,22 +25,33 @@ __global__ __launch_bounds__(THREADS) void fbq_join_pieces_kernel(const AttendAr
     const int i = t - q.x;
     if (i >= q.y) return;
 
-    int before = 0, all = 0;                                  // steps of the rows before b, of all rows
-    for (int x = lane; x < a.rows; x += 64) {
-        const int steps = few_steps(a, x);
-        all += steps;
-        before += x < b ? steps : 0;
-    }
-    all = __builtin_amdgcn_readlane(wave_scan(all), 63);
-    before = __builtin_amdgcn_readlane(wave_scan(before), 63);
-    const int shared_steps = a.shared_here ? (a.n_shared + kFewTile - 1) / kFewTile : 0, steps = few_steps(a, b);
-    const int share = few_share(a, (all + shared_steps) * a.kv_heads);
-    const int own0 = (shared_steps + before) * a.kv_heads + h * steps, own1 = own0 + steps, shared0 = h * shared_steps, shared1 = shared0 + shared_steps;
-    const bool one_own = own1 > own0 && own0 / share == (own1 - 1) / share;
-    if (one_own && !a.whole.o) return;                        // written by its piece
-    const int n_own = own1 == own0 ? 0 : (own1 - 1) / share - own0 / share + 1;
-    const int n_shared = a.shared_here ? (shared1 - 1) / share - shared0 / share + 1 : a.part_shared.o ? a.shared_splits : 0, n = n_shared + n_own;
     const long row = (long)t * a.heads + head, rows = (long)a.T * a.heads;
+    int n_own, n_shared = a.part_shared.o ? a.shared_splits : 0;
+    bool one_own;
+    int share = 1, own0 = 0, shared0 = 0;                     // few-row kernel: steps a worker, the first ones of the item and of the shared item in the line of all
+    if (few) {
+        int before = 0, all = 0;                              // steps of the rows before b, of all rows
+        for (int x = lane; x < a.rows; x += 64) {
+            const int steps = few_steps(a, x);
+            all += steps;
+            before += x < b ? steps : 0;
+        }
+        all = __builtin_amdgcn_readlane(wave_scan(all), 63);
+        before = __builtin_amdgcn_readlane(wave_scan(before), 63);
+        const int shared_steps = a.shared_here ? (a.n_shared + kFewTile - 1) / kFewTile : 0, steps = few_steps(a, b);
+        share = few_share(a, (all + shared_steps) * a.kv_heads);
+        own0 = (shared_steps + before) * a.kv_heads + h * steps;
+        shared0 = h * shared_steps;
+        n_own = steps == 0 ? 0 : (own0 + steps - 1) / share - own0 / share + 1;
+        if (a.shared_here) n_shared = (shared0 + shared_steps - 1) / share - shared0 / share + 1;
+        one_own = n_own == 1;
+        if (one_own && !a.whole.o) return;
+    } else {
+        n_own = many_pieces(a, many_steps(a, many_limit(a, row_tokens(a, b), q.y, (i * a.group + j) / kManyRows)), a.splits == 1 ? 1 << 30 : many_share(a));
+        one_own = false;
+        if (n_own == 1 && !n_shared) return;
+    }
+    const int n = n_shared + n_own;
     // where part p of the n lies: parts of one list are equally far apart but for the first of an item, which may be in a worker's other place
     const int own_w = own0 / share, shared_w = shared0 / share;
     const auto part = [&](int p, long *at) {
@@ -50,6 +61,7 @@ __global__ __launch_bounds__(THREADS) void fbq_join_pieces_kernel(const AttendAr
             const int w = shared_w + p;
             return *at = ((long)w * 2 + ((long)w * share < shared0 ? 1 : 0)) * a.slot_rows + t * a.group + j, a.piece;
         }
+        if (!few) return *at = (p - n_shared) * rows + row, a.part;
         if (one_own) return *at = row, a.whole;
         const int w = own_w + p - n_shared;
         return *at = ((long)w * 2 + ((long)w * share < own0 ? 1 : 0)) * a.slot_rows + i * a.group + j, a.piece;
@@ -103,7 +115,7 @@ __global__ __launch_bounds__(THREADS) void fbq_join_pieces_kernel(const AttendAr
     if (a.lse && tid == 0) a.lse[row] = l == 0 ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
-// Many-row kernel: LANES lanes a row, four features each, its pieces one behind the other.  No more blocks than the GPU holds: what is cut they work out once, and in most
+// Many-row kernel, many rows: LANES lanes a row, four features each, its pieces one behind the other.  No more blocks than the GPU holds: what is cut they work out once, and in most
 // calls of many rows it is nothing.
 constexpr int kJoinBlocks = 2048;
 template <class TY, int LANES>
@@ -155,8 +167,8 @@ template <class TY, int LANES>
 static hipError_t launch_join(const AttendArgs &a, bool few, hipStream_t stream)
 {
     const long rows = (long)a.T * a.heads, a_block = kJoinThreads / LANES;
-    if (few && rows >= 2048) hipLaunchKernelGGL((fbq_join_pieces_kernel<TY, LANES, 64>), dim3((unsigned)rows), dim3(64), 0, stream, a);
-    else if (few) hipLaunchKernelGGL((fbq_join_pieces_kernel<TY, LANES, kJoinThreads>), dim3((unsigned)rows), dim3(kJoinThreads), 0, stream, a);
+    if (rows < 2048) hipLaunchKernelGGL((fbq_join_pieces_kernel<TY, LANES, kJoinThreads>), dim3((unsigned)rows), dim3(kJoinThreads), 0, stream, a, few);
+    else if (few) hipLaunchKernelGGL((fbq_join_pieces_kernel<TY, LANES, 64>), dim3((unsigned)rows), dim3(64), 0, stream, a, few);
     else hipLaunchKernelGGL((fbq_join_splits_kernel<TY, LANES>), dim3((unsigned)std::min<long>(kJoinBlocks, (rows + a_block - 1) / a_block)), dim3(kJoinThreads), 0, stream, a);
     return hipGetLastError();
 }
@@ -207,7 +219,7 @@ static AttendPlan attend_plan(const fbq_attention_call &c, void *workspace)
     };
     const long room_for = many_blocks(a.D);
     const auto splits_of = [=](long blocks, long tokens) {     // so that the GPU is about filled, with 256 keys or more each
-        return (int)std::max(1L, std::min({(room_for + blocks / 2) / blocks, (tokens + 255) / 256, 32L}));
+        return (int)std::max(1L, std::min({(room_for + blocks / 2) / blocks, (tokens + 255) / 256, 64L}));
     };
     if (a.n_shared) {
         a.shared_here = p.few && all_queries <= kFewRows;
@@ -232,7 +244,7 @@ static AttendPlan attend_plan(const fbq_attention_call &c, void *workspace)
     } else {
         const long per_row = (a.group + kManyRows - 1) / kManyRows;
         const long tiles = a.q_start ? (all_queries + kManyRows - 1) / kManyRows : a.rows * per_row;
-        a.splits = (int)std::max(1L, std::min({(2 * room_for - 1) / (tiles * a.kv_heads), (own_tokens + 255) / 256, 32L, 65535 / (tiles + a.rows)}));
+        a.splits = (int)std::max(1L, std::min({(2 * room_for - 1) / (tiles * a.kv_heads), (own_tokens + 255) / 256, 128L, 65535 / (tiles + a.rows)}));
         p.join = a.splits > 1 || a.n_shared;
         if (p.join) room(&a.part, a.splits * results);
     }
