@@ -15,7 +15,7 @@ LIB = os.path.join(HERE, "libfbq.so")
 CALL = os.path.join(HERE, "_fbq_call.so")     # the binding's call of fbq_linear: host code, a CPython module
 SOURCES = ["fbq_api.cpp", "fbq_decode.hip", "fbq_decode_mfma.hip", "fbq_decode_stream.hip", "fbq_few_split.hip", "fbq_prefill.hip", "fbq_quantize.hip", "fbq_util.hip", "fbq_train.hip",
            "fbq_static.hip", "fbq_mix.hip",
-           "fbq_cache.hip", "fbq_attend_few.hip", "fbq_attend_many.hip", "fbq_attention.hip"]
+           "fbq_cache.hip", "fbq_attend_few.hip", "fbq_attend_many.hip", "fbq_attend_both.hip", "fbq_attention.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-I", INCLUDE, "-I", CSRC]
 

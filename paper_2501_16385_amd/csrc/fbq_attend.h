@@ -1,7 +1,7 @@
 // Attention over the paged cache: what its kernels share (device code, launch arguments).
 //
-// Two kernels read keys and values.  fbq_attend_few.hip: up to 16 query rows of one key/value head (query tokens times the heads that share it) against its
-// tokens, registers only.  fbq_attend_many.hip: 128 rows a block, key and value tiles in LDS.  Both can leave partial results - sum of p v, its maximum
+// Two kinds of work read keys and values.  fbq_attend_few.h: up to 16 query rows of one key/value head (query tokens times the heads that share it) against its
+// tokens, registers only.  fbq_attend_many.h: 128 rows a block, key and value tiles in LDS.  Both can leave partial results - sum of p v, its maximum
 // exponent, sum of p - for fbq_attend_join_kernel (fbq_attention.hip), which adds them up in a fixed order.
 #ifndef FBQ_ATTEND_H
 #define FBQ_ATTEND_H
@@ -183,8 +183,12 @@ struct PageList {
     }
 };
 
+constexpr int kNowhere = 1 << 30;        // an offset behind every descriptor's end: loads answer zero
+
 hipError_t launch_attend_few(const AttendArgs &a, int type, hipStream_t stream);
 hipError_t launch_attend_many(const AttendArgs &a, int type, bool shared, hipStream_t stream);   // shared: the shared tokens for all rows, else the rows' own
+
+hipError_t launch_attend_both(const AttendArgs &a, int type, hipStream_t stream);                // the shared tokens many-row, the rows' own few-row
 
 }  // namespace fbq
 

@@ -1,309 +1,12 @@
-// Attention of a few query rows against a long row of the cache: decode steps, and short prefixes of a shared prompt.
-//
-// An item is one key/value head of one table row: up to 16 query rows (its query tokens times the heads that share it) against the row's keys and values, which
-// are read once.  Bound by HBM: 2 x 2 D bytes a key, for 4 D flops a query row and key.  A step is 32 keys; all steps of all items form one line, which the waves
-// of the grid cut into equal pieces - lengths lie on the device, the line is laid out from them by a scan in each wave - so that one long row among short ones
-// occupies the whole GPU and no host value decides the cut.  A piece of an item leaves partial results for the join kernel; an item that lies
-// within one piece is written at once.
-//
-// Keys and values go from memory to registers to the matrix cores, nothing through LDS, and waves wait for nobody.  S^T = K Q^T puts a key's scores in rows and a
-// query row in a column: v_mfma_f32_16x16x32, operand A lane l key l % 16, features 8 (l / 16) and up of 32, which is how keys lie in memory.  The result has
-// column l % 16, keys 4 (l / 16) + i: a lane's eight probabilities of a step are keys 4 g .. 4 g + 3 and 16 + 4 g .. of group g = l / 16.  O^T = V^T P^T
-// takes them as operand B where they are, since the order of a contraction is free: V^T's lanes take the same eight keys.  A lane loads DP / 16
-// features (l % 16 being the piece) of its eight keys and turns them by byte permutes; row l % 16 of the j-th product is then feature (DP / 16) (l % 16) + j, and
-// a lane's results are DP / 4 features in a row of one query row.  The scale by exp(m_old - m_new) is the lane's own.
-#include "fbq_attend.h"
-#include "fbq_lds_copy.h"
+// Launches of the few-row kernel alone (fbq_attend_few.h).
+#include "fbq_attend_few.h"
 
 namespace fbq {
-
-constexpr int kNowhere = 1 << 30;             // an offset behind every descriptor's end: loads answer zero
-
-// Cache policy of a load, nt: what is read once takes no room from what is read again (16 rows of about 1000 tokens, 32 heads: 55 us, 62 without it).
-constexpr int kOnce = 2;
-
-template <int DP>
-struct Step {
-    static constexpr int kV = DP == 256 ? 2 : 1;              // 16-byte loads of a lane's features of one value row (DP 64: one of 8 bytes)
-    word4_t k[2][DP / 32];
-    word4_t v[2][4][kV];
-};
-
-// A piece of an item: what its loads and its rows need, both for the piece worked on and the one behind it.
-template <int DP>
-struct Piece {
-    int b, h, step, steps, limit;                             // table row (-1: the shared tokens), head, its first step of the item's `steps`, tokens of the item
-    int n, key0;                                              // steps of its own, its first key
-    PageList pages;
-    int t, head, sees;                                        // this lane's query row: token (-1: none), head, how many tokens it sees
-    word4_t q[DP / 32];
-};
 
 template <class TY, int DP>
 __global__ __launch_bounds__(64 * kFewWaves, DP == 256 ? 1 : 2) void fbq_attend_few_kernel(const AttendArgs a)
 {
-    constexpr int J = DP / 16;                                // features of a lane's value pieces, and products O^T of a step
-    const int lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4;
-    const int worker = uniform(blockIdx.x * kFewWaves + (threadIdx.x >> 6));
-    const int D = a.D, ps1 = (1 << a.log_ps) - 1;
-
-    Piece<DP> cur, behind;
-    int u = 0, end = 0;
-    if (a.direct) {                                           // an item a worker
-        cur.b = worker / a.kv_heads;
-        if (cur.b >= a.rows) return;
-        cur.h = worker - cur.b * a.kv_heads;
-        cur.limit = uniform(row_tokens(a, cur.b));
-        cur.steps = uniform(few_steps(a, cur.b, cur.limit));
-        cur.step = 0;
-        cur.n = cur.steps;
-    } else {
-        int own = 0;
-        for (int b = lane; b < a.rows; b += 64) own += few_steps(a, b);
-        own = __builtin_amdgcn_readlane(wave_scan(own), 63);
-        const int shared_steps = a.shared_here ? (a.n_shared + kFewTile - 1) / kFewTile : 0;
-        const int total = (own + shared_steps) * a.kv_heads;
-        const int share = few_share(a, total);
-        u = min(worker, total) * share;                       // (worker * share within an int)
-        end = min(total, u + share);
-        if (u >= end) return;
-        if (u < shared_steps * a.kv_heads) {
-            cur.b = -1;
-            cur.limit = a.n_shared;
-            cur.steps = shared_steps;
-            cur.h = u / cur.steps;
-            cur.step = u - cur.h * cur.steps;
-        } else {
-            int rest = u - shared_steps * a.kv_heads, before = 0, base = 0, tokens, mine, sum;
-            while (true) {
-                tokens = base + lane < a.rows ? row_tokens(a, base + lane) : 0;
-                mine = base + lane < a.rows ? few_steps(a, base + lane, tokens) : 0;
-                sum = wave_scan(mine);
-                const int some = __builtin_amdgcn_readlane(sum, 63);
-                if ((long)rest < (long)(before + some) * a.kv_heads) break;
-                before += some;
-                base += 64;
-                if (base >= a.rows) return;                   // (not unless lengths change under the call)
-            }
-            const int at = __builtin_ctzll(__ballot((long)(before + sum) * a.kv_heads > rest));
-            cur.b = base + at;
-            cur.steps = __builtin_amdgcn_readlane(mine, at);
-            cur.limit = __builtin_amdgcn_readlane(tokens, at);
-            rest -= (before + __builtin_amdgcn_readlane(sum, at) - cur.steps) * a.kv_heads;
-            cur.h = rest / cur.steps;
-            cur.step = rest - cur.h * cur.steps;
-        }
-        cur.n = min(end - u, cur.steps - cur.step);
-        u += cur.n;
-    }
-
-    // the item behind `x`, which ends with it; false: there is none
-    auto follow = [&](const Piece<DP> &x, Piece<DP> &to) __attribute__((always_inline)) {
-        if (u >= end) return false;
-        to.b = x.b; to.h = x.h + 1; to.steps = x.steps; to.limit = x.limit; to.step = 0;
-        if (to.h == a.kv_heads) {
-            to.h = 0;
-            do {
-                if (++to.b >= a.rows) return false;           // (not unless lengths change under the call)
-                to.limit = uniform(row_tokens(a, to.b));
-                to.steps = uniform(few_steps(a, to.b, to.limit));
-            } while (to.steps == 0);
-        }
-        to.n = min(end - u, to.steps);
-        u += to.n;
-        return true;
-    };
-    auto prepare = [&](Piece<DP> &x) __attribute__((always_inline)) {
-        const bool is_shared = x.b < 0;
-        x.key0 = (is_shared ? 0 : a.n_shared) + x.step * kFewTile;
-        x.pages.begin(is_shared ? a.shared : a.table + (long)x.b * a.max_pages, is_shared ? a.n_shared >> a.log_ps : a.max_pages, x.key0 >> a.log_ps);
-        const int i = col / a.group;
-        x.head = x.h * a.group + col - i * a.group;
-        x.t = -1;
-        x.sees = 0;
-        if (is_shared) {
-            if (i < a.T) {
-                const int row = a.q_start ? row_of_token(a.q_start, a.rows, i) : i;
-                if (row >= 0) {
-                    const int2 q = queries_of(a, row);
-                    if (i - q.x < q.y) {
-                        x.t = i;
-                        x.sees = min(row_tokens(a, row) - q.y + i - q.x + 1, x.limit);
-                    }
-                }
-            }
-        } else {
-            const int2 q = queries_of(a, x.b);
-            if (i < q.y) {
-                x.t = q.x + i;
-                x.sees = x.limit - q.y + i + 1;
-            }
-        }
-#pragma unroll
-        for (int s = 0; s < DP / 32; ++s) {
-            const int d = 32 * s + 8 * grp;
-            x.q[s] = word4_t{0, 0, 0, 0};
-            if (x.t >= 0 && d < D) x.q[s] = (*reinterpret_cast<const word4_t *>(a.q + x.t * a.q_stride + x.head * D + d) & a.q_and) ^ a.q_xor;
-        }
-    };
-
-    // offsets of this lane's loads from a half step's first key, or value
-    int k_off[DP / 32], v_off[4];
-#pragma unroll
-    for (int s = 0; s < DP / 32; ++s) k_off[s] = 32 * s + 8 * grp < D ? (col * D + 32 * s + 8 * grp) * 2 : kNowhere;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v_off[e] = J * col < D ? ((4 * grp + e) * D + J * col) * 2 : kNowhere;
-    auto load = [&](Step<DP> &to, Piece<DP> &x, int s) __attribute__((always_inline)) {
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const int key = x.key0 + s * kFewTile + 16 * half;
-            int valid = min(max(x.limit - key, 0), 16);
-            const int id = valid ? x.pages.at(key >> a.log_ps) : 0;
-            if ((unsigned)id >= (unsigned)a.pages) valid = 0;
-            const unsigned char *const at = a.kv + (valid ? id : 0) * a.page_bytes + (((long)x.h << a.log_ps) + (key & ps1)) * D * 2;
-            const __amdgpu_buffer_rsrc_t kb = buffer_of(at, valid * D * 2), vb = buffer_of(at + (a.page_bytes >> 1), valid * D * 2);
-#pragma unroll
-            for (int c = 0; c < DP / 32; ++c) to.k[half][c] = __builtin_amdgcn_raw_buffer_load_b128(kb, k_off[c], 0, kOnce);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if (DP == 64) {
-                    const word2_t w = __builtin_amdgcn_raw_buffer_load_b64(vb, v_off[e], 0, kOnce);
-                    to.v[half][e][0] = word4_t{w[0], w[1], 0, 0};
-                } else {
-#pragma unroll
-                    for (int c = 0; c < Step<DP>::kV; ++c) to.v[half][e][c] = __builtin_amdgcn_raw_buffer_load_b128(vb, v_off[e] + 16 * c, 0, kOnce);
-                }
-            }
-        }
-    };
-
-    float4_t o[J];
-    float m, l;
-    int least;                                                // what every row of the piece sees
-    auto begin = [&]() __attribute__((always_inline)) {
-#pragma unroll
-        for (int j = 0; j < J; ++j) o[j] = float4_t{0, 0, 0, 0};
-        m = kNoScore;
-        l = 0;
-        least = cur.t >= 0 ? cur.sees : cur.limit;
-#pragma unroll
-        for (int x = 8; x; x >>= 1) least = min(least, __shfl_xor(least, x));
-        least = uniform(least);
-    };
-    auto compute = [&](const Step<DP> &x, int s) __attribute__((always_inline)) {
-        float4_t z[2];
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            z[half] = float4_t{0, 0, 0, 0};
-#pragma unroll
-            for (int y = 0; y < DP / 32; ++y) z[half] = TY::mfma(x.k[half][y], cur.q[y], z[half]);
-        }
-        const int key = cur.key0 + s * kFewTile;
-        if (key + kFewTile > least) {
-#pragma unroll
-            for (int half = 0; half < 2; ++half)
-#pragma unroll
-                for (int y = 0; y < 4; ++y)
-                    if (key + 16 * half + 4 * grp + y >= cur.sees) z[half][y] = -INFINITY;
-        }
-        float top = fmaxf(fmaxf(fmaxf(z[0][0], z[0][1]), fmaxf(z[0][2], z[0][3])), fmaxf(fmaxf(z[1][0], z[1][1]), fmaxf(z[1][2], z[1][3])));
-        top = larger_of_16(top);
-        top = larger_of_32(top) * a.scale;
-        if (__ballot(top > m + kSlack)) {
-            const float to = fmaxf(top, m), by = __builtin_amdgcn_exp2f(m - to);
-            l *= by;
-#pragma unroll
-            for (int j = 0; j < J; ++j) o[j] *= by;
-            m = to;
-        }
-        word4_t p;
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-#pragma unroll
-            for (int y = 0; y < 4; ++y) {
-                z[half][y] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[half][y], a.scale, -m));
-                l += z[half][y];
-            }
-            p[2 * half] = TY::pack(z[half][0], z[half][1]);
-            p[2 * half + 1] = TY::pack(z[half][2], z[half][3]);
-        }
-#pragma unroll
-        for (int j = 0; j < J; ++j) {
-            word4_t vt;
-#pragma unroll
-            for (int y = 0; y < 4; ++y) {                     // two keys of feature j
-                const uint32_t lo = x.v[y >> 1][2 * (y & 1)][j >> 3][(j & 7) >> 1], hi = x.v[y >> 1][2 * (y & 1) + 1][j >> 3][(j & 7) >> 1];
-                vt[y] = __builtin_amdgcn_perm(hi, lo, j & 1 ? 0x07060302u : 0x05040100u);
-            }
-            o[j] = TY::mfma(vt, p, o[j]);
-        }
-    };
-    bool first = true;
-    auto finish = [&]() __attribute__((always_inline)) {
-        l += __shfl_xor(l, 16);
-        l += __shfl_xor(l, 32);
-        if (cur.t < 0) return;
-        const bool whole = cur.n == cur.steps;
-        const Partials to = whole ? (cur.b < 0 ? a.whole_shared : a.whole) : a.piece;
-        const int d0 = 4 * J * grp;
-        if (whole && !to.o) {
-            const float by = l == 0 ? 0.0f : 1.0f / l;
-            uint16_t *const at = a.out + cur.t * a.out_stride + cur.head * D + d0;
-#pragma unroll
-            for (int c = 0; c < J / 2; ++c) {                 // eight features: elements 8 c .. of o[j][i] in the order J i + j
-                word4_t w;
-#pragma unroll
-                for (int y = 0; y < 4; ++y) {
-                    const int e = 8 * c + 2 * y;
-                    w[y] = TY::pack(o[e % J][e / J] * by, o[(e + 1) % J][(e + 1) / J] * by);
-                }
-                if (d0 + 8 * c < D) *reinterpret_cast<word4_t *>(at + 8 * c) = w;
-            }
-            if (a.lse && grp == 0) a.lse[(long)cur.t * a.heads + cur.head] = l == 0 ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
-        } else {
-            const long r = whole ? (long)cur.t * a.heads + cur.head : ((long)worker * 2 + (first ? 0 : 1)) * a.slot_rows + col;
-            float *const at = to.o + r * D + d0;
-#pragma unroll
-            for (int c = 0; c < J; ++c) {
-                float4_t w;
-#pragma unroll
-                for (int y = 0; y < 4; ++y) w[y] = o[(4 * c + y) % J][(4 * c + y) / J];
-                if (d0 + 4 * c < D) *reinterpret_cast<float4_t *>(at + 4 * c) = w;
-            }
-            if (grp == 0) to.ml[r] = make_float2(m, l);
-        }
-    };
-
-    // A step's loads go out before the step before it is worked on, those of a piece's first step too: page list and queries of the piece behind come while the one
-    // before runs.
-    prepare(cur);
-    if (cur.n == 0) {                                         // (an item a worker, and this one has no tokens)
-        begin();
-        finish();
-        return;
-    }
-    bool more = follow(cur, behind);
-    if (more) prepare(behind);
-    Step<DP> x0, x1;
-    load(x0, cur, 0);
-    begin();
-    int s = 0;
-    auto turn = [&](const Step<DP> &now, Step<DP> &next) __attribute__((always_inline)) {
-        if (s + 1 < cur.n) load(next, cur, s + 1);
-        else if (more) load(next, behind, 0);
-        compute(now, s);
-        if (++s < cur.n) return false;
-        finish();
-        if (!more) return true;
-        first = false;
-        cur = behind;
-        s = 0;
-        more = follow(cur, behind);
-        if (more) prepare(behind);
-        begin();
-        return false;
-    };
-    while (!turn(x0, x1) && !turn(x1, x0)) {}
+    attend_few<TY, DP>(a, blockIdx.x);
 }
 
 template <class TY>

@@ -1,317 +1,12 @@
-// Attention of many query rows: prompts, pieces of prompts, and a shared prefix against the rows of a whole batch.
-//
-// A block has 128 rows (query tokens times the heads that share a key/value head, so grouped heads share what is read) of one key/value head, 32 a wave, and
-// goes through the keys 64 at a time: copies of the next 64 keys and values go straight to LDS while these are worked on.  Bound by the matrix cores and, nearly
-// as much, by the exponentials: 4 D flops and one exponential a pair.  S^T = K Q^T and O^T = V^T P^T in v_mfma_f32_32x32x16: a lane's column is its query
-// row throughout, so the running maximum and sum, the rescaling and P stay in the lane (two lanes share a row), and the probabilities of a step
-// are operand B of the second product where the first one left them: keys 16 x + 4 g + (0 .. 3) and 16 x + 8 + 4 g + (0 .. 3) of lane group g = l / 32; the transposed
-// reads of V from LDS take their keys in that order.  Rows of a tile end where their last query token's sight ends; later tiles, which see
-// more, come first.  Where rows x heads leave the GPU empty the keys are cut into `splits` and the join kernel adds up.
-#include "fbq_attend.h"
-#include "fbq_lds_copy.h"
+// Launches of the many-row kernel alone (fbq_attend_many.h).
+#include "fbq_attend_many.h"
 
 namespace fbq {
-
-constexpr int kNowhere = 1 << 30;
-
-// Piece (16 bytes) p of a key's row lies at p ^ key_swap: 16 (or 8) consecutive rows' equal pieces fall on different banks.  A value's row at p ^ value_swap: the four rows
-// of a transposed read, 32 bytes each for 16 lanes, do.
-__device__ __forceinline__ int key_swap(int row, int pieces) { return pieces == 8 ? piece_key(row) : row & 15; }
-__device__ __forceinline__ int value_swap(int row, int pieces) { return pieces == 8 ? 2 * (row & 3) : (4 * (row & 3)) ^ (row & 2); }
-
-__device__ __forceinline__ word2_t read_turned4(const unsigned char *at)
-{
-    typedef short four_t __attribute__((vector_size(8)));
-    typedef __attribute__((address_space(3))) four_t lds_four_t;
-    return __builtin_bit_cast(word2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_four_t *)(__attribute__((address_space(3))) const void *)at));
-}
-
-// f(0), f(1) .. f(N - 1), each with its number as a constant
-template <int N, class F>
-__device__ __forceinline__ void each(F f)
-{
-    if constexpr (N > 0) {
-        each<N - 1>(f);
-        f(std::integral_constant<int, N - 1>());
-    }
-}
 
 template <class TY, int DP>
 __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void fbq_attend_many_kernel(const AttendArgs a, const bool shared)
 {
-    constexpr int kPieces = DP == 96 ? 16 : DP / 8, kRowBytes = kPieces * 16, kTileBytes = kManyTile * kRowBytes;   // (96: rows as long as 128's, so that they fold over the banks)
-    constexpr int kRowsACopy = 64 / kPieces, kCopies = 16 / kRowsACopy;       // a wave copies 16 keys and 16 values a step
-    __shared__ __attribute__((aligned(1024))) unsigned char lds[2][2][kTileBytes];    // keys, values; two steps each
-
-    const int lane = threadIdx.x & 63, col = lane & 31, grp = lane >> 5, wave = uniform(threadIdx.x >> 6);
-    const int D = a.D, ps1 = (1 << a.log_ps) - 1;
-    const int h = blockIdx.x;
-
-    // the row of the table, the tile of its query rows and the piece of the tile's keys (for the shared tokens all query tokens are one row's)
-    int b = 0, q0 = 0, nq = a.T, limit = a.n_shared, tile = blockIdx.y, split = blockIdx.z, splits = a.shared_splits, tokens_of_row = 0;
-    if (!shared) {
-        const int share = a.splits == 1 ? 1 << 30 : many_share(a);
-        int queries, tokens, tiles, pieces, count, longest;   // of the table row that is this lane's
-        const auto look = [&](int row) {
-            queries = row < a.rows ? queries_of(a, row).y : 0;
-            tokens = row < a.rows ? row_tokens(a, row) : 0;
-            tiles = many_tiles(a, queries);
-            pieces = many_pieces(a, many_steps(a, tokens), share);
-            count = tiles * pieces;
-            longest = (many_steps(a, tokens) + pieces - 1) / pieces;
-        };
-        int all = 0;
-        for (int base = 0; base < a.rows; base += 64) {
-            look(base + lane);
-            all += __builtin_amdgcn_readlane(wave_scan(count), 63);
-        }
-        int index = blockIdx.y;
-        if (index >= all) return;                             // the grid has a block for the most there could be
-        // Long pieces first: the rows by their longest piece where a wave knows them all, the tiles of a row from its last to its first.  Blocks that are all on the GPU at once
-        // share CUs two by two, the first with the one half the grid on: then the second half goes from short to long.
-        const int half = (all + 1) / 2;
-        if (index >= half && (long)all * a.kv_heads <= many_blocks(D)) index = all - 1 - (index - half);
-        int offset = 0, base = 0;
-        if (a.rows <= 64) {
-            for (int x = 0; x < a.rows; ++x) {
-                const int other = __builtin_amdgcn_readlane(longest, x);
-                if (other > longest || (other == longest && x < lane)) offset += __builtin_amdgcn_readlane(count, x);
-            }
-        } else {
-            int before = 0;
-            while (true) {
-                look(base + lane);
-                const int sum = wave_scan(count), some = __builtin_amdgcn_readlane(sum, 63);
-                offset = before + sum - count;
-                if (index < before + some) break;
-                before += some;
-                base += 64;
-                if (base >= a.rows) return;                   // (not unless the rows change under the call)
-            }
-        }
-        const int at = __builtin_ctzll(__ballot(count > 0 && offset <= index && index < offset + count));
-        b = base + at;
-        const int rest = index - __builtin_amdgcn_readlane(offset, at), row_pieces = __builtin_amdgcn_readlane(pieces, at);
-        tile = __builtin_amdgcn_readlane(tiles, at) - 1 - rest / row_pieces;
-        split = rest % row_pieces;
-        nq = __builtin_amdgcn_readlane(queries, at);
-        q0 = uniform(queries_of(a, b).x);
-        tokens_of_row = __builtin_amdgcn_readlane(tokens, at);
-        limit = many_limit(a, tokens_of_row, nq, tile);
-        splits = many_pieces(a, many_steps(a, limit), share);
-        if (split >= splits) return;
-    }
-
-    // this lane's query row: token, head, how many tokens it sees
-    const int r = tile * kManyRows + wave * 32 + col, i = r / a.group, head = h * a.group + r - i * a.group;
-    int t = -1, sees = 0;
-    if (i < nq) {
-        if (shared) {
-            const int row = a.q_start ? row_of_token(a.q_start, a.rows, i) : i;
-            if (row >= 0) {
-                const int2 q = queries_of(a, row);
-                if (i - q.x < q.y) {
-                    t = i;
-                    sees = min(row_tokens(a, row) - q.y + i - q.x + 1, limit);
-                }
-            }
-        } else {
-            t = q0 + i;
-            sees = tokens_of_row - nq + i + 1;
-        }
-    }
-    int least = t >= 0 ? sees : limit, most = t >= 0 ? sees : 0;              // of the wave's rows
-#pragma unroll
-    for (int o = 16; o; o >>= 1) {
-        least = min(least, __shfl_xor(least, o));
-        most = max(most, __shfl_xor(most, o));
-    }
-    least = uniform(least);
-    most = uniform(most);
-    const int key0 = shared ? 0 : a.n_shared, all_steps = shared ? (limit + kManyTile - 1) / kManyTile : many_steps(a, limit);
-    const int per = (all_steps + splits - 1) / splits;
-    const int s0 = min(split * per, all_steps), s1 = min(s0 + per, all_steps);
-
-    word4_t qf[DP / 16];
-#pragma unroll
-    for (int s = 0; s < DP / 16; ++s) {
-        const int d = 16 * s + 8 * grp;
-        qf[s] = word4_t{0, 0, 0, 0};
-        if (t >= 0 && d < D) qf[s] = (*reinterpret_cast<const word4_t *>(a.q + t * a.q_stride + head * D + d) & a.q_and) ^ a.q_xor;
-    }
-
-    // where this lane's pieces of a copy come from: rows 16 wave .. of a step
-    int k_off[kCopies], v_off[kCopies];
-#pragma unroll
-    for (int c = 0; c < kCopies; ++c) {
-        const int row = c * kRowsACopy + lane / kPieces, at = lane % kPieces, kp = at ^ key_swap(row, kPieces), vp = at ^ value_swap(row, kPieces);
-        k_off[c] = 8 * kp < D ? row * D * 2 + kp * 16 : kNowhere;
-        v_off[c] = 8 * vp < D ? row * D * 2 + vp * 16 : kNowhere;
-    }
-    const int32_t *const list = shared ? a.shared : a.table + (long)b * a.max_pages;
-    const int entries = shared ? a.n_shared >> a.log_ps : a.max_pages;
-    // 16 keys, or values, a wave
-    PageList pages;
-    auto page_of = [&](int step) __attribute__((always_inline)) { return pages.at((key0 + step * kManyTile + 16 * wave) >> a.log_ps); };
-    auto copy = [&](int step, int page, bool values) __attribute__((always_inline)) {
-        const int key = key0 + step * kManyTile + 16 * wave;
-        const int valid = (unsigned)page < (unsigned)a.pages ? min(max(limit - key, 0), 16) : 0;
-        const unsigned char *const at = a.kv + (valid ? page : 0) * a.page_bytes + (values ? a.page_bytes >> 1 : 0) + (((long)h << a.log_ps) + (key & ps1)) * D * 2;
-        const __amdgpu_buffer_rsrc_t from = buffer_of(at, valid * D * 2);
-        const uint32_t to = lds_offset(&lds[values][step & 1][16 * wave * kRowBytes]);
-#pragma unroll
-        for (int c = 0; c < kCopies; ++c) copy16_to_lds(from, values ? v_off[c] : k_off[c], 0, to + c * 1024);
-    };
-
-    // reads: a key's piece s of DP / 16 pairs, and a value's column block dblk of 32
-    const int k_at = col * kRowBytes, k_piece = grp ^ key_swap(col, kPieces);
-    const int v_row = 4 * grp + ((lane & 15) >> 2), v_at = v_row * kRowBytes + 8 * (lane & 1);
-    const int v_piece = (2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ value_swap(v_row, kPieces);
-
-    float16_t o[DP / 32];
-#pragma unroll
-    for (int x = 0; x < DP / 32; ++x)
-#pragma unroll
-        for (int y = 0; y < 16; ++y) o[x][y] = 0;
-    float m = kNoScore, l = 0;
-
-    // A step is a row of slots with one matrix product each, first the next step's scores (kScores products, the two halves of its keys in turn), then this step's P V (kValues,
-    // 16 keys at a time).  Every slot asks LDS for the operand of the one kAhead slots on, and carries a share of the step's other work, which the compiler is kept from
-    // moving: exponentials of pair k of probabilities (in time for its product), and towards the end the maximum of the next step's scores.
-    constexpr int kScores = DP / 8, kValues = DP / 8, kAhead = 4, kLate = 12;
-    word4_t ring[kAhead];
-    auto fetch = [&](int i, int step) __attribute__((always_inline)) {        // operand of slot i of the step `step`
-        if (i < kScores) {
-            const int half = i & 1, x = i >> 1;
-            ring[i % kAhead] = *reinterpret_cast<const word4_t *>(lds[0][(step + 1) & 1] + k_at + ((k_piece ^ (2 * x)) << 4) + 32 * half * kRowBytes);
-        } else if (i < kScores + kValues) {
-            const int j = (i - kScores) / (DP / 32), d = (i - kScores) % (DP / 32);
-            const unsigned char *const at = lds[1][step & 1] + v_at + ((v_piece ^ (4 * d)) << 4) + 16 * j * kRowBytes;
-            const word2_t lo = read_turned4(at), hi = read_turned4(at + 8 * kRowBytes);
-            ring[i % kAhead] = word4_t{lo[0], lo[1], hi[0], hi[1]};
-        }
-    };
-    int page = 0;                                             // of the keys copied last
-    float top = -INFINITY;                                    // of this lane's scores of the step that is next
-    auto work = [&](float16_t (&z)[2], float16_t (&ahead)[2], int s) __attribute__((always_inline)) {
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");   // what was asked for a step ago is there, what a step ago was read is free
-        if (s + 1 < s1) copy(s + 1, page, true);
-        if (s + 2 < s1) {
-            page = page_of(s + 2);
-            copy(s + 2, page, false);
-        }
-        const int key = key0 + s * kManyTile;
-        if (key >= most) return;
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) fetch(i, s);         // (past the last step: of whatever lies there, its scores are not used)
-        if (key + kManyTile > least) {
-            top = -INFINITY;
-#pragma unroll
-            for (int half = 0; half < 2; ++half)
-#pragma unroll
-                for (int y = 0; y < 16; ++y) {
-                    if (key + 32 * half + 8 * (y >> 2) + 4 * grp + (y & 3) >= sees) z[half][y] = -INFINITY;
-                    top = fmaxf(top, z[half][y]);
-                }
-        }
-        const float high = larger_of_32(top) * a.scale;
-        if (__ballot(high > m + kSlack)) {
-            const float to = fmaxf(high, m), by = __builtin_amdgcn_exp2f(m - to);
-            l *= by;
-#pragma unroll
-            for (int x = 0; x < DP / 32; ++x) o[x] *= by;
-            m = to;
-        }
-        word4_t p[4];
-        auto pair = [&](int k) __attribute__((always_inline)) {
-            const int half = k >> 3, y = 2 * (k & 7);
-            const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[half][y], a.scale, -m)), p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[half][y + 1], a.scale, -m));
-            l += p0 + p1;
-            p[k >> 2][k & 3] = TY::pack(p0, p1);
-        };
-#pragma unroll
-        for (int half = 0; half < 2; ++half)
-#pragma unroll
-            for (int y = 0; y < 16; ++y) ahead[half][y] = 0;
-        each<kScores + kValues>([&](auto slot) __attribute__((always_inline)) {
-            constexpr int i = decltype(slot)::value;
-            __builtin_amdgcn_sched_barrier(0);
-            const word4_t f = ring[i % kAhead];
-            if constexpr (i < kScores) {
-                ahead[i & 1] = TY::mfma(f, qf[i >> 1], ahead[i & 1]);
-#pragma unroll
-                for (int k = 0; k < kLate; ++k)
-                    if (k * kScores / kLate == i) pair(k);
-            } else {
-                constexpr int x = i - kScores, j = x / (DP / 32), d = x % (DP / 32);
-                o[d] = TY::mfma(f, p[j], o[d]);
-#pragma unroll
-                for (int k = kLate; k < 16; ++k)
-                    if ((k - kLate) * (kValues / 2) / (16 - kLate) == x) pair(k);
-#pragma unroll
-                for (int y = 0; y < 16; ++y)
-                    if (kValues / 2 + y * (kValues / 2) / 16 == x) top = y == 0 ? fmaxf(ahead[0][0], ahead[1][0]) : fmaxf(fmaxf(top, ahead[0][y]), ahead[1][y]);
-            }
-            fetch(i + kAhead, s);
-        });
-        __builtin_amdgcn_sched_barrier(0);
-    };
-    // Keys are a step ahead of values: while step s is worked on, keys s + 1 and values s are read, keys s + 2 and values s + 1 copied.
-    float16_t z0[2], z1[2];
-    if (s0 < s1) {
-        pages.begin(list, entries, (key0 + s0 * kManyTile + 16 * wave) >> a.log_ps);
-        page = page_of(s0);
-        copy(s0, page, false);
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        copy(s0, page, true);
-        if (s0 + 1 < s1) {
-            page = page_of(s0 + 1);
-            copy(s0 + 1, page, false);
-        }
-#pragma unroll
-        for (int half = 0; half < 2; ++half)
-#pragma unroll
-            for (int y = 0; y < 16; ++y) z0[half][y] = 0;
-#pragma unroll
-        for (int i = 0; i < kScores; ++i) {
-            fetch(i, s0 - 1);
-            z0[i & 1] = TY::mfma(ring[i % kAhead], qf[i >> 1], z0[i & 1]);
-        }
-#pragma unroll
-        for (int y = 0; y < 16; ++y) top = fmaxf(fmaxf(top, z0[0][y]), z0[1][y]);
-    }
-    for (int s = s0; s < s1; s += 2) {
-        work(z0, z1, s);
-        if (s + 1 < s1) work(z1, z0, s + 1);
-    }
-    l += __shfl_xor(l, 32);
-
-    if (t < 0) return;
-    const Partials to = shared ? a.part_shared : a.part;
-    const long row = (long)t * a.heads + head;
-    if (!shared && splits == 1 && !a.part_shared.o) {
-        const float by = l == 0 ? 0.0f : 1.0f / l;
-        uint16_t *const at = a.out + t * a.out_stride + head * D;
-#pragma unroll
-        for (int x = 0; x < DP / 32; ++x)
-#pragma unroll
-            for (int y = 0; y < 4; ++y) {
-                const int d = 32 * x + 8 * y + 4 * grp;
-                if (d < D) *reinterpret_cast<word2_t *>(at + d) = word2_t{TY::pack(o[x][4 * y] * by, o[x][4 * y + 1] * by), TY::pack(o[x][4 * y + 2] * by, o[x][4 * y + 3] * by)};
-            }
-        if (a.lse && grp == 0) a.lse[row] = l == 0 ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
-        return;
-    }
-    const long at = (long)split * a.T * a.heads + row;
-    if (grp == 0) to.ml[at] = make_float2(m, l);
-    if (l == 0) return;                                       // (the join does not look at its sums)
-#pragma unroll
-    for (int x = 0; x < DP / 32; ++x)
-#pragma unroll
-        for (int y = 0; y < 4; ++y) {
-            const int d = 32 * x + 8 * y + 4 * grp;
-            if (d < D) *reinterpret_cast<float4_t *>(to.o + at * D + d) = float4_t{o[x][4 * y], o[x][4 * y + 1], o[x][4 * y + 2], o[x][4 * y + 3]};
-        }
+    attend_many<TY, DP>(a, shared, blockIdx.x, blockIdx.y, blockIdx.z);
 }
 
 template <class TY>

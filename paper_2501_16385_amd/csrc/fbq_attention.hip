@@ -217,15 +217,14 @@ static AttendPlan attend_plan(const fbq_attention_call &c, void *workspace)
         to->ml = (float2 *)((char *)workspace + at);
         at += ((size_t)n * 8 + 255) / 256 * 256;
     };
-    const long room_for = many_blocks(a.D);
-    const auto splits_of = [=](long blocks, long tokens) {     // so that the GPU is about filled, with 256 keys or more each
+    const auto splits_of = [](long blocks, long tokens, long room_for) {   // so that the GPU is about filled, with 256 keys or more each
         return (int)std::max(1L, std::min({(room_for + blocks / 2) / blocks, (tokens + 255) / 256, 64L}));
     };
     if (a.n_shared) {
         a.shared_here = p.few && all_queries <= kFewRows;
         p.shared_many = !a.shared_here;
         if (p.shared_many) {
-            a.shared_splits = splits_of((all_queries + kManyRows - 1) / kManyRows * a.kv_heads, a.n_shared);
+            a.shared_splits = splits_of((all_queries + kManyRows - 1) / kManyRows * a.kv_heads, a.n_shared, p.few ? 256 : many_blocks(a.D));   // (few: a block a CU, see fbq_attend_both.hip)
             room(&a.part_shared, a.shared_splits * results);
         } else {
             room(&a.whole_shared, results);
@@ -244,7 +243,7 @@ static AttendPlan attend_plan(const fbq_attention_call &c, void *workspace)
     } else {
         const long per_row = (a.group + kManyRows - 1) / kManyRows;
         const long tiles = a.q_start ? (all_queries + kManyRows - 1) / kManyRows : a.rows * per_row;
-        a.splits = (int)std::max(1L, std::min({(2 * room_for - 1) / (tiles * a.kv_heads), (own_tokens + 255) / 256, 128L, 65535 / (tiles + a.rows)}));
+        a.splits = (int)std::max(1L, std::min({(2L * many_blocks(a.D) - 1) / (tiles * a.kv_heads), (own_tokens + 255) / 256, 128L, 65535 / (tiles + a.rows)}));
         p.join = a.splits > 1 || a.n_shared;
         if (p.join) room(&a.part, a.splits * results);
     }
@@ -296,8 +295,9 @@ extern "C" fbq_status fbq_attention(const fbq_attention_call *c, void *workspace
     const int type = c->cache.desc.type;
     const hipStream_t s = (hipStream_t)stream;
     hipError_t e = hipSuccess;
-    if (p.shared_many) e = launch_attend_many(p.a, type, true, s);
-    if (e == hipSuccess) e = p.few ? launch_attend_few(p.a, type, s) : launch_attend_many(p.a, type, false, s);
+    if (p.shared_many && p.few) e = launch_attend_both(p.a, type, s);
+    else if (p.shared_many) e = launch_attend_many(p.a, type, true, s);
+    if (e == hipSuccess && !(p.shared_many && p.few)) e = p.few ? launch_attend_few(p.a, type, s) : launch_attend_many(p.a, type, false, s);
     if (e == hipSuccess && p.join) e = type == FBQ_F16 ? launch_join<TypeF16>(p.a, p.few, s) : launch_join<TypeBf16>(p.a, p.few, s);
     return e == hipSuccess ? FBQ_OK : FBQ_ERR_HIP;
 }
