@@ -113,6 +113,12 @@ __device__ __forceinline__ int few_steps(const AttendArgs &a, int b) { return fe
 // How many steps each worker takes, from all there are: the last ones may have none.
 __device__ __forceinline__ int few_share(const AttendArgs &a, int steps) { return max(1, (steps + a.workers - 1) / a.workers); }
 
+// Whether all workers of a block have their whole share of the item that reaches from step u0 to u1: they join their results before they write them, as the first one's.
+__device__ __forceinline__ bool few_together(int block, int share, int u0, int u1)
+{
+    return (long)block * kFewWaves * share >= u0 && (long)(block + 1) * kFewWaves * share <= u1;
+}
+
 // Many-row kernel: tiles of a row's queries; keys that a tile's last query sees; steps to there.
 __device__ __forceinline__ int many_tiles(const AttendArgs &a, int queries) { return (queries * a.group + kManyRows - 1) / kManyRows; }
 __device__ __forceinline__ int many_limit(const AttendArgs &a, int tokens, int queries, int tile)

@@ -10,13 +10,14 @@ namespace fbq {
 template <class TY, int DF, int DM>
 __global__ __launch_bounds__(256, DM == 256 ? 1 : 2) void fbq_attend_both_kernel(const AttendArgs a, const int tiles)
 {
+    __shared__ __attribute__((aligned(1024))) unsigned char room[kManyRoom<DM> > kFewRoom<DF> ? kManyRoom<DM> : kFewRoom<DF>];
     const int shared_blocks = a.kv_heads * tiles * a.shared_splits, block = blockIdx.x;
     if (block >= shared_blocks) {
-        attend_few<TY, DF>(a, block - shared_blocks);
+        attend_few<TY, DF>(a, block - shared_blocks, room);
         return;
     }
     const int rest = block / a.kv_heads, z = rest / tiles;    // a head's blocks on one XCD, where heads are a multiple of eight
-    attend_many<TY, DM>(a, true, block - rest * a.kv_heads, rest - z * tiles, z);
+    attend_many<TY, DM>(a, true, block - rest * a.kv_heads, rest - z * tiles, z, room);
 }
 
 template <class TY>

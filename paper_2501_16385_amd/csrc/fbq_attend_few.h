@@ -40,9 +40,13 @@ struct Piece {
     word4_t q[DP / 32];
 };
 
+// Bytes of LDS (aligned to 16) of a block of it.
+template <int DP>
+constexpr int kFewRoom = (kFewWaves - 1) * (DP / 4 + 2) * 256;
+
 // Block `block` of the few-row work, kFewWaves waves.
 template <class TY, int DP>
-__device__ __forceinline__ void attend_few(const AttendArgs &a, int block)
+__device__ __forceinline__ void attend_few(const AttendArgs &a, int block, unsigned char *room)
 {
     constexpr int J = DP / 16;                                // features of a lane's value pieces, and products O^T of a step
     const int lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4;
@@ -51,6 +55,7 @@ __device__ __forceinline__ void attend_few(const AttendArgs &a, int block)
 
     Piece<DP> cur, behind;
     int u = 0, end = 0;
+    bool together = false;                                    // the block's waves have a piece each of one item
     if (a.direct) {                                           // an item a worker
         cur.b = worker / a.kv_heads;
         if (cur.b >= a.rows) return;
@@ -96,6 +101,7 @@ __device__ __forceinline__ void attend_few(const AttendArgs &a, int block)
             cur.step = rest - cur.h * cur.steps;
         }
         cur.n = min(end - u, cur.steps - cur.step);
+        together = few_together(worker / kFewWaves, share, u - cur.step, u - cur.step + cur.steps);
         u += cur.n;
     }
 
@@ -244,6 +250,39 @@ __device__ __forceinline__ void attend_few(const AttendArgs &a, int block)
     auto finish = [&]() __attribute__((always_inline)) {
         l += __shfl_xor(l, 16);
         l += __shfl_xor(l, 32);
+        if (together) {                                       // then the first one joins them: a fourth of the parts to write and read again
+            float *const at = reinterpret_cast<float *>(room) + lane;
+            const int wave = uniform(threadIdx.x >> 6);
+            if (wave) {
+                float *const to = at + (wave - 1) * (4 * J + 2) * 64;
+                to[0] = m;
+                to[64] = l;
+#pragma unroll
+                for (int j = 0; j < J; ++j)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) to[(2 + 4 * j + i) * 64] = o[j][i];
+            }
+            __syncthreads();
+            if (wave) return;
+            float to = m;
+#pragma unroll
+            for (int w = 0; w < kFewWaves - 1; ++w) to = fmaxf(to, at[w * (4 * J + 2) * 64]);
+            const float by = __builtin_amdgcn_exp2f(m - to);
+            m = to;
+            l *= by;
+#pragma unroll
+            for (int j = 0; j < J; ++j) o[j] *= by;
+#pragma unroll
+            for (int w = 0; w < kFewWaves - 1; ++w) {
+                const float *const from = at + w * (4 * J + 2) * 64;
+                const float times = __builtin_amdgcn_exp2f(from[0] - m);
+                l += from[64] * times;
+#pragma unroll
+                for (int j = 0; j < J; ++j)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[j][i] += from[(2 + 4 * j + i) * 64] * times;
+            }
+        }
         if (cur.t < 0) return;
         const bool whole = cur.n == cur.steps;
         const Partials to = whole ? (cur.b < 0 ? a.whole_shared : a.whole) : a.piece;

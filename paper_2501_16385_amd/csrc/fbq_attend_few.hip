@@ -6,7 +6,8 @@ namespace fbq {
 template <class TY, int DP>
 __global__ __launch_bounds__(64 * kFewWaves, DP == 256 ? 1 : 2) void fbq_attend_few_kernel(const AttendArgs a)
 {
-    attend_few<TY, DP>(a, blockIdx.x);
+    __shared__ __attribute__((aligned(16))) unsigned char room[kFewRoom<DP>];
+    attend_few<TY, DP>(a, blockIdx.x, room);
 }
 
 template <class TY>

@@ -39,13 +39,17 @@ __device__ __forceinline__ void each(F f)
     }
 }
 
+// Bytes of LDS (aligned to 1024) of a block of it.
+template <int DP>
+constexpr int kManyRoom = 4 * kManyTile * (DP == 96 ? 256 : DP * 2);
+
 // Block (h, y, z) of the many-row work, four waves: head, tile (of the rows' own tokens: tile and piece), piece of the shared tokens.
 template <class TY, int DP>
-__device__ __forceinline__ void attend_many(const AttendArgs &a, const bool shared, const int h, const int y, const int z)
+__device__ __forceinline__ void attend_many(const AttendArgs &a, const bool shared, const int h, const int y, const int z, unsigned char *room)
 {
     constexpr int kPieces = DP == 96 ? 16 : DP / 8, kRowBytes = kPieces * 16, kTileBytes = kManyTile * kRowBytes;   // (96: rows as long as 128's, so that they fold over the banks)
     constexpr int kRowsACopy = 64 / kPieces, kCopies = 16 / kRowsACopy;       // a wave copies 16 keys and 16 values a step
-    __shared__ __attribute__((aligned(1024))) unsigned char lds[2][2][kTileBytes];    // keys, values; two steps each
+    unsigned char (*const lds)[2][kTileBytes] = reinterpret_cast<unsigned char (*)[2][kTileBytes]>(room);   // keys, values; two steps each
 
     const int lane = threadIdx.x & 63, col = lane & 31, grp = lane >> 5, wave = uniform(threadIdx.x >> 6);
     const int D = a.D, ps1 = (1 << a.log_ps) - 1;

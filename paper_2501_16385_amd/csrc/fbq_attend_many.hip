@@ -6,7 +6,8 @@ namespace fbq {
 template <class TY, int DP>
 __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void fbq_attend_many_kernel(const AttendArgs a, const bool shared)
 {
-    attend_many<TY, DP>(a, shared, blockIdx.x, blockIdx.y, blockIdx.z);
+    __shared__ __attribute__((aligned(1024))) unsigned char room[kManyRoom<DP>];
+    attend_many<TY, DP>(a, shared, blockIdx.x, blockIdx.y, blockIdx.z, room);
 }
 
 template <class TY>

@@ -9,6 +9,30 @@ constexpr int kJoinThreads = 256;
 //     out = sum_p o_p 2^(m_p - m) / sum_p l_p 2^(m_p - m),   m the largest m_p.   A part whose sum l is 0 saw nothing and has no o.
 // Bound by the latency of a chain of loads - where the parts lie, then their m, l and o at once - so as many as possible are under way together.
 
+// The parts of an item of the few-row kernel's line: pieces of the workers first .. last, those of a whole block of workers as one (see few_together).
+struct FewParts {
+    int u0, first, last, block0, blocks, count;               // its first step; whole blocks from block0 on
+    __device__ __forceinline__ void of(int u, int steps, int share)
+    {
+        u0 = u;
+        first = u / share;
+        last = steps ? (u + steps - 1) / share : first;
+        block0 = (first + kFewWaves - 1) / kFewWaves;
+        if (!few_together(block0, share, u0, u0 + steps)) ++block0;                       // (the first worker of it may have begun before the item)
+        int end = (last + 1) / kFewWaves;                                                // behind the last block that lies before `last`'s end
+        if (end > block0 && !few_together(end - 1, share, u0, u0 + steps)) --end;         // (the last worker may have less than its share of it)
+        blocks = max(0, end - block0);
+        count = steps ? last - first + 1 - (kFewWaves - 1) * blocks : 0;
+    }
+    // part p's place among the workers' places, two a worker
+    __device__ __forceinline__ long place(int p, int share) const
+    {
+        const int before = blocks ? block0 * kFewWaves - first : count;                   // single ones in front of the blocks
+        const int w = p < before ? first + p : p < before + blocks ? (block0 + p - before) * kFewWaves : first + p + (kFewWaves - 1) * blocks;
+        return (long)w * 2 + ((long)w * share < u0 ? 1 : 0);
+    }
+};
+
 // A block a row, LANES lanes a part, four features each.  The row's own part is either whole (written by its one piece: nothing left to do unless shared tokens come with it)
 // or cut into the pieces of the few-row kernel's workers w0 .. w1, or of the many-row kernel.  THREADS: 256, or a wave where there are rows enough to fill the GPU with.
 template <class TY, int LANES, int THREADS>
@@ -28,7 +52,8 @@ __global__ __launch_bounds__(THREADS) void fbq_join_pieces_kernel(const AttendAr
     const long row = (long)t * a.heads + head, rows = (long)a.T * a.heads;
     int n_own, n_shared = a.part_shared.o ? a.shared_splits : 0;
     bool one_own;
-    int share = 1, own0 = 0, shared0 = 0;                     // few-row kernel: steps a worker, the first ones of the item and of the shared item in the line of all
+    int share = 1;                                            // few-row kernel: steps a worker
+    FewParts own{}, of_shared{};
     if (few) {
         int before = 0, all = 0;                              // steps of the rows before b, of all rows
         for (int x = lane; x < a.rows; x += 64) {
@@ -40,11 +65,13 @@ __global__ __launch_bounds__(THREADS) void fbq_join_pieces_kernel(const AttendAr
         before = __builtin_amdgcn_readlane(wave_scan(before), 63);
         const int shared_steps = a.shared_here ? (a.n_shared + kFewTile - 1) / kFewTile : 0, steps = few_steps(a, b);
         share = few_share(a, (all + shared_steps) * a.kv_heads);
-        own0 = (shared_steps + before) * a.kv_heads + h * steps;
-        shared0 = h * shared_steps;
-        n_own = steps == 0 ? 0 : (own0 + steps - 1) / share - own0 / share + 1;
-        if (a.shared_here) n_shared = (shared0 + shared_steps - 1) / share - shared0 / share + 1;
-        one_own = n_own == 1;
+        own.of((shared_steps + before) * a.kv_heads + h * steps, steps, share);
+        n_own = own.count;
+        if (a.shared_here) {
+            of_shared.of(h * shared_steps, shared_steps, share);
+            n_shared = of_shared.count;
+        }
+        one_own = own.last == own.first && steps > 0;
         if (one_own && !a.whole.o) return;
     } else {
         n_own = many_pieces(a, many_steps(a, many_limit(a, row_tokens(a, b), q.y, (i * a.group + j) / kManyRows)), a.splits == 1 ? 1 << 30 : many_share(a));
@@ -52,19 +79,15 @@ __global__ __launch_bounds__(THREADS) void fbq_join_pieces_kernel(const AttendAr
         if (n_own == 1 && !n_shared) return;
     }
     const int n = n_shared + n_own;
-    // where part p of the n lies: parts of one list are equally far apart but for the first of an item, which may be in a worker's other place
-    const int own_w = own0 / share, shared_w = shared0 / share;
-    const auto part = [&](int p, long *at) {
+    const auto part = [&](int p, long *at) {                  // where part p of the n lies
         if (p < n_shared) {
             if (!a.shared_here) return *at = p * rows + row, a.part_shared;
-            if (n_shared == 1) return *at = row, a.whole_shared;
-            const int w = shared_w + p;
-            return *at = ((long)w * 2 + ((long)w * share < shared0 ? 1 : 0)) * a.slot_rows + t * a.group + j, a.piece;
+            if (of_shared.first == of_shared.last) return *at = row, a.whole_shared;
+            return *at = of_shared.place(p, share) * a.slot_rows + t * a.group + j, a.piece;
         }
         if (!few) return *at = (p - n_shared) * rows + row, a.part;
         if (one_own) return *at = row, a.whole;
-        const int w = own_w + p - n_shared;
-        return *at = ((long)w * 2 + ((long)w * share < own0 ? 1 : 0)) * a.slot_rows + i * a.group + j, a.piece;
+        return *at = own.place(p - n_shared, share) * a.slot_rows + i * a.group + j, a.piece;
     };
 
     float m = kNoScore, l = 0;

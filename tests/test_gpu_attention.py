@@ -64,6 +64,15 @@ def test_single_tokens_one_long_row_among_short_ones():
     check([7, 20000, 100], [1] * 3, 2, 1, 64, 32, BF16, seed=3)
 
 
+@pytest.mark.parametrize("lengths", [[9000, 4000, 1, 12345], [33000], [0, 16000, 31, 16001, 64], [2500] * 20, [40 * b for b in range(60)]])
+@pytest.mark.parametrize("heads,kv_heads,shared_pages", [(8, 8, 0), (16, 4, 0), (3, 1, 0), (8, 8, 2)])
+def test_single_tokens_more_steps_than_waves(lengths, heads, kv_heads, shared_pages):
+    """Rows long and many enough that a wave has several steps: pieces that begin and end anywhere, whole blocks of them in one row, rows within one piece."""
+    if shared_pages:
+        lengths = [max(n, 32) for n in lengths]
+    check(lengths, [1] * len(lengths), heads, kv_heads, 16, 16, F16, shared_pages=shared_pages, seed=sum(lengths) % 1000)
+
+
 @pytest.mark.parametrize("dtype", [F16, BF16])
 @pytest.mark.parametrize("heads,kv_heads,max_count", [(4, 4, 5), (8, 4, 8), (8, 2, 4), (6, 2, 9), (32, 1, 3), (40, 1, 7), (3, 1, 100)])
 def test_several_tokens_a_row(heads, kv_heads, max_count, dtype):
