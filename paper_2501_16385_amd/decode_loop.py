@@ -15,6 +15,9 @@ least that keeps the data flow of a decoder layer and the values bounded:
     g, u    = h Wg, h Wu               one grouped launch
     x'      = (h + (silu(g) * u) Wd) / 2
 
+With a cache (DecoderStack(cache=..)) attention is real: k and v go into the cache's pages and a = softmax(q k^T / sqrt(d)) v over what the sequences hold, in
+the same graph (see batch_decode.py for a batch of samples of one prompt).
+
 Five launches per layer: four fused ones, two of which write the averages as well, and silu(g) * u.  Weights are random packed words (speed
 does not depend on the values) unless a list of quantized layers is passed in.  Prints one JSON line.
 """
@@ -28,6 +31,7 @@ import sys
 
 import torch
 
+from . import cache as kv
 from . import fbq
 from .random_layers import random_layer
 
@@ -37,24 +41,34 @@ import fbq_synth  # noqa: E402  (byte accounting)
 NAMES = ("q", "k", "v", "o", "gate", "up", "down")
 
 
-def layer_shapes(hidden: int, inter: int):
-    """(N, K) of the seven linears of one decoder layer."""
-    return {"q": (hidden, hidden), "k": (hidden, hidden), "v": (hidden, hidden), "o": (hidden, hidden),
+def layer_shapes(hidden: int, inter: int, kv_hidden: int = 0):
+    """(N, K) of the seven linears of one decoder layer; kv_hidden: rows of k and v where heads share them (0: hidden)."""
+    kv_rows = kv_hidden or hidden
+    return {"q": (hidden, hidden), "k": (kv_rows, hidden), "v": (kv_rows, hidden), "o": (hidden, hidden),
             "gate": (inter, hidden), "up": (inter, hidden), "down": (hidden, inter)}
 
 
 class DecoderStack:
-    """layers: list (one per decoder layer) of dicts name -> fbq.DeviceLayer."""
+    """layers: list (one per decoder layer) of dicts name -> fbq.DeviceLayer.
+
+    cache: a kv.Cache with a layer for each of them; `batch` is then the number of tokens of a step, and a step appends them to the cache's rows and attends over what
+    these hold.  counts [rows]: tokens of each row in a step (None: one); shared: the pages that all rows begin with (a view of a row of the table stays
+    right when pages move).  A row that no pages are left for is not written; `lacking` [1] counts the pages that a step lacked.
+    """
 
     def __init__(self, layers, hidden: int, inter: int, keep_per_layer_buffers: bool = False, batch: int = 1,
-                 share_workspaces: bool = False):
+                 share_workspaces: bool = False, cache=None, counts=None, shared=None):
         self.layers, self.hidden, self.inter, self.batch = layers, hidden, inter, batch
+        self.cache, self.shared = cache, shared
+        if cache is not None:
+            self._attend_over(cache, counts)
+        kv_hidden = hidden if cache is None else cache.heads * cache.head_dim
         self.lib = fbq.load()
         dev = "cuda"
         f16 = lambda n: torch.zeros((batch, n), dtype=torch.float16, device=dev)
         self.x = f16(hidden)
         n_buf = len(layers) if keep_per_layer_buffers else 1
-        self.buf = [{"q": f16(hidden), "k": f16(hidden), "v": f16(hidden), "o": f16(hidden), "h": f16(hidden),
+        self.buf = [{"q": f16(hidden), "k": f16(kv_hidden), "v": f16(kv_hidden), "a": f16(hidden) if cache is not None else None, "o": f16(hidden), "h": f16(hidden),
                      "gate": f16(inter), "up": f16(inter), "act": f16(inter), "down": f16(hidden), "x_in": f16(hidden)}
                     for _ in range(n_buf)]
         # one zero-filled workspace per linear: launches of one token never share one.  A prompt pass of hundreds of rows
@@ -65,6 +79,30 @@ class DecoderStack:
         else:
             self.ws = [{n: self._workspace(l[n].desc) for n in NAMES} for l in layers]
         self.graph = None
+
+    def _attend_over(self, cache, counts):
+        """What the steps' calls of the cache need, once: tokens a row, their places, attention's workspace."""
+        rows, ints = cache.lengths.numel(), lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")
+        counts = [1] * rows if counts is None else list(counts)
+        if len(counts) != rows or sum(counts) != self.batch or cache.pool.dtype != torch.float16 or self.hidden % cache.head_dim:
+            raise ValueError("cache: an fp16 cache of whole heads, with a row for every count; counts: as many tokens as the batch")
+        edges = [0]
+        for c in counts:
+            edges.append(edges[-1] + c)
+        self.count, self.start, self.lacking = ints(counts), ints([0] * rows), ints([0])
+        self.max_q = max(counts)
+        self.q_start = None if counts == [1] * rows else ints(edges)
+        q = torch.empty((self.batch, self.hidden // cache.head_dim, cache.head_dim), dtype=torch.float16, device="cuda")
+        self.attend_ws = kv.attention_workspace(cache, q, q_start=self.q_start, max_q=self.max_q, shared=self.shared)
+
+    def _attend(self, li, b, stream):
+        """a = attention of this step's tokens over the cache, this layer's k and v in their pages first."""
+        c = self.cache
+        heads = lambda t, n: t.view(self.batch, n, c.head_dim)
+        kv.cache_append(c, li, heads(b["k"], c.heads), heads(b["v"], c.heads), self.start, q_start=self.q_start, stream=stream)
+        n = self.hidden // c.head_dim
+        kv.attention(c, li, heads(b["q"], n), q_start=self.q_start, max_q=self.max_q, shared=self.shared, out=heads(b["a"], n), workspace=self.attend_ws, stream=stream)
+        return b["a"]
 
     def _workspace(self, desc):
         need = fbq.workspace_bytes(desc, self.batch)
@@ -87,19 +125,22 @@ class DecoderStack:
         stream = stream or torch.cuda.current_stream()
         sp = ctypes.c_void_p(stream.cuda_stream)
         x = self.x
+        if self.cache is not None:
+            kv.cache_reserve(self.cache, self.count, start=self.start, info=self.lacking, stream=stream)
         for li in range(len(self.layers)):
             b = self.buf[li % len(self.buf)]
             if len(self.buf) > 1:
                 b["x_in"].copy_(x)                      # kept for inspection only
             self._group(li, ("q", "k", "v"), [x, x, x], [b["q"], b["k"], b["v"]], sp)
-            self._group(li, ("o",), [b["v"]], [b["o"]], sp, mix=(x, b["h"]))                 # h = (x + o) / 2
+            a = b["v"] if self.cache is None else self._attend(li, b, stream)
+            self._group(li, ("o",), [a], [b["o"]], sp, mix=(x, b["h"]))                      # h = (x + o) / 2
             self._group(li, ("gate", "up"), [b["h"], b["h"]], [b["gate"], b["up"]], sp)
             fbq.silu_mul(b["gate"], b["up"], b["act"], stream)
             self._group(li, ("down",), [b["act"]], [b["down"]], sp, mix=(b["h"], x))         # x = (h + down) / 2
         return x
 
     def capture(self):
-        """Records step() into a HIP graph (after one eager step on a side stream, as capture requires)."""
+        """Records step() into a HIP graph (after one eager step on a side stream, as capture requires).  With a cache that step is one of the sequences' own."""
         side = torch.cuda.Stream()
         side.wait_stream(torch.cuda.current_stream())
         with torch.cuda.stream(side):
@@ -112,10 +153,10 @@ class DecoderStack:
         return self.graph
 
 
-def random_stack(n_layers, hidden, inter, r, bits, seed=1):
+def random_stack(n_layers, hidden, inter, r, bits, seed=1, kv_hidden=0):
     gen = torch.Generator(device="cuda")
     gen.manual_seed(seed)
-    shapes = layer_shapes(hidden, inter)
+    shapes = layer_shapes(hidden, inter, kv_hidden)
     return [{n: random_layer(fbq.Desc(shapes[n][0], shapes[n][1], r, bits), gen, gain=0.5) for n in NAMES} for _ in range(n_layers)]
 
 
