@@ -48,7 +48,7 @@ struct AttendArgs {
     // few-row kernel: `workers` waves; the partial results of pieces of items, two a worker ([workers][2][slot_rows]); those of whole items where something else
     // has to be added ([T heads]), null: out is written
     int workers, slot_rows;
-    bool direct;                         // an item a worker, no partial results
+    int direct;                          // 1: an item a worker, 2: an item a block; no partial results
     bool shared_here;                    // the shared tokens are items of this kernel's own, for the rows of all sequences together
     Partials piece, whole, whole_shared;
     // many-row kernel: at most `splits` pieces of a tile's keys, partial results [splits][T heads] (null: out is written); shared_splits of the shared tokens
@@ -58,7 +58,11 @@ struct AttendArgs {
 
 // The two types: operands of the matrix cores, and two floats rounded to a word of them (to nearest, ties to even).
 struct TypeF16 {
-    typedef half8_t operand;
+    static __device__ __forceinline__ float4_t mfma(word2_t a, word2_t b, float4_t c)       // 16 x 16 x 16
+    {
+        typedef _Float16 half4_t __attribute__((ext_vector_type(4)));
+        return __builtin_amdgcn_mfma_f32_16x16x16f16(__builtin_bit_cast(half4_t, a), __builtin_bit_cast(half4_t, b), c, 0, 0, 0);
+    }
     static __device__ __forceinline__ float4_t mfma(word4_t a, word4_t b, float4_t c)
     {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8_t, a), __builtin_bit_cast(half8_t, b), c, 0, 0, 0);
@@ -75,7 +79,11 @@ struct TypeF16 {
     static __device__ __forceinline__ uint16_t one(float x) { return __builtin_bit_cast(uint16_t, (_Float16)x); }
 };
 struct TypeBf16 {
-    typedef bfloat8_t operand;
+    static __device__ __forceinline__ float4_t mfma(word2_t a, word2_t b, float4_t c)
+    {
+        typedef short short4_t __attribute__((ext_vector_type(4)));
+        return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(short4_t, a), __builtin_bit_cast(short4_t, b), c, 0, 0, 0);
+    }
     static __device__ __forceinline__ float4_t mfma(word4_t a, word4_t b, float4_t c)
     {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bfloat8_t, a), __builtin_bit_cast(bfloat8_t, b), c, 0, 0, 0);

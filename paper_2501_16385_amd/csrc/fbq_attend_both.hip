@@ -1,14 +1,15 @@
 // A batch behind a shared prefix in one launch: the shared tokens against the rows of all sequences (many rows, bound by the matrix cores) and every row's own tokens (few
 // rows, bound by HBM) at the same time.  The first blocks, one a CU, are the shared tokens' - one block alone on a CU is about as fast as two that share it - and the others,
 // as many again at a time, find their places beside them.  us, 64 sequences of 64 heads (8 of keys) behind 16384 shared tokens, about 400 of their own each: 47
-// and 27 one after the other, 59 this way, and half as many parts to join (8.5, 11.5).
+// and 27 one after the other, 59 this way, and half as many parts to join (8.5, 11.5).  Up to 128 features: beyond, a block has a
+// CU's LDS to itself.
 #include "fbq_attend_few.h"
 #include "fbq_attend_many.h"
 
 namespace fbq {
 
 template <class TY, int DF, int DM>
-__global__ __launch_bounds__(256, DM == 256 ? 1 : 2) void fbq_attend_both_kernel(const AttendArgs a, const int tiles)
+__global__ __launch_bounds__(256, 2) void fbq_attend_both_kernel(const AttendArgs a, const int tiles)
 {
     __shared__ __attribute__((aligned(1024))) unsigned char room[kManyRoom<DM> > kFewRoom<DF> ? kManyRoom<DM> : kFewRoom<DF>];
     const int shared_blocks = a.kv_heads * tiles * a.shared_splits, block = blockIdx.x;
@@ -28,8 +29,7 @@ static hipError_t launch_both(const AttendArgs &a, hipStream_t stream)
     const dim3 grid(a.kv_heads * tiles * a.shared_splits + a.workers / kFewWaves), block(256);
     if (a.D <= 64) hipLaunchKernelGGL((fbq_attend_both_kernel<TY, 64, 64>), grid, block, 0, stream, a, tiles);
     else if (a.D <= 96) hipLaunchKernelGGL((fbq_attend_both_kernel<TY, 128, 96>), grid, block, 0, stream, a, tiles);
-    else if (a.D <= 128) hipLaunchKernelGGL((fbq_attend_both_kernel<TY, 128, 128>), grid, block, 0, stream, a, tiles);
-    else hipLaunchKernelGGL((fbq_attend_both_kernel<TY, 256, 256>), grid, block, 0, stream, a, tiles);
+    else hipLaunchKernelGGL((fbq_attend_both_kernel<TY, 128, 128>), grid, block, 0, stream, a, tiles);
     return hipGetLastError();
 }
 

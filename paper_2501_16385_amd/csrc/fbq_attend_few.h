@@ -26,8 +26,9 @@ constexpr int kOnce = 2;
 template <int DP>
 struct Step {
     static constexpr int kV = DP == 256 ? 2 : 1;              // 16-byte loads of a lane's features of one value row (DP 64: one of 8 bytes)
-    word4_t k[2][DP / 32];
-    word4_t v[2][4][kV];
+    static constexpr int kHalves = DP == 256 ? 1 : 2;         // of its 32 keys that a turn loads and works on (256 features: two turns a step, or registers run out)
+    word4_t k[kHalves][DP / 32];
+    word4_t v[kHalves][4][kV];
 };
 
 // A piece of an item: what its loads and its rows need, both for the piece worked on and the one behind it.
@@ -48,7 +49,8 @@ constexpr int kFewRoom = (kFewWaves - 1) * (DP / 4 + 2) * 256;
 template <class TY, int DP>
 __device__ __forceinline__ void attend_few(const AttendArgs &a, int block, unsigned char *room)
 {
-    constexpr int J = DP / 16;                                // features of a lane's value pieces, and products O^T of a step
+    constexpr int J = DP / 16;                                // features of a lane's value pieces, and products O^T of a turn
+    constexpr int kHalves = Step<DP>::kHalves, kTurn = 16 * kHalves, kTurns = kFewTile / kTurn;   // keys a turn, turns a step
     const int lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4;
     const int worker = uniform(block * kFewWaves + (threadIdx.x >> 6));
     const int D = a.D, ps1 = (1 << a.log_ps) - 1;
@@ -56,14 +58,17 @@ __device__ __forceinline__ void attend_few(const AttendArgs &a, int block, unsig
     Piece<DP> cur, behind;
     int u = 0, end = 0;
     bool together = false;                                    // the block's waves have a piece each of one item
-    if (a.direct) {                                           // an item a worker
-        cur.b = worker / a.kv_heads;
+    if (a.direct) {                                           // an item a worker, or a part of it each for the block's workers
+        const int item = a.direct == 1 ? worker : block;
+        cur.b = item / a.kv_heads;
         if (cur.b >= a.rows) return;
-        cur.h = worker - cur.b * a.kv_heads;
+        cur.h = item - cur.b * a.kv_heads;
         cur.limit = uniform(row_tokens(a, cur.b));
         cur.steps = uniform(few_steps(a, cur.b, cur.limit));
-        cur.step = 0;
-        cur.n = cur.steps;
+        together = a.direct == 2;
+        const int share = together ? (cur.steps + kFewWaves - 1) / kFewWaves : cur.steps;
+        cur.step = together ? min((worker & (kFewWaves - 1)) * share, cur.steps) : 0;
+        cur.n = min(share, cur.steps - cur.step);
     } else {
         int own = 0;
         for (int b = lane; b < a.rows; b += 64) own += few_steps(a, b);
@@ -163,8 +168,8 @@ __device__ __forceinline__ void attend_few(const AttendArgs &a, int block, unsig
     for (int e = 0; e < 4; ++e) v_off[e] = J * col < D ? ((4 * grp + e) * D + J * col) * 2 : kNowhere;
     auto load = [&](Step<DP> &to, Piece<DP> &x, int s) __attribute__((always_inline)) {
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const int key = x.key0 + s * kFewTile + 16 * half;
+        for (int half = 0; half < kHalves; ++half) {
+            const int key = x.key0 + s * kTurn + 16 * half;
             int valid = min(max(x.limit - key, 0), 16);
             const int id = valid ? x.pages.at(key >> a.log_ps) : 0;
             if ((unsigned)id >= (unsigned)a.pages) valid = 0;
@@ -199,22 +204,24 @@ __device__ __forceinline__ void attend_few(const AttendArgs &a, int block, unsig
         least = uniform(least);
     };
     auto compute = [&](const Step<DP> &x, int s) __attribute__((always_inline)) {
-        float4_t z[2];
+        float4_t z[kHalves];
+        float top = -INFINITY;
+        const int key = cur.key0 + s * kTurn;
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
+        for (int half = 0; half < kHalves; ++half) {
             z[half] = float4_t{0, 0, 0, 0};
 #pragma unroll
             for (int y = 0; y < DP / 32; ++y) z[half] = TY::mfma(x.k[half][y], cur.q[y], z[half]);
         }
-        const int key = cur.key0 + s * kFewTile;
-        if (key + kFewTile > least) {
+        if (key + kTurn > least) {
 #pragma unroll
-            for (int half = 0; half < 2; ++half)
+            for (int half = 0; half < kHalves; ++half)
 #pragma unroll
                 for (int y = 0; y < 4; ++y)
                     if (key + 16 * half + 4 * grp + y >= cur.sees) z[half][y] = -INFINITY;
         }
-        float top = fmaxf(fmaxf(fmaxf(z[0][0], z[0][1]), fmaxf(z[0][2], z[0][3])), fmaxf(fmaxf(z[1][0], z[1][1]), fmaxf(z[1][2], z[1][3])));
+#pragma unroll
+        for (int half = 0; half < kHalves; ++half) top = fmaxf(top, fmaxf(fmaxf(z[half][0], z[half][1]), fmaxf(z[half][2], z[half][3])));
         top = larger_of_16(top);
         top = larger_of_32(top) * a.scale;
         if (__ballot(top > m + kSlack)) {
@@ -224,9 +231,9 @@ __device__ __forceinline__ void attend_few(const AttendArgs &a, int block, unsig
             for (int j = 0; j < J; ++j) o[j] *= by;
             m = to;
         }
-        word4_t p;
+        uint32_t p[2 * kHalves];
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
+        for (int half = 0; half < kHalves; ++half) {
 #pragma unroll
             for (int y = 0; y < 4; ++y) {
                 z[half][y] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[half][y], a.scale, -m));
@@ -237,13 +244,14 @@ __device__ __forceinline__ void attend_few(const AttendArgs &a, int block, unsig
         }
 #pragma unroll
         for (int j = 0; j < J; ++j) {
-            word4_t vt;
+            uint32_t vt[2 * kHalves];
 #pragma unroll
-            for (int y = 0; y < 4; ++y) {                     // two keys of feature j
+            for (int y = 0; y < 2 * kHalves; ++y) {           // two keys of feature j
                 const uint32_t lo = x.v[y >> 1][2 * (y & 1)][j >> 3][(j & 7) >> 1], hi = x.v[y >> 1][2 * (y & 1) + 1][j >> 3][(j & 7) >> 1];
                 vt[y] = __builtin_amdgcn_perm(hi, lo, j & 1 ? 0x07060302u : 0x05040100u);
             }
-            o[j] = TY::mfma(vt, p, o[j]);
+            if constexpr (kHalves == 2) o[j] = TY::mfma(word4_t{vt[0], vt[1], vt[2], vt[3]}, word4_t{p[0], p[1], p[2], p[3]}, o[j]);
+            else o[j] = TY::mfma(word2_t{vt[0], vt[1]}, word2_t{p[0], p[1]}, o[j]);
         }
     };
     bool first = true;
@@ -284,7 +292,7 @@ __device__ __forceinline__ void attend_few(const AttendArgs &a, int block, unsig
             }
         }
         if (cur.t < 0) return;
-        const bool whole = cur.n == cur.steps;
+        const bool whole = a.direct || cur.n == cur.steps;
         const Partials to = whole ? (cur.b < 0 ? a.whole_shared : a.whole) : a.piece;
         const int d0 = 4 * J * grp;
         if (whole && !to.o) {
@@ -318,7 +326,7 @@ __device__ __forceinline__ void attend_few(const AttendArgs &a, int block, unsig
     // A step's loads go out before the step before it is worked on, those of a piece's first step too: page list and queries of the piece behind come while the one
     // before runs.
     prepare(cur);
-    if (cur.n == 0) {                                         // (an item a worker, and this one has no tokens)
+    if (cur.n == 0) {                                         // (no tokens in the item, or in this worker's part)
         begin();
         finish();
         return;
@@ -330,10 +338,10 @@ __device__ __forceinline__ void attend_few(const AttendArgs &a, int block, unsig
     begin();
     int s = 0;
     auto turn = [&](const Step<DP> &now, Step<DP> &next) __attribute__((always_inline)) {
-        if (s + 1 < cur.n) load(next, cur, s + 1);
+        if (s + 1 < cur.n * kTurns) load(next, cur, s + 1);
         else if (more) load(next, behind, 0);
         compute(now, s);
-        if (++s < cur.n) return false;
+        if (++s < cur.n * kTurns) return false;
         finish();
         if (!more) return true;
         first = false;

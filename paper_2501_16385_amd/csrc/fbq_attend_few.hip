@@ -13,7 +13,7 @@ __global__ __launch_bounds__(64 * kFewWaves, DP == 256 ? 1 : 2) void fbq_attend_
 template <class TY>
 static hipError_t launch_few(const AttendArgs &a, hipStream_t stream)
 {
-    const dim3 grid(((a.direct ? a.rows * a.kv_heads : a.workers) + kFewWaves - 1) / kFewWaves), block(64 * kFewWaves);
+    const dim3 grid(a.direct == 2 ? a.rows * a.kv_heads : ((a.direct ? a.rows * a.kv_heads : a.workers) + kFewWaves - 1) / kFewWaves), block(64 * kFewWaves);
     if (a.D <= 64) hipLaunchKernelGGL((fbq_attend_few_kernel<TY, 64>), grid, block, 0, stream, a);
     else if (a.D <= 128) hipLaunchKernelGGL((fbq_attend_few_kernel<TY, 128>), grid, block, 0, stream, a);
     else hipLaunchKernelGGL((fbq_attend_few_kernel<TY, 256>), grid, block, 0, stream, a);

@@ -202,8 +202,15 @@ static hipError_t launch_join(const AttendArgs &a, bool few, hipStream_t stream)
     return a.D <= 64 ? launch_join<TY, 16>(a, few, stream) : a.D <= 128 ? launch_join<TY, 32>(a, few, stream) : launch_join<TY, 64>(a, few, stream);
 }
 
-// Few-row kernel: where a row of the table has room for no more tokens than this, a wave takes an item whole and there is nothing to join.
-constexpr long kDirectTokens = 256;
+// Few-row kernel: whether an item goes whole to a wave (1) or a block (2), with nothing to join, or the steps of all are dealt out (0), by the room that a row of the table has.
+// us, 64 query heads on 32 of 128 features, 1 / 2 / 0 (r: rows of 0.25 to 1.75 times as many tokens).  60 tokens: 2 rows 7.1 / 7.3 / 12.1, 32 rows 9.5 / 14.9 / 16.1, 128 r 29 / 52 / 43.
+// 200: 2 rows 14.2 / 9.2 / 14.9, 16 17.2 / 13.6 / 22.8, 32 19.6 / 24.9 / 30.4, 64 r 43.5 / 47.5 / 50.3.  500: 2 rows 29 / 13.0 / 15.1, 16 35 / 25 / 33, 64 r 103 / 95 / 98.  1000: 2 rows
+// 56 / 20.1 / 16.9, 8 62 / 25 / 32, 32 80 / 86 / 89, 16 r 101 / 57.5 / 55.7.  2000: 8 rows 119 / 44 / 55, but 16 r 198 / 110 / 96, where one row is all that is left at the end.
+static int few_direct(long items, long tokens)
+{
+    if (tokens <= 256 && items >= 1024) return 1;
+    return tokens <= 512 || (tokens <= 1024 && items >= 128) ? 2 : 0;
+}
 
 struct AttendPlan {
     AttendArgs a;
@@ -253,9 +260,8 @@ static AttendPlan attend_plan(const fbq_attention_call &c, void *workspace)
             room(&a.whole_shared, results);
         }
     }
-    if (p.few && !a.n_shared && own_tokens <= kDirectTokens) {
-        a.direct = true;
-    } else if (p.few) {
+    a.direct = p.few && !a.n_shared ? few_direct((long)a.rows * a.kv_heads, own_tokens) : 0;
+    if (p.few && !a.direct) {
         const long steps = ((own_tokens + kFewTile - 1) / kFewTile * a.rows + (a.shared_here ? a.n_shared / kFewTile + 1 : 0)) * a.kv_heads;
         a.workers = (int)std::min(a.D > 128 ? 1024L : 2048L, (steps + kFewWaves - 1) / kFewWaves * kFewWaves);
         a.workers = std::max(a.workers, kFewWaves);
@@ -263,7 +269,7 @@ static AttendPlan attend_plan(const fbq_attention_call &c, void *workspace)
         room(&a.piece, 2L * a.workers * a.slot_rows);
         if (a.n_shared) room(&a.whole, results);
         p.join = true;
-    } else {
+    } else if (!p.few) {
         const long per_row = (a.group + kManyRows - 1) / kManyRows;
         const long tiles = a.q_start ? (all_queries + kManyRows - 1) / kManyRows : a.rows * per_row;
         a.splits = (int)std::max(1L, std::min({(2L * many_blocks(a.D) - 1) / (tiles * a.kv_heads), (own_tokens + 255) / 256, 128L, 65535 / (tiles + a.rows)}));
@@ -318,9 +324,10 @@ extern "C" fbq_status fbq_attention(const fbq_attention_call *c, void *workspace
     const int type = c->cache.desc.type;
     const hipStream_t s = (hipStream_t)stream;
     hipError_t e = hipSuccess;
-    if (p.shared_many && p.few) e = launch_attend_both(p.a, type, s);
+    const bool both = p.shared_many && p.few && p.a.D <= 128;
+    if (both) e = launch_attend_both(p.a, type, s);
     else if (p.shared_many) e = launch_attend_many(p.a, type, true, s);
-    if (e == hipSuccess && !(p.shared_many && p.few)) e = p.few ? launch_attend_few(p.a, type, s) : launch_attend_many(p.a, type, false, s);
+    if (e == hipSuccess && !both) e = p.few ? launch_attend_few(p.a, type, s) : launch_attend_many(p.a, type, false, s);
     if (e == hipSuccess && p.join) e = type == FBQ_F16 ? launch_join<TypeF16>(p.a, p.few, s) : launch_join<TypeBf16>(p.a, p.few, s);
     return e == hipSuccess ? FBQ_OK : FBQ_ERR_HIP;
 }
