@@ -171,9 +171,10 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, const bool shar
     };
 
     // reads: a key's piece s of DP / 16 pairs, and a value's column block dblk of 32
-    const int k_at = col * kRowBytes, k_piece = grp ^ key_swap(col, kPieces);
-    const int v_row = 4 * grp + ((lane & 15) >> 2), v_at = v_row * kRowBytes + 8 * (lane & 1);
-    const int v_piece = (2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ value_swap(v_row, kPieces);
+    int k_at = col * kRowBytes, k_piece = grp ^ key_swap(col, kPieces);
+    const int v_row = 4 * grp + ((lane & 15) >> 2);
+    int v_at = v_row * kRowBytes + 8 * (lane & 1);
+    int v_piece = (2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ value_swap(v_row, kPieces);
 
     float16_t o[DP / 32];
 #pragma unroll
@@ -209,6 +210,8 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, const bool shar
         }
         const int key = key0 + s * kManyTile;
         if (key >= most) return;
+        // 256 features: all addresses of a step in registers across steps would push others out to memory, whose loads wait for the copies under way
+        if constexpr (DP == 256) asm volatile("" : "+v"(k_at), "+v"(k_piece), "+v"(v_at), "+v"(v_piece));
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) fetch(i, s);         // (past the last step: of whatever lies there, its scores are not used)
         if (key + kManyTile > least) {
