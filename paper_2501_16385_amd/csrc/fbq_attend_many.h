@@ -58,9 +58,11 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, const bool shar
     int b = 0, q0 = 0, nq = a.T, limit = a.n_shared, tile = y, split = z, splits = a.shared_splits, tokens_of_row = 0;
     if (!shared) {
         const int share = a.splits == 1 ? 1 << 30 : many_share(a);
-        int queries, tokens, tiles, pieces, count, longest;   // of the table row that is this lane's
+        int queries, query0, tokens, tiles, pieces, count, longest;   // of the table row that is this lane's
         const auto look = [&](int row) {
-            queries = row < a.rows ? queries_of(a, row).y : 0;
+            const int2 q = row < a.rows ? queries_of(a, row) : make_int2(0, 0);
+            queries = q.y;
+            query0 = q.x;
             tokens = row < a.rows ? row_tokens(a, row) : 0;
             tiles = many_tiles(a, queries);
             pieces = many_pieces(a, many_steps(a, tokens), share);
@@ -68,7 +70,7 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, const bool shar
             longest = (many_steps(a, tokens) + pieces - 1) / pieces;
         };
         int all = 0;
-        for (int base = 0; base < a.rows; base += 64) {
+        for (int base = (a.rows - 1) & ~63; base >= 0; base -= 64) {          // (the first ones last: they stay in the registers)
             look(base + lane);
             all += __builtin_amdgcn_readlane(wave_scan(count), 63);
         }
@@ -102,7 +104,7 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, const bool shar
         tile = __builtin_amdgcn_readlane(tiles, at) - 1 - rest / row_pieces;
         split = rest % row_pieces;
         nq = __builtin_amdgcn_readlane(queries, at);
-        q0 = uniform(queries_of(a, b).x);
+        q0 = __builtin_amdgcn_readlane(query0, at);
         tokens_of_row = __builtin_amdgcn_readlane(tokens, at);
         limit = many_limit(a, tokens_of_row, nq, tile);
         splits = many_pieces(a, many_steps(a, limit), share);
