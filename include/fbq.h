@@ -374,7 +374,7 @@ fbq_status fbq_cache_reserve(const fbq_cache *c, const int32_t *count, int32_t *
 
 /*
  * fbq_cache_append - writes new keys and values of one layer into their pages: token i of row b goes to position start[b] + i; nothing where start[b] < 0.
- *   T tokens; q_start device [rows + 1]: row b's are q_start[b] .. q_start[b + 1] - 1, in ascending order; NULL: T == rows, one token a row
+ *   T tokens, at most 2^23; q_start device [rows + 1]: row b's are q_start[b] .. q_start[b + 1] - 1, in ascending order; NULL: T == rows, one token a row
  *   k, v device [T][kv_heads][head_dim], rows k_stride and v_stride elements apart (multiples of 8, at least kv_heads * head_dim)
  */
 fbq_status fbq_cache_append(const fbq_cache *c, int layer, int T, const int32_t *q_start, const int32_t *start, const void *k, int64_t k_stride,
@@ -409,16 +409,17 @@ fbq_status fbq_cache_compact(const fbq_cache *c, int32_t *table_out, int32_t *re
  * and lse = ln sum_j p_j.  A query token that sees nothing gets 0 and -infinity.  Sums, maxima and exponentials are in fp32; p_j is rounded to the cache's type
  * as an operand of the matrix cores, out once at the end.
  *   T query tokens in all; q_start device [rows + 1], ascending: row b's are q_start[b] .. q_start[b + 1] - 1; NULL: T == rows, one a row.  max_q: at least the most that a
- *            row has (1 with NULL; a row's tokens past it are left alone, and so are tokens past q_start[rows])
+ *            row has (1 with NULL; the result of a row with more is unspecified).  Tokens outside q_start[0] .. q_start[rows] - 1 are left alone
  *   q, out   device [T][heads][head_dim] of the cache's type, rows q_stride and out_stride elements apart (multiples of 8, at least heads * head_dim)
+ *            (out may overlap neither q nor the pool)
  *   lse      device [T][heads] fp32, or NULL
  *   shared   device list of n_shared pages, or NULL and 0: the first n_shared entries of EVERY row's table are these.  They are read once for all rows together
  *            where few query tokens come with each row; the result is that of the call without, other last bits aside.
- *   workspace fbq_attention_workspace_bytes() of the same call (pointers are not looked at); contents do not matter.  Calls that may run concurrently must not share one.
+ *   workspace fbq_attention_workspace_bytes() of the same call (pointers are not looked at; 0: NULL will do); contents do not matter.  Calls that may run concurrently must not share one.
  */
 typedef struct {
     fbq_cache cache;    /* refs is not used */
-    int32_t layer, heads, T, max_q;
+    int32_t layer, heads, T, max_q;   /* heads: a multiple of kv_heads, at most 8192; T at most 2^20, T * heads at most 2^25 */
     const int32_t *q_start;
     const void *q;
     int64_t q_stride;

@@ -208,6 +208,7 @@ static hipError_t launch_join(const AttendArgs &a, bool few, hipStream_t stream)
 // 56 / 20.1 / 16.9, 8 62 / 25 / 32, 32 80 / 86 / 89, 16 r 101 / 57.5 / 55.7.  2000: 8 rows 119 / 44 / 55, but 16 r 198 / 110 / 96, where one row is all that is left at the end.
 static int few_direct(long items, long tokens)
 {
+    if (items > 1L << 22) return 0;                           // (a grid counts its threads in 32 bits)
     if (tokens <= 256 && items >= 1024) return 1;
     return tokens <= 512 || (tokens <= 1024 && items >= 128) ? 2 : 0;
 }
@@ -308,7 +309,7 @@ static fbq_status check_attention(const fbq_attention_call *c, bool pointers)
     const int64_t row = (int64_t)c->heads * d.head_dim;
     if (c->q_stride < row || c->out_stride < row || c->q_stride % 8 || c->out_stride % 8) return FBQ_ERR_SHAPE;
     if (c->heads > 8192 || c->T > (1 << 20) || c->q_stride > (1L << 32) || c->out_stride > (1L << 32)) return FBQ_ERR_UNSUPPORTED;
-    if ((int64_t)c->T * c->heads > (1L << 30) || ((int64_t)c->T * (c->heads / d.kv_heads)) / kManyRows + c->cache.rows > 32767) return FBQ_ERR_UNSUPPORTED;
+    if ((int64_t)c->T * c->heads > (1L << 25) || ((int64_t)c->T * (c->heads / d.kv_heads)) / kManyRows + c->cache.rows > 32767) return FBQ_ERR_UNSUPPORTED;
     if (!pointers) return FBQ_OK;
     if (!c->q || !c->out || (c->n_shared && !c->shared)) return FBQ_ERR_NULL;
     if (!aligned(c->q, 16) || !aligned(c->out, 16) || !aligned(c->lse, 4) || !aligned(c->q_start, 4) || !aligned(c->shared, 4)) return FBQ_ERR_ALIGN;

@@ -432,7 +432,7 @@ extern "C" fbq_status fbq_cache_append(const fbq_cache *c, int layer, int T, con
     const fbq_status st = check_cache(c, false);
     if (st != FBQ_OK) return st;
     const int64_t row = (int64_t)c->desc.kv_heads * c->desc.head_dim;
-    if (layer < 0 || layer >= c->desc.layers || T < 1 || T > (1 << 24) || (!q_start && T != c->rows)) return FBQ_ERR_SHAPE;
+    if (layer < 0 || layer >= c->desc.layers || T < 1 || T > (1 << 23) || (!q_start && T != c->rows)) return FBQ_ERR_SHAPE;
     if (k_stride < row || v_stride < row || k_stride % 8 || v_stride % 8 || k_stride > (1L << 32) || v_stride > (1L << 32)) return FBQ_ERR_SHAPE;
     if (!start || !k || !v) return FBQ_ERR_NULL;
     if (!aligned(q_start, 4) || !aligned(start, 4) || !aligned(k, 16) || !aligned(v, 16)) return FBQ_ERR_ALIGN;

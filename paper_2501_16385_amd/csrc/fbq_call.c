@@ -110,7 +110,7 @@ static int tokens(PyObject *t, PyObject *dtype, tokens_t *x)
 {
     long long shape[3], stride[3];
     if (!is_of(t, dtype) || !whole(PyObject_GetAttr(t, s_shape), 3, shape) || !whole(PyObject_CallMethodNoArgs(t, s_stride), 3, stride) || stride[2] != 1 ||
-        stride[1] != shape[2] || !is_true(PyObject_GetAttr(t, s_is_cuda)) || !number(PyObject_CallMethodNoArgs(t, s_data_ptr), &x->at))
+        (stride[1] != shape[2] && shape[1] > 1) || !is_true(PyObject_GetAttr(t, s_is_cuda)) || !number(PyObject_CallMethodNoArgs(t, s_data_ptr), &x->at))
         return 0;
     x->T = shape[0]; x->heads = shape[1]; x->dim = shape[2];
     x->stride = shape[0] > 1 ? stride[0] : shape[1] * shape[2];
@@ -161,6 +161,10 @@ static PyObject *attention(PyObject *self, PyObject *const *arg, Py_ssize_t n)
     ok = ok && list(arg[7], arg[3], c.cache.rows + 1LL, &q_start, &count) && list(arg[12], arg[4], q.T * q.heads, &lse, &count) && list(arg[9], arg[3], -1, &shared, &count) &&
          count <= INT32_MAX;
     if (ok) c.n_shared = (int32_t)count;
+    if (ok && lse) {
+        long long shape[2];
+        ok = whole(PyObject_GetAttr(arg[12], s_shape), 2, shape) && shape[0] == q.T && shape[1] == q.heads;
+    }
     ok = ok && pointer(arg[13], &ws) && ws && number(PyObject_CallMethodNoArgs(arg[13], s_numel), &count) && number(PyObject_CallMethodNoArgs(arg[13], s_element_size), &each);
     if (!ok) return not_as_expected();
     c.layer = (int32_t)layer; c.heads = (int32_t)q.heads; c.T = (int32_t)q.T; c.max_q = (int32_t)max_q;

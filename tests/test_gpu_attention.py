@@ -221,3 +221,56 @@ def test_other_streams_and_graph_replays():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, fbq.attention(cache, 0, q, shared=shared)), step
+
+
+def test_on_a_stream_that_is_not_the_current_one():
+    """Workspace and result of a call's own, on a side stream that is busy: what the current stream allocates meanwhile gets other memory."""
+    import paper_2501_16385_amd as fbq
+    pool, table, n, refs = make_cache([700, 33, 256], 2, 64, 16, F16, seed=4, width=90)
+    cache = to_cache(fbq, pool, table, n, refs)
+    q = torch.randn(3, 4, 64).half().cuda()
+    want = fbq.attention(cache, 0, q)
+    side, busy = torch.cuda.Stream(), torch.randn(4096, 4096, device="cuda")
+    torch.cuda.synchronize()
+    results = []
+    for _ in range(5):
+        with torch.cuda.stream(side):
+            busy = busy @ busy * 1e-3
+        results.append(fbq.attention(cache, 0, q, stream=side))
+        for _ in range(20):
+            torch.full((1 << 20,), float("nan"), device="cuda")
+    torch.cuda.synchronize()
+    for got in results:
+        assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.3, 1e-30, 3.0])
+def test_scales(scale):
+    check([100, 33], [1, 1], 4, 2, 64, 16, F16, scale=scale, seed=1, gain=0.5)
+    check([100, 33], [60, 33], 4, 2, 64, 16, BF16, scale=scale, seed=2, gain=0.5)
+
+
+def test_the_compiled_call_and_the_python_one_refuse_the_same():
+    import paper_2501_16385_amd as fbq
+    pool, table, n, refs = make_cache([40, 100], 2, 64, 16, F16, seed=9)
+    cache = to_cache(fbq, pool, table, n, refs)
+    q = torch.randn(2, 4, 64).half().cuda()
+    ws, out = torch.empty(1 << 20, dtype=torch.uint8, device="cuda"), torch.empty_like(q)
+    good = dict(out=out, workspace=ws)
+    fbq.attention(cache, 0, q, **good)
+    for bad in (dict(out=out[:1]), dict(out=out.float()), dict(lse=torch.empty(2, 4, device="cuda").half()), dict(lse=torch.empty(4, 2, device="cuda")),
+                dict(q_start=torch.zeros(2, dtype=torch.int32, device="cuda")), dict(q_start=torch.zeros(3, device="cuda")), dict(shared=torch.zeros(1, device="cuda"))):
+        for form in (good, dict()):
+            with pytest.raises(ValueError):
+                fbq.attention(cache, 0, q, **{**form, **bad})
+    for wrong in (q.cpu(), q.float(), q[0], q.transpose(1, 2), q[:, :, :32]):
+        with pytest.raises((ValueError, RuntimeError)):
+            fbq.attention(cache, 0, wrong, **good)
+    for layer, kw in ((1, {}), (-1, {}), (0, dict(max_q=2)), (0, dict(workspace=ws[:8]))):
+        with pytest.raises(fbq.FbqError):
+            fbq.attention(fbq.Cache(cache.pool, torch.cat([cache.table] * 20, 1).contiguous(), cache.lengths, cache.refs), layer, q, **{**good, **kw})
+    k = torch.randn(2, 2, 64).half().cuda()
+    start = torch.zeros(2, dtype=torch.int32, device="cuda")
+    for args in ((k.float(), k, start), (k, k[:1], start), (k, k, start.float()), (k, k, start[:1]), (k[:, :1], k[:, :1], start)):
+        with pytest.raises((ValueError, fbq.FbqError)):
+            fbq.cache_append(cache, 0, *args)
