@@ -12,6 +12,9 @@
 // takes them as operand B where they are, since the order of a contraction is free: V^T's lanes take the same eight keys.  A lane loads DP / 16
 // features (l % 16 being the piece) of its eight keys and turns them by byte permutes; row l % 16 of the j-th product is then feature (DP / 16) (l % 16) + j, and
 // a lane's results are DP / 4 features in a row of one query row.  The scale by exp(m_old - m_new) is the lane's own.
+//
+// Measured, 128 features, the join included: 64 rows of 4096 tokens, 64 heads of 8, 169 us (6.35 TB/s; a kernel that only reads 6.31); 16 rows of about 1000, 32 heads, 54 (263 MB; reading alone
+// 43.5); one row of 65537, 64 heads of 8, 55.  Two steps of 16 KB are under way in each of eight waves a CU; a wave alone on its SIMD takes 1.65 us a step.
 #ifndef FBQ_ATTEND_FEW_H
 #define FBQ_ATTEND_FEW_H
 

@@ -7,7 +7,8 @@ constexpr int kJoinThreads = 256;
 
 // The partial results of one query row, added up in an order that depends on their number alone, so that equal calls give equal bits:
 //     out = sum_p o_p 2^(m_p - m) / sum_p l_p 2^(m_p - m),   m the largest m_p.   A part whose sum l is 0 saw nothing and has no o.
-// Bound by the latency of a chain of loads - where the parts lie, then their m, l and o at once - so as many as possible are under way together.
+// Bound by the latency of a chain of loads - where the parts lie, then their m, l and o at once - so as many as possible are under way together: 64 rows of 67 parts 5.5 us (71.6 with a wave
+// going through 256 one after the other), 4096 rows of 9 parts 8.8.
 
 // The parts of an item of the few-row kernel's line: pieces of the workers first .. last, those of a whole block of workers as one (see few_together).
 struct FewParts {
