@@ -81,6 +81,8 @@ class Cache:
     refs: "object"
     _c: "object" = field(init=False, repr=False, compare=False)
     _at: int = field(init=False, repr=False, compare=False)
+    _rooms: list = field(init=False, repr=False, compare=False, default_factory=list)     # the page operations' workspaces, and ..
+    _pairs: int = field(init=False, repr=False, compare=False, default=0)                 # .. for how many pairs the last one is (see _room)
 
     def __post_init__(self):
         lib = fbq.load()
@@ -162,8 +164,14 @@ def cache_free(cache: Cache, rows, stream=None) -> None:
 
 
 def _room(cache: Cache, n: int, stream):
-    import torch
-    return _used_on(torch.empty(fbq.load().fbq_cache_workspace_bytes(cache._c.desc, n), dtype=torch.uint8, device=cache.pool.device), stream)
+    """Workspace of a page operation that was given none; the cache keeps it, since operations on one cache's rows and reference counts have to follow each other anyway.  A
+    smaller one is kept beside a larger: a captured graph may hold it."""
+    if not cache._rooms or n > cache._pairs:
+        import torch
+        cache._pairs = max(n, 256)
+        size = fbq.load().fbq_cache_workspace_bytes
+        cache._rooms.append(torch.empty(max(size(cache._c.desc, min(cache._pairs, 65536)), size(cache._c.desc, 0)), dtype=torch.uint8, device=cache.pool.device))
+    return _used_on(cache._rooms[-1], stream)
 
 
 def _size(workspace) -> int:
@@ -226,17 +234,16 @@ def attention(cache: Cache, layer: int, q, q_start=None, max_q: int = 1, shared=
     q_start [rows + 1]: the rows' tokens in q, at most max_q a row; None: one token a row.  shared: the pages that all rows' tables begin with, read once
     for all rows.  scale: head_dim ** -0.5 by default.  lse: float32 [T, heads], takes the logarithm of the softmax's sums.
     """
-    if out is None or workspace is None:
+    if out is None:
         import torch
-        if out is None:
-            out = _used_on(torch.empty(q.shape, dtype=q.dtype, device=q.device), stream)
+        out = _used_on(torch.empty(q.shape, dtype=q.dtype, device=q.device), stream)
     scale = cache.head_dim ** -0.5 if scale is None else float(scale)
-    if workspace is not None:
-        # one row of 33 tokens, us a call: 9.4 by way of ctypes' argument objects, 6.0 this way
-        rc = _call[0].attention(_call[1], cache._at, cache.pool.dtype, _int32, _float32, layer, q, q_start, max_q, shared, scale, out, lse, workspace, _stream(stream))
-        if rc is not None:
-            _check(rc, "fbq_attention")
-            return out
+    # one row of 33 tokens, us a call: 9.4 by way of ctypes' argument objects, 6.0 this way
+    rc = _call[0].attention(_call[1], cache._at, cache.pool.dtype, _int32, _float32, layer, q, q_start, max_q, shared, scale, out, lse, workspace, _stream(stream))
+    if rc is not None and (rc != 1 or workspace is not None):  # (1, a null pointer: the workspace, where none was given)
+        _check(rc, "fbq_attention")
+        return out
+    import torch
     c = _arguments(cache, layer, q, q_start, max_q, shared, scale, out, lse)
     lib = fbq.load()
     if workspace is None:

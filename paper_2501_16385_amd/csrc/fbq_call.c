@@ -165,7 +165,9 @@ static PyObject *attention(PyObject *self, PyObject *const *arg, Py_ssize_t n)
         long long shape[2];
         ok = whole(PyObject_GetAttr(arg[12], s_shape), 2, shape) && shape[0] == q.T && shape[1] == q.heads;
     }
-    ok = ok && pointer(arg[13], &ws) && ws && number(PyObject_CallMethodNoArgs(arg[13], s_numel), &count) && number(PyObject_CallMethodNoArgs(arg[13], s_element_size), &each);
+    ok = ok && pointer(arg[13], &ws);                       // (no workspace: the library says whether the call needs one)
+    count = 0;
+    if (ok && arg[13] != Py_None) ok = number(PyObject_CallMethodNoArgs(arg[13], s_numel), &count) && number(PyObject_CallMethodNoArgs(arg[13], s_element_size), &each);
     if (!ok) return not_as_expected();
     c.layer = (int32_t)layer; c.heads = (int32_t)q.heads; c.T = (int32_t)q.T; c.max_q = (int32_t)max_q;
     c.q_start = (const int32_t *)(uintptr_t)q_start;

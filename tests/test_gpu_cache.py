@@ -348,3 +348,25 @@ def test_a_step_of_every_operation_in_a_replayed_graph():
         torch.cuda.synchronize()
         assert torch.equal(x["out"], y["out"]) and torch.equal(eager.table, graphed.table) and torch.equal(eager.refs, graphed.refs), it
         assert torch.equal(eager.lengths, graphed.lengths) and torch.equal(eager.pool, graphed.pool) and torch.isfinite(x["out"]).all(), it
+
+
+def test_the_workspace_that_a_cache_keeps_serves_larger_calls_and_graphs():
+    """A captured fork goes on with the workspace it was captured with after a larger call has needed another."""
+    rows = 700
+    p = Pair(1, 900, 16, 1, 16, rows, 2)
+    p.add([20, 5] + [0] * (rows - 2))
+    parent, child = p.ints([0, 1]), p.ints([2, 3])
+    p.fork([(0, 2), (1, 3)])
+    p.free([2, 3])
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        p.fbq.cache_fork(p.c, parent, child, stream=side)
+    p.fork([(0, b) for b in range(10, 600)])                   # more pairs than the first workspace holds
+    filler = [torch.full((1 << 14,), 0x7F, dtype=torch.uint8, device="cuda") for _ in range(50)]
+    torch.cuda.synchronize()
+    graph.replay()
+    p.m.fork([(0, 2), (1, 3)])
+    p.same()
+    assert all((f == 0x7F).all() for f in filler)
+    p.compact(True)
