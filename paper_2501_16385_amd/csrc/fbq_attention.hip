@@ -214,16 +214,18 @@ static int few_direct(long items, long tokens)
     return tokens <= 512 || (tokens <= 1024 && items >= 128) ? 2 : 0;
 }
 
-// Whether the shared tokens are taken apart from the rows' own: where few queries come with a row, and what is then not read again, `saved`, is worth the launches.  A launch and a join
-// more cost what 32 MB do (11 rows of 15 tokens, 16 heads of 96, 64 shared: 23.6 us apart, 8.9 not); where short rows go to a block each, the join alone
-// costs 24.
+// Whether the shared tokens are taken apart from the rows' own: where few queries come with a row, and what is then not read again, `saved`, is worth the launches and joins.
+// us apart / not, 128 features, 32 heads of 8 keys' unless stated.  Many-row kernel: 8 rows of 16 tokens behind 16384 shared 75 / 84, of 32 106 / 101, of 64 174 / 167; 4 of 16 behind 4096
+// (50 MB) 40 / 35; 32 heads of 32, 32 rows of 20 behind 4096 97 / 195, of 64 210 / 220, of 128 410 / 303; 11 of 15, 16 heads of 96, behind 64 (5 MB) 23.6 / 8.9.  Few-row kernel: 8 of 4 behind 16384
+// 33 / 97, 2 of 4 23 / 35, 4 of 4 behind 4096 18 / 21; 64 rows of 2000 behind 512 (129 MB) 97 / 106, behind 64 (17 MB) 94.0 / 93.7, but of 600 behind 64 38 / 28: there a row is a block's
+// without a join.
 static bool worth_sharing(const fbq_attention_call &c, bool few, long row_queries)
 {
     const fbq_cache_desc &d = c.cache.desc;
     const long tokens = (long)c.n_shared * d.page_size, saved = 4L * tokens * d.kv_heads * d.head_dim * (c.cache.rows - 1);
     if (saved == 0 || row_queries > 64) return false;
-    if (!few) return saved >= 32L << 20;
-    return saved >= (few_direct((long)c.cache.rows * d.kv_heads, (long)c.cache.max_pages * d.page_size) ? 24L << 20 : 2L << 20);
+    if (!few) return saved >= (row_queries > 32 ? 96L : 32L) << 20;
+    return saved >= (few_direct((long)c.cache.rows * d.kv_heads, (long)c.cache.max_pages * d.page_size) ? 24L : 2L) << 20;
 }
 
 struct AttendPlan {

@@ -73,6 +73,21 @@ def test_single_tokens_more_steps_than_waves(lengths, heads, kv_heads, shared_pa
     check(lengths, [1] * len(lengths), heads, kv_heads, 16, 16, F16, shared_pages=shared_pages, seed=sum(lengths) % 1000)
 
 
+@pytest.mark.parametrize("counts", [None, 3])
+def test_an_item_a_wave(counts):
+    """Many short rows: a wave has a row's head to itself."""
+    lengths = [(7 * b) % 200 for b in range(300)]
+    c = [1] * 300 if counts is None else [b % counts for b in range(300)]
+    lengths = [max(n, k) for n, k in zip(lengths, c)]
+    check(lengths, c, 4, 4, 16, 16, F16, seed=8, width=16)
+
+
+def test_more_pages_than_a_register_holds():
+    """A wave that goes through more than 64 pages: in the few-row kernel's line, and along the keys of a tile."""
+    check([66000], [1], 32, 32, 16, 16, F16, seed=3)
+    check([12000], [300], 32, 32, 16, 16, BF16, seed=4)
+
+
 @pytest.mark.parametrize("dtype", [F16, BF16])
 @pytest.mark.parametrize("heads,kv_heads,max_count", [(4, 4, 5), (8, 4, 8), (8, 2, 4), (6, 2, 9), (32, 1, 3), (40, 1, 7), (3, 1, 100)])
 def test_several_tokens_a_row(heads, kv_heads, max_count, dtype):
@@ -113,6 +128,44 @@ def test_shared_prefix_and_several_tokens(counts):
     lengths = [96 + 10, 96 + 33, 96 + 70]
     lengths = [max(n, 96 + c) for n, c in zip(lengths, counts)]
     check(lengths, counts, 4, 2, 128, 16, F16, shared_pages=6, seed=sum(counts))
+
+
+def taken_apart(rows, tokens, kv_heads, heads, D, page, pages, max_count, dtype):
+    """Whether a call with these sizes reads the shared tokens apart: then its workspace is another."""
+    import paper_2501_16385_amd as fbq
+    cache = fbq.cache_create(1, pages + 1, page, kv_heads, D, rows, -(-tokens // page), dtype)
+    T = rows * max_count
+    q, starts_ = torch.empty(T, heads, D, dtype=dtype, device="cuda"), torch.empty(rows + 1, dtype=torch.int32, device="cuda") if max_count > 1 else None
+    size = lambda shared: fbq.attention_workspace(cache, q, q_start=starts_, max_q=max_count, shared=shared).numel()
+    return size(torch.empty(pages, dtype=torch.int32, device="cuda")) != size(None)
+
+
+# (rows, heads, kv_heads, D, page, shared pages): what is shared is long enough to be read apart
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("rows,heads,kv_heads,D,page,pages", [
+    (2, 4, 4, 64, 16, 200), (5, 3, 1, 128, 64, 70), (16, 2, 2, 40, 16, 150), (3, 4, 1, 256, 32, 90),          # in the few-row kernel's line
+    (20, 4, 4, 64, 16, 130), (17, 8, 1, 64, 32, 100), (40, 4, 2, 80, 16, 140), (33, 4, 4, 128, 16, 90), (150, 2, 1, 128, 128, 12), (24, 16, 1, 96, 64, 40),   # beside it
+    (20, 4, 2, 256, 16, 80), (18, 2, 2, 200, 64, 30)])                                                        # in front of it
+def test_shared_tokens_read_apart(rows, heads, kv_heads, D, page, pages, dtype):
+    lengths = [page * pages + (37 * b) % 90 for b in range(rows)]
+    lengths[1] = page * pages // 2 + 3                          # a row that ends inside the shared pages
+    if rows > 4:
+        lengths[rows - 2] = 0
+    assert taken_apart(rows, max(lengths), kv_heads, heads, D, page, pages, 1, dtype)
+    check(lengths, [1] * rows, heads, kv_heads, D, page, dtype, shared_pages=pages, seed=rows)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("rows,heads,kv_heads,D,page,pages,most", [
+    (9, 2, 2, 64, 16, 300, 3), (4, 4, 1, 128, 32, 100, 4),                                                   # few rows
+    (12, 4, 2, 64, 16, 500, 12), (10, 8, 1, 128, 64, 130, 4), (20, 2, 2, 80, 16, 600, 50), (8, 4, 4, 256, 32, 100, 30)])   # many rows, twice
+def test_shared_tokens_read_apart_for_several_tokens_a_row(rows, heads, kv_heads, D, page, pages, most, dtype):
+    counts = [1 + (5 * b) % most for b in range(rows)]
+    counts[0], counts[2] = most, 0
+    lengths = [page * pages + c + (11 * b) % 60 for b, c in enumerate(counts)]
+    lengths[3] = page * pages - 5                              # its new tokens end inside the shared pages
+    assert taken_apart(rows, max(lengths), kv_heads, heads, D, page, pages, most, dtype)
+    check(lengths, counts, heads, kv_heads, D, page, dtype, shared_pages=pages, seed=rows, token_form=False)
 
 
 def test_shared_prefix_longer_than_a_row():
