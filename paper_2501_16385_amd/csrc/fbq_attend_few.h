@@ -3,10 +3,10 @@
 // An item is one key/value head of one table row: up to 16 query rows (its query tokens times the heads that share it) against the row's keys and values, which
 // are read once.  Bound by HBM: 2 x 2 D bytes a key, for 4 D flops a query row and key.  A step is 32 keys; all steps of all items form one line, which the waves
 // of the grid cut into equal pieces - lengths lie on the device, the line is laid out from them by a scan in each wave - so that one long row among short ones
-// occupies the whole GPU and no host value decides the cut.  A piece of an item leaves partial results for the join kernel; an item that lies
+// occupies the whole GPU and no host value decides the cut.  (Where rows are short an item goes to a wave or a block whole: few_direct in fbq_attention.hip.)  A piece of an item leaves partial results for the join kernel; an item that lies
 // within one piece is written at once.
 //
-// Keys and values go from memory to registers to the matrix cores, nothing through LDS, and waves wait for nobody.  S^T = K Q^T puts a key's scores in rows and a
+// Keys and values go from memory to registers to the matrix cores, nothing through LDS, and waves wait for nobody until a block's pieces of one item are joined.  S^T = K Q^T puts a key's scores in rows and a
 // query row in a column: v_mfma_f32_16x16x32, operand A lane l key l % 16, features 8 (l / 16) and up of 32, which is how keys lie in memory.  The result has
 // column l % 16, keys 4 (l / 16) + i: a lane's eight probabilities of a step are keys 4 g .. 4 g + 3 and 16 + 4 g .. of group g = l / 16.  O^T = V^T P^T
 // takes them as operand B where they are, since the order of a contraction is free: V^T's lanes take the same eight keys.  A lane loads DP / 16

@@ -58,7 +58,17 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, const bool shar
 
     // the row of the table, the tile of its query rows and the piece of the tile's keys (for the shared tokens all query tokens are one row's)
     int b = 0, q0 = 0, nq = a.T, limit = a.n_shared, tile = y, split = z, splits = a.shared_splits, tokens_of_row = 0;
-    if (!shared) {
+    if (!shared && !a.q_start && a.rows > 64 && a.splits == 1) {             // many rows of one token: no need to look at all of them in every block
+        const int per = many_tiles(a, 1);
+        b = y / per;
+        tile = per - 1 - (y - b * per);
+        q0 = b;
+        nq = 1;
+        tokens_of_row = uniform(row_tokens(a, b));
+        limit = many_limit(a, tokens_of_row, nq, tile);
+        split = 0;
+        splits = 1;
+    } else if (!shared) {
         const int share = a.splits == 1 ? 1 << 30 : many_share(a);
         int queries, query0, tokens, tiles, pieces, count, longest;   // of the table row that is this lane's
         const auto look = [&](int row) {

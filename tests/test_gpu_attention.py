@@ -96,6 +96,12 @@ def test_several_tokens_a_row(heads, kv_heads, max_count, dtype):
     check(lengths, counts, heads, kv_heads, 64, 16, dtype, seed=heads)
 
 
+@pytest.mark.parametrize("rows,heads,kv_heads", [(80, 136, 8), (70, 1050, 5), (64, 136, 8), (66, 17, 1)])
+def test_single_tokens_of_wide_groups(rows, heads, kv_heads):
+    """More heads a key/value head than the few-row kernel has rows: one tile a row and more, for so many rows that none is cut, and for fewer."""
+    check([(13 * b) % 90 for b in range(rows)], [1] * rows, heads, kv_heads, 16, 16, F16, seed=rows)
+
+
 @pytest.mark.parametrize("dtype", [F16, BF16])
 @pytest.mark.parametrize("D", [16, 64, 80, 128, 200, 256])
 def test_prompts(D, dtype):
