@@ -16,7 +16,7 @@ from dataclasses import dataclass, field
 from typing import Optional
 
 from . import fbq
-from .fbq import FbqError, _check, _dev_ptr, _stream  # noqa: F401
+from .fbq import FbqError, _check, _dev_ptr, _on, _result, _stream  # noqa: F401
 
 
 class _CCacheDesc(ctypes.Structure):
@@ -65,13 +65,6 @@ def _ints(t, what: str, n: Optional[int] = None):
     return _dev_ptr(t)
 
 
-def _used_on(t, stream):
-    """`t`, kept from being given out again before what is enqueued on `stream` is done with it (None: the stream it was allocated on)."""
-    if stream is not None:
-        t.record_stream(stream)
-    return t
-
-
 @dataclass
 class Cache:
     """A cache made of tensors that the caller keeps (see `cache_create`); `rows(a, b)` is the same cache with rows a .. b - 1 alone."""
@@ -81,8 +74,7 @@ class Cache:
     refs: "object"
     _c: "object" = field(init=False, repr=False, compare=False)
     _at: int = field(init=False, repr=False, compare=False)
-    _rooms: list = field(init=False, repr=False, compare=False, default_factory=list)     # the page operations' workspaces, and ..
-    _pairs: int = field(init=False, repr=False, compare=False, default=0)                 # .. for how many pairs the last one is (see _room)
+    _rooms: dict = field(init=False, repr=False, compare=False, default_factory=dict)     # the page operations' workspaces: stream -> [(pairs, workspace)] (see _room)
 
     def __post_init__(self):
         lib = fbq.load()
@@ -124,7 +116,9 @@ def cache_create(layers: int, pages: int, page_size: int, kv_heads: int, head_di
 def cache_reserve(cache: Cache, count, start=None, info=None, stream=None):
     """fbq_cache_reserve: pages for count[b] more tokens of each row -> start [rows], where they begin (-1: no pages left for this row)."""
     if start is None:
-        start = _used_on(cache.lengths.new_empty(cache.lengths.shape), stream)
+        with _on(stream):
+            start = cache.lengths.new_empty(cache.lengths.shape)
+        _result(start, stream)
     rows = cache._c.rows
     _check(fbq.load().fbq_cache_reserve(cache._c, _ints(count, "count", rows), _ints(start, "start", rows), _ints(info, "info"), _stream(stream)),
            "fbq_cache_reserve")
@@ -164,14 +158,15 @@ def cache_free(cache: Cache, rows, stream=None) -> None:
 
 
 def _room(cache: Cache, n: int, stream):
-    """Workspace of a page operation that was given none; the cache keeps it, since operations on one cache's rows and reference counts have to follow each other anyway.  A
-    smaller one is kept beside a larger: a captured graph may hold it."""
-    if not cache._rooms or n > cache._pairs:
+    """Workspace of a page operation that was given none; the cache keeps one for every stream, allocated there, since operations on one cache's rows and reference counts have to
+    follow each other anyway.  A smaller one is kept beside a larger: a captured graph may hold it."""
+    rooms = cache._rooms.setdefault(_stream(stream), [])
+    if not rooms or n > rooms[-1][0]:
         import torch
-        cache._pairs = max(n, 256)
-        size = fbq.load().fbq_cache_workspace_bytes
-        cache._rooms.append(torch.empty(max(size(cache._c.desc, min(cache._pairs, 65536)), size(cache._c.desc, 0)), dtype=torch.uint8, device=cache.pool.device))
-    return _used_on(cache._rooms[-1], stream)
+        pairs, size = max(n, 256), fbq.load().fbq_cache_workspace_bytes
+        with _on(stream):
+            rooms.append((pairs, torch.empty(max(size(cache._c.desc, min(pairs, 65536)), size(cache._c.desc, 0)), dtype=torch.uint8, device=cache.pool.device)))
+    return rooms[-1][1]
 
 
 def _size(workspace) -> int:
@@ -236,7 +231,9 @@ def attention(cache: Cache, layer: int, q, q_start=None, max_q: int = 1, shared=
     """
     if out is None:
         import torch
-        out = _used_on(torch.empty(q.shape, dtype=q.dtype, device=q.device), stream)
+        with _on(stream):
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        _result(out, stream)
     scale = cache.head_dim ** -0.5 if scale is None else float(scale)
     # one row of 33 tokens, us a call: 9.4 by way of ctypes' argument objects, 6.0 this way
     rc = _call[0].attention(_call[1], cache._at, cache.pool.dtype, _int32, _float32, layer, q, q_start, max_q, shared, scale, out, lse, workspace, _stream(stream))
@@ -247,6 +244,7 @@ def attention(cache: Cache, layer: int, q, q_start=None, max_q: int = 1, shared=
     c = _arguments(cache, layer, q, q_start, max_q, shared, scale, out, lse)
     lib = fbq.load()
     if workspace is None:
-        workspace = _used_on(torch.empty(max(16, lib.fbq_attention_workspace_bytes(ctypes.byref(c))), dtype=torch.uint8, device=q.device), stream)
+        with _on(stream):
+            workspace = torch.empty(max(16, lib.fbq_attention_workspace_bytes(ctypes.byref(c))), dtype=torch.uint8, device=q.device)
     _check(lib.fbq_attention(ctypes.byref(c), _dev_ptr(workspace), _size(workspace), _stream(stream)), "fbq_attention")
     return out

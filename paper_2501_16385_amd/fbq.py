@@ -6,6 +6,7 @@ libfbq.so is missing or the GPU is absent the calls raise.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from dataclasses import dataclass
@@ -175,6 +176,26 @@ def _stream(stream=None) -> int:
             torch.cuda.init()
             _current_raw_stream = lambda: raw(device())
     return _current_raw_stream()
+
+
+_no_switch = contextlib.nullcontext()
+
+
+def _on(stream):
+    """What a call allocates (and fills) itself, it allocates under this: then the memory is `stream`'s.  Memory of the current stream's may still be written or read by what that
+    stream has been given to do for an earlier owner, and nothing orders `stream` behind it."""
+    if stream is None or stream.cuda_stream == _stream():
+        return _no_switch
+    import torch
+    return torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(stream.cuda_stream))
+
+
+def _result(t, stream):
+    """`t`, allocated under _on(stream), for a caller on the current stream: when it is freed, what that stream has been given to do with it by then is done first."""
+    if stream is not None and stream.cuda_stream != _stream():
+        import torch
+        t.record_stream(torch.cuda.current_stream())
+    return t
 
 
 @dataclass
