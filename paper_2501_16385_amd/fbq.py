@@ -198,6 +198,14 @@ def _result(t, stream):
     return t
 
 
+def _empty(shape, dtype: str, device, stream):
+    """A result, or a workspace, of a call on `stream`."""
+    import torch
+    with _on(stream):
+        t = torch.empty(shape, dtype=getattr(torch, dtype), device=device)
+    return _result(t, stream)
+
+
 @dataclass
 class PackedLayer:
     """Host-side arrays in the device layout (outputs of fbq_pack)."""
@@ -254,7 +262,7 @@ def upload_layer(p: PackedLayer, device="cuda") -> DeviceLayer:
     return DeviceLayer(p.desc, t(p.qweight), t(p.scales), t(p.zeros), t(p.At), t(p.Bt))
 
 
-def _scratch(d: Desc, M: int, device):
+def _scratch(d: Desc, M: int, device, stream=None):
     """A workspace for one call, or None.  Zeros only where the few-token kernels look for hand-over words (a size that the rows of a layer do not change); what
     else 3 to 64 tokens keep there, megabytes of partial sums, is written before it is read."""
     import torch
@@ -262,11 +270,12 @@ def _scratch(d: Desc, M: int, device):
     if need == 0:
         return None
     words = 4 * workspace_bytes(Desc(1, d.K, d.r, d.bits, d.group), 16) if 2 < M <= 64 else need
-    if need <= words:
-        return torch.zeros(need, dtype=torch.uint8, device=device)
-    workspace = torch.empty(need, dtype=torch.uint8, device=device)
-    workspace[:words].zero_()
-    return workspace
+    with _on(stream):                                   # (the zeros, too, have to be there before `stream` looks for hand-over words)
+        if need <= words:
+            return torch.zeros(need, dtype=torch.uint8, device=device)
+        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        workspace[:words].zero_()
+        return workspace
 
 
 def linear(layer: DeviceLayer, x, y=None, workspace=None, stream=None):
@@ -274,11 +283,10 @@ def linear(layer: DeviceLayer, x, y=None, workspace=None, stream=None):
     d = layer.desc
     M = int(x.shape[0])
     if y is None or workspace is None:
-        import torch
         if y is None:
-            y = torch.empty((M, d.N), dtype=torch.float16, device=x.device)
+            y = _empty((M, d.N), "float16", x.device, stream)
         if workspace is None:                           # (one that is given is checked by the library)
-            workspace = _scratch(d, M, x.device)
+            workspace = _scratch(d, M, x.device, stream)
     if _lib is None:
         load()
     # one token through 4096 x 4096, us a call: 6.1 by way of ctypes' argument objects, 5.0 this way
@@ -297,13 +305,12 @@ def linear(layer: DeviceLayer, x, y=None, workspace=None, stream=None):
 def linear_unfused(layer: DeviceLayer, x, y=None, workspace=None, stream=None):
     """fbq_linear_unfused: the comparator of Sec. 3.2 - main path, down-projection and read-modify-write
     up-projection as three launches (up to 16 tokens)."""
-    import torch
     d = layer.desc
     M = int(x.shape[0])
     if y is None:
-        y = torch.empty((M, d.N), dtype=torch.float16, device=x.device)
+        y = _empty((M, d.N), "float16", x.device, stream)
     if workspace is None:
-        workspace = _scratch(d, M, x.device)
+        workspace = _scratch(d, M, x.device, stream)
     wbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     rc = load().fbq_linear_unfused(ctypes.byref(d.c()), M, _dev_ptr(x), _dev_ptr(layer.qweight), _dev_ptr(layer.scales),
                                    _dev_ptr(layer.zeros), _dev_ptr(layer.At), _dev_ptr(layer.Bt), _dev_ptr(y), _dev_ptr(workspace),
@@ -315,11 +322,10 @@ def linear_unfused(layer: DeviceLayer, x, y=None, workspace=None, stream=None):
 def linear_static(layer: DeviceLayer, x, y=None, stream=None):
     """fbq_linear_static: fbq_linear for up to 16 tokens with the library's own scratch (nothing is allocated
     by the call; pass y to keep this wrapper from allocating the output)."""
-    import torch
     d = layer.desc
     M = int(x.shape[0])
     if y is None:
-        y = torch.empty((M, d.N), dtype=torch.float16, device=x.device)
+        y = _empty((M, d.N), "float16", x.device, stream)
     rc = load().fbq_linear_static(ctypes.byref(d.c()), M, _dev_ptr(x), _dev_ptr(layer.qweight), _dev_ptr(layer.scales),
                                   _dev_ptr(layer.zeros), _dev_ptr(layer.At), _dev_ptr(layer.Bt), _dev_ptr(y), _stream(stream))
     _check(rc, "fbq_linear_static")
@@ -338,12 +344,11 @@ def make_group(layers, xs, ys, workspaces):
 
 def linear_group(layers, xs, ys=None, workspaces=None, stream=None):
     """fbq_linear_group: several independent layers, same token count, as few launches as possible."""
-    import torch
     M = int(xs[0].shape[0])
     if ys is None:
-        ys = [torch.empty((M, l.desc.N), dtype=torch.float16, device=x.device) for l, x in zip(layers, xs)]
+        ys = [_empty((M, l.desc.N), "float16", x.device, stream) for l, x in zip(layers, xs)]
     if workspaces is None:
-        workspaces = [_scratch(l.desc, M, x.device) for l, x in zip(layers, xs)]
+        workspaces = [_scratch(l.desc, M, x.device, stream) for l, x in zip(layers, xs)]
     arr = make_group(layers, xs, ys, workspaces)
     _check(load().fbq_linear_group(arr, len(layers), M, _stream(stream)), "fbq_linear_group")
     return ys
@@ -367,9 +372,8 @@ def silu_mul(gate, up, out, stream=None):
 
 def reconstruct(layer: DeviceLayer, stream=None):
     """fbq_reconstruct: W_F [N, K] fp32 device tensor."""
-    import torch
     d = layer.desc
-    out = torch.empty((d.N, d.K), dtype=torch.float32, device=layer.qweight.device)
+    out = _empty((d.N, d.K), "float32", layer.qweight.device, stream)
     rc = load().fbq_reconstruct(ctypes.byref(d.c()), _dev_ptr(layer.qweight), _dev_ptr(layer.scales), _dev_ptr(layer.zeros),
                                 _dev_ptr(layer.At), _dev_ptr(layer.Bt), _dev_ptr(out), _stream(stream))
     _check(rc, "fbq_reconstruct")
@@ -378,9 +382,8 @@ def reconstruct(layer: DeviceLayer, stream=None):
 
 def unpack_codes(layer: DeviceLayer, stream=None):
     """fbq_unpack_codes: integer codes [N, K] uint8 device tensor."""
-    import torch
     d = layer.desc
-    out = torch.empty((d.N, d.K), dtype=torch.uint8, device=layer.qweight.device)
+    out = _empty((d.N, d.K), "uint8", layer.qweight.device, stream)
     rc = load().fbq_unpack_codes(ctypes.byref(d.c()), _dev_ptr(layer.qweight), _dev_ptr(out), _stream(stream))
     _check(rc, "fbq_unpack_codes")
     return out
@@ -388,15 +391,14 @@ def unpack_codes(layer: DeviceLayer, stream=None):
 
 def quantize_feedback(d: Desc, W, At=None, Bt=None, stream=None) -> DeviceLayer:
     """fbq_quantize_feedback: W [N, K] fp16, At [r, K], Bt [N, r] device tensors -> packed device layer."""
-    import torch
     dev = W.device
     nbytes = packed_bytes(d)
     if nbytes == 0:
         _check(int(load().fbq_check_desc(ctypes.byref(d.c()))), "fbq_quantize_feedback")
-    qw = torch.empty((d.N, nbytes // 4 // d.N), dtype=torch.int32, device=dev)
+    qw = _empty((d.N, nbytes // 4 // d.N), "int32", dev, stream)
     G = d.K // d.group
-    s = torch.empty((d.N, G), dtype=torch.int16, device=dev)
-    z = torch.empty((d.N, G), dtype=torch.int16, device=dev)
+    s = _empty((d.N, G), "int16", dev, stream)
+    z = _empty((d.N, G), "int16", dev, stream)
     rc = load().fbq_quantize_feedback(ctypes.byref(d.c()), _dev_ptr(W), _dev_ptr(At), _dev_ptr(Bt), _dev_ptr(qw), _dev_ptr(s),
                                       _dev_ptr(z), _stream(stream))
     _check(rc, "fbq_quantize_feedback")
@@ -409,11 +411,10 @@ def train_workspace_bytes(d: Desc, T: int) -> int:
 
 def gram(d: Desc, X, h_scale: float, workspace=None, stream=None):
     """fbq_gram: X [T, K] fp16 device tensor -> fp16(h_scale * X^T X) [K, K] device tensor."""
-    import torch
     T = int(X.shape[0])
     if workspace is None:
-        workspace = torch.empty(max(256, train_workspace_bytes(d, T)), dtype=torch.uint8, device=X.device)
-    H16 = torch.empty((d.K, d.K), dtype=torch.float16, device=X.device)
+        workspace = _empty((max(256, train_workspace_bytes(d, T)),), "uint8", X.device, stream)
+    H16 = _empty((d.K, d.K), "float16", X.device, stream)
     rc = load().fbq_gram(ctypes.byref(d.c()), T, _dev_ptr(X), float(h_scale), _dev_ptr(H16), _dev_ptr(workspace),
                          workspace.numel() * workspace.element_size(), _stream(stream))
     _check(rc, "fbq_gram")

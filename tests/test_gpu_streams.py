@@ -100,3 +100,39 @@ def test_workspace_of_page_operations(operation):
     # the same operation on the current stream goes on with memory of its own
     call(b)
     assert len(b._rooms) == 2
+
+
+def layer(N=640, K=1152, r=16, seed=3):
+    import paper_2501_16385_amd as fbq
+    from paper_2501_16385_amd.random_layers import random_layer
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(seed)
+    return random_layer(fbq.Desc(N, K, r, 4), gen, gain=0.5)
+
+
+@pytest.mark.parametrize("name,M", [(n, M) for n in ("linear", "linear_unfused", "linear_static", "linear_group") for M in (1, 2, 9, 40, 72, 300)
+                                    if M <= 16 or n in ("linear", "linear_group")])
+def test_linears(name, M):
+    import paper_2501_16385_amd as fbq
+    l, x, side = layer(), torch.randn(M, 1152, device="cuda").half(), torch.cuda.Stream()
+    call = (lambda **kw: fbq.linear_group([l, l], [x, x], **kw)) if name == "linear_group" else (lambda **kw: [getattr(fbq, name)(l, x, **kw)])
+    want = call()
+    busy = BusyCurrentStream(M * 640 * 2, max(1, fbq.workspace_bytes(l.desc, M)))
+    got = call(stream=side)
+    busy.check(side, *got)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_quantizer_reconstruction_and_gram():
+    import paper_2501_16385_amd as fbq
+    l, side = layer(), torch.cuda.Stream()
+    W, X = torch.randn(640, 1152, device="cuda").half() * 0.02, torch.randn(300, 1152, device="cuda").half()
+    for sizes, call in (((640 * 1152 * 4,), lambda **kw: [fbq.reconstruct(l, **kw)]),
+                        ((640 * 1152,), lambda **kw: [fbq.unpack_codes(l, **kw)]),
+                        ((640 * 1152 // 2, 640 * 9 * 2), lambda **kw: (lambda q: [q.qweight, q.scales, q.zeros])(fbq.quantize_feedback(l.desc, W, l.At, l.Bt, **kw))),
+                        ((1152 * 1152 * 2, max(256, fbq.train_workspace_bytes(l.desc, 300))), lambda **kw: [fbq.gram(l.desc, X, 1 / 300, **kw)])):
+        want = call()
+        busy = BusyCurrentStream(*sizes)
+        got = call(stream=side)
+        busy.check(side, *got)
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), sizes
