@@ -40,23 +40,28 @@ struct Piece {
     int b, h, step, steps, limit;                             // table row (-1: the shared tokens), head, its first step of the item's `steps`, tokens of the item
     int n, key0;                                              // steps of its own, its first key
     PageList pages;
-    int t, head, sees;                                        // this lane's query row: token (-1: none), head, how many tokens it sees
+    int t, sees;                                              // this lane's query row: token (-1: none), how many tokens it sees
     word4_t q[DP / 32];
 };
 
-// Bytes of LDS (aligned to 16) of a block of it.
+// Bytes of LDS (aligned to 16) of a block of it: parts of waves 1 .., and a word a wave.
 template <int DP>
-constexpr int kFewRoom = (kFewWaves - 1) * (DP / 4 + 2) * 256;
+constexpr int kFewParts = (kFewWaves - 1) * (DP / 4 + 2) * 256;
+template <int DP>
+constexpr int kFewRoom = kFewParts<DP> + 4 * kFewWaves;
 
-// Block `block` of the few-row work, kFewWaves waves.
-template <class TY, int DP>
-__device__ __forceinline__ void attend_few(const AttendArgs &a, int block, unsigned char *room)
+// The work of the block's wave (see attend_few), its results written.  AGAIN: slowly, but so that a value reaches the rows that see it and no others, whatever it is.  Without it a
+// value that is no number reaches all of the item's rows: zero times it is none either.  Whether that has happened (for all waves of a block that join theirs the same answer).
+// Four tokens behind 4000, a NaN among the last one's values: 38 us, else 22.
+template <class TY, int DP, bool AGAIN>
+__device__ __forceinline__ bool attend_few_wave(const AttendArgs &a, int block, unsigned char *room)
 {
     constexpr int J = DP / 16;                                // features of a lane's value pieces, and products O^T of a turn
     constexpr int kHalves = Step<DP>::kHalves, kTurn = 16 * kHalves, kTurns = kFewTile / kTurn;   // keys a turn, turns a step
     const int lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4;
     const int worker = uniform(block * kFewWaves + (threadIdx.x >> 6));
     const int D = a.D, ps1 = (1 << a.log_ps) - 1;
+    const int member = col % a.group;                         // of the heads that share a key/value head: this lane's
 
     Piece<DP> cur, behind;
     int u = 0, end = 0;
@@ -64,7 +69,7 @@ __device__ __forceinline__ void attend_few(const AttendArgs &a, int block, unsig
     if (a.direct) {                                           // an item a worker, or a part of it each for the block's workers
         const int item = a.direct == 1 ? worker : block;
         cur.b = item / a.kv_heads;
-        if (cur.b >= a.rows) return;
+        if (cur.b >= a.rows) return false;
         cur.h = item - cur.b * a.kv_heads;
         cur.limit = uniform(row_tokens(a, cur.b));
         cur.steps = uniform(few_steps(a, cur.b, cur.limit));
@@ -81,7 +86,7 @@ __device__ __forceinline__ void attend_few(const AttendArgs &a, int block, unsig
         const int share = few_share(a, total);
         u = min(worker, total) * share;                       // (worker * share within an int)
         end = min(total, u + share);
-        if (u >= end) return;
+        if (u >= end) return false;
         if (u < shared_steps * a.kv_heads) {
             cur.b = -1;
             cur.limit = a.n_shared;
@@ -98,7 +103,7 @@ __device__ __forceinline__ void attend_few(const AttendArgs &a, int block, unsig
                 if ((long)rest < (long)(before + some) * a.kv_heads) break;
                 before += some;
                 base += 64;
-                if (base >= a.rows) return;                   // (not unless lengths change under the call)
+                if (base >= a.rows) return false;             // (not unless lengths change under the call)
             }
             const int at = __builtin_ctzll(__ballot((long)(before + sum) * a.kv_heads > rest));
             cur.b = base + at;
@@ -134,7 +139,6 @@ __device__ __forceinline__ void attend_few(const AttendArgs &a, int block, unsig
         x.key0 = (is_shared ? 0 : a.n_shared) + x.step * kFewTile;
         x.pages.begin(is_shared ? a.shared : a.table + (long)x.b * a.max_pages, is_shared ? a.n_shared >> a.log_ps : a.max_pages, x.key0 >> a.log_ps);
         const int i = col / a.group;
-        x.head = x.h * a.group + col - i * a.group;
         x.t = -1;
         x.sees = 0;
         if (is_shared) {
@@ -159,7 +163,7 @@ __device__ __forceinline__ void attend_few(const AttendArgs &a, int block, unsig
         for (int s = 0; s < DP / 32; ++s) {
             const int d = 32 * s + 8 * grp;
             x.q[s] = word4_t{0, 0, 0, 0};
-            if (x.t >= 0 && d < D) x.q[s] = (*reinterpret_cast<const word4_t *>(a.q + x.t * a.q_stride + x.head * D + d) & a.q_and) ^ a.q_xor;
+            if (x.t >= 0 && d < D) x.q[s] = (*reinterpret_cast<const word4_t *>(a.q + x.t * a.q_stride + (x.h * a.group + member) * D + d) & a.q_and) ^ a.q_xor;
         }
     };
 
@@ -205,6 +209,43 @@ __device__ __forceinline__ void attend_few(const AttendArgs &a, int block, unsig
 #pragma unroll
         for (int x = 8; x; x >>= 1) least = min(least, __shfl_xor(least, x));
         least = uniform(least);
+    };
+    auto hide = [&](float4_t (&z)[kHalves], int key) __attribute__((always_inline)) {
+#pragma unroll
+        for (int half = 0; half < kHalves; ++half)
+#pragma unroll
+            for (int y = 0; y < 4; ++y)
+                if (key + 16 * half + 4 * grp + y >= cur.sees) z[half][y] = -INFINITY;
+    };
+    // scores of a turn into weights, the operands of the second product; maximum, sum and what was summed before go along
+    auto weigh = [&](float4_t (&z)[kHalves], uint32_t (&p)[2 * kHalves]) __attribute__((always_inline)) {
+        float top = -INFINITY;
+#pragma unroll
+        for (int half = 0; half < kHalves; ++half) top = fmaxf(top, fmaxf(fmaxf(z[half][0], z[half][1]), fmaxf(z[half][2], z[half][3])));
+        top = larger_of_16(top);
+        top = larger_of_32(top) * a.scale;
+        if (__ballot(top > m + kSlack)) {
+            const float to = fmaxf(top, m), by = __builtin_amdgcn_exp2f(m - to);
+            l *= by;
+#pragma unroll
+            for (int j = 0; j < J; ++j) o[j] *= by;
+            m = to;
+        }
+#pragma unroll
+        for (int half = 0; half < kHalves; ++half) {
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                z[half][y] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[half][y], a.scale, -m));
+                l += z[half][y];
+            }
+            p[2 * half] = TY::pack(z[half][0], z[half][1]);
+            p[2 * half + 1] = TY::pack(z[half][2], z[half][3]);
+        }
+    };
+    auto turned = [&](uint32_t lo, uint32_t hi, int j) __attribute__((always_inline)) { return __builtin_amdgcn_perm(hi, lo, j & 1 ? 0x07060302u : 0x05040100u); };   // two keys of feature j
+    auto add = [&](const uint32_t (&vt)[2 * kHalves], const uint32_t (&p)[2 * kHalves], float4_t to) __attribute__((always_inline)) {
+        if constexpr (kHalves == 2) return TY::mfma(word4_t{vt[0], vt[1], vt[2], vt[3]}, word4_t{p[0], p[1], p[2], p[3]}, to);
+        else return TY::mfma(word2_t{vt[0], vt[1]}, word2_t{p[0], p[1]}, to);
     };
     auto compute = [&](const Step<DP> &x, int s) __attribute__((always_inline)) {
         float4_t z[kHalves];
@@ -257,13 +298,73 @@ __device__ __forceinline__ void attend_few(const AttendArgs &a, int block, unsig
             else o[j] = TY::mfma(word2_t{vt[0], vt[1]}, word2_t{p[0], p[1]}, o[j]);
         }
     };
+    // AGAIN: a turn, all of it from memory.  Rows that see equally many of its keys together, the values that they do not see as zeros, the sums of the others left as they are.
+    auto compute_again = [&](int s) __attribute__((always_inline)) {
+        const int key = cur.key0 + s * kTurn;
+        // keys (or values) key + 16 half .. of which the first `end - 16 half` count
+        auto sixteen = [&](int half, int end, bool values) __attribute__((always_inline)) {
+            const int k = key + 16 * half;
+            int valid = min(max(min(cur.limit - key, end) - 16 * half, 0), 16);
+            const int id = valid ? uniform(cur.pages.list[k >> a.log_ps]) : 0;
+            if ((unsigned)id >= (unsigned)a.pages) valid = 0;
+            return buffer_of(a.kv + (valid ? id : 0) * a.page_bytes + (values ? a.page_bytes >> 1 : 0) + (((long)cur.h << a.log_ps) + (k & ps1)) * D * 2, valid * D * 2);
+        };
+        float4_t z[kHalves];
+#pragma unroll
+        for (int half = 0; half < kHalves; ++half) {
+            const __amdgpu_buffer_rsrc_t from = sixteen(half, kTurn, false);
+            z[half] = float4_t{0, 0, 0, 0};
+#pragma unroll
+            for (int y = 0; y < DP / 32; ++y) z[half] = TY::mfma(__builtin_amdgcn_raw_buffer_load_b128(from, k_off[y], 0, 0), cur.q[y], z[half]);
+        }
+        hide(z, key);
+        uint32_t p[2 * kHalves];
+        weigh(z, p);
+        const int mine = min(max(cur.sees - key, 0), kTurn);
+        for (unsigned long long left = __ballot(mine > 0); left;) {
+            const int seen = __builtin_amdgcn_readlane(mine, __builtin_ctzll(left));
+            left &= ~__ballot(mine == seen);
+#pragma unroll
+            for (int j = 0; j < J; j += 2) {                  // two features at a time: a word of a value's row
+                uint32_t lo[2 * kHalves], hi[2 * kHalves];
+#pragma unroll
+                for (int y = 0; y < 2 * kHalves; ++y) {
+                    const __amdgpu_buffer_rsrc_t from = sixteen(y >> 1, seen, true);
+                    lo[y] = __builtin_amdgcn_raw_buffer_load_b32(from, v_off[2 * (y & 1)] + 2 * j, 0, 0);
+                    hi[y] = __builtin_amdgcn_raw_buffer_load_b32(from, v_off[2 * (y & 1) + 1] + 2 * j, 0, 0);
+                }
+#pragma unroll
+                for (int k = j; k < j + 2; ++k) {
+                    uint32_t vt[2 * kHalves];
+#pragma unroll
+                    for (int y = 0; y < 2 * kHalves; ++y) vt[y] = turned(lo[y], hi[y], k);
+                    const float4_t sum = add(vt, p, o[k]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[k][i] = mine == seen ? sum[i] : o[k][i];
+                }
+                __builtin_amdgcn_sched_barrier(0);            // (few registers before speed)
+            }
+        }
+    };
+    bool again = false;
     bool first = true;
     auto finish = [&]() __attribute__((always_inline)) {
+        if (!AGAIN && least < min(cur.limit, cur.key0 + cur.n * kFewTile)) {  // (else every row sees all that the piece has)
+            float odd = 0;
+#pragma unroll
+            for (int j = 0; j < J; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) odd = __builtin_fmaf(o[j][i], 0.0f, odd);
+            again |= __ballot(cur.t >= 0 && odd != 0) != 0;
+        }
         l += __shfl_xor(l, 16);
         l += __shfl_xor(l, 32);
         if (together) {                                       // then the first one joins them: a fourth of the parts to write and read again
             float *const at = reinterpret_cast<float *>(room) + lane;
+            int *const flags = reinterpret_cast<int *>(room + kFewParts<DP>);
             const int wave = uniform(threadIdx.x >> 6);
+            if (AGAIN) __syncthreads();                       // (the first one may still read what was joined before)
+            else if (lane == 0) flags[wave] = again;
             if (wave) {
                 float *const to = at + (wave - 1) * (4 * J + 2) * 64;
                 to[0] = m;
@@ -274,6 +375,10 @@ __device__ __forceinline__ void attend_few(const AttendArgs &a, int block, unsig
                     for (int i = 0; i < 4; ++i) to[(2 + 4 * j + i) * 64] = o[j][i];
             }
             __syncthreads();
+            if (!AGAIN) {
+#pragma unroll
+                for (int w = 0; w < kFewWaves; ++w) again |= uniform(flags[w]) != 0;
+            }
             if (wave) return;
             float to = m;
 #pragma unroll
@@ -297,10 +402,10 @@ __device__ __forceinline__ void attend_few(const AttendArgs &a, int block, unsig
         if (cur.t < 0) return;
         const bool whole = a.direct || cur.n == cur.steps;
         const Partials to = whole ? (cur.b < 0 ? a.whole_shared : a.whole) : a.piece;
-        const int d0 = 4 * J * grp;
+        const int d0 = 4 * J * grp, head = cur.h * a.group + member;
         if (whole && !to.o) {
             const float by = l == 0 ? 0.0f : 1.0f / l;
-            uint16_t *const at = a.out + cur.t * a.out_stride + cur.head * D + d0;
+            uint16_t *const at = a.out + cur.t * a.out_stride + head * D + d0;
 #pragma unroll
             for (int c = 0; c < J / 2; ++c) {                 // eight features: elements 8 c .. of o[j][i] in the order J i + j
                 word4_t w;
@@ -311,9 +416,9 @@ __device__ __forceinline__ void attend_few(const AttendArgs &a, int block, unsig
                 }
                 if (d0 + 8 * c < D) *reinterpret_cast<word4_t *>(at + 8 * c) = w;
             }
-            if (a.lse && grp == 0) a.lse[(long)cur.t * a.heads + cur.head] = l == 0 ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+            if (a.lse && grp == 0) a.lse[(long)cur.t * a.heads + head] = l == 0 ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
         } else {
-            const long r = whole ? (long)cur.t * a.heads + cur.head : ((long)worker * 2 + (first ? 0 : 1)) * a.slot_rows + col;
+            const long r = whole ? (long)cur.t * a.heads + head : ((long)worker * 2 + (first ? 0 : 1)) * a.slot_rows + col;
             float *const at = to.o + r * D + d0;
 #pragma unroll
             for (int c = 0; c < J; ++c) {
@@ -326,15 +431,27 @@ __device__ __forceinline__ void attend_few(const AttendArgs &a, int block, unsig
         }
     };
 
-    // A step's loads go out before the step before it is worked on, those of a piece's first step too: page list and queries of the piece behind come while the one
-    // before runs.
     prepare(cur);
     if (cur.n == 0) {                                         // (no tokens in the item, or in this worker's part)
         begin();
         finish();
-        return;
+        return again;
     }
     bool more = follow(cur, behind);
+    if constexpr (AGAIN) {
+        while (true) {
+            begin();
+            for (int s = 0; s < cur.n * kTurns; ++s) compute_again(s);
+            finish();
+            if (!more) return false;
+            first = false;
+            cur = behind;
+            prepare(cur);
+            more = follow(cur, behind);
+        }
+    }
+    // A step's loads go out before the step before it is worked on, those of a piece's first step too: page list and queries of the piece behind come while the one
+    // before runs.
     if (more) prepare(behind);
     Step<DP> x0, x1;
     load(x0, cur, 0);
@@ -356,6 +473,16 @@ __device__ __forceinline__ void attend_few(const AttendArgs &a, int block, unsig
         return false;
     };
     while (!turn(x0, x1) && !turn(x1, x0)) {}
+    return again;
+}
+
+// Block `block` of the few-row work, kFewWaves waves.
+template <class TY, int DP>
+__device__ __forceinline__ void attend_few(const AttendArgs &a, int block, unsigned char *room)
+{
+    if (!attend_few_wave<TY, DP, false>(a, block, room)) return;
+    asm volatile("" : "+s"(block) : : "memory");              // (what was worked out from it, or read, the first time takes no registers until the second)
+    attend_few_wave<TY, DP, true>(a, block, room);
 }
 
 }  // namespace fbq
