@@ -65,6 +65,13 @@ def _ints(t, what: str, n: Optional[int] = None):
     return _dev_ptr(t)
 
 
+def _info(t, n: int):
+    """Pointer of a tensor that takes n numbers of what could not be served, or is told."""
+    if t is not None and t.numel() < n:
+        raise ValueError(f"info: expected int32, {n} of them")
+    return _ints(t, "info")
+
+
 @dataclass
 class Cache:
     """A cache made of tensors that the caller keeps (see `cache_create`); `rows(a, b)` is the same cache with rows a .. b - 1 alone."""
@@ -120,7 +127,7 @@ def cache_reserve(cache: Cache, count, start=None, info=None, stream=None):
             start = cache.lengths.new_empty(cache.lengths.shape)
         _result(start, stream)
     rows = cache._c.rows
-    _check(fbq.load().fbq_cache_reserve(cache._c, _ints(count, "count", rows), _ints(start, "start", rows), _ints(info, "info"), _stream(stream)),
+    _check(fbq.load().fbq_cache_reserve(cache._c, _ints(count, "count", rows), _ints(start, "start", rows), _info(info, 1), _stream(stream)),
            "fbq_cache_reserve")
     return start
 
@@ -178,7 +185,7 @@ def cache_fork(cache: Cache, parent, child, info=None, workspace=None, stream=No
     n = parent.numel()
     if workspace is None:
         workspace = _room(cache, n, stream)
-    _check(fbq.load().fbq_cache_fork(cache._c, n, _ints(parent, "parent"), _ints(child, "child", n), _ints(info, "info"), _dev_ptr(workspace),
+    _check(fbq.load().fbq_cache_fork(cache._c, n, _ints(parent, "parent"), _ints(child, "child", n), _info(info, 2), _dev_ptr(workspace),
                                      _size(workspace), _stream(stream)), "fbq_cache_fork")
 
 
@@ -196,7 +203,7 @@ def cache_compact(cache: Cache, out: Optional[Cache] = None, info=None, workspac
         raise ValueError("out: a cache of the same shape")
     if workspace is None:
         workspace = _room(cache, 0, stream)
-    _check(fbq.load().fbq_cache_compact(cache._c, out._c.table, out._c.refs, _ints(info, "info"), _dev_ptr(workspace), _size(workspace),
+    _check(fbq.load().fbq_cache_compact(cache._c, out._c.table, out._c.refs, _info(info, 2), _dev_ptr(workspace), _size(workspace),
                                         _stream(stream)), "fbq_cache_compact")
     return out
 

@@ -1,0 +1,53 @@
+"""What the binding of the cache refuses before it calls the library (no GPU: host tensors stand in for the device's, and nothing is launched)."""
+from types import SimpleNamespace
+
+import pytest
+import torch
+
+import paper_2501_16385_amd as fbq
+from paper_2501_16385_amd import cache as kv
+
+HERE = SimpleNamespace(cuda_stream=0)
+
+
+@pytest.fixture
+def host(monkeypatch):
+    """Addresses of host tensors pass, and a call that reaches the library raises."""
+    monkeypatch.setattr(kv, "_dev_ptr", lambda t: None if t is None else t.data_ptr())
+    monkeypatch.setattr(kv, "_stream", lambda stream=None: 0)
+
+    def reached(code, what):
+        if what != "Cache":
+            raise AssertionError(f"{what} was called")
+
+    cache = fbq.cache_create(1, 8, 16, 2, 64, 4, 3, device="cpu")
+    real = fbq.load()
+    stub = SimpleNamespace(fbq_check_cache=real.fbq_check_cache, fbq_cache_workspace_bytes=real.fbq_cache_workspace_bytes)
+    for name in ("fbq_cache_reserve", "fbq_cache_fork", "fbq_cache_compact", "fbq_cache_free", "fbq_cache_copy", "fbq_cache_append"):
+        setattr(stub, name, lambda *a: 0)
+    monkeypatch.setattr(kv.fbq, "load", lambda: stub)
+    monkeypatch.setattr(kv, "_check", reached)
+    return cache
+
+
+def ints(*v):
+    return torch.tensor(v, dtype=torch.int32)
+
+
+def calls(cache, info):
+    """(how many numbers info has to take, the call)"""
+    ws = torch.empty(1 << 12, dtype=torch.uint8)
+    return {"reserve": (1, lambda: fbq.cache_reserve(cache, ints(1, 1, 1, 1), start=ints(0, 0, 0, 0), info=info, stream=HERE)),
+            "fork": (2, lambda: fbq.cache_fork(cache, ints(0), ints(1), info=info, workspace=ws, stream=HERE)),
+            "compact": (2, lambda: fbq.cache_compact(cache, info=info, workspace=ws, stream=HERE))}
+
+
+@pytest.mark.parametrize("name", ["reserve", "fork", "compact"])
+def test_info_takes_what_is_written_there(host, name):
+    need, _ = calls(host, None)[name]
+    for short in [ints(*[0] * n) for n in range(need)] + [torch.zeros(2), torch.zeros(2, dtype=torch.int64)]:
+        with pytest.raises(ValueError, match="info"):
+            calls(host, short)[name][1]()
+    for enough in (None, ints(*[0] * need), ints(0, 0, 0)):
+        with pytest.raises(AssertionError, match="was called"):
+            calls(host, enough)[name][1]()
