@@ -196,9 +196,11 @@ def cache_copy(cache: Cache, src, dst, stream=None) -> None:
 
 
 def cache_compact(cache: Cache, out: Optional[Cache] = None, info=None, workspace=None, stream=None) -> Cache:
-    """fbq_cache_compact: live pages to the low end of the pool.  out: a Cache of the same pool whose table and refs take the new ones (None: in place).
-    info: int32 [2], pages in use and pages moved."""
+    """fbq_cache_compact: live pages to the low end of the pool.  out: a Cache of the same pool whose table and refs take the new ones (None: in place); its lengths are left
+    alone.  info: int32 [2], pages in use and pages moved."""
     out = cache if out is None else out
+    if out.pool.data_ptr() != cache.pool.data_ptr() or out.pool.shape != cache.pool.shape or out.pool.dtype != cache.pool.dtype:
+        raise ValueError("out: a cache of the same pool")
     if out.table.shape != cache.table.shape or out.refs.shape != cache.refs.shape:
         raise ValueError("out: a cache of the same shape")
     if workspace is None:

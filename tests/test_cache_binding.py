@@ -51,3 +51,17 @@ def test_info_takes_what_is_written_there(host, name):
     for enough in (None, ints(*[0] * need), ints(0, 0, 0)):
         with pytest.raises(AssertionError, match="was called"):
             calls(host, enough)[name][1]()
+
+
+def test_compact_moves_pages_of_one_pool(host):
+    """The new table names pages of the pool that they move in: `out` has to be a cache of that one."""
+    ws = torch.empty(1 << 12, dtype=torch.uint8)
+    go = lambda out: fbq.cache_compact(host, out=out, workspace=ws, stream=HERE)
+    another = lambda pool, table=host.table: fbq.Cache(pool, table.clone(), host.lengths, torch.zeros(pool.shape[1], dtype=torch.int32))
+    for wrong in (another(host.pool.clone()), another(host.pool.view(torch.bfloat16)), another(host.pool.view(1, 8, 2, 1, 16, 128)), another(host.pool[:, :4])):
+        with pytest.raises(ValueError, match="pool"):
+            go(wrong)
+    with pytest.raises(ValueError, match="shape"):
+        go(another(host.pool, host.table[:, :2]))
+    with pytest.raises(AssertionError, match="was called"):
+        go(another(host.pool))
