@@ -397,7 +397,8 @@ fbq_status fbq_cache_copy(const fbq_cache *c, int n, const int32_t *src, const i
 
 /*
  * fbq_cache_compact - moves the pages that are in use to the low end of the pool, in all layers: with n of them, those numbered n and up go, in ascending
- * order, to the free ones below n.  table_out [rows][max_pages] and refs_out [pages] are c->table and c->refs after the move; they may be c's own (in place).
+ * order, to the free ones below n.  c has to have all rows that hold pages of the pool: the entries of others would not follow.  table_out [rows][max_pages] and
+ * refs_out [pages] are c->table and c->refs after the move; they may be c's own (in place).
  * Pages are only written where they were free: with tensors of their own the old table stays valid until pages are given out again.
  *   info device, two int32 or NULL: n, pages moved;  workspace device, fbq_cache_workspace_bytes(&c->desc, 0)
  */

@@ -74,13 +74,14 @@ def _info(t, n: int):
 
 @dataclass
 class Cache:
-    """A cache made of tensors that the caller keeps (see `cache_create`); `rows(a, b)` is the same cache with rows a .. b - 1 alone."""
+    """A cache made of tensors that the caller keeps (see `cache_create`); `rows(a, b)` is the same cache with rows a .. b - 1 alone (compaction wants all of them)."""
     pool: "object"
     table: "object"
     lengths: "object"
     refs: "object"
     _c: "object" = field(init=False, repr=False, compare=False)
     _at: int = field(init=False, repr=False, compare=False)
+    _part: bool = field(init=False, repr=False, compare=False, default=False)             # rows() of another: others hold pages of the pool, too
     _rooms: dict = field(init=False, repr=False, compare=False, default_factory=dict)     # the page operations' workspaces: stream -> [(pairs, workspace)] (see _room)
 
     def __post_init__(self):
@@ -109,7 +110,9 @@ class Cache:
         return int(self.pool.shape[4])
 
     def rows(self, first: int, end: int) -> "Cache":
-        return Cache(self.pool, self.table[first:end], self.lengths[first:end], self.refs)
+        part = Cache(self.pool, self.table[first:end], self.lengths[first:end], self.refs)
+        part._part = self._part or part.table.shape[0] < self.table.shape[0]
+        return part
 
 
 def cache_create(layers: int, pages: int, page_size: int, kv_heads: int, head_dim: int, rows: int, max_pages: int, dtype=None, device="cuda") -> Cache:
@@ -199,6 +202,8 @@ def cache_compact(cache: Cache, out: Optional[Cache] = None, info=None, workspac
     """fbq_cache_compact: live pages to the low end of the pool.  out: a Cache of the same pool whose table and refs take the new ones (None: in place); its lengths are left
     alone.  info: int32 [2], pages in use and pages moved."""
     out = cache if out is None else out
+    if cache._part or out._part:                              # (the other rows' table would name pages that have moved)
+        raise ValueError("compaction: of all rows that hold pages, not of a part of them")
     if out.pool.data_ptr() != cache.pool.data_ptr() or out.pool.shape != cache.pool.shape or out.pool.dtype != cache.pool.dtype:
         raise ValueError("out: a cache of the same pool")
     if out.table.shape != cache.table.shape or out.refs.shape != cache.refs.shape:

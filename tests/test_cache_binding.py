@@ -65,3 +65,16 @@ def test_compact_moves_pages_of_one_pool(host):
         go(another(host.pool, host.table[:, :2]))
     with pytest.raises(AssertionError, match="was called"):
         go(another(host.pool))
+
+
+def test_compact_is_of_all_rows(host):
+    """Pages of rows that are not in the table would move all the same."""
+    ws = torch.empty(1 << 12, dtype=torch.uint8)
+    for part in (host.rows(0, 3), host.rows(1, 4), host.rows(1, 3).rows(0, 2)):
+        with pytest.raises(ValueError, match="all rows"):
+            fbq.cache_compact(part, workspace=ws, stream=HERE)
+        whole = fbq.Cache(host.pool, part.table.clone(), part.lengths, host.refs.clone())
+        with pytest.raises(ValueError, match="all rows"):
+            fbq.cache_compact(whole, out=part, workspace=ws, stream=HERE)
+    with pytest.raises(AssertionError, match="was called"):
+        fbq.cache_compact(host.rows(0, 4), workspace=ws, stream=HERE)
