@@ -97,6 +97,11 @@ class Cache:
         _check(lib.fbq_check_cache(ctypes.byref(d)), "Cache")
         self._at = ctypes.addressof(self._c)
 
+    def __setattr__(self, name, value):
+        if name in ("pool", "table", "lengths", "refs") and "_at" in self.__dict__:       # (their addresses are in `_c`: calls would go on with the old ones)
+            raise AttributeError(f"{name}: a Cache keeps the tensors that it was made of; write into them, or make another Cache")
+        object.__setattr__(self, name, value)
+
     @property
     def heads(self) -> int:
         return int(self.pool.shape[3])

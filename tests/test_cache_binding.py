@@ -78,3 +78,13 @@ def test_compact_is_of_all_rows(host):
             fbq.cache_compact(whole, out=part, workspace=ws, stream=HERE)
     with pytest.raises(AssertionError, match="was called"):
         fbq.cache_compact(host.rows(0, 4), workspace=ws, stream=HERE)
+
+
+@pytest.mark.parametrize("name", ["pool", "table", "lengths", "refs"])
+def test_a_cache_does_not_go_on_with_the_old_one_of_two_tensors(host, name):
+    """Calls take the addresses that the Cache was made with: another tensor in a field would be left out of them, silently."""
+    old = getattr(host, name)
+    with pytest.raises(AttributeError, match=name):
+        setattr(host, name, old.clone())
+    assert getattr(host, name) is old and old.data_ptr() == getattr(host._c, name)
+    getattr(host, name).zero_()
