@@ -61,6 +61,7 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, const bool shar
     if (!shared && !a.q_start && a.rows > 64 && a.splits == 1) {             // many rows of one token: no need to look at all of them in every block
         const int per = many_tiles(a, 1);
         b = y / per;
+        if (b >= a.rows) return;                              // (grids of many tiles are rounded up)
         tile = per - 1 - (y - b * per);
         q0 = b;
         nq = 1;
@@ -121,6 +122,8 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, const bool shar
         limit = many_limit(a, tokens_of_row, nq, tile);
         splits = many_pieces(a, many_steps(a, limit), share);
         if (split >= splits) return;
+    } else if ((long)y * kManyRows >= (long)a.T * a.group) {
+        return;
     }
 
     // this lane's query row: token, head, how many tokens it sees

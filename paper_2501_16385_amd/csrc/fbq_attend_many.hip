@@ -3,11 +3,15 @@
 
 namespace fbq {
 
+// A grid has 65535 blocks in y: more tiles than that go on in z, so many at a time.  (That is where a call of shared tokens has their pieces, but not then: it has blocks enough.)
+constexpr int kGridTiles = 32768;
+
 template <class TY, int DP>
 __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void fbq_attend_many_kernel(const AttendArgs a, const bool shared)
 {
     __shared__ __attribute__((aligned(1024))) unsigned char room[kManyRoom<DP>];
-    attend_many<TY, DP>(a, shared, blockIdx.x, blockIdx.y, blockIdx.z, room);
+    const bool pieces = shared && a.shared_splits > 1;
+    attend_many<TY, DP>(a, shared, blockIdx.x, pieces ? blockIdx.y : blockIdx.y + blockIdx.z * kGridTiles, pieces ? blockIdx.z : 0, room);
 }
 
 template <class TY>
@@ -16,7 +20,8 @@ static hipError_t launch_many(const AttendArgs &a, bool shared, hipStream_t stre
     const long rows = (long)a.T * a.group, per = (a.group + kManyRows - 1) / kManyRows;
     long tiles = (rows + kManyRows - 1) / kManyRows;          // ragged rows: each may have one more, begun
     if (!shared) tiles = (a.q_start ? std::min(a.T * per, tiles + a.rows) : a.rows * per) * a.splits;
-    const dim3 grid(a.kv_heads, (unsigned)tiles, shared ? a.shared_splits : 1), block(256);
+    const bool fits = tiles <= 65535;
+    const dim3 grid(a.kv_heads, fits ? (unsigned)tiles : kGridTiles, fits ? (shared ? a.shared_splits : 1) : (unsigned)((tiles + kGridTiles - 1) / kGridTiles)), block(256);
     if (a.D <= 64) hipLaunchKernelGGL((fbq_attend_many_kernel<TY, 64>), grid, block, 0, stream, a, shared);
     else if (a.D <= 96) hipLaunchKernelGGL((fbq_attend_many_kernel<TY, 96>), grid, block, 0, stream, a, shared);
     else if (a.D <= 128) hipLaunchKernelGGL((fbq_attend_many_kernel<TY, 128>), grid, block, 0, stream, a, shared);

@@ -312,7 +312,7 @@ static fbq_status check_attention(const fbq_attention_call *c, bool pointers)
     const int64_t row = (int64_t)c->heads * d.head_dim;
     if (c->q_stride < row || c->out_stride < row || c->q_stride % 8 || c->out_stride % 8) return FBQ_ERR_SHAPE;
     if (c->heads > 8192 || c->T > (1 << 20) || c->q_stride > (1L << 32) || c->out_stride > (1L << 32)) return FBQ_ERR_UNSUPPORTED;
-    if ((int64_t)c->T * c->heads > (1L << 25) || ((int64_t)c->T * (c->heads / d.kv_heads)) / kManyRows + c->cache.rows > 32767) return FBQ_ERR_UNSUPPORTED;
+    if ((int64_t)c->T * c->heads > (1L << 25)) return FBQ_ERR_UNSUPPORTED;
     if (!pointers) return FBQ_OK;
     if (!c->q || !c->out || (c->n_shared && !c->shared)) return FBQ_ERR_NULL;
     if (!aligned(c->q, 16) || !aligned(c->out, 16) || !aligned(c->lse, 4) || !aligned(c->q_start, 4) || !aligned(c->shared, 4)) return FBQ_ERR_ALIGN;
