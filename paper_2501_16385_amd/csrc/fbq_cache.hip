@@ -17,6 +17,8 @@ constexpr int kRefsChunk = kPlanThreads * kRefsPerThread;
 constexpr int kCopyThreads = 256, kCopyPieces = 4;
 constexpr int kCopyBytes = kCopyThreads * kCopyPieces * 16;   // 16 KiB a block
 
+constexpr int kGridChunks = 65534;            // chunks of a page in all its layers that a grid has blocks for; a block goes on with every so manieth
+
 static int chunks_of(long page_bytes) { return (int)((page_bytes + kCopyBytes - 1) / kCopyBytes); }
 
 // Sum over the block and of the threads before this one; `scratch` a word a wave.  All threads call it.
@@ -235,18 +237,22 @@ __global__ __launch_bounds__(kCopyThreads) void fbq_fork_kernel(CacheArgs c, con
         return;
     }
     if (!part) return;
-    const int src = from[full], y = blockIdx.y - 1;
+    const int src = from[full];
     if ((unsigned)src >= (unsigned)c.pages) return;
-    unsigned char *const layer = c.pool + (y / chunks) * c.layer_bytes;
-    copy_chunk(layer + src * c.page_bytes, layer + pl.y * c.page_bytes, c.page_bytes, y % chunks);
+    for (int y = blockIdx.y - 1; y < c.layers * chunks; y += kGridChunks) {
+        unsigned char *const layer = c.pool + (y / chunks) * c.layer_bytes;
+        copy_chunk(layer + src * c.page_bytes, layer + pl.y * c.page_bytes, c.page_bytes, y % chunks);
+    }
 }
 
 __global__ __launch_bounds__(kCopyThreads) void fbq_copy_pages_kernel(CacheArgs c, const int32_t *__restrict__ src, const int32_t *__restrict__ dst, int chunks)
 {
-    const int s = src[blockIdx.x], d = dst[blockIdx.x], y = blockIdx.y;
+    const int s = src[blockIdx.x], d = dst[blockIdx.x];
     if ((unsigned)s >= (unsigned)c.pages || (unsigned)d >= (unsigned)c.pages) return;
-    unsigned char *const layer = c.pool + (y / chunks) * c.layer_bytes;
-    copy_chunk(layer + s * c.page_bytes, layer + d * c.page_bytes, c.page_bytes, y % chunks);
+    for (int y = blockIdx.y; y < c.layers * chunks; y += kGridChunks) {
+        unsigned char *const layer = c.pool + (y / chunks) * c.layer_bytes;
+        copy_chunk(layer + s * c.page_bytes, layer + d * c.page_bytes, c.page_bytes, y % chunks);
+    }
 }
 
 // Compaction.  With n pages in use: the k-th free page below n (a hole) gets the k-th page in use from n up (a mover).
@@ -465,9 +471,8 @@ extern "C" fbq_status fbq_cache_fork(const fbq_cache *c, int n, const int32_t *p
     if (workspace_bytes < fbq_cache_workspace_bytes(&c->desc, n)) return FBQ_ERR_WORKSPACE;
     const CacheArgs a = cache_args(*c);
     const int chunks = chunks_of(a.page_bytes);
-    if ((long)a.layers * chunks >= 65535) return FBQ_ERR_UNSUPPORTED;
     hipLaunchKernelGGL(fbq_fork_plan_kernel, dim3(1), dim3(kPlanThreads), 0, (hipStream_t)stream, a, n, parent, child, (int2 *)workspace, info);
-    hipLaunchKernelGGL(fbq_fork_kernel, dim3(n, 1 + a.layers * chunks), dim3(kCopyThreads), 0, (hipStream_t)stream, a, parent, child, (const int2 *)workspace, chunks);
+    hipLaunchKernelGGL(fbq_fork_kernel, dim3(n, 1 + std::min(a.layers * chunks, kGridChunks)), dim3(kCopyThreads), 0, (hipStream_t)stream, a, parent, child, (const int2 *)workspace, chunks);
     return launched();
 }
 
@@ -480,8 +485,7 @@ extern "C" fbq_status fbq_cache_copy(const fbq_cache *c, int n, const int32_t *s
     if (!aligned(src, 4) || !aligned(dst, 4)) return FBQ_ERR_ALIGN;
     const CacheArgs a = cache_args(*c);
     const int chunks = chunks_of(a.page_bytes);
-    if ((long)a.layers * chunks >= 65536) return FBQ_ERR_UNSUPPORTED;
-    hipLaunchKernelGGL(fbq_copy_pages_kernel, dim3(n, a.layers * chunks), dim3(kCopyThreads), 0, (hipStream_t)stream, a, src, dst, chunks);
+    hipLaunchKernelGGL(fbq_copy_pages_kernel, dim3(n, std::min(a.layers * chunks, kGridChunks)), dim3(kCopyThreads), 0, (hipStream_t)stream, a, src, dst, chunks);
     return launched();
 }
 
