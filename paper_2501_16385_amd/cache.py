@@ -172,12 +172,13 @@ def cache_free(cache: Cache, rows, stream=None) -> None:
     _check(fbq.load().fbq_cache_free(cache._c, rows.numel(), _ints(rows, "rows"), _stream(stream)), "fbq_cache_free")
 
 
-def _room(cache: Cache, n: int, stream):
+def _room(cache: Cache, n: int, stream, number: int):
     """Workspace of a page operation that was given none; the cache keeps one for every stream, allocated there, since operations on one cache's rows and reference counts have to
     follow each other anyway.  A smaller one is kept beside a larger: a captured graph may hold it."""
-    rooms = cache._rooms.setdefault(_stream(stream), [])
-    if not rooms or n > rooms[-1][0]:
+    rooms = cache._rooms.get(number)                          # (number: the stream's)
+    if rooms is None or n > rooms[-1][0]:
         import torch
+        rooms = cache._rooms.setdefault(number, [])
         pairs, size = max(n, 256), fbq.load().fbq_cache_workspace_bytes
         with _on(stream):
             rooms.append((pairs, torch.empty(max(size(cache._c.desc, min(pairs, 65536)), size(cache._c.desc, 0)), dtype=torch.uint8, device=cache.pool.device)))
@@ -190,11 +191,11 @@ def _size(workspace) -> int:
 
 def cache_fork(cache: Cache, parent, child, info=None, workspace=None, stream=None) -> None:
     """fbq_cache_fork: row child[i] becomes a second holder of what row parent[i] holds.  info: int32 [2], pages lacking and pairs skipped."""
-    n = parent.numel()
+    n, number = parent.numel(), _stream(stream)
     if workspace is None:
-        workspace = _room(cache, n, stream)
+        workspace = _room(cache, n, stream, number)
     _check(fbq.load().fbq_cache_fork(cache._c, n, _ints(parent, "parent"), _ints(child, "child", n), _info(info, 2), _dev_ptr(workspace),
-                                     _size(workspace), _stream(stream)), "fbq_cache_fork")
+                                     _size(workspace), number), "fbq_cache_fork")
 
 
 def cache_copy(cache: Cache, src, dst, stream=None) -> None:
@@ -213,10 +214,11 @@ def cache_compact(cache: Cache, out: Optional[Cache] = None, info=None, workspac
         raise ValueError("out: a cache of the same pool")
     if out.table.shape != cache.table.shape or out.refs.shape != cache.refs.shape:
         raise ValueError("out: a cache of the same shape")
+    number = _stream(stream)
     if workspace is None:
-        workspace = _room(cache, 0, stream)
+        workspace = _room(cache, 0, stream, number)
     _check(fbq.load().fbq_cache_compact(cache._c, out._c.table, out._c.refs, _info(info, 2), _dev_ptr(workspace), _size(workspace),
-                                        _stream(stream)), "fbq_cache_compact")
+                                        number), "fbq_cache_compact")
     return out
 
 
