@@ -6,6 +6,7 @@
 #ifndef FBQ_ATTEND_H
 #define FBQ_ATTEND_H
 
+#include "fbq_attend_plan.h"
 #include "fbq_cache.h"
 #include "fbq_internal.h"
 
@@ -100,6 +101,9 @@ struct TypeBf16 {
     static __device__ __forceinline__ uint16_t one(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
 };
 
+// A value that is the same in all lanes, as one the compiler knows to be.
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
 // Query tokens of a row: the first one and how many (whatever q_start holds, inside [0, T) and at most max_q).
 __device__ __forceinline__ int2 queries_of(const AttendArgs &a, int b)
 {
@@ -135,32 +139,23 @@ __device__ __forceinline__ int many_limit(const AttendArgs &a, int tokens, int q
 }
 __device__ __forceinline__ int many_steps(const AttendArgs &a, int limit) { return (max(limit - a.n_shared, 0) + kManyTile - 1) / kManyTile; }
 
-// How many steps a piece of a tile has at most.  A piece more writes and reads 128 rows of partial results again, as dear as about six steps, and pieces that do not all fit
-// the GPU at once wait for each other: so tiles are cut into as many as there is room for, the average tile and a little taken, and where there is none, those twice as long.
-// (61 tiles of 8 heads and about 100 steps, cut in two where that was above an even share: 243 us; uncut 160.)  The whole wave calls it.
+// How many steps a piece of a tile has at most (see fbq_attend_plan.h).  The whole wave calls it.
 __host__ __device__ __forceinline__ constexpr int many_blocks(int D) { return D > 128 ? 256 : 512; }
 __device__ __forceinline__ int many_share(const AttendArgs &a)
 {
-    float steps = 0, tiles = 0;
+    uint64_t twice = 0;
+    int tiles = 0;
     for (int b = threadIdx.x & 63; b < a.rows; b += 64) {
         const int n = queries_of(a, b).y, of_row = many_tiles(a, n), tokens = row_tokens(a, b);
-        if (of_row) steps += 0.5f * of_row * (many_steps(a, many_limit(a, tokens, n, 0)) + many_steps(a, tokens));
+        if (of_row) twice += (uint64_t)of_row * (uint32_t)(many_steps(a, many_limit(a, tokens, n, 0)) + many_steps(a, tokens));
         tiles += of_row;
     }
-#pragma unroll
-    for (int o = 32; o; o >>= 1) {
-        steps += __shfl_xor(steps, o);
-        tiles += __shfl_xor(tiles, o);
-    }
-    const float mean = steps / fmaxf(tiles, 1.0f);
-    const int fit = (int)(many_blocks(a.D) / (fmaxf(tiles, 1.0f) * a.kv_heads));
-    return __builtin_amdgcn_readfirstlane(fit >= 2 ? max(4, (int)ceilf(1.2f * mean / fit)) : (int)(2 * mean) + 6);
+    // (2^18 tiles and 2^16 rows' begun ones, 2^19 steps each: the lower 20 bits and the others apart)
+    const uint32_t low = __builtin_amdgcn_readlane(wave_scan((int)(twice & 0xfffff)), 63), high = __builtin_amdgcn_readlane(wave_scan((int)(twice >> 20)), 63);
+    return uniform(share_of_steps(((uint64_t)high << 20) + low, __builtin_amdgcn_readlane(wave_scan(tiles), 63), a.kv_heads, many_blocks(a.D)));
 }
 // Pieces of a tile of so many steps.
 __device__ __forceinline__ int many_pieces(const AttendArgs &a, int steps, int share) { return max(1, min(a.splits, (steps + share - 1) / share)); }
-
-// A value that is the same in all lanes, as one the compiler knows to be.
-__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
 // The larger of x and the x of the lane 16, or 32, further round in pairs of rows of 16, or 32.
 __device__ __forceinline__ float larger_of_16(float x)
