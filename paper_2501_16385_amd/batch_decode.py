@@ -62,7 +62,8 @@ def run(layers, hidden: int, inter: int, head_dim: int, kv_heads: int, prompt: i
     torch.cuda.synchronize()
     us = lambda i, n: round(event[i].elapsed_time(event[i + 1]) / max(1, n) * 1e3, 1)
     record = {"prompt_tokens": prompt, "samples": samples, "prompt_us": us(0, 1), "us_per_step": us(2, tokens - 1), "drop_and_compact_us": us(3, 1),
-              "us_per_step_after": us(4, tokens), "fork": info.tolist(), "pages_in_use_and_moved": compacted.tolist(), "pages_lacking": int(pre.lacking) + int(dec.lacking),
+              "us_per_step_after": us(4, tokens), "fork": info.tolist(), "pages_in_use_and_moved": compacted.tolist(), "pages_lacking": max(int(pre.most_lacking), int(dec.most_lacking)),
+              "rows_left_out": [row for row, lowest in enumerate(pre.lowest_start.tolist() + dec.lowest_start.tolist()) if lowest < 0],
               "lengths": cache.lengths.tolist(), "finite": bool(torch.isfinite(dec.x[:samples - len(gone)]).all())}
     return record, cache, dec.x
 

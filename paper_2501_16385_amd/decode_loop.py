@@ -53,7 +53,8 @@ class DecoderStack:
 
     cache: a kv.Cache with a layer for each of them; `batch` is then the number of tokens of a step, and a step appends them to the cache's rows and attends over what
     these hold.  counts [rows]: tokens of each row in a step (None: one); shared: the pages that all rows begin with (a view of a row of the table stays
-    right when pages move).  A row that no pages are left for is not written; `lacking` [1] counts the pages that a step lacked.
+    right when pages move).  A row that no pages are left for, in the pool or in its row of the table, is not written in that step, and what the step makes of it means
+    nothing.  `lacking` [1]: the pages that the last step lacked, `most_lacking` [1] that any has; `lowest_start` [rows]: -1 where a step has left a row out.
     """
 
     def __init__(self, layers, hidden: int, inter: int, keep_per_layer_buffers: bool = False, batch: int = 1,
@@ -90,6 +91,7 @@ class DecoderStack:
         for c in counts:
             edges.append(edges[-1] + c)
         self.count, self.start, self.lacking = ints(counts), ints([0] * rows), ints([0])
+        self.lowest_start, self.most_lacking = ints([0] * rows), ints([0])
         self.max_q = max(counts)
         self.q_start = None if counts == [1] * rows else ints(edges)
         q = torch.empty((self.batch, self.hidden // cache.head_dim, cache.head_dim), dtype=torch.float16, device="cuda")
@@ -127,6 +129,9 @@ class DecoderStack:
         x = self.x
         if self.cache is not None:
             kv.cache_reserve(self.cache, self.count, start=self.start, info=self.lacking, stream=stream)
+            with fbq._on(stream):                       # (every step writes its own: these two stay, over the replays of a graph)
+                torch.minimum(self.lowest_start, self.start, out=self.lowest_start)
+                torch.maximum(self.most_lacking, self.lacking, out=self.most_lacking)
         for li in range(len(self.layers)):
             b = self.buf[li % len(self.buf)]
             if len(self.buf) > 1:
