@@ -135,7 +135,8 @@ class DecoderStack:
         for li in range(len(self.layers)):
             b = self.buf[li % len(self.buf)]
             if len(self.buf) > 1:
-                b["x_in"].copy_(x)                      # kept for inspection only
+                with fbq._on(stream):
+                    b["x_in"].copy_(x)                  # kept for inspection only
             self._group(li, ("q", "k", "v"), [x, x, x], [b["q"], b["k"], b["v"]], sp)
             a = b["v"] if self.cache is None else self._attend(li, b, stream)
             self._group(li, ("o",), [a], [b["o"]], sp, mix=(x, b["h"]))                      # h = (x + o) / 2

@@ -136,3 +136,18 @@ def test_quantizer_reconstruction_and_gram():
         got = call(stream=side)
         busy.check(side, *got)
         assert all(torch.equal(a, b) for a, b in zip(got, want)), sizes
+
+
+def test_a_step_of_the_decode_loop_keeps_what_its_layers_were_given():
+    from paper_2501_16385_amd.decode_loop import DecoderStack, random_stack
+    stacks = [DecoderStack(random_stack(2, 256, 640, 16, 4, seed=3), 256, 640, keep_per_layer_buffers=True, batch=2) for _ in range(2)]
+    x0 = torch.randn(2, 256, device="cuda").half()
+    for s in stacks:
+        s.x.copy_(x0)
+    stacks[0].step()
+    side, busy = torch.cuda.Stream(), BusyCurrentStream(1024)
+    stacks[1].step(side)
+    busy.check(side)
+    for a, b in zip(stacks[0].buf, stacks[1].buf):
+        assert torch.equal(a["x_in"], b["x_in"]) and torch.equal(a["down"], b["down"])
+    assert torch.equal(stacks[1].buf[0]["x_in"], x0) and torch.equal(stacks[0].x, stacks[1].x)
