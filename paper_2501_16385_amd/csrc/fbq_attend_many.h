@@ -156,13 +156,13 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, const bool shar
     const int per = (all_steps + splits - 1) / splits;
     const int s0 = min(split * per, all_steps), s1 = min(s0 + per, all_steps);
 
-    const auto query = [&](int t, int s) __attribute__((always_inline)) {
+    const auto query = [&](int t, int grp, int s) __attribute__((always_inline)) {
         const int d = 16 * s + 8 * grp;
         return t >= 0 && d < D ? (*reinterpret_cast<const word4_t *>(a.q + t * a.q_stride + head * D + d) & a.q_and) ^ a.q_xor : word4_t{0, 0, 0, 0};
     };
     word4_t qf[DP / 16];
 #pragma unroll
-    for (int s = 0; s < DP / 16; ++s) qf[s] = query(t, s);
+    for (int s = 0; s < DP / 16; ++s) qf[s] = query(t, grp, s);
 
     // where this lane's pieces of a copy come from: rows 16 wave .. of a step
     int k_off[kCopies], v_off[kCopies];
@@ -311,9 +311,39 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, const bool shar
         work(z0, z1, s);
         if (s + 1 < s1) work(z1, z0, s + 1);
     }
+    const auto write = [&](float16_t (&o)[DP / 32], float m, float l) __attribute__((always_inline)) {
+        l += __shfl_xor(l, 32);
+        if (t < 0) return;
+        const Partials to = shared ? a.part_shared : a.part;
+        const long row = (long)t * a.heads + head;
+        if (!shared && splits == 1 && !a.part_shared.o) {
+            const float by = l == 0 ? 0.0f : 1.0f / l;
+            uint16_t *const at = a.out + t * a.out_stride + head * D;
+#pragma unroll
+            for (int x = 0; x < DP / 32; ++x)
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {
+                    const int d = 32 * x + 8 * y + 4 * grp;
+                    if (d < D) *reinterpret_cast<word2_t *>(at + d) = word2_t{TY::pack(o[x][4 * y] * by, o[x][4 * y + 1] * by), TY::pack(o[x][4 * y + 2] * by, o[x][4 * y + 3] * by)};
+                }
+            if (a.lse && grp == 0) a.lse[row] = l == 0 ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+            return;
+        }
+        const long at = (long)split * a.T * a.heads + row;
+        if (grp == 0) to.ml[at] = make_float2(m, l);
+        if (l == 0) return;                                   // (the join does not look at its sums)
+#pragma unroll
+        for (int x = 0; x < DP / 32; ++x)
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                const int d = 32 * x + 8 * y + 4 * grp;
+                if (d < D) *reinterpret_cast<float4_t *>(to.o + at * D + d) = float4_t{o[x][4 * y], o[x][4 * y + 1], o[x][4 * y + 2], o[x][4 * y + 3]};
+            }
+    };
     // A value that is no number times the zero of a row that does not see it is none either, and stays in that row's sums.  Where such a sum is found and some row does not see all
     // keys, the wave does its piece again, by itself and from memory: rows that see equally many of a step's keys together, other values as zeros, the others' sums left as they are.
-    // Slow (a prompt of 2048 with a NaN among its values 430 us, else 52), but only then: otherwise the look at the sums is all, and no register is kept for it in the loop.
+    // Slow (a prompt of 2048 with a NaN among its values 430 us, else 52), but only then: otherwise the look at the sums is all.  (Results are written before, and once more: so the
+    // loop's registers are as they would be without.  256 features, a prompt of 8192: 1448 us, 1428 without.)
     bool again = false;
     if (least < min(limit, key0 + s1 * kManyTile)) {
         float odd = 0;                                        // then not zero
@@ -323,115 +353,89 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, const bool shar
             for (int y = 0; y < 16; ++y) odd = __builtin_fmaf(o[x][y], 0.0f, odd);
         again = __ballot(t >= 0 && odd != 0) != 0;
     }
-    if (again) {
-#pragma unroll
-        for (int x = 0; x < DP / 32; ++x)
-#pragma unroll
-            for (int y = 0; y < 16; ++y) o[x][y] = 0;
-        m = kNoScore;
-        l = 0;
-        for (int s = s0; s < s1; ++s) {
-            const int key = key0 + s * kManyTile;
-            if (key >= most) break;
-            int asked = t, at_col = col, at_grp = grp;
-            asm volatile("" : "+v"(asked), "+v"(at_col), "+v"(at_grp));   // (queries from memory and offsets anew every step: few registers before speed, here and below)
-            // keys (or values) key + 16 c .. of which the first `end - 16 c` count
-            auto sixteen = [&](int c, int end, bool values) __attribute__((always_inline)) {
-                int valid = min(max(min(limit - key, end) - 16 * c, 0), 16);
-                const int page = valid ? uniform(list[(key + 16 * c) >> a.log_ps]) : 0;
-                if ((unsigned)page >= (unsigned)a.pages) valid = 0;
-                return buffer_of(a.kv + (valid ? page : 0) * a.page_bytes + (values ? a.page_bytes >> 1 : 0) + (((long)h << a.log_ps) + ((key + 16 * c) & ps1)) * D * 2, valid * D * 2);
-            };
-            float16_t z[2];
-            float high = -INFINITY;
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                const __amdgpu_buffer_rsrc_t lower = sixteen(2 * half, kManyTile, false), upper = sixteen(2 * half + 1, kManyTile, false);
-#pragma unroll
-                for (int y = 0; y < 16; ++y) z[half][y] = 0;
-#pragma unroll
-                for (int x = 0; x < DP / 16; ++x) {
-                    const int d = 16 * x + 8 * at_grp, off = d < D ? ((at_col & 15) * D + d) * 2 : kNowhere;
-                    const word4_t f = __builtin_amdgcn_raw_buffer_load_b128(lower, at_col < 16 ? off : kNowhere, 0, 0) |
-                                      __builtin_amdgcn_raw_buffer_load_b128(upper, at_col < 16 ? kNowhere : off, 0, 0);
-                    z[half] = TY::mfma(f, query(asked, x), z[half]);
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-#pragma unroll
-                for (int y = 0; y < 16; ++y) {
-                    if (key + 32 * half + 8 * (y >> 2) + 4 * grp + (y & 3) >= sees) z[half][y] = -INFINITY;
-                    high = fmaxf(high, z[half][y]);
-                }
-            }
-            high = larger_of_32(high) * a.scale;
-            if (__ballot(high > m + kSlack)) {
-                const float to = fmaxf(high, m), by = __builtin_amdgcn_exp2f(m - to);
-                l *= by;
-#pragma unroll
-                for (int x = 0; x < DP / 32; ++x) o[x] *= by;
-                m = to;
-            }
-            word4_t p[4];
-#pragma unroll
-            for (int k = 0; k < 16; ++k) {
-                const int half = k >> 3, y = 2 * (k & 7);
-                const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[half][y], a.scale, -m)), p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[half][y + 1], a.scale, -m));
-                l += p0 + p1;
-                p[k >> 2][k & 3] = TY::pack(p0, p1);
-            }
-            const int mine = min(max(sees - key, 0), kManyTile);
-            for (unsigned long long left = __ballot(mine > 0); left;) {
-                const int seen = __builtin_amdgcn_readlane(mine, __builtin_ctzll(left));
-                left &= ~__ballot(mine == seen);
-#pragma unroll
-                for (int d = 0; d < DP / 32; ++d) {
-                    float16_t sum = o[d];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const __amdgpu_buffer_rsrc_t from = sixteen(j, seen, true);
-                        word4_t f;
-#pragma unroll
-                        for (int w = 0; w < 4; ++w) {         // keys 8 (w / 2) + 4 grp + 2 (w % 2) and the next of the sixteen, feature 32 d + col
-                            const int off = ((8 * (w >> 1) + 4 * at_grp + 2 * (w & 1)) * D + 32 * d + at_col) * 2;
-                            f[w] = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(from, off, 0, 0) | (uint32_t)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(from, off + D * 2, 0, 0) << 16;
-                        }
-                        sum = TY::mfma(f, p[j], sum);
-                        __builtin_amdgcn_sched_barrier(0);
-                    }
-#pragma unroll
-                    for (int y = 0; y < 16; ++y) o[d][y] = mine == seen ? sum[y] : o[d][y];
-                }
-            }
-        }
-    }
-    l += __shfl_xor(l, 32);
-
-    if (t < 0) return;
-    const Partials to = shared ? a.part_shared : a.part;
-    const long row = (long)t * a.heads + head;
-    if (!shared && splits == 1 && !a.part_shared.o) {
-        const float by = l == 0 ? 0.0f : 1.0f / l;
-        uint16_t *const at = a.out + t * a.out_stride + head * D;
-#pragma unroll
-        for (int x = 0; x < DP / 32; ++x)
-#pragma unroll
-            for (int y = 0; y < 4; ++y) {
-                const int d = 32 * x + 8 * y + 4 * grp;
-                if (d < D) *reinterpret_cast<word2_t *>(at + d) = word2_t{TY::pack(o[x][4 * y] * by, o[x][4 * y + 1] * by), TY::pack(o[x][4 * y + 2] * by, o[x][4 * y + 3] * by)};
-            }
-        if (a.lse && grp == 0) a.lse[row] = l == 0 ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
-        return;
-    }
-    const long at = (long)split * a.T * a.heads + row;
-    if (grp == 0) to.ml[at] = make_float2(m, l);
-    if (l == 0) return;                                       // (the join does not look at its sums)
+    write(o, m, l);
+    if (!again) return;
+    float16_t sums[DP / 32];
 #pragma unroll
     for (int x = 0; x < DP / 32; ++x)
 #pragma unroll
-        for (int y = 0; y < 4; ++y) {
-            const int d = 32 * x + 8 * y + 4 * grp;
-            if (d < D) *reinterpret_cast<float4_t *>(to.o + at * D + d) = float4_t{o[x][4 * y], o[x][4 * y + 1], o[x][4 * y + 2], o[x][4 * y + 3]};
+        for (int y = 0; y < 16; ++y) sums[x][y] = 0;
+    m = kNoScore;
+    l = 0;
+    for (int s = s0; s < s1; ++s) {
+        const int key = key0 + s * kManyTile;
+        if (key >= most) break;
+        int asked = t, at_col = col, at_grp = grp;
+        asm volatile("" : "+v"(asked), "+v"(at_col), "+v"(at_grp));   // (queries from memory and offsets anew every step: few registers before speed, here and below)
+        // keys (or values) key + 16 c .. of which the first `end - 16 c` count
+        auto sixteen = [&](int c, int end, bool values) __attribute__((always_inline)) {
+            int valid = min(max(min(limit - key, end) - 16 * c, 0), 16);
+            const int page = valid ? uniform(list[(key + 16 * c) >> a.log_ps]) : 0;
+            if ((unsigned)page >= (unsigned)a.pages) valid = 0;
+            return buffer_of(a.kv + (valid ? page : 0) * a.page_bytes + (values ? a.page_bytes >> 1 : 0) + (((long)h << a.log_ps) + ((key + 16 * c) & ps1)) * D * 2, valid * D * 2);
+        };
+        float16_t z[2];
+        float high = -INFINITY;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const __amdgpu_buffer_rsrc_t lower = sixteen(2 * half, kManyTile, false), upper = sixteen(2 * half + 1, kManyTile, false);
+#pragma unroll
+            for (int y = 0; y < 16; ++y) z[half][y] = 0;
+#pragma unroll
+            for (int x = 0; x < DP / 16; ++x) {
+                const int d = 16 * x + 8 * at_grp, off = d < D ? ((at_col & 15) * D + d) * 2 : kNowhere;
+                const word4_t f = __builtin_amdgcn_raw_buffer_load_b128(lower, at_col < 16 ? off : kNowhere, 0, 0) |
+                                  __builtin_amdgcn_raw_buffer_load_b128(upper, at_col < 16 ? kNowhere : off, 0, 0);
+                z[half] = TY::mfma(f, query(asked, at_grp, x), z[half]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int y = 0; y < 16; ++y) {
+                if (key + 32 * half + 8 * (y >> 2) + 4 * grp + (y & 3) >= sees) z[half][y] = -INFINITY;
+                high = fmaxf(high, z[half][y]);
+            }
         }
+        high = larger_of_32(high) * a.scale;
+        if (__ballot(high > m + kSlack)) {
+            const float to = fmaxf(high, m), by = __builtin_amdgcn_exp2f(m - to);
+            l *= by;
+#pragma unroll
+            for (int x = 0; x < DP / 32; ++x) sums[x] *= by;
+            m = to;
+        }
+        word4_t p[4];
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+            const int half = k >> 3, y = 2 * (k & 7);
+            const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[half][y], a.scale, -m)), p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[half][y + 1], a.scale, -m));
+            l += p0 + p1;
+            p[k >> 2][k & 3] = TY::pack(p0, p1);
+        }
+        const int mine = min(max(sees - key, 0), kManyTile);
+        for (unsigned long long left = __ballot(mine > 0); left;) {
+            const int seen = __builtin_amdgcn_readlane(mine, __builtin_ctzll(left));
+            left &= ~__ballot(mine == seen);
+#pragma unroll
+            for (int d = 0; d < DP / 32; ++d) {
+                float16_t sum = sums[d];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const __amdgpu_buffer_rsrc_t from = sixteen(j, seen, true);
+                    word4_t f;
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {         // keys 8 (w / 2) + 4 grp + 2 (w % 2) and the next of the sixteen, feature 32 d + col
+                        const int off = ((8 * (w >> 1) + 4 * at_grp + 2 * (w & 1)) * D + 32 * d + at_col) * 2;
+                        f[w] = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(from, off, 0, 0) | (uint32_t)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(from, off + D * 2, 0, 0) << 16;
+                    }
+                    sum = TY::mfma(f, p[j], sum);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+#pragma unroll
+                for (int y = 0; y < 16; ++y) sums[d][y] = mine == seen ? sum[y] : sums[d][y];
+            }
+        }
+    }
+    write(sums, m, l);
 }
 
 }  // namespace fbq
