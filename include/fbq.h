@@ -368,23 +368,23 @@ size_t fbq_cache_workspace_bytes(const fbq_cache_desc *d, int n);
  * fbq_cache_reserve - pages for count[b] more tokens of each row b (device [rows], negative counts as 0).  Free pages are given lowest number first, in the order of
  * the rows.  start[b] (device [rows]) = the length before, lengths[b] += count[b]; a row for which pages do not suffice - its own and all before it in this call taken
  * together - or whose table row is too short gets nothing, keeps its length, and start[b] = -1.
- *   info device, one int32 or NULL: how many pages were lacking (0: none)
+ *   info device, one int32 or NULL: how many pages were lacking (0: none; a row whose table row is too short counts none)
  */
 fbq_status fbq_cache_reserve(const fbq_cache *c, const int32_t *count, int32_t *start, int32_t *info, fbq_stream stream);
 
 /*
  * fbq_cache_append - writes new keys and values of one layer into their pages: token i of row b goes to position start[b] + i; nothing where start[b] < 0.
  *   T tokens, at most 2^23; q_start device [rows + 1]: row b's are q_start[b] .. q_start[b + 1] - 1, in ascending order; NULL: T == rows, one token a row
- *   k, v device [T][kv_heads][head_dim], rows k_stride and v_stride elements apart (multiples of 8, at least kv_heads * head_dim)
+ *   k, v device [T][kv_heads][head_dim], rows k_stride and v_stride elements apart (multiples of 8, at least kv_heads * head_dim, at most 2^32)
  */
 fbq_status fbq_cache_append(const fbq_cache *c, int layer, int T, const int32_t *q_start, const int32_t *start, const void *k, int64_t k_stride,
                             const void *v, int64_t v_stride, fbq_stream stream);
 
-/* fbq_cache_free - empties n rows (device int32 list, each at most once): their pages' refs go down by one, their table entries to -1, their lengths to 0. */
+/* fbq_cache_free - empties n rows (1..65536; device int32 list, each at most once): their pages' refs go down by one, their table entries to -1, their lengths to 0. */
 fbq_status fbq_cache_free(const fbq_cache *c, int n, const int32_t *rows, fbq_stream stream);
 
 /*
- * fbq_cache_fork - n pairs: row child[i] (empty before the call, at most once in the list) becomes a second holder of what row parent[i] holds.  Full pages are shared;
+ * fbq_cache_fork - n pairs (1..65536): row child[i] (empty before the call, at most once in the list) becomes a second holder of what row parent[i] holds.  Full pages are shared;
  * a partial last page is copied, in all layers, to a free page (lowest first, in the order of the pairs).  A pair is skipped, and its child stays empty, when the
  * pages do not suffice, a row number is outside the table, or the child is not empty.
  *   info device, two int32 or NULL: pages lacking, pairs skipped;  workspace device, fbq_cache_workspace_bytes(&c->desc, n)
@@ -392,7 +392,7 @@ fbq_status fbq_cache_free(const fbq_cache *c, int n, const int32_t *rows, fbq_st
 fbq_status fbq_cache_fork(const fbq_cache *c, int n, const int32_t *parent, const int32_t *child, int32_t *info, void *workspace, size_t workspace_bytes,
                           fbq_stream stream);
 
-/* fbq_cache_copy - n pairs: page dst[i] = page src[i], in all layers.  No page that one pair writes may appear in another; a pair with a number outside the pool is skipped. */
+/* fbq_cache_copy - n pairs (1..2^22): page dst[i] = page src[i], in all layers.  No page that one pair writes may appear in another; a pair with a number outside the pool is skipped. */
 fbq_status fbq_cache_copy(const fbq_cache *c, int n, const int32_t *src, const int32_t *dst, fbq_stream stream);
 
 /*
@@ -412,7 +412,7 @@ fbq_status fbq_cache_compact(const fbq_cache *c, int32_t *table_out, int32_t *re
  * as an operand of the matrix cores, out once at the end.
  *   T query tokens in all; q_start device [rows + 1], ascending: row b's are q_start[b] .. q_start[b + 1] - 1; NULL: T == rows, one a row.  max_q: at least the most that a
  *            row has (1 with NULL; the result of a row with more is unspecified).  Tokens outside q_start[0] .. q_start[rows] - 1 are left alone
- *   q, out   device [T][heads][head_dim] of the cache's type, rows q_stride and out_stride elements apart (multiples of 8, at least heads * head_dim)
+ *   q, out   device [T][heads][head_dim] of the cache's type, rows q_stride and out_stride elements apart (multiples of 8, at least heads * head_dim, at most 2^32)
  *            (out may overlap neither q nor the pool)
  *   lse      device [T][heads] fp32, or NULL
  *   shared   device list of n_shared pages, or NULL and 0: the first n_shared entries of EVERY row's table are these.  They are read once for all rows together
