@@ -65,6 +65,15 @@ def _ints(t, what: str, n: Optional[int] = None):
     return _dev_ptr(t)
 
 
+def _like(t, stream):
+    """A result of t's shape and type, of a call on `stream`."""
+    if stream is None:
+        return t.new_empty(t.shape)
+    with _on(stream):
+        result = t.new_empty(t.shape)
+    return _result(result, stream)
+
+
 def _info(t, n: int):
     """Pointer of a tensor that takes n numbers of what could not be served, or is told."""
     if t is not None and t.numel() < n:
@@ -131,9 +140,7 @@ def cache_create(layers: int, pages: int, page_size: int, kv_heads: int, head_di
 def cache_reserve(cache: Cache, count, start=None, info=None, stream=None):
     """fbq_cache_reserve: pages for count[b] more tokens of each row -> start [rows], where they begin (-1: no pages left for this row)."""
     if start is None:
-        with _on(stream):
-            start = cache.lengths.new_empty(cache.lengths.shape)
-        _result(start, stream)
+        start = _like(cache.lengths, stream)
     rows = cache._c.rows
     _check(fbq.load().fbq_cache_reserve(cache._c, _ints(count, "count", rows), _ints(start, "start", rows), _info(info, 1), _stream(stream)),
            "fbq_cache_reserve")
@@ -251,10 +258,7 @@ def attention(cache: Cache, layer: int, q, q_start=None, max_q: int = 1, shared=
     for all rows.  scale: head_dim ** -0.5 by default.  lse: float32 [T, heads], takes the logarithm of the softmax's sums.
     """
     if out is None:
-        import torch
-        with _on(stream):
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        _result(out, stream)
+        out = _like(q, stream)
     scale = cache.head_dim ** -0.5 if scale is None else float(scale)
     # one row of 33 tokens, us a call: 9.4 by way of ctypes' argument objects, 6.0 this way
     rc = _call[0].attention(_call[1], cache._at, cache.pool.dtype, _int32, _float32, layer, q, q_start, max_q, shared, scale, out, lse, workspace, _stream(stream))

@@ -201,6 +201,8 @@ def _result(t, stream):
 def _empty(shape, dtype: str, device, stream):
     """A result, or a workspace, of a call on `stream`."""
     import torch
+    if stream is None:
+        return torch.empty(shape, dtype=getattr(torch, dtype), device=device)
     with _on(stream):
         t = torch.empty(shape, dtype=getattr(torch, dtype), device=device)
     return _result(t, stream)
@@ -270,12 +272,14 @@ def _scratch(d: Desc, M: int, device, stream=None):
     if need == 0:
         return None
     words = 4 * workspace_bytes(Desc(1, d.K, d.r, d.bits, d.group), 16) if 2 < M <= 64 else need
-    with _on(stream):                                   # (the zeros, too, have to be there before `stream` looks for hand-over words)
-        if need <= words:
-            return torch.zeros(need, dtype=torch.uint8, device=device)
-        workspace = torch.empty(need, dtype=torch.uint8, device=device)
-        workspace[:words].zero_()
-        return workspace
+    if stream is not None:                              # (the zeros, too, have to be there before `stream` looks for hand-over words)
+        with _on(stream):
+            return _scratch(d, M, device)
+    if need <= words:
+        return torch.zeros(need, dtype=torch.uint8, device=device)
+    workspace = torch.empty(need, dtype=torch.uint8, device=device)
+    workspace[:words].zero_()
+    return workspace
 
 
 def linear(layer: DeviceLayer, x, y=None, workspace=None, stream=None):
