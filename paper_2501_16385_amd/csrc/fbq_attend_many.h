@@ -7,7 +7,7 @@
 // are operand B of the second product where the first one left them: keys 16 x + 4 g + (0 .. 3) and 16 x + 8 + 4 g + (0 .. 3) of lane group g = l / 32; the transposed
 // reads of V from LDS take their keys in that order.  Rows of a tile end where their last query token's sight ends; later tiles, which see
 // more, come first.  Where rows x heads leave the GPU empty the keys are cut into pieces and the join kernel adds up.
-// Measured, 32 heads of 128, fp16: prompt of 8192 tokens 537 to 575 us from box to box (0.96 to 1.02 PFLOP/s; 435 with zeros for data: the matrix cores' power bounds it), 4096 160,
+// Measured, 32 heads of 128, fp16: prompt of 8192 tokens 537 to 575 us from card to card (0.96 to 1.02 PFLOP/s; 435 with zeros for data: the matrix cores' power bounds it), 4096 160,
 // 2048 50 to 54 (0.63 and more: 512 blocks of unequal length, all at once; eight waves a block instead, two teams on alternating steps, 61.5).  Heads of 64 0.76 to 0.80 PFLOP/s,
 // of 80 0.78, of 256 0.76 to 0.80.
 #ifndef FBQ_ATTEND_MANY_H
