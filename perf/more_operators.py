@@ -177,7 +177,7 @@ def _maps(page, D):
     """Where the codes of a head's keys, and values, lie in a page: (nibble of [token][feature] for keys, the same for values, and both the other way round).
 
     DS = 64, 96, 128, 192 or 256 features, the least that holds D; the codes of 16 tokens are one piece of 8 DS bytes, and behind a page's codes lie its
-    scales: [token][DS / 64 groups, rounded up] words, s in the lower 16 bits and m in the upper.  Nibble n of a word is bits 4 n ..
+    scales: [token][DS / 64 groups, rounded up] words, m in the lower 16 bits and s in the upper.  Nibble n of a word is bits 4 n ..
     Keys    words [token][g < 4][w < DS / 32]: features 32 w + 8 g + e, e the number n with its three bits in reverse.
     Values  words [g < 4][r < 16][x < DS / 32]: tokens 4 g + k, and features 64 y + z r + j of product 2 x + f = 4 y + j, where z is 4, or 2 in a last half
             group; f is the lowest bit of n and k the others in reverse."""
@@ -242,7 +242,7 @@ def _packed(c, x):
     turned = _maps(page, D)[2:]
     nibbles = torch.stack([codes[..., i, :, :].index_select(-1, turned[i]) for i in (0, 1)], -3)
     low, high = nibbles[..., 0::2], nibbles[..., 1::2]
-    sm = torch.stack([s, m], -1)
+    sm = torch.stack([m, s], -1)
     groups = (DS + 63) // 64
     sm = torch.nn.functional.pad(sm.flatten(-2), (0, 2 * (groups - s.shape[-1]))).flatten(-2).contiguous().view(torch.uint8)
     return torch.cat([low | high << 4, sm], -1).view(*x.shape[:-1], _token_bytes(D))
@@ -257,7 +257,7 @@ def _values(c, pages, x):
     codes = codes.view(*flat.shape[:-1], page, D).float()
     sm = flat[..., page * DS // 2:].contiguous().view(_type(c)).view(*flat.shape[:-1], page, -1, 2).float()
     groups = (D + 63) // 64
-    s, m = (sm[..., :groups, i].repeat_interleave(64, -1)[..., :D] for i in (0, 1))
+    m, s = (sm[..., :groups, i].repeat_interleave(64, -1)[..., :D] for i in (0, 1))
     return m + s * codes
 
 
@@ -477,7 +477,7 @@ def _plain_append(s):
         heads = torch.arange(c["kv_heads"], device="cuda")
         nibbles[which[:, None, None], heads[None, :, None], place[:, None, :]] = codes
         held = nibbles[..., 0::2] | nibbles[..., 1::2] << 4
-        sm = torch.stack([sc, lo], -1).flatten(-2).contiguous().view(torch.uint8)       # [T, kv_heads, 4 groups]
+        sm = torch.stack([lo, sc], -1).flatten(-2).contiguous().view(torch.uint8)       # [T, kv_heads, 4 groups]
         where = page * DS // 2 + slot[:, None] * 4 * ((DS + 63) // 64) + torch.arange(sm.shape[-1], device="cuda")
         held[which[:, None, None], heads[None, :, None], where[:, None, :]] = sm
         held = held.view(touched.numel(), c["kv_heads"], page, _token_bytes(D))
@@ -573,7 +573,7 @@ def _decoded(s, which):
             code[:, :, :, k::4, 64 * y + j:64 * y + 16 * z:z] = nibble[..., x]
     sm = flat[..., page * DS // 2:].contiguous().view(_type(c)).double().view(P, H, page, -1, 2)
     feature = torch.arange(D, device="cuda") // 64
-    return sm[..., 1][..., feature] + sm[..., 0][..., feature] * code.view(P, H, page, DS)[..., :D]
+    return sm[..., 0][..., feature] + sm[..., 1][..., feature] * code.view(P, H, page, DS)[..., :D]
 
 
 def _exact_attend(s):
