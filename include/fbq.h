@@ -336,7 +336,7 @@ fbq_status fbq_train_step(const fbq_desc *d, const void *W, const void *H16, flo
  * The kernels bound whatever they read from these arrays: a page number outside the pool is not followed (append writes nothing there; attention reads
  * zeros there), a length counts as at most max_pages * page_size and at least 0, row numbers outside the table are skipped.
  */
-enum { FBQ_F16 = 0, FBQ_BF16 = 1 };
+enum { FBQ_F16 = 0, FBQ_BF16 = 1, FBQ_F16_4BIT = 4, FBQ_BF16_4BIT = 5 };
 
 typedef struct {
     int32_t layers;     /* 1..4096 */
@@ -344,8 +344,22 @@ typedef struct {
     int32_t page_size;  /* tokens: 16, 32, 64, 128 or 256 */
     int32_t kv_heads;   /* 1..1024 */
     int32_t head_dim;   /* 16..256, multiple of 8 */
-    int32_t type;       /* FBQ_F16 or FBQ_BF16 */
+    int32_t type;       /* FBQ_F16 or FBQ_BF16; FBQ_F16_4BIT, FBQ_BF16_4BIT: held in 4 bits (below), queries, new keys and values and results of 16 bits */
 } fbq_cache_desc;
+
+/*
+ * A cache in 4 bits: pool [layers][pages][2 (K, V)][kv_heads][page_size * b bytes], b = DS / 2 + 4 G bytes a token, where DS = 64, 96, 128, 192 or 256 is the least that holds
+ * head_dim and G = ceil(DS / 64).  64 features of a token's head are a group (the last one what is left) with a scale s and a lowest value m of the 16-bit type, and stand for
+ * m + s c, c = 0..15.  A head's keys, or values, in a page: the codes of its tokens, 16 at a time in 8 DS bytes, then a word for each [token][G]: m in the lower 16 bits, s in the
+ * upper.  Nibble n of a word is its bits 4 n .. 4 n + 3:
+ *   keys    words [16 tokens][g < 4][w < DS / 32]: feature 32 w + 8 g + e, e the number n with its three bits in reverse
+ *   values  words [g < 4][r < 16][x < DS / 32]: token 4 g + k, feature 64 y + z r + j of 2 x + f = 4 y + j, where z is 4, or 2 in a last group of 32; f is the lowest bit of n, and
+ *           k the other two in reverse
+ * Features from head_dim on have codes of 0.
+ * fbq_cache_append makes them: m the least of the group (a zero without a sign); s the least number of the type with 15 s >= largest - m, or the one before it where m + 15 s would be beyond the type;
+ * c = (x - m) / s to the nearest, ties to even (0 where s is 0), so that |x - m - s c| <= s / 2, or where s went back 0.06 s more.  Where a key or value of a token's head is not finite, its
+ * keys in that head are kept as NaN and its values as 0: a query that sees the token has NaN as its result there, one that does not see it has nothing of it.
+ */
 
 typedef struct {
     fbq_cache_desc desc;
@@ -379,6 +393,12 @@ fbq_status fbq_cache_reserve(const fbq_cache *c, const int32_t *count, int32_t *
  */
 fbq_status fbq_cache_append(const fbq_cache *c, int layer, int T, const int32_t *q_start, const int32_t *start, const void *k, int64_t k_stride,
                             const void *v, int64_t v_stride, fbq_stream stream);
+
+/*
+ * fbq_cache_read - the keys and values of one layer as the numbers that they stand for: token i of row b is what lies at position start[b] + i.  Where start[b] < 0, or there is no page, nothing is
+ * written.  T and q_start as in fbq_cache_append; k, v device [T][kv_heads][head_dim] fp32, contiguous; one of them may be NULL.
+ */
+fbq_status fbq_cache_read(const fbq_cache *c, int layer, int T, const int32_t *q_start, const int32_t *start, float *k, float *v, fbq_stream stream);
 
 /* fbq_cache_free - empties n rows (1..65536; device int32 list, each at most once): their pages' refs go down by one, their table entries to -1, their lengths to 0. */
 fbq_status fbq_cache_free(const fbq_cache *c, int n, const int32_t *rows, fbq_stream stream);

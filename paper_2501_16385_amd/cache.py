@@ -5,8 +5,11 @@ A `Cache` is a pool of pages and, on the device like it, the table that says whi
     pool    [layers, pages, 2 (K, V), kv_heads, page_size, head_dim]   fp16 or bf16
     table   [rows, max_pages] int32, -1: none        lengths [rows] int32        refs [pages] int32
 
+A cache in 4 bits has a pool of uint8, [layers, pages, 2, kv_heads, page_size, token_bytes(head_dim)], and everything else alike (layout: include/fbq.h); what goes in and comes out
+is fp16 or bf16, its `dtype`.
+
 `cache_reserve` gives rows pages for new tokens, `cache_append` writes a layer's keys and values there, `attention` reads them; `cache_fork`, `cache_free`,
-`cache_copy` and `cache_compact` move whole sequences and pages about.  Nothing here waits for the device or asks it anything, so all of it can be captured
+`cache_copy` and `cache_compact` move whole sequences and pages about; `cache_read` gives tokens back as fp32.  Nothing here waits for the device or asks it anything, so all of it can be captured
 in a graph; what could not be served stands in the `info` tensors.
 """
 from __future__ import annotations
@@ -46,6 +49,7 @@ def declare(lib) -> None:
                             ("fbq_cache_reserve", i32, [cp, vp, vp, vp, vp]), ("fbq_cache_append", i32, [cp, i32, i32, vp, vp, vp, i64, vp, i64, vp]),
                             ("fbq_cache_free", i32, [cp, i32, vp, vp]), ("fbq_cache_fork", i32, [cp, i32, vp, vp, vp, vp, sz, vp]),
                             ("fbq_cache_copy", i32, [cp, i32, vp, vp, vp]), ("fbq_cache_compact", i32, [cp, vp, vp, vp, vp, sz, vp]),
+                            ("fbq_cache_read", i32, [cp, i32, i32, vp, vp, vp, vp, vp]),
                             ("fbq_attention_workspace_bytes", sz, [ap]), ("fbq_attention", i32, [ap, vp, sz, vp])):
         f = getattr(lib, name)
         f.restype, f.argtypes = res, args
@@ -81,13 +85,22 @@ def _info(t, n: int):
     return _ints(t, "info")
 
 
+def token_bytes(head_dim: int) -> int:
+    """Bytes of a token's keys, or values, in one head of a cache in 4 bits: codes of 64, 96, 128, 192 or 256 features, and a word for each 64."""
+    features = next((n for n in (64, 96, 128, 192, 256) if n >= head_dim), 0)
+    return features // 2 + 4 * -(-features // 64)
+
+
 @dataclass
 class Cache:
-    """A cache made of tensors that the caller keeps (see `cache_create`); `rows(a, b)` is the same cache with rows a .. b - 1 alone (compaction wants all of them)."""
+    """A cache made of tensors that the caller keeps (see `cache_create`); `rows(a, b)` is the same cache with rows a .. b - 1 alone (compaction wants all of them).
+    dtype, dim: of a cache in 4 bits the type of what goes in and comes out, and the features of a head; else the pool says them."""
     pool: "object"
     table: "object"
     lengths: "object"
     refs: "object"
+    dtype: "object" = None
+    dim: int = 0
     _c: "object" = field(init=False, repr=False, compare=False)
     _at: int = field(init=False, repr=False, compare=False)
     _part: bool = field(init=False, repr=False, compare=False, default=False)             # rows() of another: others hold pages of the pool, too
@@ -95,19 +108,26 @@ class Cache:
 
     def __post_init__(self):
         lib = fbq.load()
-        if self.pool.dim() != 6 or self.pool.shape[2] != 2 or self.pool.dtype not in _types:
+        four = self.dtype is not None and self.pool.dtype not in _types
+        if self.pool.dim() != 6 or self.pool.shape[2] != 2 or (not four and self.pool.dtype not in _types):
             raise ValueError("pool: expected [layers, pages, 2, kv_heads, page_size, head_dim], float16 or bfloat16")
+        if four and (str(self.pool.dtype) != "torch.uint8" or self.dtype not in _types or self.pool.shape[5] != token_bytes(self.dim)):
+            raise ValueError("pool: in 4 bits, expected uint8 [layers, pages, 2, kv_heads, page_size, token_bytes(dim)], dtype float16 or bfloat16")
+        if not four and (self.dtype not in (None, self.pool.dtype) or self.dim not in (0, self.pool.shape[5])):
+            raise ValueError("dtype, dim: expected those of the pool")
         if self.table.dim() != 2:
             raise ValueError("table: expected [rows, max_pages]")
         layers, pages, _, kv_heads, page, dim = self.pool.shape
         rows, width = self.table.shape
-        d = _CCacheDesc(layers, pages, page, kv_heads, dim, _types[self.pool.dtype])
+        if not four:
+            self.dtype, self.dim = self.pool.dtype, int(dim)
+        d = _CCacheDesc(layers, pages, page, kv_heads, self.dim, _types[self.dtype] + (4 if four else 0))
         self._c = _CCache(d, rows, width, _dev_ptr(self.pool), _ints(self.table, "table"), _ints(self.lengths, "lengths", rows), _ints(self.refs, "refs", pages))
         _check(lib.fbq_check_cache(ctypes.byref(d)), "Cache")
         self._at = ctypes.addressof(self._c)
 
     def __setattr__(self, name, value):
-        if name in ("pool", "table", "lengths", "refs") and "_at" in self.__dict__:       # (their addresses are in `_c`: calls would go on with the old ones)
+        if name in ("pool", "table", "lengths", "refs", "dtype", "dim") and "_at" in self.__dict__:       # (their addresses are in `_c`: calls would go on with the old ones)
             raise AttributeError(f"{name}: a Cache keeps the tensors that it was made of; write into them, or make another Cache")
         object.__setattr__(self, name, value)
 
@@ -117,24 +137,27 @@ class Cache:
 
     @property
     def head_dim(self) -> int:
-        return int(self.pool.shape[5])
+        return self.dim
 
     @property
     def page_size(self) -> int:
         return int(self.pool.shape[4])
 
     def rows(self, first: int, end: int) -> "Cache":
-        part = Cache(self.pool, self.table[first:end], self.lengths[first:end], self.refs)
+        part = Cache(self.pool, self.table[first:end], self.lengths[first:end], self.refs, self.dtype, self.dim)
         part._part = self._part or part.table.shape[0] < self.table.shape[0]
         return part
 
 
-def cache_create(layers: int, pages: int, page_size: int, kv_heads: int, head_dim: int, rows: int, max_pages: int, dtype=None, device="cuda") -> Cache:
-    """An empty cache: `rows` sequences of up to max_pages * page_size tokens, out of `pages` pages in all.  dtype: torch.float16 (default) or torch.bfloat16."""
+def cache_create(layers: int, pages: int, page_size: int, kv_heads: int, head_dim: int, rows: int, max_pages: int, dtype=None, device="cuda", bits: int = 16) -> Cache:
+    """An empty cache: `rows` sequences of up to max_pages * page_size tokens, out of `pages` pages in all.  dtype: torch.float16 (default) or torch.bfloat16.  bits: 16, or 4."""
     import torch
+    if bits not in (4, 16):
+        raise ValueError("bits: expected 16 or 4")
     i32 = lambda v, *shape: torch.full(shape, v, dtype=torch.int32, device=device)
-    pool = torch.empty((layers, pages, 2, kv_heads, page_size, head_dim), dtype=dtype or torch.float16, device=device)
-    return Cache(pool, i32(-1, rows, max_pages), i32(0, rows), i32(0, pages))
+    dtype = dtype or torch.float16
+    pool = torch.empty((layers, pages, 2, kv_heads, page_size, head_dim if bits == 16 else token_bytes(head_dim)), dtype=dtype if bits == 16 else torch.uint8, device=device)
+    return Cache(pool, i32(-1, rows, max_pages), i32(0, rows), i32(0, pages), dtype, head_dim)
 
 
 def cache_reserve(cache: Cache, count, start=None, info=None, stream=None):
@@ -149,7 +172,7 @@ def cache_reserve(cache: Cache, count, start=None, info=None, stream=None):
 
 def _tokens(cache: Cache, t, what: str, heads: Optional[int] = None):
     """(pointer, elements between rows, tokens) of a [T, heads, head_dim] tensor of the cache's type whose rows may lie further apart."""
-    if t.dim() != 3 or t.dtype != cache.pool.dtype or t.shape[2] != cache.head_dim or (heads is not None and t.shape[1] != heads):
+    if t.dim() != 3 or t.dtype != cache.dtype or t.shape[2] != cache.head_dim or (heads is not None and t.shape[1] != heads):
         raise ValueError(f"{what}: expected [T, heads, head_dim] of the cache's type")
     if t.stride(2) != 1 or (t.stride(1) != t.shape[2] and t.shape[1] > 1):
         raise ValueError(f"{what}: a token's heads have to lie in one piece")
@@ -162,7 +185,7 @@ def _tokens(cache: Cache, t, what: str, heads: Optional[int] = None):
 def cache_append(cache: Cache, layer: int, k, v, start, q_start=None, stream=None) -> None:
     """fbq_cache_append: k, v [T, kv_heads, head_dim] of one layer into the pages of their rows, from position start[b] on (see cache_reserve).
     q_start [rows + 1]: the rows' tokens in k and v; None: one token a row."""
-    rc = _call[0].append(_call[2], cache._at, cache.pool.dtype, _int32, layer, k, v, start, q_start, _stream(stream))
+    rc = _call[0].append(_call[2], cache._at, cache.dtype, _int32, layer, k, v, start, q_start, _stream(stream))
     if rc is not None:                                        # (None: something is not as it should be; below it is named)
         return _check(rc, "fbq_cache_append")
     kp, ks, T = _tokens(cache, k, "k", cache.heads)
@@ -172,6 +195,20 @@ def cache_append(cache: Cache, layer: int, k, v, start, q_start=None, stream=Non
     rows = cache._c.rows
     _check(fbq.load().fbq_cache_append(cache._c, int(layer), T, _ints(q_start, "q_start", rows + 1), _ints(start, "start", rows), kp, ks, vp, vs,
                                        _stream(stream)), "fbq_cache_append")
+
+
+def cache_read(cache: Cache, layer: int, tokens: int, start, q_start=None, k=None, v=None, stream=None):
+    """fbq_cache_read: the tokens from position start[b] on of each row as numbers -> (k, v), float32 [tokens, kv_heads, head_dim].  q_start [rows + 1]: how many of each row, and where
+    they go; None: one a row, and `tokens` is the number of rows.  Where start[b] is -1, or there is no page, nothing is written."""
+    shape = (tokens, cache.heads, cache.head_dim)
+    rows = cache._c.rows
+    for t, what in ((k, "k"), (v, "v")):
+        if t is not None and (t.dtype != _float32 or tuple(t.shape) != shape):
+            raise ValueError(f"{what}: expected float32 [tokens, kv_heads, head_dim]")
+    at, places = _ints(start, "start", rows), _ints(q_start, "q_start", rows + 1)
+    k, v = (fbq._empty(shape, "float32", cache.pool.device, stream) if t is None else t for t in (k, v))
+    _check(fbq.load().fbq_cache_read(cache._c, int(layer), tokens, places, at, _dev_ptr(k), _dev_ptr(v), _stream(stream)), "fbq_cache_read")
+    return k, v
 
 
 def cache_free(cache: Cache, rows, stream=None) -> None:
@@ -261,7 +298,7 @@ def attention(cache: Cache, layer: int, q, q_start=None, max_q: int = 1, shared=
         out = _like(q, stream)
     scale = cache.head_dim ** -0.5 if scale is None else float(scale)
     # one row of 33 tokens, us a call: 9.4 by way of ctypes' argument objects, 6.0 this way
-    rc = _call[0].attention(_call[1], cache._at, cache.pool.dtype, _int32, _float32, layer, q, q_start, max_q, shared, scale, out, lse, workspace, _stream(stream))
+    rc = _call[0].attention(_call[1], cache._at, cache.dtype, _int32, _float32, layer, q, q_start, max_q, shared, scale, out, lse, workspace, _stream(stream))
     if rc is not None and (rc != 1 or workspace is not None):  # (1, a null pointer: the workspace, where none was given)
         _check(rc, "fbq_attention")
         return out

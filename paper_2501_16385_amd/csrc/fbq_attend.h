@@ -199,6 +199,10 @@ constexpr int kNowhere = 1 << 30;        // an offset behind every descriptor's 
 hipError_t launch_attend_few(const AttendArgs &a, int type, hipStream_t stream);
 hipError_t launch_attend_many(const AttendArgs &a, int type, bool shared, hipStream_t stream);   // shared: the shared tokens for all rows, else the rows' own
 
+// of a cache in 4 bits
+hipError_t launch_attend4_few(const AttendArgs &a, int type, hipStream_t stream);
+hipError_t launch_attend4_many(const AttendArgs &a, int type, bool shared, hipStream_t stream);
+
 hipError_t launch_attend_both(const AttendArgs &a, int type, hipStream_t stream);                // the shared tokens many-row, the rows' own few-row
 
 }  // namespace fbq

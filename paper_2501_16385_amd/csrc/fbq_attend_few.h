@@ -44,40 +44,29 @@ struct Piece {
     word4_t q[DP / 32];
 };
 
-// Bytes of LDS (aligned to 16) of a block of it: parts of waves 1 .., and a word a wave.
-template <int DP>
-constexpr int kFewParts = (kFewWaves - 1) * (DP / 4 + 2) * 256;
-template <int DP>
-constexpr int kFewRoom = kFewParts<DP> + 4 * kFewWaves;
-
-// The work of the block's wave (see attend_few), its results written.  AGAIN: slowly, but so that a value reaches the rows that see it and no others, whatever it is.  Without it a
-// value that is no number reaches all of the item's rows: zero times it is none either.  Whether that has happened (for all waves of a block that join theirs the same answer).
-// Four tokens behind 4000, a NaN among the last one's values: 38 us, else 22.
-template <class TY, int DP, bool AGAIN>
-__device__ __forceinline__ bool attend_few_wave(const AttendArgs &a, int block, unsigned char *room)
-{
-    constexpr int J = DP / 16;                                // features of a lane's value pieces, and products O^T of a turn
-    constexpr int kHalves = Step<DP>::kHalves, kTurn = 16 * kHalves, kTurns = kFewTile / kTurn;   // keys a turn, turns a step
-    const int lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4;
-    const int worker = uniform(block * kFewWaves + (threadIdx.x >> 6));
-    const int D = a.D, ps1 = (1 << a.log_ps) - 1;
-    const int member = col % a.group;                         // of the heads that share a key/value head: this lane's
-
-    Piece<DP> cur, behind;
+// The pieces of a worker, one behind the other along the line of all items' steps.  P: a Piece, what it is made of.
+struct FewLine {
     int u = 0, end = 0;
     bool together = false;                                    // the block's waves have a piece each of one item
-    if (a.direct) {                                           // an item a worker, or a part of it each for the block's workers
-        const int item = a.direct == 1 ? worker : block;
-        cur.b = item / a.kv_heads;
-        if (cur.b >= a.rows) return false;
-        cur.h = item - cur.b * a.kv_heads;
-        cur.limit = uniform(row_tokens(a, cur.b));
-        cur.steps = uniform(few_steps(a, cur.b, cur.limit));
-        together = a.direct == 2;
-        const int share = together ? (cur.steps + kFewWaves - 1) / kFewWaves : cur.steps;
-        cur.step = together ? min((worker & (kFewWaves - 1)) * share, cur.steps) : 0;
-        cur.n = min(share, cur.steps - cur.step);
-    } else {
+
+    // The worker's first piece; false: it has none.
+    template <class P>
+    __device__ __forceinline__ bool first(const AttendArgs &a, int block, int worker, P &cur)
+    {
+        const int lane = threadIdx.x & 63;
+        if (a.direct) {                                       // an item a worker, or a part of it each for the block's workers
+            const int item = a.direct == 1 ? worker : block;
+            cur.b = item / a.kv_heads;
+            if (cur.b >= a.rows) return false;
+            cur.h = item - cur.b * a.kv_heads;
+            cur.limit = uniform(row_tokens(a, cur.b));
+            cur.steps = uniform(few_steps(a, cur.b, cur.limit));
+            together = a.direct == 2;
+            const int share = together ? (cur.steps + kFewWaves - 1) / kFewWaves : cur.steps;
+            cur.step = together ? min((worker & (kFewWaves - 1)) * share, cur.steps) : 0;
+            cur.n = min(share, cur.steps - cur.step);
+            return true;
+        }
         int own = 0;
         for (int b = lane; b < a.rows; b += 64) own += few_steps(a, b);
         own = __builtin_amdgcn_readlane(wave_scan(own), 63);
@@ -116,10 +105,13 @@ __device__ __forceinline__ bool attend_few_wave(const AttendArgs &a, int block, 
         cur.n = min(end - u, cur.steps - cur.step);
         together = few_together(worker / kFewWaves, share, u - cur.step, u - cur.step + cur.steps);
         u += cur.n;
+        return true;
     }
 
-    // the item behind `x`, which ends with it; false: there is none
-    auto follow = [&](const Piece<DP> &x, Piece<DP> &to) __attribute__((always_inline)) {
+    // The piece behind `x`, which ends with its item; false: there is none.
+    template <class P>
+    __device__ __forceinline__ bool follow(const AttendArgs &a, const P &x, P &to)
+    {
         if (u >= end) return false;
         to.b = x.b; to.h = x.h + 1; to.steps = x.steps; to.limit = x.limit; to.step = 0;
         if (to.h == a.kv_heads) {
@@ -133,32 +125,64 @@ __device__ __forceinline__ bool attend_few_wave(const AttendArgs &a, int block, 
         to.n = min(end - u, to.steps);
         u += to.n;
         return true;
-    };
-    auto prepare = [&](Piece<DP> &x) __attribute__((always_inline)) {
-        const bool is_shared = x.b < 0;
-        x.key0 = (is_shared ? 0 : a.n_shared) + x.step * kFewTile;
-        x.pages.begin(is_shared ? a.shared : a.table + (long)x.b * a.max_pages, is_shared ? a.n_shared >> a.log_ps : a.max_pages, x.key0 >> a.log_ps);
-        const int i = col / a.group;
-        x.t = -1;
-        x.sees = 0;
-        if (is_shared) {
-            if (i < a.T) {
-                const int row = a.q_start ? row_of_token(a.q_start, a.rows, i) : i;
-                if (row >= 0) {
-                    const int2 q = queries_of(a, row);
-                    if (i - q.x < q.y) {
-                        x.t = i;
-                        x.sees = min(row_tokens(a, row) - q.y + i - q.x + 1, x.limit);
-                    }
+    }
+};
+
+// A piece's first key and pages, and what the lane's query row `col` sees of it.
+template <class P>
+__device__ __forceinline__ void few_sight(const AttendArgs &a, P &x, int col)
+{
+    const bool is_shared = x.b < 0;
+    x.key0 = (is_shared ? 0 : a.n_shared) + x.step * kFewTile;
+    x.pages.begin(is_shared ? a.shared : a.table + (long)x.b * a.max_pages, is_shared ? a.n_shared >> a.log_ps : a.max_pages, x.key0 >> a.log_ps);
+    const int i = col / a.group;
+    x.t = -1;
+    x.sees = 0;
+    if (is_shared) {
+        if (i < a.T) {
+            const int row = a.q_start ? row_of_token(a.q_start, a.rows, i) : i;
+            if (row >= 0) {
+                const int2 q = queries_of(a, row);
+                if (i - q.x < q.y) {
+                    x.t = i;
+                    x.sees = min(row_tokens(a, row) - q.y + i - q.x + 1, x.limit);
                 }
             }
-        } else {
-            const int2 q = queries_of(a, x.b);
-            if (i < q.y) {
-                x.t = q.x + i;
-                x.sees = x.limit - q.y + i + 1;
-            }
         }
+    } else {
+        const int2 q = queries_of(a, x.b);
+        if (i < q.y) {
+            x.t = q.x + i;
+            x.sees = x.limit - q.y + i + 1;
+        }
+    }
+}
+
+// Bytes of LDS (aligned to 16) of a block of it: parts of waves 1 .., and a word a wave.
+template <int DP>
+constexpr int kFewParts = (kFewWaves - 1) * (DP / 4 + 2) * 256;
+template <int DP>
+constexpr int kFewRoom = kFewParts<DP> + 4 * kFewWaves;
+
+// The work of the block's wave (see attend_few), its results written.  AGAIN: slowly, but so that a value reaches the rows that see it and no others, whatever it is.  Without it a
+// value that is no number reaches all of the item's rows: zero times it is none either.  Whether that has happened (for all waves of a block that join theirs the same answer).
+// Four tokens behind 4000, a NaN among the last one's values: 38 us, else 22.
+template <class TY, int DP, bool AGAIN>
+__device__ __forceinline__ bool attend_few_wave(const AttendArgs &a, int block, unsigned char *room)
+{
+    constexpr int J = DP / 16;                                // features of a lane's value pieces, and products O^T of a turn
+    constexpr int kHalves = Step<DP>::kHalves, kTurn = 16 * kHalves, kTurns = kFewTile / kTurn;   // keys a turn, turns a step
+    const int lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4;
+    const int worker = uniform(block * kFewWaves + (threadIdx.x >> 6));
+    const int D = a.D, ps1 = (1 << a.log_ps) - 1;
+    const int member = col % a.group;                         // of the heads that share a key/value head: this lane's
+
+    Piece<DP> cur, behind;
+    FewLine line;
+    if (!line.first(a, block, worker, cur)) return false;
+    const bool together = line.together;
+    auto prepare = [&](Piece<DP> &x) __attribute__((always_inline)) {
+        few_sight(a, x, col);
 #pragma unroll
         for (int s = 0; s < DP / 32; ++s) {
             const int d = 32 * s + 8 * grp;
@@ -437,7 +461,7 @@ __device__ __forceinline__ bool attend_few_wave(const AttendArgs &a, int block, 
         finish();
         return again;
     }
-    bool more = follow(cur, behind);
+    bool more = line.follow(a, cur, behind);
     if constexpr (AGAIN) {
         while (true) {
             begin();
@@ -447,7 +471,7 @@ __device__ __forceinline__ bool attend_few_wave(const AttendArgs &a, int block, 
             first = false;
             cur = behind;
             prepare(cur);
-            more = follow(cur, behind);
+            more = line.follow(a, cur, behind);
         }
     }
     // A step's loads go out before the step before it is worked on, those of a piece's first step too: page list and queries of the piece behind come while the one
@@ -467,7 +491,7 @@ __device__ __forceinline__ bool attend_few_wave(const AttendArgs &a, int block, 
         first = false;
         cur = behind;
         s = 0;
-        more = follow(cur, behind);
+        more = line.follow(a, cur, behind);
         if (more) prepare(behind);
         begin();
         return false;

@@ -16,6 +16,7 @@
 #include <type_traits>
 
 #include "fbq_attend.h"
+#include "fbq_attend_codes.h"
 #include "fbq_lds_copy.h"
 
 namespace fbq {
@@ -42,12 +43,24 @@ __device__ __forceinline__ void each(F f)
     }
 }
 
+// A grid has 65535 blocks in y: more tiles than that go on in z, so many at a time.  (That is where a call of shared tokens has their pieces, but not then: it has blocks enough.)
+constexpr int kGridTiles = 32768;
+inline dim3 many_grid(const AttendArgs &a, bool shared)
+{
+    const long rows = (long)a.T * a.group, per = (a.group + kManyRows - 1) / kManyRows;
+    long tiles = (rows + kManyRows - 1) / kManyRows;          // ragged rows: each may have one more, begun
+    if (!shared) tiles = (a.q_start ? std::min(a.T * per, tiles + a.rows) : a.rows * per) * a.splits;
+    const bool fits = tiles <= 65535;
+    return dim3(a.kv_heads, fits ? (unsigned)tiles : kGridTiles, fits ? (shared ? a.shared_splits : 1) : (unsigned)((tiles + kGridTiles - 1) / kGridTiles));
+}
+
 // Bytes of LDS (aligned to 1024) of a block of it.
 template <int DP>
 constexpr int kManyRoom = 4 * kManyTile * (DP == 96 ? 256 : DP * 2);
 
-// Block (h, y, z) of the many-row work, four waves: head, tile (of the rows' own tokens: tile and piece), piece of the shared tokens.
-template <class TY, int DP>
+// Block (h, y, z) of the many-row work, four waves: head, tile (of the rows' own tokens: tile and piece), piece of the shared tokens.  FOUR: a Codes (fbq_attend_codes.h), where the cache is
+// in 4 bits and keys and values are made on their way to LDS; void: it is not.
+template <class TY, int DP, class FOUR = void>
 __device__ __forceinline__ void attend_many(const AttendArgs &a, const bool shared, const int h, const int y, const int z, unsigned char *room)
 {
     constexpr int kPieces = DP == 96 ? 16 : DP / 8, kRowBytes = kPieces * 16, kTileBytes = kManyTile * kRowBytes;   // (96: rows as long as 128's, so that they fold over the banks)
@@ -177,8 +190,16 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, const bool shar
     const int entries = shared ? a.n_shared >> a.log_ps : a.max_pages;
     // 16 keys, or values, a wave
     PageList pages;
+    typename std::conditional<std::is_void<FOUR>::value, NoCodes, FOUR>::type codes;
+    codes.begin(a);
     auto page_of = [&](int step) __attribute__((always_inline)) { return pages.at((key0 + step * kManyTile + 16 * wave) >> a.log_ps); };
+    // In 4 bits a copy is only asked for; it is made, and put down, a step later.
     auto copy = [&](int step, int page, bool values) __attribute__((always_inline)) {
+        if constexpr (!std::is_void<FOUR>::value) {
+            const int at = key0 + step * kManyTile + 16 * wave;
+            codes.ask(a, h, page, at, limit, values);
+            return;
+        }
         const int key = key0 + step * kManyTile + 16 * wave;
         const int valid = (unsigned)page < (unsigned)a.pages ? min(max(limit - key, 0), 16) : 0;
         const unsigned char *const at = a.kv + (valid ? page : 0) * a.page_bytes + (values ? a.page_bytes >> 1 : 0) + (((long)h << a.log_ps) + (key & ps1)) * D * 2;
@@ -188,6 +209,12 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, const bool shar
         for (int c = 0; c < kCopies; ++c) copy16_to_lds(from, values ? v_off[c] : k_off[c], 0, to + c * 1024);
     };
 
+    auto put = [&](int step, bool values) __attribute__((always_inline)) {
+        if constexpr (!std::is_void<FOUR>::value) {
+            if (values) codes.put_values(lds[1][step & 1], wave);
+            else codes.template put_keys<kPieces>(lds[0][step & 1], wave);
+        }
+    };
     // reads: a key's piece s of DP / 16 pairs, and a value's column block dblk of 32
     int k_at = col * kRowBytes, k_piece = grp ^ key_swap(col, kPieces);
     const int v_row = 4 * grp + ((lane & 15) >> 2);
@@ -212,6 +239,10 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, const bool shar
             ring[i % kAhead] = *reinterpret_cast<const word4_t *>(lds[0][(step + 1) & 1] + k_at + ((k_piece ^ (2 * x)) << 4) + 32 * half * kRowBytes);
         } else if (i < kScores + kValues) {
             const int j = (i - kScores) / (DP / 32), d = (i - kScores) % (DP / 32);
+            if constexpr (!std::is_void<FOUR>::value) {
+                ring[i % kAhead] = *reinterpret_cast<const word4_t *>(lds[1][step & 1] + turned_at(32 * d + col, 2 * j + grp));
+                return;
+            }
             const unsigned char *const at = lds[1][step & 1] + v_at + ((v_piece ^ (4 * d)) << 4) + 16 * j * kRowBytes;
             const word2_t lo = read_turned4(at), hi = read_turned4(at + 8 * kRowBytes);
             ring[i % kAhead] = word4_t{lo[0], lo[1], hi[0], hi[1]};
@@ -221,10 +252,22 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, const bool shar
     float top = -INFINITY;                                    // of this lane's scores of the step that is next
     auto work = [&](float16_t (&z)[2], float16_t (&ahead)[2], int s) __attribute__((always_inline)) {
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");   // what was asked for a step ago is there, what a step ago was read is free
-        if (s + 1 < s1) copy(s + 1, page, true);
-        if (s + 2 < s1) {
-            page = page_of(s + 2);
-            copy(s + 2, page, false);
+        if constexpr (std::is_void<FOUR>::value) {
+            if (s + 1 < s1) copy(s + 1, page, true);
+            if (s + 2 < s1) {
+                page = page_of(s + 2);
+                copy(s + 2, page, false);
+            }
+        } else {
+            if (s + 1 < s1) put(s + 1, true);
+            if (s + 2 < s1) {
+                put(s + 2, false);
+                copy(s + 2, page, true);
+            }
+            if (s + 3 < s1) {
+                page = page_of(s + 3);
+                copy(s + 3, page, false);
+            }
         }
         const int key = key0 + s * kManyTile;
         if (key >= most) return;
@@ -290,11 +333,23 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, const bool shar
         pages.begin(list, entries, (key0 + s0 * kManyTile + 16 * wave) >> a.log_ps);
         page = page_of(s0);
         copy(s0, page, false);
+        put(s0, false);
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
         copy(s0, page, true);
         if (s0 + 1 < s1) {
             page = page_of(s0 + 1);
             copy(s0 + 1, page, false);
+        }
+        if constexpr (!std::is_void<FOUR>::value) {
+            put(s0, true);
+            if (s0 + 1 < s1) {
+                put(s0 + 1, false);
+                copy(s0 + 1, page, true);
+            }
+            if (s0 + 2 < s1) {
+                page = page_of(s0 + 2);
+                copy(s0 + 2, page, false);
+            }
         }
 #pragma unroll
         for (int half = 0; half < 2; ++half)
@@ -346,7 +401,7 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, const bool shar
     // Slow (a prompt of 2048 with a NaN among its values 430 us, else 52), but only then: otherwise the look at the sums is all.  (Results are written before, and once more: so the
     // loop's registers are as they would be without.  256 features, a prompt of 8192: 1448 us, 1428 without.)
     bool again = false;
-    if (least < min(limit, key0 + s1 * kManyTile)) {
+    if (std::is_void<FOUR>::value && least < min(limit, key0 + s1 * kManyTile)) {
         float odd = 0;                                        // then not zero
 #pragma unroll
         for (int x = 0; x < DP / 32; ++x)
@@ -355,7 +410,7 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, const bool shar
         again = __ballot(t >= 0 && odd != 0) != 0;
     }
     write(o, m, l);
-    if (!again) return;
+    if (!again || !std::is_void<FOUR>::value) return;         // (a cache in 4 bits has no such values)
     float16_t sums[DP / 32];
 #pragma unroll
     for (int x = 0; x < DP / 32; ++x)

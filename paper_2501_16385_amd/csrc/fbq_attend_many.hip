@@ -3,9 +3,6 @@
 
 namespace fbq {
 
-// A grid has 65535 blocks in y: more tiles than that go on in z, so many at a time.  (That is where a call of shared tokens has their pieces, but not then: it has blocks enough.)
-constexpr int kGridTiles = 32768;
-
 template <class TY, int DP>
 __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void fbq_attend_many_kernel(const AttendArgs a, const bool shared)
 {
@@ -17,11 +14,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void fbq_attend_many_kernel
 template <class TY>
 static hipError_t launch_many(const AttendArgs &a, bool shared, hipStream_t stream)
 {
-    const long rows = (long)a.T * a.group, per = (a.group + kManyRows - 1) / kManyRows;
-    long tiles = (rows + kManyRows - 1) / kManyRows;          // ragged rows: each may have one more, begun
-    if (!shared) tiles = (a.q_start ? std::min(a.T * per, tiles + a.rows) : a.rows * per) * a.splits;
-    const bool fits = tiles <= 65535;
-    const dim3 grid(a.kv_heads, fits ? (unsigned)tiles : kGridTiles, fits ? (shared ? a.shared_splits : 1) : (unsigned)((tiles + kGridTiles - 1) / kGridTiles)), block(256);
+    const dim3 grid = many_grid(a, shared), block(256);
     if (a.D <= 64) hipLaunchKernelGGL((fbq_attend_many_kernel<TY, 64>), grid, block, 0, stream, a, shared);
     else if (a.D <= 96) hipLaunchKernelGGL((fbq_attend_many_kernel<TY, 96>), grid, block, 0, stream, a, shared);
     else if (a.D <= 128) hipLaunchKernelGGL((fbq_attend_many_kernel<TY, 128>), grid, block, 0, stream, a, shared);

@@ -9,6 +9,13 @@
 
 namespace fbq {
 
+// Caches in 4 bits (layout: fbq.h).  Features that a head's are kept as, groups of 64 of them, bytes of a token's keys, or values, in a head.
+inline bool in_4_bits(int type) { return (type & 4) != 0; }
+__host__ __device__ __forceinline__ constexpr int features4(int D) { return D <= 64 ? 64 : D <= 96 ? 96 : D <= 128 ? 128 : D <= 192 ? 192 : 256; }
+__host__ __device__ __forceinline__ constexpr int groups4(int DS) { return (DS + 63) / 64; }
+__host__ __device__ __forceinline__ constexpr int token_bytes4(int D) { return features4(D) / 2 + 4 * groups4(features4(D)); }
+inline long token_bytes(const fbq_cache_desc &d) { return in_4_bits(d.type) ? token_bytes4(d.head_dim) : 2L * d.head_dim; }
+
 struct CacheArgs {
     unsigned char *pool;
     int32_t *table, *lengths, *refs;
@@ -24,11 +31,14 @@ inline CacheArgs cache_args(const fbq_cache &c)
     a.pool = (unsigned char *)c.pool;
     a.table = c.table; a.lengths = c.lengths; a.refs = c.refs;
     a.log_ps = __builtin_ctz(d.page_size);
-    a.page_bytes = 4L * d.kv_heads * d.page_size * d.head_dim;
+    a.page_bytes = 2L * d.kv_heads * d.page_size * token_bytes(d);
     a.layer_bytes = a.page_bytes * d.pages;
     a.pages = d.pages; a.layers = d.layers; a.max_pages = c.max_pages; a.rows = c.rows; a.kv_heads = d.kv_heads; a.D = d.head_dim;
     return a;
 }
+
+hipError_t launch_append4(const CacheArgs &c, int type, long layer_offset, int T, const int32_t *q_start, const int32_t *start, const void *k, long k_stride, const void *v,
+                          long v_stride, hipStream_t stream);
 
 // FBQ_OK, or what is wrong with the cache itself (`refs` whether the call uses them).  Host only.
 fbq_status check_cache(const fbq_cache *c, bool refs);

@@ -406,14 +406,14 @@ extern "C" fbq_status fbq_check_cache(const fbq_cache_desc *d)
     if (d->layers < 1 || d->layers > 4096 || d->pages < 1 || d->pages > (1 << 22) || d->kv_heads < 1 || d->kv_heads > 1024) return FBQ_ERR_SHAPE;
     if (d->head_dim < 16 || d->head_dim > 256 || d->head_dim % 8) return FBQ_ERR_SHAPE;
     if (d->page_size < 16 || d->page_size > 256 || (d->page_size & (d->page_size - 1))) return FBQ_ERR_UNSUPPORTED;
-    if (d->type != FBQ_F16 && d->type != FBQ_BF16) return FBQ_ERR_UNSUPPORTED;
+    if ((d->type & ~4) != FBQ_F16 && (d->type & ~4) != FBQ_BF16) return FBQ_ERR_UNSUPPORTED;
     return FBQ_OK;
 }
 
 extern "C" size_t fbq_cache_bytes(const fbq_cache_desc *d)
 {
     if (fbq_check_cache(d) != FBQ_OK) return 0;
-    return 4 * (size_t)d->kv_heads * d->page_size * d->head_dim * d->pages * d->layers;
+    return 2 * (size_t)token_bytes(*d) * d->kv_heads * d->page_size * d->pages * d->layers;
 }
 
 extern "C" size_t fbq_cache_workspace_bytes(const fbq_cache_desc *d, int n)
@@ -444,6 +444,8 @@ extern "C" fbq_status fbq_cache_append(const fbq_cache *c, int layer, int T, con
     if (!start || !k || !v) return FBQ_ERR_NULL;
     if (!aligned(q_start, 4) || !aligned(start, 4) || !aligned(k, 16) || !aligned(v, 16)) return FBQ_ERR_ALIGN;
     const CacheArgs a = cache_args(*c);
+    if (in_4_bits(c->desc.type))
+        return launch_append4(a, c->desc.type, layer * a.layer_bytes, T, q_start, start, k, k_stride, v, v_stride, (hipStream_t)stream) == hipSuccess ? FBQ_OK : FBQ_ERR_HIP;
     hipLaunchKernelGGL(fbq_append_kernel, dim3(T), dim3(256), 0, (hipStream_t)stream, a, layer * a.layer_bytes, q_start, start, (const uint16_t *)k, (long)k_stride,
                        (const uint16_t *)v, (long)v_stride);
     return launched();

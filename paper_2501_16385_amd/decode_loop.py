@@ -85,7 +85,7 @@ class DecoderStack:
         """What the steps' calls of the cache need, once: tokens a row, their places, attention's workspace."""
         rows, ints = cache.lengths.numel(), lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")
         counts = [1] * rows if counts is None else list(counts)
-        if len(counts) != rows or sum(counts) != self.batch or cache.pool.dtype != torch.float16 or self.hidden % cache.head_dim:
+        if len(counts) != rows or sum(counts) != self.batch or cache.dtype != torch.float16 or self.hidden % cache.head_dim:
             raise ValueError("cache: an fp16 cache of whole heads, with a row for every count; counts: as many tokens as the batch")
         edges = [0]
         for c in counts:
