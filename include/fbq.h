@@ -456,6 +456,33 @@ typedef struct {
 size_t fbq_attention_workspace_bytes(const fbq_attention_call *a);
 fbq_status fbq_attention(const fbq_attention_call *a, void *workspace, size_t workspace_bytes, fbq_stream stream);
 
+/*
+ * fbq_attention_weights - how much each key was attended to, added up for every key/value head over the call's query tokens i and the heads h that share it:
+ *     out[b][hk][j] = decay * weights[b][hk][j] + sum_i sum_h exp(scale q_ih . k_j - lse_ih),   j < lengths[b] and j < width, i over the tokens that see j
+ * where the row's new tokens (the last n_b of lengths[b]) begin without the first term, whatever lies there.  Places from lengths[b] on are left alone.  The sums are in fp32, over the query
+ * tokens in an order that the sizes alone decide.
+ *   a        the call of fbq_attention that it follows: its cache, layer, heads, T, max_q, q_start, q, q_stride, scale, and lse as that wrote it (not NULL; a token that sees nothing
+ *            counts nowhere); out and shared are not used
+ *   weights  device [rows][kv_heads][width] fp32, or NULL: no first term (nor with decay 0, whatever lies there);  out the same, and may be `weights`, but not lie over a part of it
+ *   decay    0 .. 1;  width 1 .. 2^24;  rows * kv_heads at most 2^23
+ */
+fbq_status fbq_attention_weights(const fbq_attention_call *a, const float *weights, float *out, int32_t width, float decay, fbq_stream stream);
+
+/*
+ * fbq_cache_evict - cuts rows back to keep[b] tokens (device [rows]) in every layer and key/value head, each head by its own weights: of the row's L = lengths[b] tokens the first `first` and the
+ * last `recent` stay, and of the others those with the largest weights (equal ones: the earlier; a weight that is no number counts as the least), keep[b] in all.  They move, in their order, to
+ * positions 0 .. keep[b] - 1, their weights with them; the row's weights from there to L become 0.  lengths[b] = keep[b], and pages without a token are freed.
+ * A row with keep[b] < 0 or keep[b] >= L is left as it is (and nothing of it written to weights_out).  So is, and counts as skipped, one with keep[b] < first + recent, with L > width, or where a page from position `first` on is held
+ * by another row too or is none of the pool's: what fork has shared can stay only as a part of the first tokens.
+ *   weights  device [layers][rows][kv_heads][width] fp32, layer_stride elements from layer to layer (at least rows * kv_heads * width);  weights_out the same, and may be `weights`, but
+ *            not lie over a part of it;  layers * rows * kv_heads at most 2^31
+ *   info     device, two int32 or NULL: rows cut back, rows skipped;  workspace fbq_cache_evict_workspace_bytes(c, width) (pointers are not looked at)
+ * Positions in the pages that stay, from keep[b] on, are left as they were.  Attention's causality goes by positions in the row: tokens that come later still see all that stay.
+ */
+size_t fbq_cache_evict_workspace_bytes(const fbq_cache *c, int32_t width);
+fbq_status fbq_cache_evict(const fbq_cache *c, const float *weights, float *weights_out, int64_t layer_stride, int32_t width, const int32_t *keep, int32_t first, int32_t recent, int32_t *info,
+                           void *workspace, size_t workspace_bytes, fbq_stream stream);
+
 #ifdef __cplusplus
 }
 #endif

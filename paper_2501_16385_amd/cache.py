@@ -49,7 +49,8 @@ def declare(lib) -> None:
                             ("fbq_cache_reserve", i32, [cp, vp, vp, vp, vp]), ("fbq_cache_append", i32, [cp, i32, i32, vp, vp, vp, i64, vp, i64, vp]),
                             ("fbq_cache_free", i32, [cp, i32, vp, vp]), ("fbq_cache_fork", i32, [cp, i32, vp, vp, vp, vp, sz, vp]),
                             ("fbq_cache_copy", i32, [cp, i32, vp, vp, vp]), ("fbq_cache_compact", i32, [cp, vp, vp, vp, vp, sz, vp]),
-                            ("fbq_cache_read", i32, [cp, i32, i32, vp, vp, vp, vp, vp]),
+                            ("fbq_attention_weights", i32, [ap, vp, vp, i32, ctypes.c_float, vp]), ("fbq_cache_evict_workspace_bytes", sz, [cp, i32]),
+                            ("fbq_cache_evict", i32, [cp, vp, vp, i64, i32, vp, i32, i32, vp, vp, sz, vp]), ("fbq_cache_read", i32, [cp, i32, i32, vp, vp, vp, vp, vp]),
                             ("fbq_attention_workspace_bytes", sz, [ap]), ("fbq_attention", i32, [ap, vp, sz, vp])):
         f = getattr(lib, name)
         f.restype, f.argtypes = res, args
@@ -309,4 +310,66 @@ def attention(cache: Cache, layer: int, q, q_start=None, max_q: int = 1, shared=
         with _on(stream):
             workspace = torch.empty(max(16, lib.fbq_attention_workspace_bytes(ctypes.byref(c))), dtype=torch.uint8, device=q.device)
     _check(lib.fbq_attention(ctypes.byref(c), _dev_ptr(workspace), _size(workspace), _stream(stream)), "fbq_attention")
+    return out
+
+
+def _weights(t, what: str, shape):
+    """Pointer of a float32 device tensor of the shape [rows, kv_heads, ..], the last one any."""
+    if t is None:
+        return None
+    if t.dtype != _float32 or t.dim() != len(shape) + 1 or tuple(t.shape[:-1]) != shape:
+        raise ValueError(f"{what}: expected float32 [{', '.join(['layers'] * (len(shape) - 2) + ['rows', 'kv_heads', 'width'])}] of the cache")
+    return _dev_ptr(t)
+
+
+def attention_weights(cache: Cache, layer: int, q, lse, weights, q_start=None, max_q: int = 1, scale=None, decay: float = 1.0, out=None, stream=None):
+    """fbq_attention_weights, after attention() of the same q, q_start, max_q and scale, which wrote lse: what each key was attended to, for every key/value head over its queries -> out.
+
+    weights: float32 [rows, kv_heads, width], what earlier calls added up (times decay; the row's new tokens begin at 0), or None; out: the same shape, weights itself by default.
+    Tokens from width on are not counted; places without a token are left alone.
+    """
+    if out is None:
+        out = weights
+    if out is None:
+        raise ValueError("weights or out: expected one of them")
+    heads = (int(cache._c.rows), cache.heads)
+    to, at = _weights(out, "out", heads), _weights(weights, "weights", heads)
+    if weights is not None and weights.shape != out.shape:
+        raise ValueError("out: expected the shape of weights")
+    if lse is None:
+        raise ValueError("lse: expected what attention() wrote")
+    c = _arguments(cache, layer, q, q_start, max_q, None, scale, None, lse)
+    _check(fbq.load().fbq_attention_weights(ctypes.byref(c), at, to, out.shape[-1], float(decay), _stream(stream)), "fbq_attention_weights")
+    return out
+
+
+def cache_evict_workspace(cache: Cache, weights):
+    """A workspace for cache_evict() calls with weights like these."""
+    import torch
+    need = fbq.load().fbq_cache_evict_workspace_bytes(cache._c, weights.shape[-1])
+    return torch.empty(max(16, need), dtype=torch.uint8, device=cache.pool.device)
+
+
+def cache_evict(cache: Cache, weights, keep, first: int = 0, recent: int = 0, out=None, info=None, workspace=None, stream=None):
+    """fbq_cache_evict: rows cut back to keep[b] tokens (int32 [rows]; -1, or as many as there are: left as it is) in every layer and head: the first `first`, the last `recent`, and of
+    the others those with the largest weights.
+
+    weights: float32 [layers, rows, kv_heads, width] (a layer's rows may be a part of more: weights[:, a:b] goes with cache.rows(a, b)); out: takes them as they are afterwards, weights
+    itself by default.  info: int32 [2], rows cut back and rows skipped (see the header: what other rows hold too cannot move).
+    """
+    out = weights if out is None else out
+    rows, layers = int(cache._c.rows), int(cache.pool.shape[0])
+    stride = None
+    for t, what in ((weights, "weights"), (out, "out")):
+        if t.dtype != _float32 or t.dim() != 4 or tuple(t.shape[:3]) != (layers, rows, cache.heads) or (stride is not None and t.shape != weights.shape):
+            raise ValueError(f"{what}: expected float32 [layers, rows, kv_heads, width] of the cache")
+        if not t[0].is_contiguous() or (layers > 1 and stride is not None and t.stride(0) != stride):
+            raise ValueError(f"{what}: a layer's have to lie in one piece, and out's layers as far apart as those of weights")
+        stride = t.stride(0) if layers > 1 else t[0].numel()
+    at, to = (_dev_ptr(t[0]) for t in (weights, out))
+    if workspace is None:
+        with _on(stream):
+            workspace = cache_evict_workspace(cache, weights)
+    _check(fbq.load().fbq_cache_evict(cache._c, at, to, stride, weights.shape[3], _ints(keep, "keep", rows), int(first), int(recent), _info(info, 2), _dev_ptr(workspace), _size(workspace),
+                                      _stream(stream)), "fbq_cache_evict")
     return out

@@ -1,0 +1,350 @@
+// fbq_cache_evict: rows cut back to the tokens that matter, each layer and key/value head by its own weights.
+//
+// Four launches: which rows (their pages looked at as they are before the call); which tokens of each layer, row and head stay, and their weights; the tokens moved; tables, lengths and pages.
+// Choosing: the least weight that stays is found 8 bits at a time from counts of the digits in LDS (whole numbers: their order does not matter); of those equal to it the earliest stay.
+// Moving is in place: position i takes token src[i] >= i.  A block has some columns - 64 bytes of every key, or value - of one row and head to itself and goes through the positions
+// upwards, reading a round's tokens before it writes them: what it writes lies before all that it still reads.  Bound by HBM: every token that moves is read and written once.
+#include <algorithm>
+
+#include "fbq_attend.h"
+#include "fbq_cache4.h"
+#include "fbq_internal.h"
+
+namespace fbq {
+
+constexpr int kChooseThreads = 256, kChooseEach = 4;
+constexpr int kMoveThreads = 256;        // (what four threads a token, and sixteen four tokens, count on)
+constexpr int kEvictBlocks = 1 << 20;    // of a grid at most; they go on with every so manieth item
+
+struct EvictArgs {
+    CacheArgs c;
+    const float *weights;
+    float *weights_out;
+    long layer_stride;
+    const int32_t *keep;
+    int width, first, recent;
+    int32_t *rows;                       // tokens of a row that is cut back, -1: left as it is, -2: skipped
+    int32_t *src;                        // [items][width]: which tokens stay
+    long items;                          // layers x rows x heads
+};
+
+__global__ __launch_bounds__(256) void fbq_evict_rows_kernel(const EvictArgs e)
+{
+    __shared__ int bad;
+    const CacheArgs &c = e.c;
+    const int b = blockIdx.x, tokens = tokens_of(c.lengths[b], c.max_pages << c.log_ps), keep = e.keep[b];
+    if (threadIdx.x == 0) bad = 0;
+    __syncthreads();
+    if (keep < 0 || keep >= tokens) {
+        if (threadIdx.x == 0) e.rows[b] = -1;
+        return;
+    }
+    const int pages = (tokens + (1 << c.log_ps) - 1) >> c.log_ps;
+    for (int i = (min(e.first, tokens) >> c.log_ps) + threadIdx.x; i < pages; i += 256) {
+        const int page = c.table[(long)b * c.max_pages + i];
+        if ((unsigned)page >= (unsigned)c.pages || c.refs[page] != 1) bad = 1;            // (any of them writes the same)
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) e.rows[b] = bad || tokens > e.width || (long)e.first + e.recent > keep ? -2 : tokens;
+}
+
+// Sums over the block of two counts of up to 2^16 - 1 in a word, of the threads before this one; all threads call it.
+__device__ __forceinline__ int block_before(int v, int *scratch, int *total)
+{
+    constexpr int kWaves = kChooseThreads / 64;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, s = wave_scan(v);
+    __syncthreads();
+    if (lane == 63) scratch[wave] = s;
+    __syncthreads();
+    int before = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        before += w < wave ? scratch[w] : 0;
+        all += scratch[w];
+    }
+    *total = all;
+    return before + s - v;
+}
+
+// A weight as a whole number in the order of weights; what is no number is the least.
+__device__ __forceinline__ uint32_t order_of(float x)
+{
+    if (!(x == x)) return 0;
+    const uint32_t u = __builtin_bit_cast(uint32_t, x + 0.0f);             // (no zero with a sign)
+    return u >> 31 ? ~u : u | 0x80000000u;
+}
+
+__global__ __launch_bounds__(kChooseThreads) void fbq_evict_choose_kernel(const EvictArgs e)
+{
+    __shared__ int counts[256], scratch[kChooseThreads / 64], found[2];
+    const CacheArgs &c = e.c;
+    const int tid = threadIdx.x;
+    for (long item = blockIdx.x; item < e.items; item += gridDim.x) {
+        const long of_layer = (long)c.rows * c.kv_heads, layer = item / of_layer, rest = item - layer * of_layer;
+        const int b = (int)(rest / c.kv_heads), tokens = e.rows[b];
+        if (tokens < 0) continue;
+        const long at = layer * e.layer_stride + rest * e.width;
+        const float *const from = e.weights + at;
+        float *const to = e.weights_out + at;
+        int32_t *const src = e.src + item * e.width;
+        const int first = e.first, end = tokens - e.recent, keep = e.keep[b];
+        int wanted = keep - first - e.recent;                 // of the middle, first <= j < end (more than those: some go)
+        uint32_t least = 0, mask = 0;                         // what all weights that may still be the least one that stays begin with
+        if (wanted > 0) {
+            for (int shift = 24; shift >= 0; shift -= 8) {
+                counts[tid] = 0;
+                __syncthreads();
+                for (int j = first + tid; j < end; j += kChooseThreads) {
+                    const uint32_t u = order_of(from[j]);
+                    if ((u & mask) == least) atomicAdd(&counts[u >> shift & 255], 1);
+                }
+                __syncthreads();
+                int total;
+                const int mine = counts[255 - tid], above = block_before(mine, scratch, &total);   // of larger digits than this thread's
+                if (above < wanted && above + mine >= wanted) {
+                    found[0] = 255 - tid;
+                    found[1] = above;
+                }
+                __syncthreads();
+                least |= (uint32_t)found[0] << shift;
+                mask |= 0xffu << shift;
+                wanted -= found[1];
+            }
+        } else {
+            least = 0xffffffffu;                              // (above every weight)
+        }
+        // those larger than `least` stay, and the first `wanted` of those equal to it
+        int larger = 0, equal = 0;                            // so far
+        for (int j0 = 0; j0 < tokens; j0 += kChooseThreads * kChooseEach) {
+            float w[kChooseEach];
+            bool over[kChooseEach], same[kChooseEach];
+            int mine = 0, all;
+#pragma unroll
+            for (int i = 0; i < kChooseEach; ++i) {
+                const int j = j0 + tid * kChooseEach + i;
+                w[i] = j < tokens ? from[j] : 0;
+                const bool always = j < first || (j >= end && j < tokens), middle = j >= first && j < end;
+                const uint32_t u = order_of(w[i]);
+                over[i] = always || (middle && u > least);
+                same[i] = middle && u == least && wanted > 0;
+                mine += over[i] + (same[i] << 16);
+            }
+            const int before = block_before(mine, scratch, &all);         // (all reads of the chunk are done behind it)
+            int o = larger + (before & 0xffff), s = equal + (before >> 16);
+#pragma unroll
+            for (int i = 0; i < kChooseEach; ++i) {
+                const int j = j0 + tid * kChooseEach + i;
+                if (over[i] || (same[i] && s < wanted)) {
+                    const int place = o + min(s, max(wanted, 0));
+                    src[place] = j;
+                    to[place] = w[i];
+                }
+                o += over[i];
+                s += same[i];
+            }
+            larger += all & 0xffff;
+            equal += all >> 16;
+        }
+        __syncthreads();
+        for (int j = keep + tid; j < tokens; j += kChooseThreads) to[j] = 0;
+        __syncthreads();
+    }
+}
+
+// What a block has to itself of an item: 64 bytes of a row of bytes that every token has (a key or value of 16 bits, a key's codes), the four bytes each of a token's scales, or, of value codes of
+// 4 bits, 16 words of every four tokens.
+struct MovePart {
+    bool values, codes;                  // codes: the value codes of 4 bits
+    int at, end, row;                    // bytes at .. end of rows of `row` bytes; of value codes the first word
+    bool scales;
+};
+template <bool FOUR>
+__host__ __device__ __forceinline__ int move_parts(int D)
+{
+    if (!FOUR) return 2 * ((2 * D + 63) / 64);
+    const int DS = features4(D);
+    return (DS / 2 + 63) / 64 + DS / 32 + 2;
+}
+template <bool FOUR>
+__device__ __forceinline__ MovePart move_part(int D, int i)
+{
+    if (!FOUR) {
+        const int n = (2 * D + 63) / 64;
+        return MovePart{i >= n, false, 64 * (i % n), 2 * D, 2 * D, false};
+    }
+    const int DS = features4(D), n = (DS / 2 + 63) / 64;
+    if (i < n) return MovePart{false, false, 64 * i, DS / 2, DS / 2, false};
+    if (i < n + DS / 32) return MovePart{true, true, 16 * (i - n), 0, 0, false};
+    return MovePart{i > n + DS / 32, false, 0, 4 * groups4(DS), 4 * groups4(DS), true};
+}
+
+// Rows of a token each: four threads a token, a piece W each, kEach tokens a thread and round.
+template <class W, class Place>
+__device__ __forceinline__ void move_rows(const int32_t *__restrict__ src, int lowest, int keep, bool there, Place place)
+{
+    constexpr int kStep = kMoveThreads / 4, kEach = 8;
+    for (int i0 = lowest; i0 < keep; i0 += kStep * kEach) {
+        int j[kEach];
+        W v[kEach];
+#pragma unroll
+        for (int y = 0; y < kEach; ++y) j[y] = src[min(i0 + y * kStep + ((int)threadIdx.x >> 2), keep - 1)];
+#pragma unroll
+        for (int y = 0; y < kEach; ++y)
+            if (there) v[y] = *reinterpret_cast<const W *>(place(j[y]));
+        __syncthreads();
+#pragma unroll
+        for (int y = 0; y < kEach; ++y) {
+            const int i = i0 + y * kStep + ((int)threadIdx.x >> 2);
+            if (there && i < keep && i != j[y]) *reinterpret_cast<W *>(place(i)) = v[y];
+        }
+    }
+}
+
+template <bool FOUR>
+__global__ __launch_bounds__(kMoveThreads) void fbq_evict_move_kernel(const EvictArgs e)
+{
+    const CacheArgs &c = e.c;
+    const int tid = threadIdx.x, ps1 = (1 << c.log_ps) - 1, parts = move_parts<FOUR>(c.D), DS = features4(c.D);
+    const long head_bytes = (c.page_bytes >> 1) / c.kv_heads, jobs = e.items * parts;
+    for (long job = blockIdx.x; job < jobs; job += gridDim.x) {
+        const long item = job / parts, of_layer = (long)c.rows * c.kv_heads, layer = item / of_layer, rest = item - layer * of_layer;
+        const int b = (int)(rest / c.kv_heads), h = (int)(rest - (long)b * c.kv_heads);
+        if (e.rows[b] < 0) continue;
+        const MovePart part = move_part<FOUR>(c.D, (int)(job - item * parts));
+        const int keep = e.keep[b];
+        const int32_t *const src = e.src + item * e.width, *const list = c.table + (long)b * c.max_pages;
+        unsigned char *const heads = c.pool + layer * c.layer_bytes + (part.values ? c.page_bytes >> 1 : 0) + h * head_bytes;
+        const auto head_of = [&](int token) { return heads + list[token >> c.log_ps] * c.page_bytes; };
+        if (FOUR && part.scales) {
+            const int at = (tid & 3) * 4;
+            move_rows<uint32_t>(src, e.first, keep, at < part.end, [&](int token) { return head_of(token) + scales_at4(c.log_ps, token & ps1, DS) + at; });
+        } else if (!FOUR || !part.codes) {
+            const int at = part.at + (tid & 3) * 16;
+            move_rows<word4_t>(src, e.first, keep, at < part.end, [&](int token) {
+                const int slot = token & ps1;
+                return head_of(token) + (FOUR ? codes_at4(slot, DS) + (slot & 15) * part.row : (long)slot * part.row) + at;
+            });
+        } else {
+            // four tokens' codes a word: each byte from where its token's is
+            constexpr int kStep = kMoveThreads / 16, kEach = 4;
+            const int word = part.at + (tid & 15), words = DS / 2;            // of each four tokens
+            const auto place = [&](int token) {
+                const int slot = token & ps1;
+                return reinterpret_cast<uint32_t *>(head_of(token) + codes_at4(slot, DS)) + (slot >> 2 & 3) * words + word;
+            };
+            for (int q0 = e.first >> 2; 4 * q0 < keep; q0 += kStep * kEach) {
+                uint32_t v[kEach][4], old[kEach];
+                int j[kEach][4];
+#pragma unroll
+                for (int y = 0; y < kEach; ++y)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) j[y][k] = src[min(4 * (q0 + y * kStep + (tid >> 4)) + k, keep - 1)];
+#pragma unroll
+                for (int y = 0; y < kEach; ++y) {
+                    const int i = 4 * (q0 + y * kStep + (tid >> 4));
+                    old[y] = i < keep && i + 4 > keep ? *place(i) : 0;        // (places behind the last token stay as they are)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) v[y][k] = *place(j[y][k]);
+                }
+                __syncthreads();
+#pragma unroll
+                for (int y = 0; y < kEach; ++y) {
+                    const int i = 4 * (q0 + y * kStep + (tid >> 4));
+                    if (i >= keep) continue;
+                    uint32_t to = 0;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int at = 8 * byte_of_token4(k);
+                        to |= i + k < keep ? (v[y][k] >> 8 * byte_of_token4(j[y][k] & 3) & 0xff) << at : old[y] & 0xffu << at;
+                    }
+                    *place(i) = to;
+                }
+            }
+        }
+    }
+}
+
+__global__ __launch_bounds__(256) void fbq_evict_rows_done_kernel(const EvictArgs e, int32_t *info)
+{
+    const CacheArgs &c = e.c;
+    const int b = blockIdx.x;
+    if (info && b == 0) {                                     // rows cut back, rows skipped
+        __shared__ int done, skipped;
+        if (threadIdx.x == 0) done = skipped = 0;
+        __syncthreads();
+        int d = 0, s = 0;
+        for (int i = threadIdx.x; i < c.rows; i += 256) {
+            d += e.rows[i] >= 0;
+            s += e.rows[i] == -2;
+        }
+        if (d) atomicAdd(&done, d);
+        if (s) atomicAdd(&skipped, s);
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            info[0] = done;
+            info[1] = skipped;
+        }
+    }
+    const int tokens = e.rows[b];
+    if (tokens < 0) return;
+    const int keep = e.keep[b], pages = (tokens + (1 << c.log_ps) - 1) >> c.log_ps;
+    for (int i = ((keep + (1 << c.log_ps) - 1) >> c.log_ps) + threadIdx.x; i < pages; i += 256) {
+        int32_t *const at = c.table + (long)b * c.max_pages + i;
+        const int page = *at;
+        if ((unsigned)page < (unsigned)c.pages) atomicSub(c.refs + page, 1);
+        *at = -1;
+    }
+    if (threadIdx.x == 0) c.lengths[b] = keep;
+}
+
+}  // namespace fbq
+
+using namespace fbq;
+
+extern "C" size_t fbq_cache_evict_workspace_bytes(const fbq_cache *c, int32_t width)
+{
+    if (!c || fbq_check_cache(&c->desc) != FBQ_OK || c->rows < 1 || c->rows > 65536 || width < 1 || width > (1 << 24)) return 0;
+    const long items = (long)c->desc.layers * c->rows * c->desc.kv_heads;
+    return items > (1L << 31) ? 0 : ((size_t)c->rows * 4 + 255) / 256 * 256 + (size_t)items * width * 4;
+}
+
+extern "C" fbq_status fbq_cache_evict(const fbq_cache *c, const float *weights, float *weights_out, int64_t layer_stride, int32_t width, const int32_t *keep, int32_t first, int32_t recent,
+                                      int32_t *info, void *workspace, size_t workspace_bytes, fbq_stream stream)
+{
+    const fbq_status st = check_cache(c, true);
+    if (st != FBQ_OK) return st;
+    const int64_t of_layer = (int64_t)c->rows * c->desc.kv_heads, items = of_layer * c->desc.layers;
+    if (width < 1 || width > (1 << 24) || first < 0 || recent < 0 || first > (1 << 24) || recent > (1 << 24) || layer_stride < of_layer * width) return FBQ_ERR_SHAPE;
+    if (items > (1L << 31) || layer_stride > (1L << 48)) return FBQ_ERR_UNSUPPORTED;
+    if (!weights || !weights_out || !keep || !workspace) return FBQ_ERR_NULL;
+    if (!aligned(weights, 4) || !aligned(weights_out, 4) || !aligned(keep, 4) || !aligned(info, 4) || !aligned(workspace, 16)) return FBQ_ERR_ALIGN;
+    if (workspace_bytes < fbq_cache_evict_workspace_bytes(c, width)) return FBQ_ERR_WORKSPACE;
+    const uintptr_t all = ((uintptr_t)(c->desc.layers - 1) * layer_stride + of_layer * width) * 4, a = (uintptr_t)weights, b = (uintptr_t)weights_out;
+    if (a != b && a < b + all && b < a + all) return FBQ_ERR_UNSUPPORTED;                 // (one over a part of the other)
+    EvictArgs e{};
+    e.c = cache_args(*c);
+    e.weights = weights; e.weights_out = weights_out; e.layer_stride = layer_stride; e.keep = keep; e.width = width; e.first = first; e.recent = recent;
+    e.rows = (int32_t *)workspace;
+    e.src = (int32_t *)((char *)workspace + ((size_t)c->rows * 4 + 255) / 256 * 256);
+    e.items = items;
+    const bool four = in_4_bits(c->desc.type);
+    const long jobs = items * (four ? move_parts<true>(e.c.D) : move_parts<false>(e.c.D));
+    const hipStream_t s = (hipStream_t)stream;
+    hipLaunchKernelGGL(fbq_evict_rows_kernel, dim3(c->rows), dim3(256), 0, s, e);
+    hipError_t err = hipGetLastError();
+    if (err == hipSuccess) {
+        hipLaunchKernelGGL(fbq_evict_choose_kernel, dim3((unsigned)std::min<long>(items, kEvictBlocks)), dim3(kChooseThreads), 0, s, e);
+        err = hipGetLastError();
+    }
+    if (err == hipSuccess) {
+        const dim3 grid((unsigned)std::min<long>(jobs, kEvictBlocks));
+        if (four) hipLaunchKernelGGL(fbq_evict_move_kernel<true>, grid, dim3(kMoveThreads), 0, s, e);
+        else hipLaunchKernelGGL(fbq_evict_move_kernel<false>, grid, dim3(kMoveThreads), 0, s, e);
+        err = hipGetLastError();
+    }
+    if (err == hipSuccess) {
+        hipLaunchKernelGGL(fbq_evict_rows_done_kernel, dim3(c->rows), dim3(256), 0, s, e, info);
+        err = hipGetLastError();
+    }
+    return err == hipSuccess ? FBQ_OK : FBQ_ERR_HIP;
+}

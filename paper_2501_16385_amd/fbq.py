@@ -25,7 +25,8 @@ EXPORTED_SYMBOLS = ["fbq_status_string", "fbq_check_desc", "fbq_packed_bytes", "
                     "fbq_train_workspace_bytes", "fbq_gram", "fbq_train_step", "fbq_test_set_spin_limit",
                     "fbq_measure_read_stream",
                     "fbq_check_cache", "fbq_cache_bytes", "fbq_cache_workspace_bytes", "fbq_cache_reserve", "fbq_cache_append", "fbq_cache_free", "fbq_cache_fork",
-                    "fbq_cache_copy", "fbq_cache_compact", "fbq_attention_workspace_bytes", "fbq_attention", "fbq_cache_read"]
+                    "fbq_cache_copy", "fbq_cache_compact", "fbq_attention_workspace_bytes", "fbq_attention", "fbq_cache_read",
+                    "fbq_attention_weights", "fbq_cache_evict_workspace_bytes", "fbq_cache_evict"]
 
 
 class FbqError(RuntimeError):
