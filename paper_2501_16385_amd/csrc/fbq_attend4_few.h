@@ -1,14 +1,16 @@
 // Attention of a few query rows against a long row of a cache in 4 bits: the work of fbq_attend_few.h (its items, pieces and join) over codes.
 //
 // Codes go into the matrix cores as they are, fp16 numbers below the normal ones (fbq_cache4.h), and are multiplied exactly; scales come in afterwards, in 32 bits.
-//   scores   k = m + s c of a key's group:  q . k = sum over groups of  s (q . c) + m sum(q):  16 keys' q . c is two products a group, of the codes at low and at high bits, and the
-//            sums of q over a group are made once a piece.  Queries of bf16 are fp16 here, times a power of two for the row (which goes into its scale): bf16 has fewer digits, so
-//            only what is 2^-28 of the row's largest feature and less loses any.
-//   results  sum p v = sum (p s) c + sum p m:  p s is operand B of the second product, a rounding to fp16 where fbq_attend_few.h rounds p; the second sum stays in 32 bits, in the lane.
-//            p s has to be in fp16's range whatever the scales: p is relative to 2^e too, e the exponent of the largest scale so far, less 5, and follows when it is passed by 2^7.
+//   scores   k = m + s c of a key's group:  q . k = sum over groups of  s (q . c) + m sum(q).  Queries are fp16 here, times a power of two for the row (which goes into its scale): the row's
+//            largest feature is near 2^15, and those of codes at high bits are divided by 16, so that only what is 2^-24 of the largest and less loses any.
+//   results  sum p v = sum (p s) (c - 8) + sum p (m + 8 s):  p s is operand B of the second product, a rounding to fp16 where fbq_attend_few.h rounds p; the 8 is a product of its own with the
+//            rounded numbers, and the second sum stays in 32 bits, in the lane.  (Without the 8 the rounding is that of numbers three times as large, which add up to the same: relative L2
+//            against 64 bits 5.4e-4 instead of 3e-4 for 1000 keys in fp16.)  p s has to be in fp16's range whatever the scales: p is relative to 2^e too, e the exponent of the largest 2^10 s
+//            so far, less 5, and follows when it is passed by 2^7.
+//   scales   A key's scale is wanted in all 16 lanes that have its row of a product.  The matrix cores, which have time, put it there: the scale words as operand A, [key][group] with m and s as
+//            neighbours, times constants as operand B are s, m + 8 s, and, with the sums of q in three parts of 16 bits each, m sum(q) - in 32 bits, exactly but for the last addition.
+//            (Vector instructions instead, neighbours' words by quad_perm: 350 a step, 100 of them for this, and 5.2 TB/s where it is now 5.9.)
 // A value that nobody sees has weight zero and finite scales, so nothing of it is added, whatever it is: no second look is needed.
-//
-// Bound by HBM in long rows: D / 2 + 4 G bytes a key and a value, a third to a fourth of 16 bits' - and close behind by the vector instructions, about 250 for 32 keys of 128 features.
 #ifndef FBQ_ATTEND4_FEW_H
 #define FBQ_ATTEND4_FEW_H
 
@@ -20,94 +22,117 @@
 
 namespace fbq {
 
+constexpr int kFew4Parts = kFewTile / 16;                     // of a step, 16 keys each
+
 template <int NW>
 struct Step4 {
-    static constexpr int G = groups4(32 * NW);
-    uint32_t k[2][NW], v[2][NW];                              // of 16 keys each
-    word4_t ks[2][G], vs[2][G];                               // scales of this lane's four of them: [key][group]
+    static constexpr int kParts = kFew4Parts;
+    uint32_t k[kParts][NW], v[kParts][NW];
+    uint32_t ks[kParts], vs[kParts];                          // scale word of key l % 16 and group l / 16
 };
 
 template <int NW>
-__device__ __forceinline__ void load_words(uint32_t (&to)[NW], __amdgpu_buffer_rsrc_t from, int off)
+struct Piece4 {
+    int b, h, step, steps, limit, n, key0, t, sees;           // as in Piece
+    word4_t q[NW];
+    int pages[kFew4Parts];                                    // of its first step
+};
+
+// A page number by a scalar load: vector loads are waited for in their order, and one among a step's would hold up those behind it.
+__device__ __forceinline__ int page_of(const int32_t *list, int index, int count)
+{
+    typedef const __attribute__((address_space(4))) int32_t *scalar_t;
+    return ((scalar_t)(uintptr_t)list)[uniform(max(min(index, count - 1), 0))];
+}
+
+template <int N, int POLICY>
+__device__ __forceinline__ void load_words(uint32_t (&to)[N], __amdgpu_buffer_rsrc_t from, int off)
 {
     typedef uint32_t word3_t __attribute__((ext_vector_type(3)));
 #pragma unroll
-    for (int i = 0; i < NW / 4; ++i) {
-        const word4_t w = __builtin_amdgcn_raw_buffer_load_b128(from, off + 16 * i, 0, kOnce);
+    for (int i = 0; i < N / 4; ++i) {
+        const word4_t w = __builtin_amdgcn_raw_buffer_load_b128(from, off + 16 * i, 0, POLICY);
 #pragma unroll
         for (int e = 0; e < 4; ++e) to[4 * i + e] = w[e];
     }
-    if constexpr (NW % 4 == 2) {
-        const word2_t w = __builtin_amdgcn_raw_buffer_load_b64(from, off + 4 * (NW - 2), 0, kOnce);
-        to[NW - 2] = w[0];
-        to[NW - 1] = w[1];
+    if constexpr (N % 4 == 1) to[N - 1] = __builtin_amdgcn_raw_buffer_load_b32(from, off + 4 * (N - 1), 0, POLICY);
+    if constexpr (N % 4 == 2) {
+        const word2_t w = __builtin_amdgcn_raw_buffer_load_b64(from, off + 4 * (N - 2), 0, POLICY);
+        to[N - 2] = w[0];
+        to[N - 1] = w[1];
     }
-    if constexpr (NW == 3) {
-        const word3_t w = __builtin_amdgcn_raw_buffer_load_b96(from, off, 0, kOnce);
-        to[0] = w[0];
-        to[1] = w[1];
-        to[2] = w[2];
+    if constexpr (N % 4 == 3) {
+        const word3_t w = __builtin_amdgcn_raw_buffer_load_b96(from, off + 4 * (N - 3), 0, POLICY);
+        to[N - 3] = w[0];
+        to[N - 2] = w[1];
+        to[N - 1] = w[2];
     }
 }
 
-// The queries of a wave's 16 rows as operands for codes: of a group, those at low bits and those at high bits; the group's sums of them, times 2^-24; what scores are to be multiplied by.
-template <class NT, int NW>
+// The queries of a wave's 16 rows: operands for codes, of a group those at low bits and those at high bits; for scale words, what makes 2^10 s of a group and m sum(q) of all; and what scores
+// are to be multiplied by.
+template <class TY, class NT, int NW>
 struct Queries4 {
     static constexpr int G = groups4(32 * NW);
-    word4_t at[G][2];
-    float sum[G];
+    word4_t at[G][2], sums;
+    word2_t pick[G];
     float unit;
 
     // q: the words of features 32 w + 8 (lane / 16) .., of the lane's row
     __device__ __forceinline__ void of(const word4_t (&q)[NW], float scale)
     {
+        float most = 0;
+#pragma unroll
+        for (int w = 0; w < NW; ++w)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) most = fmaxf(most, fmaxf(fabsf(NT::of(q[w][e] & 0xffff)), fabsf(NT::of_upper(q[w][e]))));
+        const int up = __builtin_amdgcn_frexp_expf(larger_of_32(larger_of_16(most))) - 15;
+        unit = ldexpf(scale * 0x1p14f, up);
         word4_t h[NW];
-        unit = scale * 0x1p24f;
-        if constexpr (std::is_same<NT, NumberF16>::value) {
 #pragma unroll
-            for (int w = 0; w < NW; ++w) h[w] = q[w];
-        } else {
-            float most = 0;
+        for (int w = 0; w < NW; ++w)
 #pragma unroll
-            for (int w = 0; w < NW; ++w)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) most = fmaxf(most, fmaxf(fabsf(NT::of(q[w][e] & 0xffff)), fabsf(NT::of_upper(q[w][e]))));
-            const int up = __builtin_amdgcn_frexp_expf(larger_of_32(larger_of_16(most))) - 15;
-            unit = ldexpf(unit, up);
-#pragma unroll
-            for (int w = 0; w < NW; ++w)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) h[w][e] = TypeF16::pack(ldexpf(NT::of(q[w][e] & 0xffff), -up), ldexpf(NT::of_upper(q[w][e]), -up));
-        }
-        const word4_t one{0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u};
+            for (int e = 0; e < 4; ++e) {
+                const int by = e < 2 ? -up : -up - 4;
+                h[w][e] = TypeF16::pack(ldexpf(NT::of(q[w][e] & 0xffff), by), ldexpf(NT::of_upper(q[w][e]), by));
+            }
+        const word4_t one{0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u}, sixteen{0x4c004c00u, 0x4c004c00u, 0x4c004c00u, 0x4c004c00u};
+        const int grp = (threadIdx.x & 63) >> 4;
+        float sum = 0;                                        // of group l / 16
 #pragma unroll
         for (int y = 0; y < G; ++y) {
             const word4_t a = h[2 * y], b = 2 * y + 1 < NW ? h[std::min(2 * y + 1, NW - 1)] : word4_t{0, 0, 0, 0};
             at[y][0] = word4_t{a[0], a[1], b[0], b[1]};
             at[y][1] = word4_t{a[2], a[3], b[2], b[3]};
-            const float4_t s = TypeF16::mfma(one, at[y][1], TypeF16::mfma(one, at[y][0], float4_t{0, 0, 0, 0}));
-            sum[y] = s[0] * 0x1p-24f;
+            const float4_t s = TypeF16::mfma(sixteen, at[y][1], TypeF16::mfma(one, at[y][0], float4_t{0, 0, 0, 0}));
+            sum = grp == y ? s[0] * 0x1p-14f : sum;
+            pick[y] = word2_t{grp == y ? NT::bits(1024.0f) << 16 : 0u, 0u};
         }
+        const uint32_t high = NT::bits(sum);
+        const float rest = sum - NT::of(high);
+        const uint32_t middle = NT::bits(rest);
+        sums = word4_t{high, middle, NT::bits(rest - NT::of(middle)), 0u};
     }
 };
 
-// Scores of 16 keys, 2^24 / unit of them: keys 4 (l / 16) + i in z[i], the lane's query row.
-template <class NT, int NW>
-__device__ __forceinline__ float4_t scores4(const uint32_t (&k)[NW], const word4_t (&ks)[groups4(32 * NW)], const Queries4<NT, NW> &q)
+// Of 16 keys, a lane's four (4 (l / 16) + i): 2^10 of their scales in a group.
+template <class TY>
+__device__ __forceinline__ float4_t scales_of(uint32_t words, word2_t pick) { return TY::mfma(word2_t{words, 0u}, pick, float4_t{0, 0, 0, 0}); }
+
+// Scores of 16 keys, 1 / unit of them: keys 4 (l / 16) + i in z[i], the lane's query row.
+template <class TY, class NT, int NW>
+__device__ __forceinline__ float4_t scores4(const uint32_t (&k)[NW], uint32_t ks, const Queries4<TY, NT, NW> &q)
 {
     constexpr int G = groups4(32 * NW);
-    float4_t z{0, 0, 0, 0};
+    float4_t z = TY::mfma(word4_t{ks, ks, ks, 0u}, q.sums, float4_t{0, 0, 0, 0});
 #pragma unroll
     for (int y = 0; y < G; ++y) {
         const uint32_t a = k[2 * y], b = 2 * y + 1 < NW ? k[std::min(2 * y + 1, NW - 1)] : 0;
         const float4_t low = TypeF16::mfma(word4_t{a & kLowCodes, a >> 8 & kLowCodes, b & kLowCodes, b >> 8 & kLowCodes}, q.at[y][0], float4_t{0, 0, 0, 0});
-        const float4_t high = TypeF16::mfma(word4_t{a & kHighCodes, a >> 8 & kHighCodes, b & kHighCodes, b >> 8 & kHighCodes}, q.at[y][1], float4_t{0, 0, 0, 0});
+        const float4_t all = TypeF16::mfma(word4_t{a & kHighCodes, a >> 8 & kHighCodes, b & kHighCodes, b >> 8 & kHighCodes}, q.at[y][1], low);
+        const float4_t s = scales_of<TY>(ks, q.pick[y]);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t word = ks[(i * G + y) / 4][(i * G + y) % 4];
-            z[i] = __builtin_fmaf(NT::of(word & 0xffff), q.sum[y], y ? z[i] : 0.0f);
-            z[i] = __builtin_fmaf(NT::of_upper(word), __builtin_fmaf(high[i], 0.0625f, low[i]), z[i]);
-        }
+        for (int i = 0; i < 4; ++i) z[i] = __builtin_fmaf(s[i], all[i], z[i]);
     }
     return z;
 }
@@ -120,18 +145,21 @@ template <class TY, class NT, int NW>
 __device__ __forceinline__ void attend4_few(const AttendArgs &a, int block, unsigned char *room)
 {
     constexpr int DS = 32 * NW, G = groups4(DS), J = 2 * NW;   // products of the results
+    constexpr int kParts = kFew4Parts;
     const int lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4;
     const int worker = uniform(block * kFewWaves + (threadIdx.x >> 6));
     const int D = a.D, ps1 = (1 << a.log_ps) - 1;
     const int member = col % a.group;
     const long head_bytes = (a.page_bytes >> 1) / a.kv_heads;
 
-    Piece<DS> cur, behind;
+    Piece4<NW> cur, behind;
     FewLine line;
     if (!line.first(a, block, worker, cur)) return;
     const bool together = line.together;
-    auto prepare = [&](Piece<DS> &x) __attribute__((always_inline)) {
+    auto prepare = [&](Piece4<NW> &x) __attribute__((always_inline)) {
         few_sight(a, x, col);
+#pragma unroll
+        for (int part = 0; part < kParts; ++part) x.pages[part] = page_of(few_pages(a, x), (x.key0 + 16 * part) >> a.log_ps, few_page_count(a, x));
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
             const int d = 32 * w + 8 * grp;
@@ -139,30 +167,44 @@ __device__ __forceinline__ void attend4_few(const AttendArgs &a, int block, unsi
             if (x.t >= 0 && d < D) x.q[w] = (*reinterpret_cast<const word4_t *>(a.q + x.t * a.q_stride + (x.h * a.group + member) * D + d) & a.q_and) ^ a.q_xor;
         }
     };
-    auto load = [&](Step4<NW> &to, Piece<DS> &x, int s) __attribute__((always_inline)) {
+    // The step that is asked for next: its first key (behind the last of the piece: none), pages, where the piece's keys end, the head; and the list that the pages come from.
+    int ask_key = 0, ask_end = 0, ask_h = 0, ask_pages[kParts], ask_count = 1;
+    const int32_t *ask_list = a.table;
+    auto aim = [&](const Piece4<NW> &x, bool there) __attribute__((always_inline)) {
+        ask_key = x.key0;
+        ask_end = there ? min(x.limit, x.key0 + x.n * kFewTile) : 0;
+        ask_h = x.h;
+        ask_list = few_pages(a, x);
+        ask_count = few_page_count(a, x);
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const int key = x.key0 + s * kFewTile + 16 * half;
-            int valid = min(max(x.limit - key, 0), 16);
-            const int id = valid ? x.pages.at(key >> a.log_ps) : 0;
-            if ((unsigned)id >= (unsigned)a.pages) valid = 0;
-            const unsigned char *const keys = a.kv + (valid ? id : 0) * a.page_bytes + x.h * head_bytes, *const values = keys + (a.page_bytes >> 1);
+        for (int part = 0; part < kParts; ++part) ask_pages[part] = x.pages[part];
+    };
+    const int scale_off = grp < G ? (col * G + grp) * 4 : kNowhere;
+    // Always as many loads, of nothing where there is nothing: then the waits for a step's know how many came behind it.
+    auto load = [&](Step4<NW> &to) __attribute__((always_inline)) {
+#pragma unroll
+        for (int part = 0; part < kParts; ++part) {
+            const int key = ask_key + 16 * part, id = ask_pages[part];
+            const int valid = (unsigned)id < (unsigned)a.pages ? min(max(ask_end - key, 0), 16) : 0;
+            const unsigned char *const keys = a.kv + (valid ? id : 0) * a.page_bytes + ask_h * head_bytes, *const values = keys + (a.page_bytes >> 1);
             const long codes = codes_at4(key & ps1, DS), scales = scales_at4(a.log_ps, key & ps1, DS);
             const int all = valid ? 8 * DS : 0;               // (codes of places without a token do no harm: their scales are zeros)
-            load_words<NW>(to.k[half], buffer_of(keys + codes, all), (col * 4 + grp) * NW * 4);
-            load_words<NW>(to.v[half], buffer_of(values + codes, all), lane * NW * 4);
-            const __amdgpu_buffer_rsrc_t kb = buffer_of(keys + scales, valid * 4 * G), vb = buffer_of(values + scales, valid * 4 * G);
-#pragma unroll
-            for (int y = 0; y < G; ++y) {
-                to.ks[half][y] = __builtin_amdgcn_raw_buffer_load_b128(kb, grp * 16 * G + 16 * y, 0, 0);
-                to.vs[half][y] = __builtin_amdgcn_raw_buffer_load_b128(vb, grp * 16 * G + 16 * y, 0, 0);
-            }
+            load_words<NW, kOnce>(to.k[part], buffer_of(keys + codes, all), (col * 4 + grp) * NW * 4);
+            to.ks[part] = __builtin_amdgcn_raw_buffer_load_b32(buffer_of(keys + scales, valid * 4 * G), scale_off, 0, 0);
+            load_words<NW, kOnce>(to.v[part], buffer_of(values + codes, all), lane * NW * 4);
+            to.vs[part] = __builtin_amdgcn_raw_buffer_load_b32(buffer_of(values + scales, valid * 4 * G), scale_off, 0, 0);
         }
+        ask_key += kFewTile;                                  // (the pages of the one behind it, needed a step from now)
+#pragma unroll
+        for (int part = 0; part < kParts; ++part) ask_pages[part] = page_of(ask_list, (ask_key + 16 * part) >> a.log_ps, ask_count);
     };
 
-    Queries4<NT, NW> q;
-    float4_t o[J];
-    float m, l, lows[G];                                      // lows: sum p m, of the lane's keys
+    Queries4<TY, NT, NW> q;
+    word2_t eighths[G];                                       // what makes m + 8 s of a group's scale words
+#pragma unroll
+    for (int y = 0; y < G; ++y) eighths[y] = word2_t{grp == y ? NT::bits(8.0f) << 16 | NT::bits(1.0f) : 0u, 0u};
+    float4_t o[J], eights[G];                                 // eights: sums of 8 p s as it is rounded, times 2^-14 like those of p s c in o
+    float m, l, lows[G];                                      // lows: sum p (m + 8 s), of the lane's keys
     int least, e;                                             // what every row of the piece sees; the exponent that p is relative to
     uint32_t most;                                            // the largest scale word that goes with e
     auto begin = [&]() __attribute__((always_inline)) {
@@ -170,7 +212,10 @@ __device__ __forceinline__ void attend4_few(const AttendArgs &a, int block, unsi
 #pragma unroll
         for (int j = 0; j < J; ++j) o[j] = float4_t{0, 0, 0, 0};
 #pragma unroll
-        for (int y = 0; y < G; ++y) lows[y] = 0;
+        for (int y = 0; y < G; ++y) {
+            lows[y] = 0;
+            eights[y] = float4_t{0, 0, 0, 0};
+        }
         m = kNoScore;
         l = 0;
         e = 0;
@@ -181,26 +226,24 @@ __device__ __forceinline__ void attend4_few(const AttendArgs &a, int block, unsi
         least = uniform(least);
     };
     auto compute = [&](const Step4<NW> &x, int s) __attribute__((always_inline)) {
-        float4_t z[2];
+        float4_t z[kParts];
         float top = -INFINITY;
         const int key = cur.key0 + s * kFewTile;
 #pragma unroll
-        for (int half = 0; half < 2; ++half) z[half] = scores4<NT, NW>(x.k[half], x.ks[half], q);
+        for (int part = 0; part < kParts; ++part) z[part] = scores4<TY, NT, NW>(x.k[part], x.ks[part], q);
         if (key + kFewTile > least) {
+            const int sees = cur.sees - key - 4 * grp;
 #pragma unroll
-            for (int half = 0; half < 2; ++half)
+            for (int part = 0; part < kParts; ++part)
 #pragma unroll
-                for (int y = 0; y < 4; ++y)
-                    if (key + 16 * half + 4 * grp + y >= cur.sees) z[half][y] = -INFINITY;
+                for (int i = 0; i < 4; ++i)
+                    if (16 * part + i >= sees) z[part][i] = -INFINITY;
         }
         uint32_t largest = 0;                                 // scale word: scales are in its upper half, and not negative
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            top = fmaxf(top, fmaxf(fmaxf(z[half][0], z[half][1]), fmaxf(z[half][2], z[half][3])));
-#pragma unroll
-            for (int y = 0; y < G; ++y)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) largest = max(largest, x.vs[half][y][i]);
+        for (int part = 0; part < kParts; ++part) {
+            top = fmaxf(top, fmaxf(fmaxf(z[part][0], z[part][1]), fmaxf(z[part][2], z[part][3])));
+            largest = max(largest, x.vs[part]);
         }
         top = larger_of_16(top);
         top = larger_of_32(top) * q.unit;
@@ -210,8 +253,8 @@ __device__ __forceinline__ void attend4_few(const AttendArgs &a, int block, unsi
             for (int w = 32; w; w >>= 1) largest = max(largest, (uint32_t)__shfl_xor((int)largest, w));
             largest = uniform(largest);
             if (largest > most) {
-                e = uniform(max(__builtin_amdgcn_frexp_expf(NT::of_upper(largest)) - 5, -100));
-                const uint32_t beyond = NT::bits(ldexpf(1.0f, e + 7));                    // (an infinity: no scale is)
+                e = uniform(max(__builtin_amdgcn_frexp_expf(NT::of_upper(largest)) + 5, -90));
+                const uint32_t beyond = NT::bits(ldexpf(1.0f, e - 3));                    // (an infinity: no scale is)
                 most = uniform((beyond << 16) - 1);
             }
             const float to = fmaxf(top, m - (float)before) + (float)e, by = __builtin_amdgcn_exp2f(m - to);
@@ -219,36 +262,41 @@ __device__ __forceinline__ void attend4_few(const AttendArgs &a, int block, unsi
 #pragma unroll
             for (int j = 0; j < J; ++j) o[j] *= by;
 #pragma unroll
-            for (int y = 0; y < G; ++y) lows[y] *= by;
+            for (int y = 0; y < G; ++y) {
+                lows[y] *= by;
+                eights[y] *= by;
+            }
             m = to;
         }
-        uint32_t ps[G][4];
+        uint32_t ps[G][2 * kParts];
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
+        for (int part = 0; part < kParts; ++part) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                z[half][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[half][i], q.unit, -m));
-                l += z[half][i];
+                z[part][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[part][i], q.unit, -m));
+                l += z[part][i];
             }
 #pragma unroll
             for (int y = 0; y < G; ++y) {
+                const float4_t s = scales_of<TY>(x.vs[part], q.pick[y]), low = scales_of<TY>(x.vs[part], eighths[y]);
                 float of[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const uint32_t word = x.vs[half][(i * G + y) / 4][(i * G + y) % 4];
-                    lows[y] = __builtin_fmaf(z[half][i], NT::of(word & 0xffff), lows[y]);
-                    of[i] = z[half][i] * NT::of_upper(word);
+                    lows[y] = __builtin_fmaf(low[i], z[part][i], lows[y]);
+                    of[i] = s[i] * z[part][i];
                 }
-                ps[y][2 * half] = TypeF16::pack(of[0], of[1]);
-                ps[y][2 * half + 1] = TypeF16::pack(of[2], of[3]);
+                ps[y][2 * part] = TypeF16::pack(of[0], of[1]);
+                ps[y][2 * part + 1] = TypeF16::pack(of[2], of[3]);
             }
         }
+        const word4_t eight{0x00080008u, 0x00080008u, 0x00080008u, 0x00080008u};
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
             const uint32_t a = x.v[0][w], b = x.v[1][w];
             const word4_t p{ps[w / 2][0], ps[w / 2][1], ps[w / 2][2], ps[w / 2][3]};
             o[2 * w] = TypeF16::mfma(word4_t{a & kLowCodes, a >> 8 & kLowCodes, b & kLowCodes, b >> 8 & kLowCodes}, p, o[2 * w]);
             o[2 * w + 1] = TypeF16::mfma(word4_t{a & kHighCodes, a >> 8 & kHighCodes, b & kHighCodes, b >> 8 & kHighCodes}, p, o[2 * w + 1]);
+            if (w % 2 == 0) eights[w / 2] = TypeF16::mfma(eight, p, eights[w / 2]);
         }
     };
     bool first = true;
@@ -263,7 +311,7 @@ __device__ __forceinline__ void attend4_few(const AttendArgs &a, int block, unsi
 #pragma unroll
         for (int j = 0; j < J; ++j)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) o[j][i] = __builtin_fmaf(o[j][i], j & 1 ? 0x1p20f : 0x1p24f, lows[j / 4]);
+            for (int i = 0; i < 4; ++i) o[j][i] = __builtin_fmaf(j & 1 ? __builtin_fmaf(o[j][i], 0.0625f, -eights[j / 4][i]) : o[j][i] - eights[j / 4][i], 0x1p14f, lows[j / 4]);
         if (together) {                                       // the first wave joins the block's, as in attend_few_wave
             float *const at = reinterpret_cast<float *>(room) + lane;
             const int wave = uniform(threadIdx.x >> 6);
@@ -328,15 +376,17 @@ __device__ __forceinline__ void attend4_few(const AttendArgs &a, int block, unsi
         finish();
         return;
     }
+    behind = cur;                                             // (where there is none, something that is one)
     bool more = line.follow(a, cur, behind);
     if (more) prepare(behind);
     Step4<NW> x0, x1;
-    load(x0, cur, 0);
+    aim(cur, true);
+    load(x0);
     begin();
     int s = 0;
     auto turn = [&](const Step4<NW> &now, Step4<NW> &next) __attribute__((always_inline)) {
-        if (s + 1 < cur.n) load(next, cur, s + 1);
-        else if (more) load(next, behind, 0);
+        if (s + 1 == cur.n) aim(behind, more);
+        load(next);
         compute(now, s);
         if (++s < cur.n) return false;
         finish();

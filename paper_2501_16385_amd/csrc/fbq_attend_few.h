@@ -128,13 +128,18 @@ struct FewLine {
     }
 };
 
-// A piece's first key and pages, and what the lane's query row `col` sees of it.
+// The pages of a piece's item, and how many there are.
+template <class P>
+__device__ __forceinline__ const int32_t *few_pages(const AttendArgs &a, const P &x) { return x.b < 0 ? a.shared : a.table + (long)x.b * a.max_pages; }
+template <class P>
+__device__ __forceinline__ int few_page_count(const AttendArgs &a, const P &x) { return x.b < 0 ? a.n_shared >> a.log_ps : a.max_pages; }
+
+// A piece's first key, and what the lane's query row `col` sees of it.
 template <class P>
 __device__ __forceinline__ void few_sight(const AttendArgs &a, P &x, int col)
 {
     const bool is_shared = x.b < 0;
     x.key0 = (is_shared ? 0 : a.n_shared) + x.step * kFewTile;
-    x.pages.begin(is_shared ? a.shared : a.table + (long)x.b * a.max_pages, is_shared ? a.n_shared >> a.log_ps : a.max_pages, x.key0 >> a.log_ps);
     const int i = col / a.group;
     x.t = -1;
     x.sees = 0;
@@ -183,6 +188,7 @@ __device__ __forceinline__ bool attend_few_wave(const AttendArgs &a, int block, 
     const bool together = line.together;
     auto prepare = [&](Piece<DP> &x) __attribute__((always_inline)) {
         few_sight(a, x, col);
+        x.pages.begin(few_pages(a, x), few_page_count(a, x), x.key0 >> a.log_ps);
 #pragma unroll
         for (int s = 0; s < DP / 32; ++s) {
             const int d = 32 * s + 8 * grp;

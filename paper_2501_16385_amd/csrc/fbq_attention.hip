@@ -207,9 +207,13 @@ static hipError_t launch_join(const AttendArgs &a, bool few, hipStream_t stream)
 // us, 64 query heads on 32 of 128 features, 1 / 2 / 0 (r: rows of 0.25 to 1.75 times as many tokens).  60 tokens: 2 rows 7.1 / 7.3 / 12.1, 32 rows 9.5 / 14.9 / 16.1, 128 r 29 / 52 / 43.
 // 200: 2 rows 14.2 / 9.2 / 14.9, 16 17.2 / 13.6 / 22.8, 32 19.6 / 24.9 / 30.4, 64 r 43.5 / 47.5 / 50.3.  500: 2 rows 29 / 13.0 / 15.1, 16 35 / 25 / 33, 64 r 103 / 95 / 98.  1000: 2 rows
 // 56 / 20.1 / 16.9, 8 62 / 25 / 32, 32 80 / 86 / 89, 16 r 101 / 57.5 / 55.7.  2000: 8 rows 119 / 44 / 55, but 16 r 198 / 110 / 96, where one row is all that is left at the end.
-static int few_direct(long items, long tokens)
+// In 4 bits, where what is streamed is a third and the join costs the same (a wave / a block / dealt out).  60 tokens: 256 items 8.9 / 9.1 / 13.2, 1024 8.9 / 16.9 / 15.5.  500: 256 22.6 / 12.5 /
+// 18.2, 512 22.4 / 15.2 / 21.7, 1024 23.1 / 27.9 / 26.6.  1000: 256 38 / 16.4 / 21.5, 512 38 / 21.0 / 27.8, 1024 38.3 / 39.3 / 38.6; r 512 58 / 28.5 / 30.7.  2000: 128 68 / 24.4 / 22.8, 256 68 /
+// 24.7 / 30.3, 512 68 / 33.4 / 42.8, but r 256 109 / 35.8 / 32.0.  4000: 128 129 / 40.6 / 29.5, 256 131 / 42 / 45.
+static int few_direct(long items, long tokens, bool four)
 {
     if (items > 1L << 22) return 0;                           // (a grid counts its threads in 32 bits)
+    if (four) return tokens <= 1024 ? (items >= 1024 ? 1 : 2) : tokens <= 2048 && items >= 256 ? 2 : 0;
     if (tokens <= 256 && items >= 1024) return 1;
     return tokens <= 512 || (tokens <= 1024 && items >= 128) ? 2 : 0;
 }
@@ -225,7 +229,7 @@ static bool worth_sharing(const fbq_attention_call &c, bool few, long row_querie
     const long tokens = (long)c.n_shared * d.page_size, saved = 4L * tokens * d.kv_heads * d.head_dim * (c.cache.rows - 1);
     if (saved == 0 || row_queries > 64) return false;
     if (!few) return saved >= (row_queries > 32 ? 96L : 32L) << 20;
-    return saved >= (few_direct((long)c.cache.rows * d.kv_heads, (long)c.cache.max_pages * d.page_size) ? 24L : 2L) << 20;
+    return saved >= (few_direct((long)c.cache.rows * d.kv_heads, (long)c.cache.max_pages * d.page_size, in_4_bits(d.type)) ? 24L : 2L) << 20;
 }
 
 struct AttendPlan {
@@ -275,7 +279,7 @@ static AttendPlan attend_plan(const fbq_attention_call &c, void *workspace)
             room(&a.whole_shared, results);
         }
     }
-    a.direct = p.few && !a.n_shared ? few_direct((long)a.rows * a.kv_heads, own_tokens) : 0;
+    a.direct = p.few && !a.n_shared ? few_direct((long)a.rows * a.kv_heads, own_tokens, in_4_bits(c.cache.desc.type)) : 0;
     if (p.few && !a.direct) {
         const long steps = ((own_tokens + kFewTile - 1) / kFewTile * a.rows + (a.shared_here ? a.n_shared / kFewTile + 1 : 0)) * a.kv_heads;
         a.workers = (int)std::min(a.D > 128 ? 1024L : 2048L, (steps + kFewWaves - 1) / kFewWaves * kFewWaves);
