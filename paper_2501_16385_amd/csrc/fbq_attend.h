@@ -194,6 +194,13 @@ struct PageList {
     }
 };
 
+// A page number by a scalar load: vector loads are waited for in their order, and one among a step's would hold up those behind it.
+__device__ __forceinline__ int page_of(const int32_t *list, int index, int count)
+{
+    typedef const __attribute__((address_space(4))) int32_t *scalar_t;
+    return ((scalar_t)(uintptr_t)list)[uniform(max(min(index, count - 1), 0))];
+}
+
 constexpr int kNowhere = 1 << 30;        // an offset behind every descriptor's end: loads answer zero
 
 hipError_t launch_attend_few(const AttendArgs &a, int type, hipStream_t stream);

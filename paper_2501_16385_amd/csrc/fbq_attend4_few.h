@@ -17,6 +17,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "fbq_attend_codes.h"
 #include "fbq_attend_few.h"
 #include "fbq_cache4.h"
 
@@ -37,37 +38,6 @@ struct Piece4 {
     word4_t q[NW];
     int pages[kFew4Parts];                                    // of its first step
 };
-
-// A page number by a scalar load: vector loads are waited for in their order, and one among a step's would hold up those behind it.
-__device__ __forceinline__ int page_of(const int32_t *list, int index, int count)
-{
-    typedef const __attribute__((address_space(4))) int32_t *scalar_t;
-    return ((scalar_t)(uintptr_t)list)[uniform(max(min(index, count - 1), 0))];
-}
-
-template <int N, int POLICY>
-__device__ __forceinline__ void load_words(uint32_t (&to)[N], __amdgpu_buffer_rsrc_t from, int off)
-{
-    typedef uint32_t word3_t __attribute__((ext_vector_type(3)));
-#pragma unroll
-    for (int i = 0; i < N / 4; ++i) {
-        const word4_t w = __builtin_amdgcn_raw_buffer_load_b128(from, off + 16 * i, 0, POLICY);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) to[4 * i + e] = w[e];
-    }
-    if constexpr (N % 4 == 1) to[N - 1] = __builtin_amdgcn_raw_buffer_load_b32(from, off + 4 * (N - 1), 0, POLICY);
-    if constexpr (N % 4 == 2) {
-        const word2_t w = __builtin_amdgcn_raw_buffer_load_b64(from, off + 4 * (N - 2), 0, POLICY);
-        to[N - 2] = w[0];
-        to[N - 1] = w[1];
-    }
-    if constexpr (N % 4 == 3) {
-        const word3_t w = __builtin_amdgcn_raw_buffer_load_b96(from, off + 4 * (N - 3), 0, POLICY);
-        to[N - 3] = w[0];
-        to[N - 2] = w[1];
-        to[N - 1] = w[2];
-    }
-}
 
 // The queries of a wave's 16 rows: operands for codes, of a group those at low bits and those at high bits; for scale words, what makes 2^10 s of a group and m sum(q) of all; and what scores
 // are to be multiplied by.

@@ -3,13 +3,27 @@
 
 namespace fbq {
 
+// Block (h, y, z) of attend_many over codes.
+template <class TY, class MAKE, int NW>
+__device__ __forceinline__ void attend4_many(const AttendArgs &a, bool shared, int h, int y, int z, unsigned char *room)
+{
+    constexpr int DP = NW == 6 ? 256 : 32 * NW;
+    bool odd = false;
+    attend_many<TY, DP, Codes<MAKE, NW, DP>>(a, shared, h, y, z, room, &odd);
+    if constexpr (MAKE::kChecked) {
+        if (!odd) return;
+        asm volatile("" : "+s"(h), "+s"(y), "+s"(z) : : "memory");           // (what was worked out from them the first time takes no registers until the second)
+        attend_many<TY, DP, Codes<MakeBf16, NW, DP>>(a, shared, h, y, z, room);
+    }
+}
+
 template <class TY, class MAKE, int NW>
 __global__ __launch_bounds__(256, NW > 4 ? 1 : 2) void fbq_attend4_many_kernel(const AttendArgs a, const bool shared)
 {
     constexpr int DP = NW == 6 ? 256 : 32 * NW;
-    __shared__ __attribute__((aligned(1024))) unsigned char room[kManyRoom<DP>];
+    __shared__ __attribute__((aligned(1024))) unsigned char room[kMany4Room<DP>];
     const bool pieces = shared && a.shared_splits > 1;
-    attend_many<TY, DP, Codes<MAKE, NW, DP>>(a, shared, blockIdx.x, pieces ? blockIdx.y : blockIdx.y + blockIdx.z * kGridTiles, pieces ? blockIdx.z : 0, room);
+    attend4_many<TY, MAKE, NW>(a, shared, blockIdx.x, pieces ? blockIdx.y : blockIdx.y + blockIdx.z * kGridTiles, pieces ? blockIdx.z : 0, room);
 }
 
 template <class TY, class MAKE>
@@ -28,7 +42,7 @@ static hipError_t launch_many(const AttendArgs &a, bool shared, hipStream_t stre
 
 hipError_t launch_attend4_many(const AttendArgs &a, int type, bool shared, hipStream_t stream)
 {
-    return type == FBQ_F16_4BIT ? launch_many<TypeF16, MakeF16>(a, shared, stream) : launch_many<TypeBf16, MakeBf16>(a, shared, stream);
+    return type == FBQ_F16_4BIT ? launch_many<TypeF16, MakeF16>(a, shared, stream) : launch_many<TypeBf16, MakeHalf>(a, shared, stream);
 }
 
 }  // namespace fbq

@@ -57,12 +57,23 @@ inline dim3 many_grid(const AttendArgs &a, bool shared)
 // Bytes of LDS (aligned to 1024) of a block of it.
 template <int DP>
 constexpr int kManyRoom = 4 * kManyTile * (DP == 96 ? 256 : DP * 2);
+template <int DP>
+constexpr int kMany4Room = kManyRoom<DP> + 1024;              // (scale words, see Codes)
+
+template <class CODES, class TY>
+struct OperandOf { typedef typename CODES::Make::Operand type; };
+template <class TY>
+struct OperandOf<NoCodes, TY> { typedef TY type; };
 
 // Block (h, y, z) of the many-row work, four waves: head, tile (of the rows' own tokens: tile and piece), piece of the shared tokens.  FOUR: a Codes (fbq_attend_codes.h), where the cache is
 // in 4 bits and keys and values are made on their way to LDS; void: it is not.
+// `odd`: set where the operands that it makes are not made for what it has met, and its results mean nothing (for the whole block).
 template <class TY, int DP, class FOUR = void>
-__device__ __forceinline__ void attend_many(const AttendArgs &a, const bool shared, const int h, const int y, const int z, unsigned char *room)
+__device__ __forceinline__ void attend_many(const AttendArgs &a, const bool shared, const int h, const int y, const int z, unsigned char *room, bool *odd = nullptr)
 {
+    constexpr bool kFour = !std::is_void<FOUR>::value;
+    typedef typename std::conditional<kFour, FOUR, NoCodes>::type CODES;
+    typedef typename OperandOf<CODES, TY>::type OT;           // of the products
     constexpr int kPieces = DP == 96 ? 16 : DP / 8, kRowBytes = kPieces * 16, kTileBytes = kManyTile * kRowBytes;   // (96: rows as long as 128's, so that they fold over the banks)
     constexpr int kRowsACopy = 64 / kPieces, kCopies = 16 / kRowsACopy;       // a wave copies 16 keys and 16 values a step
     unsigned char (*const lds)[2][kTileBytes] = reinterpret_cast<unsigned char (*)[2][kTileBytes]>(room);   // keys, values; two steps each
@@ -177,6 +188,23 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, const bool shar
     word4_t qf[DP / 16];
 #pragma unroll
     for (int s = 0; s < DP / 16; ++s) qf[s] = query(t, grp, s);
+    float unit = a.scale;                                     // what scores are multiplied by
+    if constexpr (kFour) {
+        if constexpr (CODES::Make::kScaled) {
+            float most = 0;
+            const auto each_of = [](uint32_t word, auto f) { return TypeF16::pack(f(CODES::Make::Number::of(word & 0xffff)), f(CODES::Make::Number::of_upper(word))); };
+#pragma unroll
+            for (int s = 0; s < DP / 16; ++s)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) each_of(qf[s][e], [&](float x) { most = fmaxf(most, fabsf(x)); return x; });
+            const int up = __builtin_amdgcn_frexp_expf(larger_of_32(most)) - 15;
+            unit = ldexpf(unit, up);
+#pragma unroll
+            for (int s = 0; s < DP / 16; ++s)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) qf[s][e] = each_of(qf[s][e], [&](float x) { return ldexpf(x, -up); });
+        }
+    }
 
     // where this lane's pieces of a copy come from: rows 16 wave .. of a step
     int k_off[kCopies], v_off[kCopies];
@@ -190,16 +218,13 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, const bool shar
     const int entries = shared ? a.n_shared >> a.log_ps : a.max_pages;
     // 16 keys, or values, a wave
     PageList pages;
-    typename std::conditional<std::is_void<FOUR>::value, NoCodes, FOUR>::type codes;
-    codes.begin(a);
-    auto page_of = [&](int step) __attribute__((always_inline)) { return pages.at((key0 + step * kManyTile + 16 * wave) >> a.log_ps); };
-    // In 4 bits a copy is only asked for; it is made, and put down, a step later.
+    CODES codes;
+    if constexpr (kFour) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) codes.template begin<kPieces>(a, lds[0][i], lds[1][i], room + 4 * kTileBytes, wave);
+    }
+    auto next_page = [&](int step) __attribute__((always_inline)) { return pages.at((key0 + step * kManyTile + 16 * wave) >> a.log_ps); };
     auto copy = [&](int step, int page, bool values) __attribute__((always_inline)) {
-        if constexpr (!std::is_void<FOUR>::value) {
-            const int at = key0 + step * kManyTile + 16 * wave;
-            codes.ask(a, h, page, at, limit, values);
-            return;
-        }
         const int key = key0 + step * kManyTile + 16 * wave;
         const int valid = (unsigned)page < (unsigned)a.pages ? min(max(limit - key, 0), 16) : 0;
         const unsigned char *const at = a.kv + (valid ? page : 0) * a.page_bytes + (values ? a.page_bytes >> 1 : 0) + (((long)h << a.log_ps) + (key & ps1)) * D * 2;
@@ -209,10 +234,16 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, const bool shar
         for (int c = 0; c < kCopies; ++c) copy16_to_lds(from, values ? v_off[c] : k_off[c], 0, to + c * 1024);
     };
 
-    auto put = [&](int step, bool values) __attribute__((always_inline)) {
-        if constexpr (!std::is_void<FOUR>::value) {
-            if (values) codes.put_values(lds[1][step & 1], wave);
-            else codes.template put_keys<kPieces>(lds[0][step & 1], wave);
+    // In 4 bits codes are asked for, and made and put down a step later; behind the last step there are none, and nobody looks at what is put down for it.
+    auto ask = [&](int step, int page, bool values) __attribute__((always_inline)) {
+        if constexpr (kFour) codes.ask(a, h, page, key0 + step * kManyTile + 16 * wave, step < s1 ? limit : 0, values);
+    };
+    auto scalar_page = [&](int step) __attribute__((always_inline)) { return page_of(list, (key0 + step * kManyTile + 16 * wave) >> a.log_ps, entries); };
+    auto put = [&](int share, int step) __attribute__((always_inline)) {      // of the values of `step` and the keys of the one behind it
+        if constexpr (kFour) {
+            if (share % codes.kWords == 0) codes.spread(share == 0);
+            if (share < codes.kWords) codes.put_values(share, lds[1][step & 1]);
+            else codes.put_keys(share - codes.kWords, lds[0][(step + 1) & 1]);
         }
     };
     // reads: a key's piece s of DP / 16 pairs, and a value's column block dblk of 32
@@ -231,7 +262,7 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, const bool shar
     // A step is a row of slots with one matrix product each, first the next step's scores (kScores products, the two halves of its keys in turn), then this step's P V (kValues,
     // 16 keys at a time).  Every slot asks LDS for the operand of the one kAhead slots on, and carries a share of the step's other work, which the compiler is kept from
     // moving: exponentials of pair k of probabilities (in time for its product), and towards the end the maximum of the next step's scores.
-    constexpr int kScores = DP / 8, kValues = DP / 8, kAhead = 4, kLate = 12;
+    constexpr int kScores = DP / 8, kValues = DP / 8, kAhead = kFour ? 2 : 4 /* (4 bits: registers for more run out) */, kLate = 12;
     word4_t ring[kAhead];
     auto fetch = [&](int i, int step) __attribute__((always_inline)) {        // operand of slot i of the step `step`
         if (i < kScores) {
@@ -239,7 +270,7 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, const bool shar
             ring[i % kAhead] = *reinterpret_cast<const word4_t *>(lds[0][(step + 1) & 1] + k_at + ((k_piece ^ (2 * x)) << 4) + 32 * half * kRowBytes);
         } else if (i < kScores + kValues) {
             const int j = (i - kScores) / (DP / 32), d = (i - kScores) % (DP / 32);
-            if constexpr (!std::is_void<FOUR>::value) {
+            if constexpr (kFour) {
                 ring[i % kAhead] = *reinterpret_cast<const word4_t *>(lds[1][step & 1] + turned_at(32 * d + col, 2 * j + grp));
                 return;
             }
@@ -251,28 +282,33 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, const bool shar
     int page = 0;                                             // of the keys copied last
     float top = -INFINITY;                                    // of this lane's scores of the step that is next
     auto work = [&](float16_t (&z)[2], float16_t (&ahead)[2], int s) __attribute__((always_inline)) {
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");   // what was asked for a step ago is there, what a step ago was read is free
-        if constexpr (std::is_void<FOUR>::value) {
+        if constexpr (kFour) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");   // what was asked for a step ago is there, what a step ago was read is free
+        if constexpr (!kFour) {
             if (s + 1 < s1) copy(s + 1, page, true);
             if (s + 2 < s1) {
-                page = page_of(s + 2);
+                page = next_page(s + 2);
                 copy(s + 2, page, false);
             }
-        } else {
-            if (s + 1 < s1) put(s + 1, true);
-            if (s + 2 < s1) {
-                put(s + 2, false);
-                copy(s + 2, page, true);
-            }
-            if (s + 3 < s1) {
-                page = page_of(s + 3);
-                copy(s + 3, page, false);
-            }
+        }
+        int next = 0, behind = 0;                             // 4 bits: pages of the values and keys that are asked for at this step's end
+        if constexpr (kFour) {
+            next = scalar_page(s + 2);
+            behind = scalar_page(s + 3);
         }
         const int key = key0 + s * kManyTile;
-        if (key >= most) return;
+        if (key >= most) {
+            if constexpr (kFour) {
+#pragma unroll
+                for (int x = 0; x < 2 * codes.kWords; ++x) put(x, s + 1);
+                ask(s + 2, next, true);
+                ask(s + 3, behind, false);
+            }
+            return;
+        }
         // 256 features: all addresses of a step in registers across steps would push others out to memory, whose loads wait for the copies under way
         if constexpr (DP == 256) asm volatile("" : "+v"(k_at), "+v"(k_piece), "+v"(v_at), "+v"(v_piece));
+        if constexpr (kFour) codes.step();
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) fetch(i, s);         // (past the last step: of whatever lies there, its scores are not used)
         if (key + kManyTile > least) {
@@ -285,7 +321,7 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, const bool shar
                     top = fmaxf(top, z[half][y]);
                 }
         }
-        const float high = larger_of_32(top) * a.scale;
+        const float high = larger_of_32(top) * unit;
         if (__ballot(high > m + kSlack)) {
             const float to = fmaxf(high, m), by = __builtin_amdgcn_exp2f(m - to);
             l *= by;
@@ -296,9 +332,9 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, const bool shar
         word4_t p[4];
         auto pair = [&](int k) __attribute__((always_inline)) {
             const int half = k >> 3, y = 2 * (k & 7);
-            const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[half][y], a.scale, -m)), p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[half][y + 1], a.scale, -m));
+            const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[half][y], unit, -m)), p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[half][y + 1], unit, -m));
             l += p0 + p1;
-            p[k >> 2][k & 3] = TY::pack(p0, p1);
+            p[k >> 2][k & 3] = OT::pack(p0, p1);
         };
 #pragma unroll
         for (int half = 0; half < 2; ++half)
@@ -309,13 +345,13 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, const bool shar
             __builtin_amdgcn_sched_barrier(0);
             const word4_t f = ring[i % kAhead];
             if constexpr (i < kScores) {
-                ahead[i & 1] = TY::mfma(f, qf[i >> 1], ahead[i & 1]);
+                ahead[i & 1] = OT::mfma(f, qf[i >> 1], ahead[i & 1]);
 #pragma unroll
                 for (int k = 0; k < kLate; ++k)
                     if (k * kScores / kLate == i) pair(k);
             } else {
                 constexpr int x = i - kScores, j = x / (DP / 32), d = x % (DP / 32);
-                o[d] = TY::mfma(f, p[j], o[d]);
+                o[d] = OT::mfma(f, p[j], o[d]);
 #pragma unroll
                 for (int k = kLate; k < 16; ++k)
                     if ((k - kLate) * (kValues / 2) / (16 - kLate) == x) pair(k);
@@ -324,31 +360,44 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, const bool shar
                     if (kValues / 2 + y * (kValues / 2) / 16 == x) top = y == 0 ? fmaxf(ahead[0][0], ahead[1][0]) : fmaxf(fmaxf(top, ahead[0][y]), ahead[1][y]);
             }
             fetch(i + kAhead, s);
+            // shares of codes in the second half of the step: what was asked for in the one before has had three quarters of one to come
+            if constexpr (kFour) {
+                constexpr int kShares = 2 * FOUR::kWords, kHalf = (kScores + kValues) / 2;
+#pragma unroll
+                for (int k = 0; k < kShares; ++k)
+                    if (kHalf + k * kHalf / kShares == i) {
+                        put(k, s + 1);
+                        if (k == FOUR::kWords - 1) ask(s + 2, next, true);
+                    }
+            }
         });
         __builtin_amdgcn_sched_barrier(0);
+        if constexpr (kFour) ask(s + 3, behind, false);
     };
     // Keys are a step ahead of values: while step s is worked on, keys s + 1 and values s are read, keys s + 2 and values s + 1 copied.
     float16_t z0[2], z1[2];
     if (s0 < s1) {
-        pages.begin(list, entries, (key0 + s0 * kManyTile + 16 * wave) >> a.log_ps);
-        page = page_of(s0);
-        copy(s0, page, false);
-        put(s0, false);
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        copy(s0, page, true);
-        if (s0 + 1 < s1) {
-            page = page_of(s0 + 1);
-            copy(s0 + 1, page, false);
-        }
-        if constexpr (!std::is_void<FOUR>::value) {
-            put(s0, true);
+        if constexpr (kFour) {
+            const int page0 = scalar_page(s0), page1 = scalar_page(s0 + 1);
+            ask(s0, page0, false);
+#pragma unroll
+            for (int x = 0; x < codes.kWords; ++x) put(codes.kWords + x, s0 - 1);
+            ask(s0, page0, true);
+            ask(s0 + 1, page1, false);
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+#pragma unroll
+            for (int x = 0; x < 2 * codes.kWords; ++x) put(x, s0);
+            ask(s0 + 1, page1, true);
+            ask(s0 + 2, scalar_page(s0 + 2), false);
+        } else {
+            pages.begin(list, entries, (key0 + s0 * kManyTile + 16 * wave) >> a.log_ps);
+            page = next_page(s0);
+            copy(s0, page, false);
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            copy(s0, page, true);
             if (s0 + 1 < s1) {
-                put(s0 + 1, false);
-                copy(s0 + 1, page, true);
-            }
-            if (s0 + 2 < s1) {
-                page = page_of(s0 + 2);
-                copy(s0 + 2, page, false);
+                page = next_page(s0 + 1);
+                copy(s0 + 1, page, false);
             }
         }
 #pragma unroll
@@ -358,7 +407,7 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, const bool shar
 #pragma unroll
         for (int i = 0; i < kScores; ++i) {
             fetch(i, s0 - 1);
-            z0[i & 1] = TY::mfma(ring[i % kAhead], qf[i >> 1], z0[i & 1]);
+            z0[i & 1] = OT::mfma(ring[i % kAhead], qf[i >> 1], z0[i & 1]);
         }
 #pragma unroll
         for (int y = 0; y < 16; ++y) top = fmaxf(fmaxf(top, z0[0][y]), z0[1][y]);
@@ -400,8 +449,18 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, const bool shar
     // keys, the wave does its piece again, by itself and from memory: rows that see equally many of a step's keys together, other values as zeros, the others' sums left as they are.
     // Slow (a prompt of 2048 with a NaN among its values 430 us, else 52), but only then: otherwise the look at the sums is all.  (Results are written before, and once more: so the
     // loop's registers are as they would be without.  256 features, a prompt of 8192: 1448 us, 1428 without.)
+    if constexpr (kFour) {
+        if (CODES::Make::kChecked) {
+            int *const flags = reinterpret_cast<int *>(room);
+            __syncthreads();                                  // (tiles are read no more)
+            if (lane == 0) flags[wave] = codes.met != 0;
+            __syncthreads();
+            *odd = uniform(flags[0] | flags[1] | flags[2] | flags[3]) != 0;
+            __syncthreads();
+        }
+    }
     bool again = false;
-    if (std::is_void<FOUR>::value && least < min(limit, key0 + s1 * kManyTile)) {
+    if (!kFour && least < min(limit, key0 + s1 * kManyTile)) {
         float odd = 0;                                        // then not zero
 #pragma unroll
         for (int x = 0; x < DP / 32; ++x)
@@ -410,7 +469,7 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, const bool shar
         again = __ballot(t >= 0 && odd != 0) != 0;
     }
     write(o, m, l);
-    if (!again || !std::is_void<FOUR>::value) return;         // (a cache in 4 bits has no such values)
+    if (!again || kFour) return;         // (a cache in 4 bits has no such values)
     float16_t sums[DP / 32];
 #pragma unroll
     for (int x = 0; x < DP / 32; ++x)

@@ -234,3 +234,25 @@ def test_a_captured_call_follows_lengths_and_tables():
         got = out.clone()
         assert torch.equal(got, step(caches[1])), i
     assert caches[0].lengths.tolist() == caches[1].lengths.tolist() == [45, 21, 34]
+
+
+@pytest.mark.parametrize("k_size,v_size", [(1e-6, 1.0), (1.0, 1e-6), (1e5, 1.0), (1.0, 1e5), (1e-30, 1e30)])
+def test_prompts_over_scales_that_fp16_operands_are_not_made_for(k_size, v_size):
+    """bf16: a part of the rows has such keys or values, another has ordinary ones; constant groups and zeros among them."""
+    import paper_2501_16385_amd as fbq
+    from cache4_cases import unpack
+    from cache_cases import make_cache
+    D, page, counts = 128, 16, [60, 30, 50]
+    x, table, n, refs = make_cache([200, 77, 130], 2, D, page, BF16, seed=3)
+    for i, size in ((0, k_size), (1, v_size)):
+        x[0, table[0].long().clamp(min=0)[:13], i] = (x[0, table[0].long().clamp(min=0)[:13], i].double() * size).to(BF16)
+        x[0, table[2, :4].long(), i, :, :8] = 0.0 if size < 1 else 3.0
+    pool = pack(x, page)
+    values = unpack(pool, BF16, D)
+    q = torch.randn(sum(counts), 4, D, generator=torch.Generator().manual_seed(9)).to(BF16)
+    q[:60] = (q[:60].double() / k_size).to(BF16)
+    want, _, bound, _ = attention4_64(values, table, n, 0, q, counts, D ** -0.5, False)
+    bound = bound - 2.0 ** -24 + 2.0 ** -24 * min(1.0, v_size)
+    cache = to_cache4(fbq, pool, table, n, refs, BF16, D)
+    got = fbq.attention(cache, 0, q.cuda(), q_start=starts(counts).cuda(), max_q=max(counts)).cpu().double()
+    assert ((got - want).abs() <= bound).all()
