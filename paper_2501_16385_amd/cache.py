@@ -326,7 +326,7 @@ def attention_weights(cache: Cache, layer: int, q, lse, weights, q_start=None, m
     """fbq_attention_weights, after attention() of the same q, q_start, max_q and scale, which wrote lse: what each key was attended to, for every key/value head over its queries -> out.
 
     weights: float32 [rows, kv_heads, width], what earlier calls added up (times decay; the row's new tokens begin at 0), or None; out: the same shape, weights itself by default.
-    Tokens from width on are not counted; places without a token are left alone.
+    Tokens from width on are not counted; places without a token, and rows without queries, are left alone.
     """
     if out is None:
         out = weights

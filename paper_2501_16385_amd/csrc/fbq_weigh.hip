@@ -1,15 +1,17 @@
 // fbq_attention_weights: what attention's softmax gave each key, added up over the queries and heads of a key/value head.
 //
-// The softmax's sums are known (lse), so a key's weights are exp(scale q . k - lse) and nothing runs along the keys: a wave keeps 64 keys as operands of the matrix cores and goes through the query
-// rows 16 at a time, S^T = K Q^T in v_mfma 16x16x32 as in fbq_attend_few.h, adds the exponentials up in the lane and over its 16 columns at the end.  Bound by reading the keys where rows are few
-// (half of what attention reads), by the exponentials and the products where they are many.
-// A block's four waves have 64 keys each, or, where a row of the table has many query rows, the same 64 keys and a fourth of the query tiles each, added up in LDS in a fixed order.
-// Codes of 4 bits are small whole numbers of the queries' type, exactly; a group's scale and lowest value come in behind the product, in 32 bits, with the sums of q over the group.
+// The softmax's sums are known (lse), so a key's weights are exp(scale q . k - lse) and nothing runs along the keys.  S^T = K Q^T in v_mfma 16x16x32 as in fbq_attend_few.h; the exponentials are
+// added up in the lane and over its 16 columns at the end.
+//   few   up to 16 query rows of a key/value head (fbq_weigh_few_kernel): bound by reading the keys, half of what attention reads.  The waves of the grid share the steps of all rows and heads
+//         as attention's do (FewLine), a step's keys asked for a step ahead; there is nothing to join, since a key's sum is a wave's own.
+//   many  (fbq_weigh_many_kernel) bound by the exponentials and the products.  A wave keeps 64 keys as operands and goes through the query rows 16 at a time.  A block's four waves have 64 keys
+//         each, or, where a row of the table has many query rows, the same 64 keys and a fourth of the query tiles each, added up in LDS in a fixed order.
+// Codes of 4 bits: few, as in fbq_attend4_few.h; many, as small whole numbers of the queries' type, exactly, and scales come in behind the product, in 32 bits: the matrix cores spread them over
+// the lanes once for 64 keys, and make m sum(q) of the sums of q over a group in parts of 16 bits.
 #include <algorithm>
 #include <cmath>
 
-#include "fbq_attend.h"
-#include "fbq_cache4.h"
+#include "fbq_attend4_few.h"
 #include "fbq_internal.h"
 #include "fbq_lds_copy.h"
 
@@ -25,7 +27,7 @@ struct WeighArgs {
     float *out;
     int width, parts;                    // blocks of a row and head
     float decay;
-    bool together;                       // a block's waves have the same keys
+    bool few, together;                  // few: the few-row kernel; together: a block's waves have the same keys
 };
 
 // Eight codes of a word as numbers of the type, features in their order.
@@ -62,25 +64,168 @@ __device__ __forceinline__ float row_sum(float x)
     return x;
 }
 
+// A step's keys, 16 a part, on their way to a wave: in 16 bits operands, in 4 bits codes and scale words; and what the sums begin with.
+template <bool FOUR, int NW>
+struct WeighStep {
+    word4_t k[kFew4Parts][FOUR ? 1 : NW];
+    uint32_t codes[kFew4Parts][FOUR ? NW : 1], scales[kFew4Parts];
+    float before;
+};
+
 template <class TY, bool FOUR, int NW>
-__global__ __launch_bounds__(64 * kWeighWaves, NW > 4 ? 1 : 2) void fbq_weigh_kernel(const WeighArgs w)
+__global__ __launch_bounds__(64 * kFewWaves, 2) void fbq_weigh_few_kernel(const WeighArgs w)
 {
-    constexpr int DS = 32 * NW, G = FOUR ? groups4(DS) : 1, kTiles = kWeighKeys / 16;
+    constexpr int DS = 32 * NW, G = groups4(DS), kParts = kFew4Parts;
+    typedef typename TY::Number NT;
+    const AttendArgs &a = w.a;
+    const int lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4, D = a.D, ps1 = (1 << a.log_ps) - 1;
+    const int worker = uniform(blockIdx.x * kFewWaves + (threadIdx.x >> 6)), member = col % a.group;
+    const long head_bytes = (a.page_bytes >> 1) / a.kv_heads;
+    const int mine = 16 * (col >> 2) + 4 * grp + (col & 3);   // this lane's key of a step, of those lanes that have one
+    const bool has = col < 4 * kParts;
+
+    Piece4<NW> cur, behind;
+    float lse = 0, lse_behind = 0;
+    FewLine line;
+    if (!line.first(a, blockIdx.x, worker, cur)) return;
+    auto prepare = [&](Piece4<NW> &x, float &l) __attribute__((always_inline)) {
+        few_sight(a, x, col);
+#pragma unroll
+        for (int part = 0; part < kParts; ++part) x.pages[part] = page_of(few_pages(a, x), (x.key0 + 16 * part) >> a.log_ps, few_page_count(a, x));
+        const int head = x.h * a.group + member;
+        l = x.t >= 0 ? a.lse[(long)x.t * a.heads + head] : 0;
+#pragma unroll
+        for (int y = 0; y < NW; ++y) {
+            const int d = 32 * y + 8 * grp;
+            x.q[y] = word4_t{0, 0, 0, 0};
+            if (x.t >= 0 && d < D) x.q[y] = *reinterpret_cast<const word4_t *>(a.q + x.t * a.q_stride + head * D + d);
+        }
+    };
+    int k_off[FOUR ? 1 : NW];
+    if constexpr (!FOUR) {
+#pragma unroll
+        for (int y = 0; y < NW; ++y) k_off[y] = 32 * y + 8 * grp < D ? (col * D + 32 * y + 8 * grp) * 2 : kNowhere;
+    }
+    const int scale_off = grp < G ? (col * G + grp) * 4 : kNowhere;
+    int ask_key = 0, ask_end = 0, ask_h = 0, ask_b = 0, ask_old = 0, ask_pages[kParts];
+    auto aim = [&](const Piece4<NW> &x, bool there) __attribute__((always_inline)) {
+        ask_key = x.key0;
+        ask_end = there ? min(x.limit, x.key0 + x.n * kFewTile) : 0;
+        ask_h = x.h;
+        ask_b = x.b;
+        ask_old = w.weights ? min(min(ask_end, w.width), x.limit - queries_of(a, x.b).y) : 0;        // where tokens that are there begin to be new
+#pragma unroll
+        for (int part = 0; part < kParts; ++part) ask_pages[part] = x.pages[part];
+    };
+    auto load = [&](WeighStep<FOUR, NW> &to) __attribute__((always_inline)) {     // always as many loads: see attend4_few
+#pragma unroll
+        for (int part = 0; part < kParts; ++part) {
+            const int key = ask_key + 16 * part, id = ask_pages[part];
+            const int valid = (unsigned)id < (unsigned)a.pages ? min(max(ask_end - key, 0), 16) : 0;
+            const unsigned char *const keys = a.kv + (valid ? id : 0) * a.page_bytes + ask_h * head_bytes;
+            if constexpr (FOUR) {
+                load_words<NW, kOnce>(to.codes[part], buffer_of(keys + codes_at4(key & ps1, DS), valid ? 8 * DS : 0), (col * 4 + grp) * NW * 4);
+                to.scales[part] = __builtin_amdgcn_raw_buffer_load_b32(buffer_of(keys + scales_at4(a.log_ps, key & ps1, DS), valid * 4 * G), scale_off, 0, 0);
+            } else {
+                const __amdgpu_buffer_rsrc_t from = buffer_of(keys + (long)(key & ps1) * D * 2, valid * D * 2);
+#pragma unroll
+                for (int y = 0; y < NW; ++y) to.k[part][y] = __builtin_amdgcn_raw_buffer_load_b128(from, k_off[y], 0, kOnce);
+            }
+        }
+        const float *const row = w.weights + ((long)ask_b * a.kv_heads + ask_h) * w.width + ask_key;
+        to.before = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(buffer_of(w.weights ? row : w.out, max(min(ask_old - ask_key, kFewTile), 0) * 4), has ? mine * 4 : kNowhere, 0, 0));
+        ask_key += kFewTile;
+        const int32_t *const list = a.table + (long)ask_b * a.max_pages;
+#pragma unroll
+        for (int part = 0; part < kParts; ++part) ask_pages[part] = page_of(list, (ask_key + 16 * part) >> a.log_ps, a.max_pages);
+    };
+
+    Queries4<TY, NT, NW> codes_q;
+    word4_t q[FOUR ? 1 : NW];
+    float unit = a.scale, less = 0;
+    auto begin = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int y = 0; y < NW; ++y) cur.q[y] = (cur.q[y] & a.q_and) ^ a.q_xor;
+        if constexpr (FOUR) {
+            codes_q.of(cur.q, a.scale);
+            unit = codes_q.unit;
+        } else {
+#pragma unroll
+            for (int y = 0; y < NW; ++y) q[y] = cur.q[y];
+        }
+        less = lse * 1.4426950408889634f;
+    };
+    auto compute = [&](const WeighStep<FOUR, NW> &x, int s) __attribute__((always_inline)) {
+        const int key = cur.key0 + s * kFewTile, sees = cur.sees - key - 4 * grp;
+        float sum = 0;
+#pragma unroll
+        for (int part = 0; part < kParts; ++part) {
+            float4_t z{0, 0, 0, 0};
+            if constexpr (FOUR) {
+                z = scores4<TY, NT, NW>(x.codes[part], x.scales[part], codes_q);
+            } else {
+#pragma unroll
+                for (int y = 0; y < NW; ++y) z = TY::mfma(x.k[part][y], q[y], z);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i], unit, -less));
+                const float all = row_sum(16 * part + i < sees ? p : 0.0f);
+                sum = col == 4 * part + i ? all : sum;
+            }
+        }
+        if (has && key + mine < min(min(cur.limit, cur.key0 + cur.n * kFewTile), w.width))
+            w.out[((long)cur.b * a.kv_heads + cur.h) * w.width + key + mine] = __builtin_fmaf(x.before, w.decay, sum);
+    };
+
+    prepare(cur, lse);
+    behind = cur;                                             // (where there is none, something that is one)
+    bool more = line.follow(a, cur, behind);
+    if (more) prepare(behind, lse_behind);
+    WeighStep<FOUR, NW> x0, x1;
+    aim(cur, true);
+    load(x0);
+    begin();
+    int s = 0;
+    auto turn = [&](const WeighStep<FOUR, NW> &now, WeighStep<FOUR, NW> &next) __attribute__((always_inline)) {
+        if (s + 1 == cur.n) aim(behind, more);
+        load(next);
+        compute(now, s);
+        if (++s < cur.n) return false;
+        if (!more) return true;
+        cur = behind;
+        lse = lse_behind;
+        s = 0;
+        more = line.follow(a, cur, behind);
+        if (more) prepare(behind, lse_behind);
+        begin();
+        return false;
+    };
+    while (!turn(x0, x1) && !turn(x1, x0)) {}
+}
+
+template <class TY, bool FOUR, int NW>
+__global__ __launch_bounds__(64 * kWeighWaves, NW > 4 ? 1 : 2) void fbq_weigh_many_kernel(const WeighArgs w)
+{
+    constexpr int DS = 32 * NW, G = groups4(DS), kTiles = kWeighKeys / 16;
     typedef typename TY::Number NT;
     __shared__ float sums[kWeighWaves][kWeighKeys];
     const AttendArgs &a = w.a;
     const int lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4, wave = uniform(threadIdx.x >> 6);
     const int h = blockIdx.x % a.kv_heads, b = blockIdx.x / a.kv_heads, D = a.D, ps1 = (1 << a.log_ps) - 1;
     const int2 of = queries_of(a, b);
+    if (of.y == 0) return;                                    // (no queries: left as it is)
     const int q0 = uniform(of.x), nq = uniform(of.y), tokens = uniform(row_tokens(a, b)), limit = min(tokens, w.width);
     const long head_bytes = (a.page_bytes >> 1) / a.kv_heads, at = ((long)b * a.kv_heads + h) * w.width;
     const int32_t *const list = a.table + (long)b * a.max_pages;
+    const float unit = (a.q_xor ? -a.scale : a.scale) * (FOUR ? 128.0f : 1.0f);          // (a sign is the scale's here)
     const int a_block = w.together ? kWeighKeys : kWeighWaves * kWeighKeys, stride = w.parts * a_block;
     const int rows = nq * a.group, tiles = (rows + 15) / 16;
 
     for (int base = blockIdx.y * a_block; base < limit; base += stride) {
         const int key0 = base + (w.together ? 0 : wave * kWeighKeys);
-        word4_t k[kTiles][NW], scales[kTiles][FOUR ? G : 1];
+        word4_t k[kTiles][NW];
+        uint32_t words[kTiles];                               // 4 bits: scale word of key l % 16, group l / 16
 #pragma unroll
         for (int t = 0; t < kTiles; ++t) {
             const int key = key0 + 16 * t;
@@ -90,11 +235,11 @@ __global__ __launch_bounds__(64 * kWeighWaves, NW > 4 ? 1 : 2) void fbq_weigh_ke
             const unsigned char *const head = a.kv + (valid ? id : 0) * a.page_bytes + h * head_bytes;
             if constexpr (FOUR) {
                 const __amdgpu_buffer_rsrc_t codes = buffer_of(head + codes_at4(key & ps1, DS), valid ? 8 * DS : 0);
-                const __amdgpu_buffer_rsrc_t words = buffer_of(head + scales_at4(a.log_ps, key & ps1, DS), valid * 4 * G);
+                uint32_t of[NW];
+                load_words<NW, 0>(of, codes, (col * 4 + grp) * NW * 4);
 #pragma unroll
-                for (int x = 0; x < NW; ++x) k[t][x][0] = __builtin_amdgcn_raw_buffer_load_b32(codes, ((col * 4 + grp) * NW + x) * 4, 0, 0);
-#pragma unroll
-                for (int y = 0; y < G; ++y) scales[t][y] = __builtin_amdgcn_raw_buffer_load_b128(words, grp * 16 * G + 16 * y, 0, 0);
+                for (int x = 0; x < NW; ++x) k[t][x][0] = of[x];
+                words[t] = __builtin_amdgcn_raw_buffer_load_b32(buffer_of(head + scales_at4(a.log_ps, key & ps1, DS), valid * 4 * G), grp < G ? (col * G + grp) * 4 : kNowhere, 0, 0);
             } else {
                 const __amdgpu_buffer_rsrc_t from = buffer_of(head + (long)(key & ps1) * D * 2, valid * D * 2);
 #pragma unroll
@@ -107,61 +252,112 @@ __global__ __launch_bounds__(64 * kWeighWaves, NW > 4 ? 1 : 2) void fbq_weigh_ke
 #pragma unroll
                 for (int x = 0; x < NW; ++x) k[t][x] = TY::codes(k[t][x][0]);
         }
+        float4_t scales[kTiles][FOUR ? G : 1];                // 2^-7 of the lane's four keys' (so that sums of q, times as much, are in fp16's range)
+        if constexpr (FOUR) {
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                for (int y = 0; y < G; ++y) scales[t][y] = scales_of<TY>(words[t], word2_t{grp == y ? NT::bits(0x1p-7f) << 16 : 0u, 0u});
+        }
         float4_t sum[kTiles];
 #pragma unroll
         for (int t = 0; t < kTiles; ++t) sum[t] = float4_t{0, 0, 0, 0};
 
         struct Queries { word4_t q[NW]; float lse; int sees; };
+        // (rows past the last one are that one, and see nothing; features past the last are zeros: only words from kSure on can have some)
+        constexpr int kSure = NW == 2 ? 0 : NW == 8 ? 6 : NW == 6 ? 4 : NW - 1;
         auto ask = [&](Queries &x, int tile) __attribute__((always_inline)) {
-            const int r = tile * 16 + col, i = r / a.group, head = h * a.group + r - i * a.group, t = q0 + i;
-            const bool there = r < rows;
-            x.sees = there ? tokens - nq + i + 1 : 0;
-            x.lse = there ? a.lse[(long)t * a.heads + head] : 0;
+            const int r = tile * 16 + col, row = min(r, rows - 1), i = row / a.group, head = h * a.group + row - i * a.group, t = q0 + i;
+            x.sees = r < rows ? tokens - nq + i + 1 : 0;
+            x.lse = a.lse[(long)t * a.heads + head];
+            const uint16_t *const from = a.q + t * a.q_stride + head * D;
 #pragma unroll
             for (int y = 0; y < NW; ++y) {
                 const int d = 32 * y + 8 * grp;
-                x.q[y] = word4_t{0, 0, 0, 0};
-                if (there && d < D) x.q[y] = *reinterpret_cast<const word4_t *>(a.q + t * a.q_stride + head * D + d);
+                x.q[y] = *reinterpret_cast<const word4_t *>(from + (y < kSure || d < D ? d : 0));
             }
         };
         auto add = [&](Queries &x) __attribute__((always_inline)) {
-            float group_sum[G];
 #pragma unroll
-            for (int y = 0; y < NW; ++y) x.q[y] = (x.q[y] & a.q_and) ^ a.q_xor;
+            for (int y = kSure; y < NW; ++y)
+                if (32 * y + 8 * grp >= D) x.q[y] = word4_t{0, 0, 0, 0};
+            if (a.q_and == 0) {                               // (scale 0)
+                asm volatile("");
+#pragma unroll
+                for (int y = 0; y < NW; ++y) x.q[y] = word4_t{0, 0, 0, 0};
+            }
+            float4_t z[kTiles];
             if constexpr (FOUR) {
+                // 2^-7 of the sum of q over group l / 16, and 2^12 of what is left of it in two parts
                 const word4_t one{TY::kOne, TY::kOne, TY::kOne, TY::kOne};
+                word2_t high{0, 0}, rest{0, 0};
+                float4_t sums[G];
+                float sum = 0;
 #pragma unroll
                 for (int y = 0; y < G; ++y) {
-                    float4_t s = TY::mfma(one, x.q[2 * y], float4_t{0, 0, 0, 0});
-                    if (2 * y + 1 < NW) s = TY::mfma(one, x.q[std::min(2 * y + 1, NW - 1)], s);
-                    group_sum[y] = s[0];
+                    sums[y] = TY::mfma(one, x.q[2 * y], float4_t{0, 0, 0, 0});
+                    if (2 * y + 1 < NW) sums[y] = TY::mfma(one, x.q[std::min(2 * y + 1, NW - 1)], sums[y]);
                 }
+                // two tiles' products at a time, and nothing of the next two before their sums (or the compiler puts each product before its use, and waits for it)
+#pragma unroll
+                for (int t0 = 0; t0 < kTiles; t0 += 2) {
+                    float4_t c[2][G], lower[2];
+#pragma unroll
+                    for (int t = 0; t < 2; ++t)
+#pragma unroll
+                        for (int y = 0; y < G; ++y) {
+                            c[t][y] = TY::mfma(k[t0 + t][2 * y], x.q[2 * y], float4_t{0, 0, 0, 0});
+                            if (2 * y + 1 < NW) c[t][y] = TY::mfma(k[t0 + t][std::min(2 * y + 1, NW - 1)], x.q[std::min(2 * y + 1, NW - 1)], c[t][y]);
+                        }
+                    if (t0 == 0) {
+#pragma unroll
+                        for (int y = 0; y < G; ++y) sum = grp == y ? sums[y][0] * 0x1p-7f : sum;
+                        high[0] = NT::bits(sum);
+                        const float left = (sum - NT::of(high[0])) * 0x1p12f;
+                        rest[0] = NT::bits(left);
+                        rest[1] = NT::bits(left - NT::of(rest[0]));
+                    }
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        z[t0 + t] = TY::mfma(word2_t{words[t0 + t], 0u}, high, float4_t{0, 0, 0, 0});
+                        lower[t] = TY::mfma(word2_t{words[t0 + t], words[t0 + t]}, rest, float4_t{0, 0, 0, 0});
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int t = 0; t < 2; ++t)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+#pragma unroll
+                            for (int y = 0; y < G; ++y) z[t0 + t][i] = __builtin_fmaf(scales[t0 + t][y][i], c[t][y][i], z[t0 + t][i]);
+                            z[t0 + t][i] = __builtin_fmaf(lower[t][i], 0x1p-12f, z[t0 + t][i]);
+                        }
+                    if (t0 + 2 < kTiles) __builtin_amdgcn_sched_barrier(0);
+                }
+            } else {
+#pragma unroll
+                for (int t = 0; t < kTiles; ++t) {
+                    z[t] = float4_t{0, 0, 0, 0};
+#pragma unroll
+                    for (int y = 0; y < NW; ++y) z[t] = TY::mfma(k[t][y], x.q[y], z[t]);
+                }
+                __builtin_amdgcn_sched_barrier(0);
             }
             const float less = x.lse * 1.4426950408889634f;
 #pragma unroll
-            for (int t = 0; t < kTiles; ++t) {
-                float4_t z{0, 0, 0, 0};
-                if constexpr (FOUR) {
+            for (int t = 0; t < kTiles; ++t)
 #pragma unroll
-                    for (int y = 0; y < G; ++y) {
-                        float4_t c = TY::mfma(k[t][2 * y], x.q[2 * y], float4_t{0, 0, 0, 0});
-                        if (2 * y + 1 < NW) c = TY::mfma(k[t][std::min(2 * y + 1, NW - 1)], x.q[std::min(2 * y + 1, NW - 1)], c);
+                for (int i = 0; i < 4; ++i) z[t][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[t][i], unit, -less));
+            if (__ballot(x.sees < key0 + kWeighKeys)) {       // some row does not see all of the keys
+                const int sees = x.sees - key0 - 4 * grp;
+                asm volatile("");
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const uint32_t word = scales[t][(i * G + y) / 4][(i * G + y) % 4];
-                            z[i] = __builtin_fmaf(NT::of_upper(word), c[i], __builtin_fmaf(NT::of(word & 0xffff), group_sum[y], z[i]));
-                        }
-                    }
-                } else {
+                for (int t = 0; t < kTiles; ++t)
 #pragma unroll
-                    for (int y = 0; y < NW; ++y) z = TY::mfma(k[t][y], x.q[y], z);
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i], a.scale, -less));
-                    sum[t][i] += key0 + 16 * t + 4 * grp + i < x.sees ? p : 0.0f;
-                }
+                    for (int i = 0; i < 4; ++i)
+                        if (16 * t + i >= sees) z[t][i] = 0;
             }
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) sum[t] += z[t];
         };
         // the first tile with a row that sees the first key; those before see none of these
         const int first = uniform(max(0, (int)((long)max(key0 - (tokens - nq), 0) * a.group / 16)));
@@ -171,11 +367,11 @@ __global__ __launch_bounds__(64 * kWeighWaves, NW > 4 ? 1 : 2) void fbq_weigh_ke
             Queries x0, x1;
             ask(x0, tile);
             while (true) {
-                if (tile + step < tiles) ask(x1, tile + step);
+                ask(x1, min(tile + step, tiles - 1));         // (always as many loads: then the waits for those before know how many came behind)
                 add(x0);
                 tile += step;
                 if (tile >= tiles) break;
-                if (tile + step < tiles) ask(x0, tile + step);
+                ask(x0, min(tile + step, tiles - 1));
                 add(x1);
                 tile += step;
                 if (tile >= tiles) break;
@@ -205,16 +401,22 @@ __global__ __launch_bounds__(64 * kWeighWaves, NW > 4 ? 1 : 2) void fbq_weigh_ke
     }
 }
 
+template <class TY, bool FOUR, int NW>
+static void launch_weigh(const WeighArgs &w, hipStream_t stream)
+{
+    if (w.few) hipLaunchKernelGGL((fbq_weigh_few_kernel<TY, FOUR, NW>), dim3(w.a.workers / kFewWaves), dim3(64 * kFewWaves), 0, stream, w);
+    else hipLaunchKernelGGL((fbq_weigh_many_kernel<TY, FOUR, NW>), dim3(w.a.kv_heads * w.a.rows, w.parts), dim3(64 * kWeighWaves), 0, stream, w);
+}
+
 template <class TY, bool FOUR>
 static hipError_t launch_weigh(const WeighArgs &w, hipStream_t stream)
 {
-    const dim3 grid(w.a.kv_heads * w.a.rows, w.parts), block(64 * kWeighWaves);
     switch (features4(w.a.D) / 32) {
-    case 2: hipLaunchKernelGGL((fbq_weigh_kernel<TY, FOUR, 2>), grid, block, 0, stream, w); break;
-    case 3: hipLaunchKernelGGL((fbq_weigh_kernel<TY, FOUR, 3>), grid, block, 0, stream, w); break;
-    case 4: hipLaunchKernelGGL((fbq_weigh_kernel<TY, FOUR, 4>), grid, block, 0, stream, w); break;
-    case 6: hipLaunchKernelGGL((fbq_weigh_kernel<TY, FOUR, 6>), grid, block, 0, stream, w); break;
-    default: hipLaunchKernelGGL((fbq_weigh_kernel<TY, FOUR, 8>), grid, block, 0, stream, w); break;
+    case 2: launch_weigh<TY, FOUR, 2>(w, stream); break;
+    case 3: launch_weigh<TY, FOUR, 3>(w, stream); break;
+    case 4: launch_weigh<TY, FOUR, 4>(w, stream); break;
+    case 6: launch_weigh<TY, FOUR, 6>(w, stream); break;
+    default: launch_weigh<TY, FOUR, 8>(w, stream); break;
     }
     return hipGetLastError();
 }
@@ -252,6 +454,9 @@ extern "C" fbq_status fbq_attention_weights(const fbq_attention_call *c, const f
     a.q_xor = c->scale < 0 ? 0x80008000u : 0u;
     w.weights = decay == 0 ? nullptr : weights;
     w.out = out; w.width = width; w.decay = decay;
+    w.few = (long)a.max_q * a.group <= kFewRows;
+    const long steps = (((long)a.max_pages << a.log_ps) + kFewTile - 1) / kFewTile * a.rows * a.kv_heads;
+    a.workers = (int)std::min(a.D > 128 ? 2048L : 4096L, (steps + kFewWaves - 1) / kFewWaves * kFewWaves);                 // (as many waves as the GPU holds)
     w.together = (long)a.max_q * a.group > 16 * kWeighWaves;
     const long most = std::min((long)a.max_pages << a.log_ps, (long)width), items = (long)a.rows * a.kv_heads;
     const int a_block = w.together ? kWeighKeys : kWeighWaves * kWeighKeys;

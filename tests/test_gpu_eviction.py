@@ -27,12 +27,13 @@ def weights64(values, table, lengths, layer, q, lse, counts, scale, before, deca
     want, bound = out.double().clone(), torch.zeros_like(out, dtype=torch.float64)
     width, t = out.shape[2], 0
     for b, c in enumerate(counts):
+        if c == 0:                                             # (left as it is)
+            continue
         n = int(lengths[b])
         m = min(n, width)
         k = values[layer, table[b, :math.ceil(n / page)].long(), 0].permute(1, 0, 2, 3).reshape(kv_heads, -1, D)[:, :n]
         want[b, :, :m] = before[b, :, :m].double() * decay if before is not None and decay else 0.0
-        if c:
-            want[b, :, max(0, n - c):m] = 0.0
+        want[b, :, max(0, n - c):m] = 0.0
         bound[b, :, :m] = want[b, :, :m].abs() * 2.0 ** -22
         for i in range(c):
             sees = n - c + i + 1
@@ -75,6 +76,9 @@ def check_weights(bits, lengths, counts, heads, kv_heads, D, page, dtype, seed=0
     got = got.cpu()
     for b, n in enumerate(lengths):
         m = min(n, width)
+        if counts[b] == 0:
+            assert torch.equal(torch.nan_to_num(got[b], nan=-1.0), torch.nan_to_num(out[b], nan=-1.0))
+            continue
         off = (got[b, :, :m].double() - want[b, :, :m]).abs()
         assert (off <= bound[b, :, :m]).all(), (b, float((off / bound[b, :, :m].clamp(min=1e-300)).max()))
         assert torch.equal(torch.nan_to_num(got[b, :, m:], nan=-1.0), torch.nan_to_num(out[b, :, m:], nan=-1.0))
