@@ -1,9 +1,11 @@
 // fbq_cache_evict: rows cut back to the tokens that matter, each layer and key/value head by its own weights.
 //
-// Four launches: which rows (their pages looked at as they are before the call); which tokens of each layer, row and head stay, and their weights; the tokens moved; tables, lengths and pages.
-// Choosing: the least weight that stays is found 8 bits at a time from counts of the digits in LDS (whole numbers: their order does not matter); of those equal to it the earliest stay.
-// Moving is in place: position i takes token src[i] >= i.  A block has some columns - 64 bytes of every key, or value - of one row and head to itself and goes through the positions
-// upwards, reading a round's tokens before it writes them: what it writes lies before all that it still reads.  Bound by HBM: every token that moves is read and written once.
+// Three launches: which tokens of each layer, row and head stay, and their weights; the tokens moved; tables, lengths and pages.  What is cut back is decided by the first from the pages as they
+// are before the call, by every block for its row.
+// Choosing: the least weight that stays is found 11 bits at a time from counts of the digits in LDS (whole numbers: their order does not matter); of those equal to it the earliest stay.
+// Moving is in place: position i takes token src[i] >= i.  A block has some columns - 64 bytes of every key, or value - of one row and head to itself and goes through the positions upwards: a
+// round's tokens are read before the round before it is written, and all that is written lies before all that is still to be read.  Bound by HBM: every token that moves is read and written
+// once.
 #include <algorithm>
 
 #include "fbq_attend.h"
@@ -12,7 +14,9 @@
 
 namespace fbq {
 
-constexpr int kChooseThreads = 256, kChooseEach = 4;
+constexpr int kChooseEach = 4;           // weights a thread and round of the choosing
+constexpr int kShortRows = 2048;         // up to so many weights a row a block of 256 chooses, else one of 1024
+constexpr int kDigits = 2048;
 constexpr int kMoveThreads = 256;        // (what four threads a token, and sixteen four tokens, count on)
 constexpr int kEvictBlocks = 1 << 20;    // of a grid at most; they go on with every so manieth item
 
@@ -24,46 +28,45 @@ struct EvictArgs {
     const int32_t *keep;
     int width, first, recent;
     int32_t *rows;                       // tokens of a row that is cut back, -1: left as it is, -2: skipped
-    int32_t *src;                        // [items][width]: which tokens stay
+    int32_t *src;                        // [items][width]: where the tokens that stay lie, page * page_size + place in it
     long items;                          // layers x rows x heads
 };
 
-__global__ __launch_bounds__(256) void fbq_evict_rows_kernel(const EvictArgs e)
+// Tokens of row b if it is to be cut back, else -1, or -2 if it cannot be (see fbq.h).  The whole block calls it.
+template <int THREADS>
+__device__ __forceinline__ int tokens_to_cut(const EvictArgs &e, int b, int *scratch)
 {
-    __shared__ int bad;
     const CacheArgs &c = e.c;
-    const int b = blockIdx.x, tokens = tokens_of(c.lengths[b], c.max_pages << c.log_ps), keep = e.keep[b];
-    if (threadIdx.x == 0) bad = 0;
-    __syncthreads();
-    if (keep < 0 || keep >= tokens) {
-        if (threadIdx.x == 0) e.rows[b] = -1;
-        return;
-    }
+    const int tokens = tokens_of(c.lengths[b], c.max_pages << c.log_ps), keep = e.keep[b];
+    if (keep < 0 || keep >= tokens) return -1;
+    if (tokens > e.width || (long)e.first + e.recent > keep) return -2;
     const int pages = (tokens + (1 << c.log_ps) - 1) >> c.log_ps;
-    for (int i = (min(e.first, tokens) >> c.log_ps) + threadIdx.x; i < pages; i += 256) {
+    bool bad = false;
+    for (int i = (e.first >> c.log_ps) + threadIdx.x; i < pages; i += THREADS) {
         const int page = c.table[(long)b * c.max_pages + i];
-        if ((unsigned)page >= (unsigned)c.pages || c.refs[page] != 1) bad = 1;            // (any of them writes the same)
+        bad |= (unsigned)page >= (unsigned)c.pages || c.refs[page] != 1;
     }
+    __syncthreads();                                          // (scratch may still be read)
+    if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = 0;
+    if (__ballot(bad) && (threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = 1;
     __syncthreads();
-    if (threadIdx.x == 0) e.rows[b] = bad || tokens > e.width || (long)e.first + e.recent > keep ? -2 : tokens;
+    for (int w = 0; w < THREADS / 64; ++w)
+        if (scratch[w]) return -2;
+    return tokens;
 }
 
-// Sums over the block of two counts of up to 2^16 - 1 in a word, of the threads before this one; all threads call it.
+// Sum over the threads before this one, and of all; all threads call it.
+template <int THREADS>
 __device__ __forceinline__ int block_before(int v, int *scratch, int *total)
 {
-    constexpr int kWaves = kChooseThreads / 64;
+    constexpr int kWaves = THREADS / 64;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, s = wave_scan(v);
     __syncthreads();
     if (lane == 63) scratch[wave] = s;
     __syncthreads();
-    int before = 0, all = 0;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-        before += w < wave ? scratch[w] : 0;
-        all += scratch[w];
-    }
-    *total = all;
-    return before + s - v;
+    const int mine = lane < kWaves ? scratch[lane] : 0, sums = wave_scan(mine);
+    *total = __builtin_amdgcn_readlane(sums, 63);
+    return __builtin_amdgcn_readlane(sums - mine, uniform(wave)) + s - v;
 }
 
 // A weight as a whole number in the order of weights; what is no number is the least.
@@ -74,48 +77,64 @@ __device__ __forceinline__ uint32_t order_of(float x)
     return u >> 31 ? ~u : u | 0x80000000u;
 }
 
-__global__ __launch_bounds__(kChooseThreads) void fbq_evict_choose_kernel(const EvictArgs e)
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void fbq_evict_choose_kernel(const EvictArgs e)
 {
-    __shared__ int counts[256], scratch[kChooseThreads / 64], found[2];
+    constexpr int kHeld = THREADS == 256 ? kShortRows : 16384, kOwn = kDigits / THREADS;   // weights kept in LDS; digits of a thread
+    __shared__ int counts[kDigits], scratch[THREADS / 64], found[2];
+    __shared__ uint32_t held[kHeld];
     const CacheArgs &c = e.c;
     const int tid = threadIdx.x;
     for (long item = blockIdx.x; item < e.items; item += gridDim.x) {
         const long of_layer = (long)c.rows * c.kv_heads, layer = item / of_layer, rest = item - layer * of_layer;
-        const int b = (int)(rest / c.kv_heads), tokens = e.rows[b];
+        const int b = (int)(rest / c.kv_heads), tokens = tokens_to_cut<THREADS>(e, b, scratch);
+        if (layer == 0 && rest == (long)b * c.kv_heads && tid == 0) e.rows[b] = tokens;
         if (tokens < 0) continue;
         const long at = layer * e.layer_stride + rest * e.width;
         const float *const from = e.weights + at;
         float *const to = e.weights_out + at;
         int32_t *const src = e.src + item * e.width;
+        const int32_t *const list = c.table + (long)b * c.max_pages;
         const int first = e.first, end = tokens - e.recent, keep = e.keep[b];
         int wanted = keep - first - e.recent;                 // of the middle, first <= j < end (more than those: some go)
-        uint32_t least = 0, mask = 0;                         // what all weights that may still be the least one that stays begin with
-        if (wanted > 0) {
-            for (int shift = 24; shift >= 0; shift -= 8) {
-                counts[tid] = 0;
-                __syncthreads();
-                for (int j = first + tid; j < end; j += kChooseThreads) {
-                    const uint32_t u = order_of(from[j]);
-                    if ((u & mask) == least) atomicAdd(&counts[u >> shift & 255], 1);
+        uint32_t least = wanted > 0 ? 0 : 0xffffffffu, mask = 0;           // what all weights that may still be the least one that stays begin with (or above every weight)
+        for (int shift = 21; wanted > 0 && shift >= -1; shift -= 11) {
+            const int low = max(shift, 0);                    // the last digit has ten bits
+#pragma unroll
+            for (int i = 0; i < kOwn; ++i) counts[tid + i * THREADS] = 0;
+            __syncthreads();
+            for (int j = first + tid; j < end; j += THREADS) {
+                uint32_t u;
+                if (shift == 21) {
+                    u = order_of(from[j]);
+                    if (j - first < kHeld) held[j - first] = u;
+                } else {
+                    u = j - first < kHeld ? held[j - first] : order_of(from[j]);
                 }
-                __syncthreads();
-                int total;
-                const int mine = counts[255 - tid], above = block_before(mine, scratch, &total);   // of larger digits than this thread's
-                if (above < wanted && above + mine >= wanted) {
-                    found[0] = 255 - tid;
+                if ((u & mask) == least) atomicAdd(&counts[u >> low & (shift < 0 ? 1023 : 2047)], 1);
+            }
+            __syncthreads();
+            int own[kOwn], mine = 0, total;                   // digits from the largest down
+#pragma unroll
+            for (int i = 0; i < kOwn; ++i) mine += own[i] = counts[kDigits - 1 - (tid * kOwn + i)];
+            int above = block_before<THREADS>(mine, scratch, &total);
+#pragma unroll
+            for (int i = 0; i < kOwn; ++i) {
+                if (above < wanted && above + own[i] >= wanted) {
+                    found[0] = kDigits - 1 - (tid * kOwn + i);
                     found[1] = above;
                 }
-                __syncthreads();
-                least |= (uint32_t)found[0] << shift;
-                mask |= 0xffu << shift;
-                wanted -= found[1];
+                above += own[i];
             }
-        } else {
-            least = 0xffffffffu;                              // (above every weight)
+            __syncthreads();
+            least |= (uint32_t)found[0] << low;
+            mask |= (shift < 0 ? 1023u : 2047u) << low;
+            wanted -= found[1];
+            __syncthreads();
         }
         // those larger than `least` stay, and the first `wanted` of those equal to it
         int larger = 0, equal = 0;                            // so far
-        for (int j0 = 0; j0 < tokens; j0 += kChooseThreads * kChooseEach) {
+        for (int j0 = 0; j0 < tokens; j0 += THREADS * kChooseEach) {
             float w[kChooseEach];
             bool over[kChooseEach], same[kChooseEach];
             int mine = 0, all;
@@ -129,14 +148,14 @@ __global__ __launch_bounds__(kChooseThreads) void fbq_evict_choose_kernel(const 
                 same[i] = middle && u == least && wanted > 0;
                 mine += over[i] + (same[i] << 16);
             }
-            const int before = block_before(mine, scratch, &all);         // (all reads of the chunk are done behind it)
+            const int before = block_before<THREADS>(mine, scratch, &all);    // (all reads of the chunk are done behind it)
             int o = larger + (before & 0xffff), s = equal + (before >> 16);
 #pragma unroll
             for (int i = 0; i < kChooseEach; ++i) {
                 const int j = j0 + tid * kChooseEach + i;
                 if (over[i] || (same[i] && s < wanted)) {
                     const int place = o + min(s, max(wanted, 0));
-                    src[place] = j;
+                    src[place] = list[j >> c.log_ps] << c.log_ps | (j & ((1 << c.log_ps) - 1));
                     to[place] = w[i];
                 }
                 o += over[i];
@@ -146,7 +165,7 @@ __global__ __launch_bounds__(kChooseThreads) void fbq_evict_choose_kernel(const 
             equal += all >> 16;
         }
         __syncthreads();
-        for (int j = keep + tid; j < tokens; j += kChooseThreads) to[j] = 0;
+        for (int j = keep + tid; j < tokens; j += THREADS) to[j] = 0;
         __syncthreads();
     }
 }
@@ -165,6 +184,7 @@ __host__ __device__ __forceinline__ int move_parts(int D)
     const int DS = features4(D);
     return (DS / 2 + 63) / 64 + DS / 32 + 2;
 }
+__host__ __device__ __forceinline__ long move_jobs(long items, int parts) { return (items + 7) / 8 * 8 * parts; }
 template <bool FOUR>
 __device__ __forceinline__ MovePart move_part(int D, int i)
 {
@@ -178,25 +198,35 @@ __device__ __forceinline__ MovePart move_part(int D, int i)
     return MovePart{i > n + DS / 32, false, 0, 4 * groups4(DS), 4 * groups4(DS), true};
 }
 
-// Rows of a token each: four threads a token, a piece W each, kEach tokens a thread and round.
-template <class W, class Place>
-__device__ __forceinline__ void move_rows(const int32_t *__restrict__ src, int lowest, int keep, bool there, Place place)
+// Rows of a token each: four threads a token, a piece W each, kEach tokens a thread and round; two rounds' at a time.  place: of a token by where it lies; where: position i's.
+template <class W, class Place, class Where>
+__device__ __forceinline__ void move_rows(const int32_t *__restrict__ src, int lowest, int keep, bool there, Place place, Where where)
 {
     constexpr int kStep = kMoveThreads / 4, kEach = 8;
-    for (int i0 = lowest; i0 < keep; i0 += kStep * kEach) {
-        int j[kEach];
-        W v[kEach];
+    struct Round { int from[kEach]; W v[kEach]; };
+    const auto read = [&](Round &x, int i0) __attribute__((always_inline)) {
 #pragma unroll
-        for (int y = 0; y < kEach; ++y) j[y] = src[min(i0 + y * kStep + ((int)threadIdx.x >> 2), keep - 1)];
+        for (int y = 0; y < kEach; ++y) x.from[y] = src[min(i0 + y * kStep + ((int)threadIdx.x >> 2), keep - 1)];
 #pragma unroll
         for (int y = 0; y < kEach; ++y)
-            if (there) v[y] = *reinterpret_cast<const W *>(place(j[y]));
-        __syncthreads();
+            if (there) x.v[y] = *reinterpret_cast<const W *>(place(x.from[y]));
+    };
+    const auto write = [&](const Round &x, int i0) __attribute__((always_inline)) {
 #pragma unroll
         for (int y = 0; y < kEach; ++y) {
-            const int i = i0 + y * kStep + ((int)threadIdx.x >> 2);
-            if (there && i < keep && i != j[y]) *reinterpret_cast<W *>(place(i)) = v[y];
+            const int i = i0 + y * kStep + ((int)threadIdx.x >> 2), to = where(min(i, keep - 1));
+            if (there && i < keep && to != x.from[y]) *reinterpret_cast<W *>(place(to)) = x.v[y];
         }
+    };
+    Round a, b;
+    read(a, lowest);
+    for (int i0 = lowest; i0 < keep; i0 += 2 * kStep * kEach) {
+        read(b, i0 + kStep * kEach);
+        __syncthreads();                                      // (all have read the round that is written, and those behind it read later lie behind it)
+        write(a, i0);
+        read(a, i0 + 2 * kStep * kEach);
+        __syncthreads();
+        write(b, i0 + kStep * kEach);
     }
 }
 
@@ -205,25 +235,32 @@ __global__ __launch_bounds__(kMoveThreads) void fbq_evict_move_kernel(const Evic
 {
     const CacheArgs &c = e.c;
     const int tid = threadIdx.x, ps1 = (1 << c.log_ps) - 1, parts = move_parts<FOUR>(c.D), DS = features4(c.D);
-    const long head_bytes = (c.page_bytes >> 1) / c.kv_heads, jobs = e.items * parts;
+    const long head_bytes = (c.page_bytes >> 1) / c.kv_heads, jobs = move_jobs(e.items, parts);
     for (long job = blockIdx.x; job < jobs; job += gridDim.x) {
-        const long item = job / parts, of_layer = (long)c.rows * c.kv_heads, layer = item / of_layer, rest = item - layer * of_layer;
+        // The parts of an item on one XCD: they share lines of 128 bytes in its L2.  Blocks go round the eight in turn, so eight items' parts are dealt out part by part.
+        const long eight = job / (8 * parts);
+        const int in_eight = (int)(job - eight * (8 * parts));
+        const long item = eight * 8 + (in_eight & 7);
+        if (item >= e.items) continue;
+        const long of_layer = (long)c.rows * c.kv_heads, layer = item / of_layer, rest = item - layer * of_layer;
         const int b = (int)(rest / c.kv_heads), h = (int)(rest - (long)b * c.kv_heads);
         if (e.rows[b] < 0) continue;
-        const MovePart part = move_part<FOUR>(c.D, (int)(job - item * parts));
+        const MovePart part = move_part<FOUR>(c.D, in_eight >> 3);
         const int keep = e.keep[b];
+        if (keep <= e.first) continue;                        // (nothing moves; with none kept there is no src, either)
         const int32_t *const src = e.src + item * e.width, *const list = c.table + (long)b * c.max_pages;
         unsigned char *const heads = c.pool + layer * c.layer_bytes + (part.values ? c.page_bytes >> 1 : 0) + h * head_bytes;
-        const auto head_of = [&](int token) { return heads + list[token >> c.log_ps] * c.page_bytes; };
+        const auto head_of = [&](int at) { return heads + (long)(at >> c.log_ps) * c.page_bytes; };                 // of a token by where it lies
+        const auto where = [&](int i) { return list[i >> c.log_ps] << c.log_ps | (i & ps1); };
         if (FOUR && part.scales) {
             const int at = (tid & 3) * 4;
-            move_rows<uint32_t>(src, e.first, keep, at < part.end, [&](int token) { return head_of(token) + scales_at4(c.log_ps, token & ps1, DS) + at; });
+            move_rows<uint32_t>(src, e.first, keep, at < part.end, [&](int token) { return head_of(token) + scales_at4(c.log_ps, token & ps1, DS) + at; }, where);
         } else if (!FOUR || !part.codes) {
             const int at = part.at + (tid & 3) * 16;
             move_rows<word4_t>(src, e.first, keep, at < part.end, [&](int token) {
                 const int slot = token & ps1;
                 return head_of(token) + (FOUR ? codes_at4(slot, DS) + (slot & 15) * part.row : (long)slot * part.row) + at;
-            });
+            }, where);
         } else {
             // four tokens' codes a word: each byte from where its token's is
             constexpr int kStep = kMoveThreads / 16, kEach = 4;
@@ -242,7 +279,7 @@ __global__ __launch_bounds__(kMoveThreads) void fbq_evict_move_kernel(const Evic
 #pragma unroll
                 for (int y = 0; y < kEach; ++y) {
                     const int i = 4 * (q0 + y * kStep + (tid >> 4));
-                    old[y] = i < keep && i + 4 > keep ? *place(i) : 0;        // (places behind the last token stay as they are)
+                    old[y] = i < keep && i + 4 > keep ? *place(where(i)) : 0; // (places behind the last token stay as they are)
 #pragma unroll
                     for (int k = 0; k < 4; ++k) v[y][k] = *place(j[y][k]);
                 }
@@ -257,7 +294,7 @@ __global__ __launch_bounds__(kMoveThreads) void fbq_evict_move_kernel(const Evic
                         const int at = 8 * byte_of_token4(k);
                         to |= i + k < keep ? (v[y][k] >> 8 * byte_of_token4(j[y][k] & 3) & 0xff) << at : old[y] & 0xffu << at;
                     }
-                    *place(i) = to;
+                    *place(where(i)) = to;
                 }
             }
         }
@@ -328,14 +365,12 @@ extern "C" fbq_status fbq_cache_evict(const fbq_cache *c, const float *weights, 
     e.src = (int32_t *)((char *)workspace + ((size_t)c->rows * 4 + 255) / 256 * 256);
     e.items = items;
     const bool four = in_4_bits(c->desc.type);
-    const long jobs = items * (four ? move_parts<true>(e.c.D) : move_parts<false>(e.c.D));
+    const long jobs = move_jobs(items, four ? move_parts<true>(e.c.D) : move_parts<false>(e.c.D));
     const hipStream_t s = (hipStream_t)stream;
-    hipLaunchKernelGGL(fbq_evict_rows_kernel, dim3(c->rows), dim3(256), 0, s, e);
+    const unsigned blocks = (unsigned)std::min<long>(items, kEvictBlocks);
+    if (std::min((long)width, (long)c->max_pages * c->desc.page_size) <= kShortRows) hipLaunchKernelGGL(fbq_evict_choose_kernel<256>, dim3(blocks), dim3(256), 0, s, e);
+    else hipLaunchKernelGGL(fbq_evict_choose_kernel<1024>, dim3(blocks), dim3(1024), 0, s, e);
     hipError_t err = hipGetLastError();
-    if (err == hipSuccess) {
-        hipLaunchKernelGGL(fbq_evict_choose_kernel, dim3((unsigned)std::min<long>(items, kEvictBlocks)), dim3(kChooseThreads), 0, s, e);
-        err = hipGetLastError();
-    }
     if (err == hipSuccess) {
         const dim3 grid((unsigned)std::min<long>(jobs, kEvictBlocks));
         if (four) hipLaunchKernelGGL(fbq_evict_move_kernel<true>, grid, dim3(kMoveThreads), 0, s, e);
