@@ -7,130 +7,157 @@
 
 namespace fbq {
 
-// Append: a wave takes one head's new tokens of one block of 16, keys and values, a block four heads; the first such token's block does it.  Lane l has token l % 16, features 32 w + 8 g ..
-// of g = l / 16: a group's least and largest are over a lane's own and three neighbours'.  Key codes are then the lane's own words.  Values lie four tokens to a word: their codes go
-// through LDS, one byte each, and where some of a word's tokens are not of this call the rest of the word is kept.  Nobody else writes the word: a partial page has one holder.
-template <class NT, int NW>
+// Append: a wave takes one head's new tokens of one block of 16, keys and values, a block four heads.  Lane l has token l % 16, features 32 w + 8 g .. of g = l / 16: a group's least and largest
+// are over a lane's own and three neighbours'.  Key codes are then the lane's own words.  Values lie four tokens to a word: their codes go through LDS, one byte each, and where some of a
+// word's tokens are not of this call the rest of the word is kept.  Nobody else writes the word: a partial page has one holder.
+// Of a block of 16's new tokens the first is the one that it is done for.  A grid block looks at WINDOW tokens for such ones: at one where rows have few, and its keys and values are then on their
+// way before it knows where they go; at 16 where they have many (16 times as many blocks that find nothing: 62 us for 4267 tokens of 32 heads, 37 this way).
+template <class NT, int NW, int WINDOW>
 __global__ __launch_bounds__(256) void fbq_append4_kernel(CacheArgs c, long layer_offset, int T, const int32_t *__restrict__ q_start, const int32_t *__restrict__ start,
                                                           const uint16_t *__restrict__ k, long k_stride, const uint16_t *__restrict__ v, long v_stride)
 {
     constexpr int DS = 32 * NW, G = groups4(DS), kRow = DS + 16;
     __shared__ __attribute__((aligned(16))) unsigned char room[4][16 * kRow];
-    const int t = blockIdx.x;
-    const int b = q_start ? row_of_token(q_start, c.rows, t) : t;
-    if (b < 0) return;
-    const int first = start[b];
-    if (first < 0) return;
-    const int i = q_start ? t - q_start[b] : 0, count = q_start ? q_start[b + 1] - q_start[b] : 1;
-    const long pos = (long)first + i;
-    if (i > 0 && (pos & 15) != 0) return;                     // (its block of 16 is another token's)
-    if (pos >= (long)c.max_pages << c.log_ps) return;
-    const int page = c.table[(long)b * c.max_pages + (pos >> c.log_ps)];
-    if ((unsigned)page >= (unsigned)c.pages) return;
-
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, slot = lane & 15, g = lane >> 4;
-    const int s0 = (int)pos & 15, s1 = min(16, s0 + min(count - i, T - t));           // slots of the block that get a token
-    const int h = blockIdx.y * 4 + wave;
-    const bool mine = h < c.kv_heads && slot >= s0 && slot < s1;
-    const int place = (int)pos & ((1 << c.log_ps) - 1) & ~15;                         // of the block, in its page
+    const int h = blockIdx.y * 4 + wave, head = min(h, c.kv_heads - 1);
     const long head_bytes = (c.page_bytes >> 1) / c.kv_heads;
-    unsigned char *const keys = c.pool + layer_offset + page * c.page_bytes + min(h, c.kv_heads - 1) * head_bytes, *const values = keys + (c.page_bytes >> 1);
 
     word4_t x[2][NW];
-    bool odd = false;                                         // something that is not finite
+    const auto ask = [&](int token, bool mine) __attribute__((always_inline)) {
 #pragma unroll
-    for (int which = 0; which < 2; ++which) {
-        const uint16_t *const from = (which ? v + (t + slot - s0) * v_stride : k + (t + slot - s0) * k_stride) + (long)h * c.D;
+        for (int which = 0; which < 2; ++which) {
+            const uint16_t *const from = (which ? v + token * v_stride : k + token * k_stride) + (long)head * c.D;
 #pragma unroll
-        for (int w = 0; w < NW; ++w) {
-            x[which][w] = word4_t{0, 0, 0, 0};
-            if (mine && 32 * w + 8 * g < c.D) x[which][w] = *reinterpret_cast<const word4_t *>(from + 32 * w + 8 * g);
-#pragma unroll
-            for (int y = 0; y < 4; ++y)
-                odd |= (x[which][w][y] & NT::kExponent) == NT::kExponent || (x[which][w][y] >> 16 & NT::kExponent) == NT::kExponent;
+            for (int w = 0; w < NW; ++w) {
+                x[which][w] = word4_t{0, 0, 0, 0};
+                if (mine && 32 * w + 8 * g < c.D) x[which][w] = *reinterpret_cast<const word4_t *>(from + 32 * w + 8 * g);
+            }
+        }
+    };
+    if (WINDOW == 1) ask(blockIdx.x, true);                   // (of the first token in every lane: of others later, where there are any)
+
+    // which of the window's tokens blocks of 16 are done for: a lane each
+    const int mine_t = blockIdx.x * WINDOW + lane % WINDOW;
+    int of_row = -1, of_count = 0, of_page = -1;
+    long of_pos = 0;
+    if (mine_t < T) {
+        const int b = q_start ? row_of_token(q_start, c.rows, mine_t) : mine_t;
+        const int first = b < 0 ? -1 : start[b];
+        if (first >= 0) {
+            const int i = q_start ? mine_t - q_start[b] : 0;
+            of_pos = (long)first + i;
+            of_count = (q_start ? q_start[b + 1] - q_start[b] : 1) - i;
+            if ((i == 0 || (of_pos & 15) == 0) && of_pos < (long)c.max_pages << c.log_ps) of_row = b;
+            if (of_row >= 0) of_page = c.table[(long)b * c.max_pages + (of_pos >> c.log_ps)];
+            if ((unsigned)of_page >= (unsigned)c.pages) of_row = -1;
         }
     }
-    const unsigned long long bad = __ballot(odd);
-    odd = ((bad | bad >> 16 | bad >> 32 | bad >> 48) >> slot & 1) != 0;               // ... in any of the token's four lanes
+    for (unsigned long long left = __ballot(of_row >= 0) & ((1ull << WINDOW) - 1); left; left &= left - 1) {
+        const int who = __builtin_ctzll(left), t = blockIdx.x * WINDOW + who;
+        const int page = __builtin_amdgcn_readlane(of_page, who), low = __builtin_amdgcn_readlane((int)of_pos, who);      // (below 2^24)
+        const int s0 = low & 15, s1 = min(16, s0 + min(__builtin_amdgcn_readlane(of_count, who), T - t));             // slots of the block that get a token
+        const bool mine = h < c.kv_heads && slot >= s0 && slot < s1;
+        const int place = low & ((1 << c.log_ps) - 1) & ~15;                          // of the block, in its page
+        unsigned char *const keys = c.pool + layer_offset + page * c.page_bytes + head * head_bytes, *const values = keys + (c.page_bytes >> 1);
+        if (WINDOW > 1 || s1 - s0 > 1) ask(t + slot - s0, mine);
 
-    uint32_t key_codes[NW];
+        // values: lane r = l % 16 of tokens 4 g .. 4 g + 3 writes its words of all products; `keep` has the bits of the tokens that are not this call's
+        uint32_t keep = 0, old[NW];
 #pragma unroll
-    for (int which = 0; which < 2; ++which) {
+        for (int j = 0; j < 4; ++j)
+            if (4 * g + j < s0 || 4 * g + j >= s1) keep |= 0xffu << 8 * byte_of_token4(j);
+        const bool writes = h < c.kv_heads && keep != 0xffffffffu;
+        uint32_t *const words = reinterpret_cast<uint32_t *>(values + codes_at4(place, DS)) + lane * NW;          // (lane = 16 g + r)
 #pragma unroll
-        for (int y = 0; y < G; ++y) {
-            // halves throughout, so that no difference is beyond fp32 (of bf16 numbers)
-            float low = INFINITY, high = -INFINITY;
+        for (int w = 0; w < NW; ++w) old[w] = writes && keep ? words[w] : 0;
+
+        uint32_t above = 0;                                   // halves with an exponent of ones are not finite
 #pragma unroll
-            for (int w = 2 * y; w < std::min(2 * y + 2, NW); ++w)
-                if (32 * w + 8 * g < c.D)
+        for (int which = 0; which < 2; ++which)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float x0 = NT::of(x[which][w][e] & 0xffff) * 0.5f, x1 = NT::of_upper(x[which][w][e]) * 0.5f;
-                        low = fminf(low, fminf(x0, x1));
-                        high = fmaxf(high, fmaxf(x0, x1));
-                    }
-            low = -larger_of_32(larger_of_16(-low)) + 0.0f;   // (no zero with a sign)
-            high = larger_of_32(larger_of_16(high));
-            const float d = high - low;                       // (head_dim reaches into every group of DS)
-            uint32_t s = NT::bits(d / 7.5f);
-            if (NT::of(s) * 7.5f < d) ++s;
-            if (s && __builtin_fmaf(NT::of(s), 15.0f, 2.0f * low) > NT::kMost) --s;
-            const float half = NT::of(s) * 0.5f;
-            uint32_t word = s << 16 | NT::bits(2.0f * low);
-            if (odd) word = which ? 0u : NT::kNaN << 16;
-            if (mine && g == y) *reinterpret_cast<uint32_t *>((which ? values : keys) + scales_at4(c.log_ps, place + slot, DS) + 4 * y) = word;
+            for (int w = 0; w < NW; ++w)
 #pragma unroll
-            for (int w = 2 * y; w < std::min(2 * y + 2, NW); ++w) {
-                uint32_t code[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const uint32_t word = x[which][w][e >> 1];
-                    const float at = (e & 1 ? NT::of_upper(word) : NT::of(word & 0xffff)) * 0.5f - low;
-                    const float q = half > 0 ? rintf(at / half) : 0.0f;
-                    code[e] = 32 * w + 8 * g < c.D ? (uint32_t)(int)fminf(fmaxf(q, 0.0f), 15.0f) : 0u;
+                for (int y = 0; y < 4; ++y) {
+                    typedef uint16_t short2_t __attribute__((ext_vector_type(2)));
+                    above = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(short2_t, above), __builtin_bit_cast(short2_t, x[which][w][y] & 0x7fff7fffu)));
                 }
-                if (which == 0) {                             // nibble n: feature e, n with its bits in reverse
-                    key_codes[w] = code[0] | code[4] << 4 | code[2] << 8 | code[6] << 12 | code[1] << 16 | code[5] << 20 | code[3] << 24 | code[7] << 28;
-                } else {
-                    const word2_t bytes{code[0] | code[1] << 8 | code[2] << 16 | code[3] << 24, code[4] | code[5] << 8 | code[6] << 16 | code[7] << 24};
-                    *reinterpret_cast<word2_t *>(&room[wave][slot * kRow + 32 * w + 8 * g]) = bytes;
+        bool odd = mine && ((above & 0xffff) >= NT::kExponent || above >> 16 >= NT::kExponent);
+        const unsigned long long bad = __ballot(odd);
+        odd = ((bad | bad >> 16 | bad >> 32 | bad >> 48) >> slot & 1) != 0;           // ... in any of the token's four lanes
+
+        uint32_t key_codes[NW];
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+#pragma unroll
+            for (int y = 0; y < G; ++y) {
+                // halves throughout, so that no difference is beyond fp32 (of bf16 numbers)
+                float low = INFINITY, high = -INFINITY;
+#pragma unroll
+                for (int w = 2 * y; w < std::min(2 * y + 2, NW); ++w)
+                    if (32 * w + 8 * g < c.D)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float x0 = NT::of(x[which][w][e] & 0xffff) * 0.5f, x1 = NT::of_upper(x[which][w][e]) * 0.5f;
+                            low = fminf(low, fminf(x0, x1));
+                            high = fmaxf(high, fmaxf(x0, x1));
+                        }
+                low = -larger_of_32(larger_of_16(-low)) + 0.0f;       // (no zero with a sign)
+                high = larger_of_32(larger_of_16(high));
+                const float d = high - low;                           // (head_dim reaches into every group of DS)
+                uint32_t s = NT::bits(d / 7.5f);
+                if (NT::of(s) * 7.5f < d) ++s;
+                if (s && __builtin_fmaf(NT::of(s), 15.0f, 2.0f * low) > NT::kMost) --s;
+                // x / half to the nearest number: x times the reciprocal, itself the nearest, and one step of correction, which is exact; where the reciprocal is no number, by division
+                const float half = NT::of(s) * 0.5f, by = half > 0 ? 1.0f / half : 0.0f;
+                const bool plain = __ballot(half > 0 && half < 0x1p-120f) == 0;
+                uint32_t word = s << 16 | NT::bits(2.0f * low);
+                if (odd) word = which ? 0u : NT::kNaN << 16;
+                if (mine && g == y) *reinterpret_cast<uint32_t *>((which ? values : keys) + scales_at4(c.log_ps, place + slot, DS) + 4 * y) = word;
+#pragma unroll
+                for (int w = 2 * y; w < std::min(2 * y + 2, NW); ++w) {
+                    uint32_t code[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const uint32_t word = x[which][w][e >> 1];
+                        const float at = (e & 1 ? NT::of_upper(word) : NT::of(word & 0xffff)) * 0.5f - low, near = at * by;
+                        float q = __builtin_fmaf(__builtin_fmaf(-near, half, at), by, near);
+                        if (!plain) q = half > 0 ? at / half : 0.0f;
+                        code[e] = 32 * w + 8 * g < c.D ? (uint32_t)(int)fminf(fmaxf(rintf(q), 0.0f), 15.0f) : 0u;
+                    }
+                    if (which == 0) {                         // nibble n: feature e, n with its bits in reverse
+                        key_codes[w] = code[0] | code[4] << 4 | code[2] << 8 | code[6] << 12 | code[1] << 16 | code[5] << 20 | code[3] << 24 | code[7] << 28;
+                    } else {
+                        const word2_t bytes{code[0] | code[1] << 8 | code[2] << 16 | code[3] << 24, code[4] | code[5] << 8 | code[6] << 16 | code[7] << 24};
+                        *reinterpret_cast<word2_t *>(&room[wave][slot * kRow + 32 * w + 8 * g]) = bytes;
+                    }
                 }
             }
         }
-    }
-    if (mine) {
-        uint32_t *const to = reinterpret_cast<uint32_t *>(keys + codes_at4(place, DS)) + (slot * 4 + g) * NW;
+        if (mine) {
+            uint32_t *const to = reinterpret_cast<uint32_t *>(keys + codes_at4(place, DS)) + (slot * 4 + g) * NW;
 #pragma unroll
-        for (int w = 0; w < NW; ++w) to[w] = key_codes[w];
-    }
-    __syncthreads();
-    if (h >= c.kv_heads) return;
-    // values: lane r = l % 16 of tokens 4 g .. 4 g + 3 has its words of all products
-    uint32_t keep = 0;                                        // bits of the tokens that are not this call's
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-        if (4 * g + j < s0 || 4 * g + j >= s1) keep |= 0xffu << 8 * byte_of_token4(j);
-    if (keep == 0xffffffffu) return;
-    uint32_t *const to = reinterpret_cast<uint32_t *>(values + codes_at4(place, DS)) + lane * NW;                 // (lane = 16 g + r)
-#pragma unroll
-    for (int y = 0; y < G; ++y) {
-        constexpr int kFull = 4;
-        const int z = lane_features4(DS, y);
-        uint32_t pairs[4];                                    // two codes of a token in bits 0 .. 7, two more in bits 16 .. 23
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const unsigned char *const at = &room[wave][(4 * g + j) * kRow + 64 * y + z * slot];
-            const uint32_t codes = z == kFull ? *reinterpret_cast<const uint32_t *>(at) : *reinterpret_cast<const uint16_t *>(at);
-            pairs[j] = codes | codes >> 4;
+            for (int w = 0; w < NW; ++w) to[w] = key_codes[w];
         }
+        __syncthreads();
 #pragma unroll
-        for (int x = 0; x < z / 2; ++x) {
-            uint32_t word = 0;
+        for (int y = 0; y < G; ++y) {
+            const int z = lane_features4(DS, y);
+            uint32_t pairs[4];                                // two codes of a token in bits 0 .. 7, two more in bits 16 .. 23
 #pragma unroll
-            for (int j = 0; j < 4; ++j) word |= (pairs[j] >> 16 * x & 0xff) << 8 * byte_of_token4(j);
-            uint32_t *const at = to + 2 * y + x;
-            *at = keep ? (word & ~keep) | (*at & keep) : word;
+            for (int j = 0; j < 4; ++j) {
+                const unsigned char *const at = &room[wave][(4 * g + j) * kRow + 64 * y + z * slot];
+                const uint32_t codes = z == 4 ? *reinterpret_cast<const uint32_t *>(at) : *reinterpret_cast<const uint16_t *>(at);
+                pairs[j] = codes | codes >> 4;
+            }
+#pragma unroll
+            for (int w = 2 * y; w < 2 * y + z / 2; ++w) {
+                uint32_t word = 0;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) word |= (pairs[j] >> 16 * (w & 1) & 0xff) << 8 * byte_of_token4(j);
+                if (writes) words[w] = (word & ~keep) | (old[w] & keep);
+            }
         }
+        __syncthreads();
     }
 }
 
@@ -138,15 +165,17 @@ template <class NT>
 static hipError_t launch_append(const CacheArgs &c, long layer_offset, int T, const int32_t *q_start, const int32_t *start, const void *k, long k_stride, const void *v, long v_stride,
                                 hipStream_t stream)
 {
-    const auto go = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, dim3(T, ceil_div(c.kv_heads, 4)), dim3(256), 0, stream, c, layer_offset, T, q_start, start, (const uint16_t *)k, k_stride, (const uint16_t *)v, v_stride);
+    const auto go = [&](auto few, auto many) {
+        const bool wide = q_start && T > 4L * c.rows;
+        hipLaunchKernelGGL(wide ? many : few, dim3(wide ? ceil_div(T, 16) : T, ceil_div(c.kv_heads, 4)), dim3(256), 0, stream, c, layer_offset, T, q_start, start, (const uint16_t *)k, k_stride,
+                           (const uint16_t *)v, v_stride);
     };
     switch (features4(c.D) / 32) {
-    case 2: go(fbq_append4_kernel<NT, 2>); break;
-    case 3: go(fbq_append4_kernel<NT, 3>); break;
-    case 4: go(fbq_append4_kernel<NT, 4>); break;
-    case 6: go(fbq_append4_kernel<NT, 6>); break;
-    default: go(fbq_append4_kernel<NT, 8>); break;
+    case 2: go(fbq_append4_kernel<NT, 2, 1>, fbq_append4_kernel<NT, 2, 16>); break;
+    case 3: go(fbq_append4_kernel<NT, 3, 1>, fbq_append4_kernel<NT, 3, 16>); break;
+    case 4: go(fbq_append4_kernel<NT, 4, 1>, fbq_append4_kernel<NT, 4, 16>); break;
+    case 6: go(fbq_append4_kernel<NT, 6, 1>, fbq_append4_kernel<NT, 6, 16>); break;
+    default: go(fbq_append4_kernel<NT, 8, 1>, fbq_append4_kernel<NT, 8, 16>); break;
     }
     return hipGetLastError();
 }
