@@ -209,6 +209,7 @@ hipError_t launch_attend_many(const AttendArgs &a, int type, bool shared, hipStr
 // of a cache in 4 bits
 hipError_t launch_attend4_few(const AttendArgs &a, int type, hipStream_t stream);
 hipError_t launch_attend4_many(const AttendArgs &a, int type, bool shared, hipStream_t stream);
+hipError_t launch_attend4_both(const AttendArgs &a, int type, hipStream_t stream);
 
 hipError_t launch_attend_both(const AttendArgs &a, int type, hipStream_t stream);                // the shared tokens many-row, the rows' own few-row
 

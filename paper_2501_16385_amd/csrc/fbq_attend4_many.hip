@@ -1,21 +1,7 @@
-// Launches of the many-row kernel over a cache in 4 bits (fbq_attend_many.h, fbq_attend_codes.h).
-#include "fbq_attend_many.h"
+// Launches of the many-row kernel over a cache in 4 bits (fbq_attend4_many.h).
+#include "fbq_attend4_many.h"
 
 namespace fbq {
-
-// Block (h, y, z) of attend_many over codes.
-template <class TY, class MAKE, int NW>
-__device__ __forceinline__ void attend4_many(const AttendArgs &a, bool shared, int h, int y, int z, unsigned char *room)
-{
-    constexpr int DP = NW == 6 ? 256 : 32 * NW;
-    bool odd = false;
-    attend_many<TY, DP, Codes<MAKE, NW, DP>>(a, shared, h, y, z, room, &odd);
-    if constexpr (MAKE::kChecked) {
-        if (!odd) return;
-        asm volatile("" : "+s"(h), "+s"(y), "+s"(z) : : "memory");           // (what was worked out from them the first time takes no registers until the second)
-        attend_many<TY, DP, Codes<MakeBf16, NW, DP>>(a, shared, h, y, z, room);
-    }
-}
 
 template <class TY, class MAKE, int NW>
 __global__ __launch_bounds__(256, NW > 4 ? 1 : 2) void fbq_attend4_many_kernel(const AttendArgs a, const bool shared)

@@ -343,10 +343,10 @@ extern "C" fbq_status fbq_attention(const fbq_attention_call *c, void *workspace
     const int type = c->cache.desc.type;
     const hipStream_t s = (hipStream_t)stream;
     hipError_t e = hipSuccess;
-    const bool four = in_4_bits(type), both = p.shared_many && p.few && p.a.D <= 128 && !four;
+    const bool four = in_4_bits(type), both = p.shared_many && p.few && p.a.D <= 128;
     const auto launch_few = four ? launch_attend4_few : launch_attend_few;
     const auto launch_many = four ? launch_attend4_many : launch_attend_many;
-    if (both) e = launch_attend_both(p.a, type, s);
+    if (both) e = (four ? launch_attend4_both : launch_attend_both)(p.a, type, s);
     else if (p.shared_many) e = launch_many(p.a, type, true, s);
     if (e == hipSuccess && !both) e = p.few ? launch_few(p.a, type, s) : launch_many(p.a, type, false, s);
     if (e == hipSuccess && p.join) e = (type & ~4) == FBQ_F16 ? launch_join<TypeF16>(p.a, p.few, s) : launch_join<TypeBf16>(p.a, p.few, s);
