@@ -28,6 +28,7 @@ import ctypes
 import json
 import os
 import sys
+from dataclasses import dataclass
 
 import torch
 
@@ -48,6 +49,26 @@ def layer_shapes(hidden: int, inter: int, kv_hidden: int = 0):
             "gate": (inter, hidden), "up": (inter, hidden), "down": (hidden, inter)}
 
 
+@dataclass(frozen=True)
+class Budget:
+    """What the rows of a cache may hold: at most `keep` tokens, the first `first` and the last `recent` ones among them, and those of the others that were attended to most; what a token
+    was given counts `decay` times as much a step later."""
+    keep: int
+    first: int = 0
+    recent: int = 1
+    decay: float = 1.0
+
+
+@dataclass(frozen=True)
+class Budget:
+    """What the rows of a cache may hold: at most `keep` tokens, the first `first` and the last `recent` ones among them, and those of the others that were attended to most; what a token
+    was given counts `decay` times as much a step later."""
+    keep: int
+    first: int = 0
+    recent: int = 1
+    decay: float = 1.0
+
+
 class DecoderStack:
     """layers: list (one per decoder layer) of dicts name -> fbq.DeviceLayer.
 
@@ -55,14 +76,19 @@ class DecoderStack:
     these hold.  counts [rows]: tokens of each row in a step (None: one); shared: the pages that all rows begin with (a view of a row of the table stays
     right when pages move).  A row that no pages are left for, in the pool or in its row of the table, is not written in that step, and what the step makes of it means
     nothing.  `lacking` [1]: the pages that the last step lacked, `most_lacking` [1] that any has; `lowest_start` [rows]: -1 where a step has left a row out.
+
+    The cache may be one of 4 bits.  budget: a Budget; then every step adds up the attention weights in `weights` [layers, rows, kv_heads, tokens] and ends with the rows cut back
+    (a row that begins with another's tokens, as a forked one does, wants that one's weights copied there); `evicted` [2]: rows cut back by the last step, and rows that could not be.
     """
 
     def __init__(self, layers, hidden: int, inter: int, keep_per_layer_buffers: bool = False, batch: int = 1,
-                 share_workspaces: bool = False, cache=None, counts=None, shared=None):
+                 share_workspaces: bool = False, cache=None, counts=None, shared=None, budget=None):
         self.layers, self.hidden, self.inter, self.batch = layers, hidden, inter, batch
-        self.cache, self.shared = cache, shared
+        self.cache, self.shared, self.budget = cache, shared, budget
         if cache is not None:
             self._attend_over(cache, counts)
+        elif budget is not None:
+            raise ValueError("budget: of a cache's rows")
         kv_hidden = hidden if cache is None else cache.heads * cache.head_dim
         self.lib = fbq.load()
         dev = "cuda"
@@ -96,6 +122,12 @@ class DecoderStack:
         self.q_start = None if counts == [1] * rows else ints(edges)
         q = torch.empty((self.batch, self.hidden // cache.head_dim, cache.head_dim), dtype=torch.float16, device="cuda")
         self.attend_ws = kv.attention_workspace(cache, q, q_start=self.q_start, max_q=self.max_q, shared=self.shared)
+        if self.budget is not None:
+            width = cache.table.shape[1] * cache.page_size
+            self.lse = torch.empty(q.shape[:2], dtype=torch.float32, device="cuda")
+            self.weights = torch.zeros((cache.pool.shape[0], rows, cache.heads, width), dtype=torch.float32, device="cuda")
+            self.keep, self.evicted = ints([self.budget.keep] * rows), ints([0, 0])
+            self.evict_ws = kv.cache_evict_workspace(cache, self.weights)
 
     def _attend(self, li, b, stream):
         """a = attention of this step's tokens over the cache, this layer's k and v in their pages first."""
@@ -103,7 +135,10 @@ class DecoderStack:
         heads = lambda t, n: t.view(self.batch, n, c.head_dim)
         kv.cache_append(c, li, heads(b["k"], c.heads), heads(b["v"], c.heads), self.start, q_start=self.q_start, stream=stream)
         n = self.hidden // c.head_dim
-        kv.attention(c, li, heads(b["q"], n), q_start=self.q_start, max_q=self.max_q, shared=self.shared, out=heads(b["a"], n), workspace=self.attend_ws, stream=stream)
+        q, lse = heads(b["q"], n), None if self.budget is None else self.lse
+        kv.attention(c, li, q, q_start=self.q_start, max_q=self.max_q, shared=self.shared, out=heads(b["a"], n), lse=lse, workspace=self.attend_ws, stream=stream)
+        if lse is not None:
+            kv.attention_weights(c, li, q, lse, self.weights[li], q_start=self.q_start, max_q=self.max_q, decay=self.budget.decay, stream=stream)
         return b["a"]
 
     def _workspace(self, desc):
@@ -143,6 +178,8 @@ class DecoderStack:
             self._group(li, ("gate", "up"), [b["h"], b["h"]], [b["gate"], b["up"]], sp)
             fbq.silu_mul(b["gate"], b["up"], b["act"], stream)
             self._group(li, ("down",), [b["act"]], [b["down"]], sp, mix=(b["h"], x))         # x = (h + down) / 2
+        if self.budget is not None:
+            kv.cache_evict(self.cache, self.weights, self.keep, first=self.budget.first, recent=self.budget.recent, info=self.evicted, workspace=self.evict_ws, stream=stream)
         return x
 
     def capture(self):
