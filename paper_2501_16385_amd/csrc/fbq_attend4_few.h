@@ -340,36 +340,35 @@ __device__ __forceinline__ void attend4_few(const AttendArgs &a, int block, unsi
         else if (a.lse) a.lse[(long)cur.t * a.heads + head] = l == 0 ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
     };
 
+    // One copy of `finish` and of all that a new piece takes: the kernel is long, and where there is little to do it waits for its instructions.
     prepare(cur);
-    if (cur.n == 0) {                                         // (no tokens in the item, or in this worker's part)
-        begin();
-        finish();
-        return;
-    }
     behind = cur;                                             // (where there is none, something that is one)
     bool more = line.follow(a, cur, behind);
     if (more) prepare(behind);
     Step4<NW> x0, x1;
-    aim(cur, true);
+    aim(cur, cur.n > 0);
     load(x0);
-    begin();
-    int s = 0;
-    auto turn = [&](const Step4<NW> &now, Step4<NW> &next) __attribute__((always_inline)) {
-        if (s + 1 == cur.n) aim(behind, more);
-        load(next);
-        compute(now, s);
-        if (++s < cur.n) return false;
+    while (true) {
+        begin();
+        for (int s = 0; s < cur.n; s += 2) {                  // (a piece without steps: no tokens in the item, or in this worker's part)
+            if (s + 1 >= cur.n) aim(behind, more);
+            load(x1);
+            compute(x0, s);
+            if (s + 1 < cur.n) {
+                if (s + 2 >= cur.n) aim(behind, more);
+                load(x0);
+                compute(x1, s + 1);
+            } else {
+                x0 = x1;
+            }
+        }
         finish();
-        if (!more) return true;
+        if (!more) return;
         first = false;
         cur = behind;
-        s = 0;
         more = line.follow(a, cur, behind);
         if (more) prepare(behind);
-        begin();
-        return false;
-    };
-    while (!turn(x0, x1) && !turn(x1, x0)) {}
+    }
 }
 
 }  // namespace fbq
