@@ -59,7 +59,6 @@ struct AttendArgs {
     // many-row kernel: at most `splits` pieces of a tile's keys, partial results [splits][T heads] (null: out is written); shared_splits of the shared tokens
     int splits, shared_splits;
     Partials part, part_shared;
-    int32_t *odd;                        // a place for each of its blocks, where a cache of bf16 is in 4 bits: whether it has met what fp16 operands are not made for
 };
 
 // The two types: operands of the matrix cores, and two floats rounded to a word of them (to nearest, ties to even).
@@ -142,8 +141,6 @@ __device__ __forceinline__ int many_limit(const AttendArgs &a, int tokens, int q
 }
 __device__ __forceinline__ int many_steps(const AttendArgs &a, int limit) { return (max(limit - a.n_shared, 0) + kManyTile - 1) / kManyTile; }
 
-__device__ __forceinline__ long odd_place(const AttendArgs &a, int h, int y, int z) { return ((long)z * many_tiles(a, a.T) + y) * a.kv_heads + h; }
-
 // How many steps a piece of a tile has at most (see fbq_attend_plan.h).  The whole wave calls it.
 __host__ __device__ __forceinline__ constexpr int many_blocks(int D) { return D > 128 ? 256 : 512; }
 __device__ __forceinline__ int many_share(const AttendArgs &a)
@@ -212,8 +209,6 @@ hipError_t launch_attend_many(const AttendArgs &a, int type, bool shared, hipStr
 // of a cache in 4 bits
 hipError_t launch_attend4_few(const AttendArgs &a, int type, hipStream_t stream);
 hipError_t launch_attend4_many(const AttendArgs &a, int type, bool shared, hipStream_t stream);
-long attend4_odd_places(const AttendArgs &a, bool shared);                                        // blocks of the many-row kernel's grid
-hipError_t launch_attend4_again(const AttendArgs &a, bool shared, hipStream_t stream);           // behind a many-row launch over a cache of bf16
 hipError_t launch_attend4_both(const AttendArgs &a, int type, hipStream_t stream);
 
 hipError_t launch_attend_both(const AttendArgs &a, int type, hipStream_t stream);                // the shared tokens many-row, the rows' own few-row

@@ -8,12 +8,18 @@
 
 namespace fbq {
 
-// Block (h, y, z) of attend_many over codes.  What it has met goes to its place in a.odd, for fbq_attend4_again_kernel.
+// Block (h, y, z) of attend_many over codes.
 template <class TY, class MAKE, int NW>
 __device__ __forceinline__ void attend4_many(const AttendArgs &a, bool shared, int h, int y, int z, unsigned char *room)
 {
     constexpr int DP = NW == 6 ? 256 : 32 * NW;
-    attend_many<TY, DP, Codes<MAKE, NW, DP>>(a, shared, h, y, z, room, MAKE::kChecked ? a.odd + odd_place(a, h, y, z) : nullptr);
+    bool odd = false;
+    attend_many<TY, DP, Codes<MAKE, NW, DP>>(a, shared, h, y, z, room, &odd);
+    if constexpr (MAKE::kChecked) {
+        if (!odd) return;
+        asm volatile("" : "+s"(h), "+s"(y), "+s"(z) : : "memory");           // (what was worked out from them the first time takes no registers until the second)
+        attend_many<TY, DP, Codes<MakeBf16, NW, DP>>(a, shared, h, y, z, room);
+    }
 }
 
 }  // namespace fbq

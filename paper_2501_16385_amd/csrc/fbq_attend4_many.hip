@@ -12,19 +12,6 @@ __global__ __launch_bounds__(256, NW > 4 ? 1 : 2) void fbq_attend4_many_kernel(c
     attend4_many<TY, MAKE, NW>(a, shared, blockIdx.x, pieces ? blockIdx.y : blockIdx.y + blockIdx.z * kGridTiles, pieces ? blockIdx.z : 0, room);
 }
 
-// The blocks that have met what fp16 operands are not made for do their work again, with operands of bf16.  A launch of its own: in the kernel before, its registers would cost that a fifth of its
-// time, and a launch whose blocks leave at once costs 2.5 us.  (A block that had no work has written nothing, and finds here that it has none.)
-template <int NW>
-__global__ __launch_bounds__(256, NW > 4 ? 1 : 2) void fbq_attend4_again_kernel(const AttendArgs a, const bool shared)
-{
-    constexpr int DP = NW == 6 ? 256 : 32 * NW;
-    __shared__ __attribute__((aligned(1024))) unsigned char room[kMany4Room<DP>];
-    const bool pieces = shared && a.shared_splits > 1;
-    const int h = blockIdx.x, y = pieces ? blockIdx.y : blockIdx.y + blockIdx.z * kGridTiles, z = pieces ? blockIdx.z : 0;
-    if (a.odd[odd_place(a, h, y, z)] == 0) return;
-    attend4_many<TypeBf16, MakeBf16, NW>(a, shared, h, y, z, room);
-}
-
 template <class TY, class MAKE>
 static hipError_t launch_many(const AttendArgs &a, bool shared, hipStream_t stream)
 {
@@ -37,25 +24,6 @@ static hipError_t launch_many(const AttendArgs &a, bool shared, hipStream_t stre
     default: hipLaunchKernelGGL((fbq_attend4_many_kernel<TY, MAKE, 8>), grid, block, 0, stream, a, shared); break;
     }
     return hipGetLastError();
-}
-
-hipError_t launch_attend4_again(const AttendArgs &a, bool shared, hipStream_t stream)
-{
-    const dim3 grid = many_grid(a, shared), block(256);
-    switch (features4(a.D) / 32) {
-    case 2: hipLaunchKernelGGL(fbq_attend4_again_kernel<2>, grid, block, 0, stream, a, shared); break;
-    case 3: hipLaunchKernelGGL(fbq_attend4_again_kernel<3>, grid, block, 0, stream, a, shared); break;
-    case 4: hipLaunchKernelGGL(fbq_attend4_again_kernel<4>, grid, block, 0, stream, a, shared); break;
-    case 6: hipLaunchKernelGGL(fbq_attend4_again_kernel<6>, grid, block, 0, stream, a, shared); break;
-    default: hipLaunchKernelGGL(fbq_attend4_again_kernel<8>, grid, block, 0, stream, a, shared); break;
-    }
-    return hipGetLastError();
-}
-
-long attend4_odd_places(const AttendArgs &a, bool shared)
-{
-    const dim3 grid = many_grid(a, shared);
-    return (long)grid.x * grid.y * grid.z;
 }
 
 hipError_t launch_attend4_many(const AttendArgs &a, int type, bool shared, hipStream_t stream)

@@ -67,9 +67,9 @@ struct OperandOf<NoCodes, TY> { typedef TY type; };
 
 // Block (h, y, z) of the many-row work, four waves: head, tile (of the rows' own tokens: tile and piece), piece of the shared tokens.  FOUR: a Codes (fbq_attend_codes.h), where the cache is
 // in 4 bits and keys and values are made on their way to LDS; void: it is not.
-// `odd`: takes whether it has met what the operands that it makes are not made for; then its results mean nothing.
+// `odd`: set where the operands that it makes are not made for what it has met, and its results mean nothing (for the whole block).
 template <class TY, int DP, class FOUR = void>
-__device__ __forceinline__ void attend_many(const AttendArgs &a, const bool shared, const int h, const int y, const int z, unsigned char *room, int32_t *odd = nullptr)
+__device__ __forceinline__ void attend_many(const AttendArgs &a, const bool shared, const int h, const int y, const int z, unsigned char *room, bool *odd = nullptr)
 {
     constexpr bool kFour = !std::is_void<FOUR>::value;
     typedef typename std::conditional<kFour, FOUR, NoCodes>::type CODES;
@@ -455,7 +455,8 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, const bool shar
             __syncthreads();                                  // (tiles are read no more)
             if (lane == 0) flags[wave] = codes.met != 0;
             __syncthreads();
-            if (threadIdx.x == 0) *odd = flags[0] | flags[1] | flags[2] | flags[3];
+            *odd = uniform(flags[0] | flags[1] | flags[2] | flags[3]) != 0;
+            __syncthreads();
         }
     }
     bool again = false;

@@ -295,11 +295,6 @@ static AttendPlan attend_plan(const fbq_attention_call &c, void *workspace)
         p.join = a.splits > 1 || a.n_shared;
         if (p.join) room(&a.part, a.splits * results);
     }
-    if (c.cache.desc.type == FBQ_BF16_4BIT && (!p.few || p.shared_many)) {
-        const long places = std::max(p.few ? 0L : attend4_odd_places(a, false), p.shared_many ? attend4_odd_places(a, true) : 0L);
-        a.odd = (int32_t *)((char *)workspace + at);
-        at += ((size_t)places * 4 + 255) / 256 * 256;
-    }
     p.bytes = at;
     return p;
 }
@@ -353,9 +348,7 @@ extern "C" fbq_status fbq_attention(const fbq_attention_call *c, void *workspace
     const auto launch_many = four ? launch_attend4_many : launch_attend_many;
     if (both) e = (four ? launch_attend4_both : launch_attend_both)(p.a, type, s);
     else if (p.shared_many) e = launch_many(p.a, type, true, s);
-    if (e == hipSuccess && p.shared_many && p.a.odd) e = launch_attend4_again(p.a, true, s);
     if (e == hipSuccess && !both) e = p.few ? launch_few(p.a, type, s) : launch_many(p.a, type, false, s);
-    if (e == hipSuccess && !p.few && p.a.odd) e = launch_attend4_again(p.a, false, s);
     if (e == hipSuccess && p.join) e = (type & ~4) == FBQ_F16 ? launch_join<TypeF16>(p.a, p.few, s) : launch_join<TypeBf16>(p.a, p.few, s);
     return e == hipSuccess ? FBQ_OK : FBQ_ERR_HIP;
 }
