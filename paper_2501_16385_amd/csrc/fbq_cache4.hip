@@ -7,7 +7,7 @@
 
 namespace fbq {
 
-// Append: a wave takes one head's new tokens of one block of 16, keys and values, a block four heads.  Lane l has token l % 16, features 32 w + 8 g .. of g = l / 16: a group's least and largest
+// Append: a wave takes one head's new tokens of one block of 16.  Lane l has token l % 16, features 32 w + 8 g .. of g = l / 16: a group's least and largest
 // are over a lane's own and three neighbours'.  Key codes are then the lane's own words.  Values lie four tokens to a word: their codes go through LDS, one byte each, and where some of a
 // word's tokens are not of this call the rest of the word is kept.  Nobody else writes the word: a partial page has one holder.
 // Of a block of 16's new tokens the first is the one that it is done for.  A grid block looks at WINDOW tokens for such ones: at one where rows have few, and its keys and values are then on their
@@ -19,7 +19,9 @@ __global__ __launch_bounds__(256) void fbq_append4_kernel(CacheArgs c, long laye
     constexpr int DS = 32 * NW, G = groups4(DS), kRow = DS + 16;
     __shared__ __attribute__((aligned(16))) unsigned char room[4][16 * kRow];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, slot = lane & 15, g = lane >> 4;
-    const int h = blockIdx.y * 4 + wave, head = min(h, c.kv_heads - 1);
+    // (at one token a wave makes the keys or the values alone: half as long a chain)
+    const int h = WINDOW == 1 ? blockIdx.y * 2 + (wave >> 1) : blockIdx.y * 4 + wave, head = min(h, c.kv_heads - 1);
+    const bool has_keys = WINDOW > 1 || (wave & 1) == 0, has_values = WINDOW > 1 || (wave & 1);
     const long head_bytes = (c.page_bytes >> 1) / c.kv_heads;
 
     word4_t x[2][NW];
@@ -66,7 +68,7 @@ __global__ __launch_bounds__(256) void fbq_append4_kernel(CacheArgs c, long laye
 #pragma unroll
         for (int j = 0; j < 4; ++j)
             if (4 * g + j < s0 || 4 * g + j >= s1) keep |= 0xffu << 8 * byte_of_token4(j);
-        const bool writes = h < c.kv_heads && keep != 0xffffffffu;
+        const bool writes = has_values && h < c.kv_heads && keep != 0xffffffffu;
         uint32_t *const words = reinterpret_cast<uint32_t *>(values + codes_at4(place, DS)) + lane * NW;          // (lane = 16 g + r)
 #pragma unroll
         for (int w = 0; w < NW; ++w) old[w] = writes && keep ? words[w] : 0;
@@ -88,6 +90,7 @@ __global__ __launch_bounds__(256) void fbq_append4_kernel(CacheArgs c, long laye
         uint32_t key_codes[NW];
 #pragma unroll
         for (int which = 0; which < 2; ++which) {
+            if (!(which ? has_values : has_keys)) continue;
 #pragma unroll
             for (int y = 0; y < G; ++y) {
                 // halves throughout, so that no difference is beyond fp32 (of bf16 numbers)
@@ -133,7 +136,7 @@ __global__ __launch_bounds__(256) void fbq_append4_kernel(CacheArgs c, long laye
                 }
             }
         }
-        if (mine) {
+        if (mine && has_keys) {
             uint32_t *const to = reinterpret_cast<uint32_t *>(keys + codes_at4(place, DS)) + (slot * 4 + g) * NW;
 #pragma unroll
             for (int w = 0; w < NW; ++w) to[w] = key_codes[w];
@@ -167,7 +170,7 @@ static hipError_t launch_append(const CacheArgs &c, long layer_offset, int T, co
 {
     const auto go = [&](auto few, auto many) {
         const bool wide = q_start && T > 4L * c.rows;
-        hipLaunchKernelGGL(wide ? many : few, dim3(wide ? ceil_div(T, 16) : T, ceil_div(c.kv_heads, 4)), dim3(256), 0, stream, c, layer_offset, T, q_start, start, (const uint16_t *)k, k_stride,
+        hipLaunchKernelGGL(wide ? many : few, dim3(wide ? ceil_div(T, 16) : T, ceil_div(c.kv_heads, wide ? 4 : 2)), dim3(256), 0, stream, c, layer_offset, T, q_start, start, (const uint16_t *)k, k_stride,
                            (const uint16_t *)v, v_stride);
     };
     switch (features4(c.D) / 32) {
