@@ -27,6 +27,9 @@ __device__ __forceinline__ void copy4_to_lds(__amdgpu_buffer_rsrc_t buf, int lan
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(dst), "v"(lane_off), "s"(buf), "s"(row_off) : "m0");
 }
+// The same from an address of each lane's own.
+__device__ __forceinline__ void copy16_to_lds(const void *from, uint32_t dst) { asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(dst), "v"(from) : "m0"); }
+__device__ __forceinline__ void copy4_to_lds(const void *from, uint32_t dst) { asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(dst), "v"(from) : "m0"); }
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void *p, long bytes)
 {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, (int)bytes, 0x00020000);

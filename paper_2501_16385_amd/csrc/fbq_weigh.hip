@@ -3,11 +3,14 @@
 // The softmax's sums are known (lse), so a key's weights are exp(scale q . k - lse) and nothing runs along the keys.  S^T = K Q^T in v_mfma 16x16x32 as in fbq_attend_few.h; the exponentials are
 // added up in the lane and over its 16 columns at the end.
 //   few   up to 16 query rows of a key/value head (fbq_weigh_few_kernel): bound by reading the keys, half of what attention reads.  The waves of the grid share the steps of all rows and heads
-//         as attention's do (FewLine), a step's keys asked for a step ahead; there is nothing to join, since a key's sum is a wave's own.
-//   many  (fbq_weigh_many_kernel) bound by the exponentials and the products.  A wave keeps 64 keys as operands and goes through the query rows 16 at a time.  A block's four waves have 64 keys
-//         each, or, where a row of the table has many query rows, the same 64 keys and a fourth of the query tiles each, added up in LDS in a fixed order.
+//         as attention's do (FewLine), a step's keys asked for a step ahead; there is nothing to join, since a key's sum is a wave's own.  16 rows of about 1000 tokens, 32 heads of 128 in 16
+//         bits, 136 MB: 28 us.  (Written as attention's loop, two steps at a time, the same.)
+//   many  (fbq_weigh_many_kernel) bound by vector instructions and matrix products one behind the other in two waves a SIMD.  A wave keeps 64 keys as operands and goes through the query rows 16
+//         at a time, which come through LDS.  One, two or all four of a block's waves have the same 64 keys, and share the query tiles; their sums are added up in LDS in a fixed order.
+//         us, two rows of 4000 tokens, 512 of them queries, 32 heads of 128 to 8 of the keys': 66 in 4 bits, 47 in 16 (queries from memory as operands: 75 and 68; all four waves with
+//         the same keys, too: 78 and 72); 16000 tokens: 221 in 4 bits (252, 274).
 // Codes of 4 bits: few, as in fbq_attend4_few.h; many, as small whole numbers of the queries' type, exactly, and scales come in behind the product, in 32 bits: the matrix cores spread them over
-// the lanes once for 64 keys, and make m sum(q) of the sums of q over a group in parts of 16 bits.
+// the lanes once for 64 keys, and make m sum(q) of the sums of q over a group in parts of 16 bits, three of them (what bf16 leaves is 2^-24 of a sum), so that weights are as exact as lse is.
 #include <algorithm>
 #include <cmath>
 
@@ -27,13 +30,15 @@ struct WeighArgs {
     float *out;
     int width, parts;                    // blocks of a row and head
     float decay;
-    bool few, together;                  // few: the few-row kernel; together: a block's waves have the same keys
+    bool few;                            // the few-row kernel
+    int log_share;                       // many rows: 2 to this waves of a block have the same keys, and a share of the query tiles each
 };
 
 // Eight codes of a word as numbers of the type, features in their order.
 struct WholeF16 : TypeF16 {
     typedef NumberF16 Number;
     static constexpr uint32_t kOne = 0x3c003c00u;
+    static constexpr bool kWide = false;
     static __device__ __forceinline__ word4_t codes(uint32_t w)
     {
         typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
@@ -44,6 +49,7 @@ struct WholeF16 : TypeF16 {
 struct WholeBf16 : TypeBf16 {
     typedef NumberBf16 Number;
     static constexpr uint32_t kOne = 0x3f803f80u;
+    static constexpr bool kWide = true;                       // has fp32's range
     static __device__ __forceinline__ word4_t codes(uint32_t w)
     {
         const auto low = [](uint32_t c) { return pack((float)(c & 15), (float)(c >> 16 & 15)); };
@@ -209,7 +215,9 @@ __global__ __launch_bounds__(64 * kWeighWaves, NW > 4 ? 1 : 2) void fbq_weigh_ma
 {
     constexpr int DS = 32 * NW, G = groups4(DS), kTiles = kWeighKeys / 16;
     typedef typename TY::Number NT;
+    constexpr int kPieces = 4 * NW, kBuffer = 1024 * NW + 256;                // a tile's queries, 16 bytes a piece, and their lse
     __shared__ float sums[kWeighWaves][kWeighKeys];
+    __shared__ __attribute__((aligned(16))) unsigned char room[kWeighWaves][2][kBuffer];
     const AttendArgs &a = w.a;
     const int lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4, wave = uniform(threadIdx.x >> 6);
     const int h = blockIdx.x % a.kv_heads, b = blockIdx.x / a.kv_heads, D = a.D, ps1 = (1 << a.log_ps) - 1;
@@ -218,12 +226,15 @@ __global__ __launch_bounds__(64 * kWeighWaves, NW > 4 ? 1 : 2) void fbq_weigh_ma
     const int q0 = uniform(of.x), nq = uniform(of.y), tokens = uniform(row_tokens(a, b)), limit = min(tokens, w.width);
     const long head_bytes = (a.page_bytes >> 1) / a.kv_heads, at = ((long)b * a.kv_heads + h) * w.width;
     const int32_t *const list = a.table + (long)b * a.max_pages;
-    const float unit = (a.q_xor ? -a.scale : a.scale) * (FOUR ? 128.0f : 1.0f);          // (a sign is the scale's here)
-    const int a_block = w.together ? kWeighKeys : kWeighWaves * kWeighKeys, stride = w.parts * a_block;
+    // (A sign is the scale's here.)  Codes of bf16: the scale goes into the keys' scales and the sums of q, and sums begin at -lse.  In fp16, whose range an arbitrary scale would leave, it comes
+    // in with lse, sums of q are 2^-7 of them, and what is left of them 2^12.
+    constexpr bool kFolded = FOUR && TY::kWide;
+    const float unit = (a.q_xor ? -a.scale : a.scale) * (FOUR && !kFolded ? 128.0f : 1.0f);
+    const int share = 1 << w.log_share, part = wave & (share - 1), a_block = kWeighKeys * (kWeighWaves >> w.log_share), stride = w.parts * a_block;
     const int rows = nq * a.group, tiles = (rows + 15) / 16;
 
     for (int base = blockIdx.y * a_block; base < limit; base += stride) {
-        const int key0 = base + (w.together ? 0 : wave * kWeighKeys);
+        const int key0 = base + (wave >> w.log_share) * kWeighKeys;
         word4_t k[kTiles][NW];
         uint32_t words[kTiles];                               // 4 bits: scale word of key l % 16, group l / 16
 #pragma unroll
@@ -252,32 +263,67 @@ __global__ __launch_bounds__(64 * kWeighWaves, NW > 4 ? 1 : 2) void fbq_weigh_ma
 #pragma unroll
                 for (int x = 0; x < NW; ++x) k[t][x] = TY::codes(k[t][x][0]);
         }
-        float4_t scales[kTiles][FOUR ? G : 1];                // 2^-7 of the lane's four keys' (so that sums of q, times as much, are in fp16's range)
+        float4_t scales[kTiles][FOUR ? G : 1];                // of the lane's four keys, 2^-7 of them as of the sums of q, or times the scale
         if constexpr (FOUR) {
 #pragma unroll
             for (int t = 0; t < kTiles; ++t)
 #pragma unroll
-                for (int y = 0; y < G; ++y) scales[t][y] = scales_of<TY>(words[t], word2_t{grp == y ? NT::bits(0x1p-7f) << 16 : 0u, 0u});
+                for (int y = 0; y < G; ++y) {
+                    scales[t][y] = scales_of<TY>(words[t], word2_t{grp == y ? NT::bits(kFolded ? 1.0f : 0x1p-7f) << 16 : 0u, 0u});
+                    if (kFolded) scales[t][y] *= unit;
+                }
         }
         float4_t sum[kTiles];
 #pragma unroll
         for (int t = 0; t < kTiles; ++t) sum[t] = float4_t{0, 0, 0, 0};
 
-        struct Queries { word4_t q[NW]; float lse; int sees; };
-        // (rows past the last one are that one, and see nothing; features past the last are zeros: only words from kSure on can have some)
+        // Tiles of queries come through LDS, two ahead: a row's sixteen pieces are neighbours' copies, where operands read from memory are sixteen rows' pieces and take four times as long.
+        // Piece p of a row lies at p ^ swap.  (Rows past the last one are that one; words from kSure on can have features past the last: these are zeros.)
         constexpr int kSure = NW == 2 ? 0 : NW == 8 ? 6 : NW == 6 ? 4 : NW - 1;
-        auto ask = [&](Queries &x, int tile) __attribute__((always_inline)) {
-            const int r = tile * 16 + col, row = min(r, rows - 1), i = row / a.group, head = h * a.group + row - i * a.group, t = q0 + i;
-            x.sees = r < rows ? tokens - nq + i + 1 : 0;
-            x.lse = a.lse[(long)t * a.heads + head];
-            const uint16_t *const from = a.q + t * a.q_stride + head * D;
+        const auto swap = [](int row) { return kPieces == 8 ? piece_key(row) : kPieces == 12 ? row >> 2 & 3 : kPieces == 24 ? row & 7 : row & 15; };
+        const int first = uniform(max(0, (int)((long)max(key0 - (tokens - nq), 0) * a.group / 16)));   // the first tile with a row that sees the first key; those before see none of these
+        const int clear = uniform((int)(((long)max(key0 + kWeighKeys - 1 - (tokens - nq), 0) * a.group + 15) / 16));   // from this one on all rows see all keys
+        const long tokens_on = 16 * share / a.group;          // from a wave's tile to its next, where it is whole tokens
+        const bool even = 16 * share % a.group == 0;
+        int tile = first + part;
+        const unsigned char *from[NW];
+        const float *lse_from;
+        auto place = [&](int tile) __attribute__((always_inline)) {
+            const auto row = [&](int r, long *token) { r = min(16 * tile + r, rows - 1); const int i = r / a.group; *token = q0 + i; return h * a.group + r - i * a.group; };
+            long t;
 #pragma unroll
-            for (int y = 0; y < NW; ++y) {
-                const int d = 32 * y + 8 * grp;
-                x.q[y] = *reinterpret_cast<const word4_t *>(from + (y < kSure || d < D ? d : 0));
+            for (int x = 0; x < NW; ++x) {
+                const int r = (64 * x + lane) / kPieces, p = (64 * x + lane) % kPieces ^ swap(r), head = row(r, &t);
+                from[x] = reinterpret_cast<const unsigned char *>(a.q + t * a.q_stride + head * D + (8 * p < D ? 8 * p : 0));
             }
+            const int head = row(col, &t);
+            lse_from = a.lse + t * a.heads + head;
         };
-        auto add = [&](Queries &x) __attribute__((always_inline)) {
+        auto copy = [&](int to) __attribute__((always_inline)) {
+            const uint32_t at = uniform(lds_offset(room[wave][to]));
+#pragma unroll
+            for (int x = 0; x < NW; ++x) copy16_to_lds(from[x], at + 1024 * x);
+            copy4_to_lds(lse_from, at + 1024 * NW);
+        };
+        struct { word4_t q[NW]; float lse; } x;
+        auto add = [&](int in) __attribute__((always_inline)) {
+            if (tile + share < tiles) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(NW + 1) : "memory");
+            else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#pragma unroll
+            for (int y = 0; y < NW; ++y) x.q[y] = *reinterpret_cast<const word4_t *>(room[wave][in] + (col * kPieces + ((4 * y + grp) ^ swap(col))) * 16);
+            x.lse = *reinterpret_cast<const float *>(room[wave][in] + 1024 * NW + lane * 4);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            const int next = tile + 2 * share;
+            if (next < tiles) {
+                if (even && 16 * next + 16 <= rows) {
+#pragma unroll
+                    for (int y = 0; y < NW; ++y) from[y] += tokens_on * a.q_stride * 2;
+                    lse_from += tokens_on * a.heads;
+                } else {
+                    place(next);
+                }
+                copy(in);
+            }
 #pragma unroll
             for (int y = kSure; y < NW; ++y)
                 if (32 * y + 8 * grp >= D) x.q[y] = word4_t{0, 0, 0, 0};
@@ -287,8 +333,9 @@ __global__ __launch_bounds__(64 * kWeighWaves, NW > 4 ? 1 : 2) void fbq_weigh_ma
                 for (int y = 0; y < NW; ++y) x.q[y] = word4_t{0, 0, 0, 0};
             }
             float4_t z[kTiles];
+            const float less = x.lse * 1.4426950408889634f;
             if constexpr (FOUR) {
-                // 2^-7 of the sum of q over group l / 16, and 2^12 of what is left of it in two parts
+                // the sum of q over group l / 16, times the scale or 2^-7, and what is left of it in two parts
                 const word4_t one{TY::kOne, TY::kOne, TY::kOne, TY::kOne};
                 word2_t high{0, 0}, rest{0, 0};
                 float4_t sums[G];
@@ -298,57 +345,52 @@ __global__ __launch_bounds__(64 * kWeighWaves, NW > 4 ? 1 : 2) void fbq_weigh_ma
                     sums[y] = TY::mfma(one, x.q[2 * y], float4_t{0, 0, 0, 0});
                     if (2 * y + 1 < NW) sums[y] = TY::mfma(one, x.q[std::min(2 * y + 1, NW - 1)], sums[y]);
                 }
-                // two tiles' products at a time, and nothing of the next two before their sums (or the compiler puts each product before its use, and waits for it)
+                // (products that follow from each other stand apart)
+                float4_t c[kTiles][G], lower[kTiles];
 #pragma unroll
-                for (int t0 = 0; t0 < kTiles; t0 += 2) {
-                    float4_t c[2][G], lower[2];
+                for (int half = 0; half < 2; ++half)
 #pragma unroll
-                    for (int t = 0; t < 2; ++t)
+                    for (int y = 0; y < G; ++y)
 #pragma unroll
-                        for (int y = 0; y < G; ++y) {
-                            c[t][y] = TY::mfma(k[t0 + t][2 * y], x.q[2 * y], float4_t{0, 0, 0, 0});
-                            if (2 * y + 1 < NW) c[t][y] = TY::mfma(k[t0 + t][std::min(2 * y + 1, NW - 1)], x.q[std::min(2 * y + 1, NW - 1)], c[t][y]);
+                        for (int t = 0; t < kTiles; ++t) {
+                            if (half == 0) c[t][y] = TY::mfma(k[t][2 * y], x.q[2 * y], float4_t{0, 0, 0, 0});
+                            else if (2 * y + 1 < NW) c[t][y] = TY::mfma(k[t][std::min(2 * y + 1, NW - 1)], x.q[std::min(2 * y + 1, NW - 1)], c[t][y]);
                         }
-                    if (t0 == 0) {
 #pragma unroll
-                        for (int y = 0; y < G; ++y) sum = grp == y ? sums[y][0] * 0x1p-7f : sum;
-                        high[0] = NT::bits(sum);
-                        const float left = (sum - NT::of(high[0])) * 0x1p12f;
-                        rest[0] = NT::bits(left);
-                        rest[1] = NT::bits(left - NT::of(rest[0]));
-                    }
-#pragma unroll
-                    for (int t = 0; t < 2; ++t) {
-                        z[t0 + t] = TY::mfma(word2_t{words[t0 + t], 0u}, high, float4_t{0, 0, 0, 0});
-                        lower[t] = TY::mfma(word2_t{words[t0 + t], words[t0 + t]}, rest, float4_t{0, 0, 0, 0});
-                    }
-                    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                    for (int t = 0; t < 2; ++t)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-#pragma unroll
-                            for (int y = 0; y < G; ++y) z[t0 + t][i] = __builtin_fmaf(scales[t0 + t][y][i], c[t][y][i], z[t0 + t][i]);
-                            z[t0 + t][i] = __builtin_fmaf(lower[t][i], 0x1p-12f, z[t0 + t][i]);
-                        }
-                    if (t0 + 2 < kTiles) __builtin_amdgcn_sched_barrier(0);
-                }
-            } else {
+                for (int y = 0; y < G; ++y) sum = grp == y ? sums[y][0] * (kFolded ? unit : 0x1p-7f) : sum;
+                high[0] = NT::bits(sum);
+                const float left = (sum - NT::of(high[0])) * (kFolded ? 1.0f : 0x1p12f);
+                rest[0] = NT::bits(left);
+                rest[1] = NT::bits(left - NT::of(rest[0]));
 #pragma unroll
                 for (int t = 0; t < kTiles; ++t) {
-                    z[t] = float4_t{0, 0, 0, 0};
-#pragma unroll
-                    for (int y = 0; y < NW; ++y) z[t] = TY::mfma(k[t][y], x.q[y], z[t]);
+                    z[t] = TY::mfma(word2_t{words[t], 0u}, high, kFolded ? float4_t{-less, -less, -less, -less} : float4_t{0, 0, 0, 0});
+                    lower[t] = TY::mfma(word2_t{words[t], words[t]}, rest, kFolded ? z[t] : float4_t{0, 0, 0, 0});
                 }
                 __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        float x = kFolded ? lower[t][i] : z[t][i];
+#pragma unroll
+                        for (int y = 0; y < G; ++y) x = __builtin_fmaf(scales[t][y][i], c[t][y][i], x);
+                        if (!kFolded) x = __builtin_fmaf(__builtin_fmaf(lower[t][i], 0x1p-12f, x), unit, -less);
+                        z[t][i] = __builtin_amdgcn_exp2f(x);
+                    }
+            } else {
+#pragma unroll
+                for (int y = 0; y < NW; ++y)
+#pragma unroll
+                    for (int t = 0; t < kTiles; ++t) z[t] = TY::mfma(k[t][y], x.q[y], y ? z[t] : float4_t{0, 0, 0, 0});
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) z[t][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[t][i], unit, -less));
             }
-            const float less = x.lse * 1.4426950408889634f;
-#pragma unroll
-            for (int t = 0; t < kTiles; ++t)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) z[t][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[t][i], unit, -less));
-            if (__ballot(x.sees < key0 + kWeighKeys)) {       // some row does not see all of the keys
-                const int sees = x.sees - key0 - 4 * grp;
+            if (tile < clear || 16 * tile + 16 > rows) {      // some row does not see all of the keys
+                const int r = 16 * tile + col, sees = (r < rows ? tokens - nq + r / a.group + 1 : 0) - key0 - 4 * grp;
                 asm volatile("");
 #pragma unroll
                 for (int t = 0; t < kTiles; ++t)
@@ -359,23 +401,14 @@ __global__ __launch_bounds__(64 * kWeighWaves, NW > 4 ? 1 : 2) void fbq_weigh_ma
 #pragma unroll
             for (int t = 0; t < kTiles; ++t) sum[t] += z[t];
         };
-        // the first tile with a row that sees the first key; those before see none of these
-        const int first = uniform(max(0, (int)((long)max(key0 - (tokens - nq), 0) * a.group / 16)));
-        const int step = w.together ? kWeighWaves : 1;
-        int tile = first + (w.together ? wave : 0);
         if (key0 < limit && tile < tiles) {
-            Queries x0, x1;
-            ask(x0, tile);
-            while (true) {
-                ask(x1, min(tile + step, tiles - 1));         // (always as many loads: then the waits for those before know how many came behind)
-                add(x0);
-                tile += step;
-                if (tile >= tiles) break;
-                ask(x0, min(tile + step, tiles - 1));
-                add(x1);
-                tile += step;
-                if (tile >= tiles) break;
+            place(tile);
+            copy(0);
+            if (tile + share < tiles) {
+                place(tile + share);
+                copy(1);
             }
+            for (int in = 0; tile < tiles; tile += share, in ^= 1) add(in);
         }
         // lane (grp, col) takes key 16 (col / 4) + 4 grp + col % 4
         float mine = 0;
@@ -387,12 +420,13 @@ __global__ __launch_bounds__(64 * kWeighWaves, NW > 4 ? 1 : 2) void fbq_weigh_ma
                 mine = col == 4 * t + i ? all : mine;
             }
         const int key = key0 + 16 * (col >> 2) + 4 * grp + (col & 3);
-        if (w.together) {
+        if (share > 1) {
             __syncthreads();                                  // (the sums may still be read from the keys before)
             sums[wave][lane] = mine;
             __syncthreads();
-            if (wave) continue;
-            mine = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
+            if (part) continue;
+            mine += sums[wave + 1][lane];
+            if (share == 4) mine += sums[2][lane] + sums[3][lane];
         }
         if (key < limit) {
             if (w.weights && key < tokens - nq) mine = __builtin_fmaf(w.weights[at + key], w.decay, mine);
@@ -457,9 +491,13 @@ extern "C" fbq_status fbq_attention_weights(const fbq_attention_call *c, const f
     w.few = (long)a.max_q * a.group <= kFewRows;
     const long steps = (((long)a.max_pages << a.log_ps) + kFewTile - 1) / kFewTile * a.rows * a.kv_heads;
     a.workers = (int)std::min(a.D > 128 ? 2048L : 4096L, (steps + kFewWaves - 1) / kFewWaves * kFewWaves);                 // (as many waves as the GPU holds)
-    w.together = (long)a.max_q * a.group > 16 * kWeighWaves;
-    const long most = std::min((long)a.max_pages << a.log_ps, (long)width), items = (long)a.rows * a.kv_heads;
-    const int a_block = w.together ? kWeighKeys : kWeighWaves * kWeighKeys;
+    // Making keys ready takes a wave about as long as ten tiles of queries: so many waves to the same keys as make rounds of the GPU's waves, times that and a share of the tiles, least.
+    const long most = std::min((long)a.max_pages << a.log_ps, (long)width), items = (long)a.rows * a.kv_heads, waves = (most + kWeighKeys - 1) / kWeighKeys * items;
+    const long tiles = ((long)a.max_q * a.group + 15) / 16, at_once = a.D > 128 ? 1024 : 2048;
+    const auto takes = [&](int log_share) { return ((waves << log_share) + at_once - 1) / at_once * (10 + (tiles >> log_share)); };
+    for (int x = 1; x <= 2; ++x)
+        if (takes(x) < takes(w.log_share)) w.log_share = x;
+    const int a_block = kWeighKeys * (kWeighWaves >> w.log_share);
     w.parts = (int)std::max(1L, std::min({(most + a_block - 1) / a_block, (kWeighBlocks + items - 1) / items, 65535L}));
     hipError_t e;
     switch (d.type) {

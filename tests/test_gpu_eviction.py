@@ -120,6 +120,14 @@ def test_weights_of_long_rows_and_many(bits):
 
 
 @pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("rows", [16, 33])
+@pytest.mark.parametrize("heads", [96, 128])
+def test_weights_of_many_heads_and_tokens(heads, rows, bits):
+    """Enough keys that two waves, or one, and not four, share 64 of them; 3 and 4 heads to one of the keys', so that a tile ends inside a token, and not."""
+    check_weights(bits, [128, 100, 61] + [20 + b for b in range(rows - 3)], [40, 33, 17] + [2] * (rows - 3), heads, 32, 64, 16, BF16 if heads == 96 else F16, seed=rows, decay=0.25)
+
+
+@pytest.mark.parametrize("bits", [16, 4])
 def test_weights_sum_to_what_was_asked(bits):
     """Each query's weights are one in all: the sums over a row's keys are its queries times heads; equal calls give equal bits."""
     import paper_2501_16385_amd as fbq
