@@ -121,6 +121,14 @@ def test_shared_tokens_are_read_apart_in_both_kernels():
     check([8192 + 3 * b for b in range(40)], [1] * 40, 8, 4, 128, 64, BF16, shared_pages=128, seed=6)
 
 
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("D,kv_heads,rows,count", [(64, 8, 18, 1), (80, 4, 30, 1), (128, 4, 18, 1), (192, 2, 24, 1), (64, 4, 34, 20), (136, 4, 18, 17)])
+def test_shared_tokens_of_the_many_row_kernel(D, kv_heads, rows, count, dtype):
+    """17 query rows and more of a head behind 8192 tokens, 256 MiB and more of the 16-bit rule's bytes: a launch with the rows' own tokens, or one of their own (192 features; 17 tokens and more)."""
+    assert 4 * 8192 * kv_heads * D * (rows - 1) >= 256 << 20
+    check([8192 + count + 7 * b for b in range(rows)], [count] + [1 + b % count for b in range(rows - 1)], kv_heads, kv_heads, D, 64, dtype, shared_pages=128, seed=D)
+
+
 @pytest.mark.parametrize("scale", [0.0, -0.3, 1e-8, 3.0])
 def test_scales(scale):
     check([90, 40], [1, 1], 4, 2, 64, 16, F16, seed=1, scale=scale, gain=1.0)
