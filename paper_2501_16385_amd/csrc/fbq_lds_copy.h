@@ -15,18 +15,11 @@ namespace fbq {
 // a copy waits for it by count and passes a barrier (both with a memory clobber).  The compiler's own counted waits only
 // get stricter by the copies it does not know of.  M0, the LDS address, is declared as overwritten: the compiler may keep a value there.
 __device__ __forceinline__ uint32_t lds_offset(const void *p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void *)p; }
-__device__ __forceinline__ void copy16_to_lds(__amdgpu_buffer_rsrc_t buf, int lane_off, int row_off, uint32_t dst)
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(dst), "v"(lane_off), "s"(buf), "s"(row_off) : "m0");
-}
-__device__ __forceinline__ void copy12_to_lds(__amdgpu_buffer_rsrc_t buf, int lane_off, int row_off, uint32_t dst)   // (12 bytes per lane, but 16 l apart in LDS)
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx3 %1, %2, %3 offen lds" ::"s"(dst), "v"(lane_off), "s"(buf), "s"(row_off) : "m0");
-}
-__device__ __forceinline__ void copy4_to_lds(__amdgpu_buffer_rsrc_t buf, int lane_off, int row_off, uint32_t dst)    // (4 bytes: dst + 4 l)
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(dst), "v"(lane_off), "s"(buf), "s"(row_off) : "m0");
-}
+#define FBQ_COPY_TO_LDS(load) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\t" load " %1, %2, %3 offen lds" ::"s"(dst), "v"(lane_off), "s"(buf), "s"(row_off) : "m0");
+__device__ __forceinline__ void copy16_to_lds(__amdgpu_buffer_rsrc_t buf, int lane_off, int row_off, uint32_t dst) { FBQ_COPY_TO_LDS("buffer_load_dwordx4") }
+__device__ __forceinline__ void copy12_to_lds(__amdgpu_buffer_rsrc_t buf, int lane_off, int row_off, uint32_t dst) { FBQ_COPY_TO_LDS("buffer_load_dwordx3") }   // (12 bytes per lane, but 16 l apart in LDS)
+__device__ __forceinline__ void copy4_to_lds(__amdgpu_buffer_rsrc_t buf, int lane_off, int row_off, uint32_t dst) { FBQ_COPY_TO_LDS("buffer_load_dword") }      // (4 bytes: dst + 4 l)
+#undef FBQ_COPY_TO_LDS
 // The same from an address of each lane's own.
 __device__ __forceinline__ void copy16_to_lds(const void *from, uint32_t dst) { asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(dst), "v"(from) : "m0"); }
 __device__ __forceinline__ void copy4_to_lds(const void *from, uint32_t dst) { asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(dst), "v"(from) : "m0"); }
