@@ -1,5 +1,7 @@
 // Keys and values of a cache in 4 bits on their way to the many-row kernel's LDS (fbq_attend_many.h): asked for in their codes, a step later made into 16 bits and put down where that
-// kernel reads them.  With 128 query rows to a block, rows are too many for scales that come in behind the products, as they do in fbq_attend4_few.h: m + s c is rounded to the operand once.
+// kernel reads them.  With 128 query rows to a block, rows are too many for scales that come in behind the products, as they do in fbq_attend4_few.h: m + s c is rounded to the operand once.  (Whole
+// codes of keys as operands, 32 scores a lane times a scale for each group: relative L2 against 64 bits 3.4e-4 instead of 5.7e-4 for scores with a standard deviation of 2 - the codes themselves are 0.19
+// off what they stand for there - and 254 us instead of 208 for 1000 tokens each behind 5000 of three rows, heads of 80.)
 // The operands are fp16 also for a cache of bf16 - queries too, times a power of two a row - since that is eight times as exact and takes half the instructions: relative L2 against 64 bits
 // 1.7e-3 instead of 4.2e-3, of which rounding the result is 1.6e-3.  That wants scales from 2^-13 to 2^11 and lowest values up to 2^15 (or groups of zeros); a block that meets others does
 // its work again with operands of bf16.

@@ -117,7 +117,10 @@ struct FewLine {
         if (to.h == a.kv_heads) {
             to.h = 0;
             do {
-                if (++to.b >= a.rows) return false;           // (not unless lengths change under the call)
+                if (++to.b >= a.rows) {                       // (not unless lengths change under the call; its pages may still be looked at)
+                    to.b = x.b;
+                    return false;
+                }
                 to.limit = uniform(row_tokens(a, to.b));
                 to.steps = uniform(few_steps(a, to.b, to.limit));
             } while (to.steps == 0);

@@ -5,7 +5,9 @@
 // Choosing: the least weight that stays is found 11 bits at a time from counts of the digits in LDS (whole numbers: their order does not matter); of those equal to it the earliest stay.
 // Moving is in place: position i takes token src[i] >= i.  A block has some columns - 64 bytes of every key, or value - of one row and head to itself and goes through the positions upwards: a
 // round's tokens are read before the round before it is written, and all that is written lies before all that is still to be read.  Bound by HBM: every token that moves is read and written
-// once.
+// once.  16 rows of up to 1280 tokens to 1024, 4 layers of 8 heads of 128 in 16 bits: 110 us for 533 MB (4.9 TB/s, as a large copy; of lines of 128 bytes that are read for 64 the rest is another
+// block's of the same XCD).  3 rows of up to 8500 to 6000, heads of 80: 370 MB in 115, few blocks that go through long rows.  Choosing takes 9 to 15 us for rows up to 2048, 22 for 8500: three passes over the
+// digits and one over the tokens, each a few barriers.
 #include <algorithm>
 
 #include "fbq_attend.h"

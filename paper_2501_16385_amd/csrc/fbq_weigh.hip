@@ -7,8 +7,8 @@
 //         bits, 136 MB: 28 us.  (Written as attention's loop, two steps at a time, the same.)
 //   many  (fbq_weigh_many_kernel) bound by vector instructions and matrix products one behind the other in two waves a SIMD.  A wave keeps 64 keys as operands and goes through the query rows 16
 //         at a time, which come through LDS.  One, two or all four of a block's waves have the same 64 keys, and share the query tiles; their sums are added up in LDS in a fixed order.
-//         us, two rows of 4000 tokens, 512 of them queries, 32 heads of 128 to 8 of the keys': 66 in 4 bits, 47 in 16 (queries from memory as operands: 75 and 68; all four waves with
-//         the same keys, too: 78 and 72); 16000 tokens: 221 in 4 bits (252, 274).
+//         us, two rows of 4000 tokens, 512 of them queries, 32 heads of 128 to 8 of the keys': 63 in 4 bits, 45 in 16 (queries from memory as operands: 75 and 68; all four waves with
+//         the same keys, too: 78 and 72); 16000 tokens: 207 in 4 bits (252, 274).
 // Codes of 4 bits: few, as in fbq_attend4_few.h; many, as small whole numbers of the queries' type, exactly, and scales come in behind the product, in 32 bits: the matrix cores spread them over
 // the lanes once for 64 keys, and make m sum(q) of the sums of q over a group in parts of 16 bits, three of them (what bf16 leaves is 2^-24 of a sum), so that weights are as exact as lse is.
 #include <algorithm>
