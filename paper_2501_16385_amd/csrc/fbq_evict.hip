@@ -3,11 +3,10 @@
 // Three launches: which tokens of each layer, row and head stay, and their weights; the tokens moved; tables, lengths and pages.  What is cut back is decided by the first from the pages as they
 // are before the call, by every block for its row.
 // Choosing: the least weight that stays is found 11 bits at a time from counts of the digits in LDS (whole numbers: their order does not matter); of those equal to it the earliest stay.
-// Moving is in place: position i takes token src[i] >= i.  A block has some columns - 64 bytes of every key, or value - of one row and head to itself and goes through the positions upwards: a
+// Moving is in place: position i takes token src[i] >= i.  A block has some columns - 128 bytes of every key, say - of one row and head to itself and goes through the positions upwards: a
 // round's tokens are read before the round before it is written, and all that is written lies before all that is still to be read.  Bound by HBM: every token that moves is read and written
-// once.  16 rows of up to 1280 tokens to 1024, 4 layers of 8 heads of 128 in 16 bits: 110 us for 533 MB (4.9 TB/s, as a large copy; of lines of 128 bytes that are read for 64 the rest is another
-// block's of the same XCD).  3 rows of up to 8500 to 6000, heads of 80: 370 MB in 115, few blocks that go through long rows.  Choosing takes 9 to 15 us for rows up to 2048, 22 for 8500: three passes over the
-// digits and one over the tokens, each a few barriers.
+// once.  16 rows of up to 1280 tokens to 1024, 4 layers of 8 heads of 128 in 16 bits: 105 us for 533 MB (5.0 TB/s, as a large copy).  3 rows of up to 8500 to 6000, heads of 80: 89 for 370 MB, few
+// blocks that go through long rows.  Choosing takes 9 to 15 us for rows up to 2048, 22 for 8500: three passes over the digits and one over the tokens, each a few barriers.
 #include <algorithm>
 
 #include "fbq_attend.h"
@@ -19,7 +18,8 @@ namespace fbq {
 constexpr int kChooseEach = 4;           // weights a thread and round of the choosing
 constexpr int kShortRows = 2048;         // up to so many weights a row a block of 256 chooses, else one of 1024
 constexpr int kDigits = 2048;
-constexpr int kMoveThreads = 256;        // (what four threads a token, and sixteen four tokens, count on)
+template <bool FOUR>
+constexpr int kMoveThreads = FOUR ? 256 : 512;                // (4 bits: what four threads a token, and sixteen four tokens, count on)
 constexpr int kEvictBlocks = 1 << 20;    // of a grid at most; they go on with every so manieth item
 
 struct EvictArgs {
@@ -172,17 +172,18 @@ __global__ __launch_bounds__(THREADS) void fbq_evict_choose_kernel(const EvictAr
     }
 }
 
-// What a block has to itself of an item: 64 bytes of a row of bytes that every token has (a key or value of 16 bits, a key's codes), the four bytes each of a token's scales, or, of value codes of
-// 4 bits, 16 words of every four tokens.
+// What a block has to itself of an item.  16 bits: 128 bytes of every key, or value, where they are so many lines of 128, else all of it: a line that two blocks write in parts goes out twice (in pieces of
+// 64 bytes 16 rows of 1280 to 1024 tokens, 128 features, took 110 us for 105, 3 of 8500 to 6000, 80 features, 116 for 89).  4 bits, where wider pieces leave too few blocks (112 for 85 and 211 for
+// 103, calls as a whole): 64 bytes of a key's codes, the four bytes each of a token's scales, or, of value codes, 16 words of every four tokens.
 struct MovePart {
     bool values, codes;                  // codes: the value codes of 4 bits
-    int at, end, row;                    // bytes at .. end of rows of `row` bytes; of value codes the first word
+    int at, end, row;                    // bytes at .. end of rows of `row` bytes (16 bits) or at .. at + 64 of it (4); of value codes the first word
     bool scales;
 };
 template <bool FOUR>
 __host__ __device__ __forceinline__ int move_parts(int D)
 {
-    if (!FOUR) return 2 * ((2 * D + 63) / 64);
+    if (!FOUR) return 2 * (D % 64 ? 1 : D / 64);
     const int DS = features4(D);
     return (DS / 2 + 63) / 64 + DS / 32 + 2;
 }
@@ -191,8 +192,8 @@ template <bool FOUR>
 __device__ __forceinline__ MovePart move_part(int D, int i)
 {
     if (!FOUR) {
-        const int n = (2 * D + 63) / 64;
-        return MovePart{i >= n, false, 64 * (i % n), 2 * D, 2 * D, false};
+        const int n = D % 64 ? 1 : D / 64, width = 2 * D / n, at = i % n * width;
+        return MovePart{i >= n, false, at, at + width, 2 * D, false};
     }
     const int DS = features4(D), n = (DS / 2 + 63) / 64;
     if (i < n) return MovePart{false, false, 64 * i, DS / 2, DS / 2, false};
@@ -200,15 +201,15 @@ __device__ __forceinline__ MovePart move_part(int D, int i)
     return MovePart{i > n + DS / 32, false, 0, 4 * groups4(DS), 4 * groups4(DS), true};
 }
 
-// Rows of a token each: four threads a token, a piece W each, kEach tokens a thread and round; two rounds' at a time.  place: of a token by where it lies; where: position i's.
-template <class W, class Place, class Where>
-__device__ __forceinline__ void move_rows(const int32_t *__restrict__ src, int lowest, int keep, bool there, Place place, Where where)
+// Rows of a token each: `step` tokens a pass, this thread's token of them `mine`, a piece W of it; EACH passes a round; two rounds' at a time.  place: of a token by where it lies; where: position i's.
+template <class W, int EACH, class Place, class Where>
+__device__ __forceinline__ void move_rows(const int32_t *__restrict__ src, int lowest, int keep, int step, int mine, bool there, Place place, Where where)
 {
-    constexpr int kStep = kMoveThreads / 4, kEach = 8;
+    constexpr int kEach = EACH;
     struct Round { int from[kEach]; W v[kEach]; };
     const auto read = [&](Round &x, int i0) __attribute__((always_inline)) {
 #pragma unroll
-        for (int y = 0; y < kEach; ++y) x.from[y] = src[min(i0 + y * kStep + ((int)threadIdx.x >> 2), keep - 1)];
+        for (int y = 0; y < kEach; ++y) x.from[y] = src[min(i0 + y * step + mine, keep - 1)];
 #pragma unroll
         for (int y = 0; y < kEach; ++y)
             if (there) x.v[y] = *reinterpret_cast<const W *>(place(x.from[y]));
@@ -216,24 +217,24 @@ __device__ __forceinline__ void move_rows(const int32_t *__restrict__ src, int l
     const auto write = [&](const Round &x, int i0) __attribute__((always_inline)) {
 #pragma unroll
         for (int y = 0; y < kEach; ++y) {
-            const int i = i0 + y * kStep + ((int)threadIdx.x >> 2), to = where(min(i, keep - 1));
+            const int i = i0 + y * step + mine, to = where(min(i, keep - 1));
             if (there && i < keep && to != x.from[y]) *reinterpret_cast<W *>(place(to)) = x.v[y];
         }
     };
     Round a, b;
     read(a, lowest);
-    for (int i0 = lowest; i0 < keep; i0 += 2 * kStep * kEach) {
-        read(b, i0 + kStep * kEach);
+    for (int i0 = lowest; i0 < keep; i0 += 2 * step * kEach) {
+        read(b, i0 + step * kEach);
         __syncthreads();                                      // (all have read the round that is written, and those behind it read later lie behind it)
         write(a, i0);
-        read(a, i0 + 2 * kStep * kEach);
+        read(a, i0 + 2 * step * kEach);
         __syncthreads();
-        write(b, i0 + kStep * kEach);
+        write(b, i0 + step * kEach);
     }
 }
 
 template <bool FOUR>
-__global__ __launch_bounds__(kMoveThreads) void fbq_evict_move_kernel(const EvictArgs e)
+__global__ __launch_bounds__(kMoveThreads<FOUR>, FOUR ? 2 : 4) void fbq_evict_move_kernel(const EvictArgs e)
 {
     const CacheArgs &c = e.c;
     const int tid = threadIdx.x, ps1 = (1 << c.log_ps) - 1, parts = move_parts<FOUR>(c.D), DS = features4(c.D);
@@ -254,18 +255,19 @@ __global__ __launch_bounds__(kMoveThreads) void fbq_evict_move_kernel(const Evic
         unsigned char *const heads = c.pool + layer * c.layer_bytes + (part.values ? c.page_bytes >> 1 : 0) + h * head_bytes;
         const auto head_of = [&](int at) { return heads + (long)(at >> c.log_ps) * c.page_bytes; };                 // of a token by where it lies
         const auto where = [&](int i) { return list[i >> c.log_ps] << c.log_ps | (i & ps1); };
-        if (FOUR && part.scales) {
+        if (!FOUR) {
+            const int pieces = (part.end - part.at) / 16, step = kMoveThreads<FOUR> / pieces, mine = tid / pieces, at = part.at + (tid - mine * pieces) * 16;
+            move_rows<word4_t, 6>(src, e.first, keep, step, mine, mine < step, [&](int token) { return head_of(token) + (long)(token & ps1) * part.row + at; }, where);
+        } else if (part.scales) {
             const int at = (tid & 3) * 4;
-            move_rows<uint32_t>(src, e.first, keep, at < part.end, [&](int token) { return head_of(token) + scales_at4(c.log_ps, token & ps1, DS) + at; }, where);
-        } else if (!FOUR || !part.codes) {
+            move_rows<uint32_t, 8>(src, e.first, keep, kMoveThreads<FOUR> / 4, tid >> 2, at < part.end, [&](int token) { return head_of(token) + scales_at4(c.log_ps, token & ps1, DS) + at; }, where);
+        } else if (!part.codes) {
             const int at = part.at + (tid & 3) * 16;
-            move_rows<word4_t>(src, e.first, keep, at < part.end, [&](int token) {
-                const int slot = token & ps1;
-                return head_of(token) + (FOUR ? codes_at4(slot, DS) + (slot & 15) * part.row : (long)slot * part.row) + at;
-            }, where);
+            move_rows<word4_t, 8>(src, e.first, keep, kMoveThreads<FOUR> / 4, tid >> 2, at < part.end,
+                                  [&](int token) { return head_of(token) + codes_at4(token & ps1, DS) + (token & 15) * part.row + at; }, where);
         } else {
             // four tokens' codes a word: each byte from where its token's is
-            constexpr int kStep = kMoveThreads / 16, kEach = 4;
+            constexpr int kStep = kMoveThreads<FOUR> / 16, kEach = 4;
             const int word = part.at + (tid & 15), words = DS / 2;            // of each four tokens
             const auto place = [&](int token) {
                 const int slot = token & ps1;
@@ -375,8 +377,8 @@ extern "C" fbq_status fbq_cache_evict(const fbq_cache *c, const float *weights, 
     hipError_t err = hipGetLastError();
     if (err == hipSuccess) {
         const dim3 grid((unsigned)std::min<long>(jobs, kEvictBlocks));
-        if (four) hipLaunchKernelGGL(fbq_evict_move_kernel<true>, grid, dim3(kMoveThreads), 0, s, e);
-        else hipLaunchKernelGGL(fbq_evict_move_kernel<false>, grid, dim3(kMoveThreads), 0, s, e);
+        if (four) hipLaunchKernelGGL(fbq_evict_move_kernel<true>, grid, dim3(kMoveThreads<true>), 0, s, e);
+        else hipLaunchKernelGGL(fbq_evict_move_kernel<false>, grid, dim3(kMoveThreads<false>), 0, s, e);
         err = hipGetLastError();
     }
     if (err == hipSuccess) {
