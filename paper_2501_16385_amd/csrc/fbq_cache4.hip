@@ -19,6 +19,7 @@ __global__ __launch_bounds__(256) void fbq_append4_kernel(CacheArgs c, long laye
                                                           const uint16_t *__restrict__ k, long k_stride, const uint16_t *__restrict__ v, long v_stride)
 {
     constexpr int DS = 32 * NW, G = groups4(DS), kRow = DS + 16;
+    constexpr int kSure = NW == 2 ? 0 : NW == 8 ? 6 : NW == 6 ? 4 : NW - 1;       // words before it have no feature past the last
     __shared__ __attribute__((aligned(16))) unsigned char room[4][16 * kRow];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, slot = lane & 15, g = lane >> 4;
     // (at one token a wave makes the keys or the values alone: half as long a chain)
@@ -118,24 +119,26 @@ __global__ __launch_bounds__(256) void fbq_append4_kernel(CacheArgs c, long laye
                 uint32_t word = s << 16 | NT::bits(2.0f * low);
                 if (odd) word = which ? 0u : NT::kNaN << 16;
                 if (mine && g == y) *reinterpret_cast<uint32_t *>((which ? values : keys) + scales_at4(c.log_ps, place + slot, DS) + 4 * y) = word;
+                const auto make = [&](auto quotient) __attribute__((always_inline)) {
 #pragma unroll
-                for (int w = 2 * y; w < std::min(2 * y + 2, NW); ++w) {
-                    uint32_t code[8];
+                    for (int w = 2 * y; w < std::min(2 * y + 2, NW); ++w) {
+                        // keys: nibble n is feature e, n with its bits in reverse; values: a byte each
+                        uint32_t lower = 0, upper = 0;        // features 0 .. 3 and 4 .. 7
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const uint32_t word = x[which][w][e >> 1];
-                        const float at = (e & 1 ? NT::of_upper(word) : NT::of(word & 0xffff)) * 0.5f - low, near = at * by;
-                        float q = __builtin_fmaf(__builtin_fmaf(-near, half, at), by, near);
-                        if (!plain) q = half > 0 ? at / half : 0.0f;
-                        code[e] = 32 * w + 8 * g < c.D ? (uint32_t)(int)fminf(fmaxf(rintf(q), 0.0f), 15.0f) : 0u;
+                        for (int e = 0; e < 8; ++e) {
+                            const uint32_t word = x[which][w][e >> 1];
+                            const float at = __builtin_fmaf(e & 1 ? NT::of_upper(word) : NT::of(word & 0xffff), 0.5f, -low), code = fminf(fmaxf(rintf(quotient(at)), 0.0f), 15.0f);
+                            const int byte = which ? e & 3 : (e & 1) << 1 | (e >> 1 & 1);
+                            if (e < 4) lower = __builtin_amdgcn_cvt_pk_u8_f32(code, byte, lower);
+                            else upper = __builtin_amdgcn_cvt_pk_u8_f32(code, byte, upper);
+                        }
+                        if (w >= kSure && 32 * w + 8 * g >= c.D) lower = upper = 0;
+                        if (which == 0) key_codes[w] = lower | upper << 4;
+                        else *reinterpret_cast<word2_t *>(&room[wave][slot * kRow + 32 * w + 8 * g]) = word2_t{lower, upper};
                     }
-                    if (which == 0) {                         // nibble n: feature e, n with its bits in reverse
-                        key_codes[w] = code[0] | code[4] << 4 | code[2] << 8 | code[6] << 12 | code[1] << 16 | code[5] << 20 | code[3] << 24 | code[7] << 28;
-                    } else {
-                        const word2_t bytes{code[0] | code[1] << 8 | code[2] << 16 | code[3] << 24, code[4] | code[5] << 8 | code[6] << 16 | code[7] << 24};
-                        *reinterpret_cast<word2_t *>(&room[wave][slot * kRow + 32 * w + 8 * g]) = bytes;
-                    }
-                }
+                };
+                if (plain) make([&](float at) { const float near = at * by; return __builtin_fmaf(__builtin_fmaf(-near, half, at), by, near); });
+                else make([&](float at) { return half > 0 ? at / half : 0.0f; });
             }
         }
         if (mine && has_keys) {
