@@ -11,8 +11,8 @@ namespace fbq {
 // are over a lane's own and three neighbours'.  Key codes are then the lane's own words.  Values lie four tokens to a word: their codes go through LDS, one byte each, and where some of a
 // word's tokens are not of this call the rest of the word is kept.  Nobody else writes the word: a partial page has one holder.
 // Of a block of 16's new tokens the first is the one that it is done for.  A grid block looks at WINDOW tokens for such ones: at one where rows have few, and its keys and values are then on their
-// way before it knows where they go; at 16 where they have many (16 times as many blocks that find nothing: 62 us for 4267 tokens of 32 heads, 36 this way).  At one a wave has the keys or the
-// values alone: 16 tokens of 32 heads 5.0 us for 6.6, a chain of loads, minima and quotients that no size shortens.  At 16: 70 MB read and 20 written, 2.5 TB/s, bound by the instructions that
+// way before it knows where they go; at 16 where they have many (16 times as many blocks that find nothing: 62 us for 4267 tokens of 32 heads, 33 this way).  At one a wave has the keys or the
+// values alone: 16 tokens of 32 heads 5.0 us for 6.6, a chain of loads, minima and quotients that no size shortens.  At 16, 70 MB read and 20 written: 2.7 TB/s, bound by the instructions that
 // make codes.
 template <class NT, int NW, int WINDOW>
 __global__ __launch_bounds__(256) void fbq_append4_kernel(CacheArgs c, long layer_offset, int T, const int32_t *__restrict__ q_start, const int32_t *__restrict__ start,
@@ -196,12 +196,13 @@ hipError_t launch_append4(const CacheArgs &c, int type, long layer_offset, int T
 }
 
 // Read: a block a token.  Four features a thread and step; what is written is seven times what is read, and bounds it (4267
-// tokens of 32 heads of 128, 140 MB written and 20 read: 36 us, 4.4 TB/s; a large copy moves 4.9).
+// tokens of 32 heads of 128, 140 MB written and 20 read: 32 us, 5.0 TB/s; a large copy moves 4.9).
 template <class NT, bool FOUR>
 __global__ __launch_bounds__(256) void fbq_cache_read_kernel(CacheArgs c, long layer_offset, const int32_t *__restrict__ q_start, const int32_t *__restrict__ start, float *__restrict__ k,
                                                              float *__restrict__ v)
 {
-    const int t = blockIdx.x;
+    // Sixteen tokens in a row on one XCD (blocks go round the eight in turn): four share words, and lines (36 us without).
+    const int of = blockIdx.x & 127, t = blockIdx.x - of + 128 <= gridDim.x ? blockIdx.x - of + (of & 7) * 16 + (of >> 3) : blockIdx.x;
     const int b = q_start ? row_of_token(q_start, c.rows, t) : t;
     if (b < 0) return;
     const int first = start[b];

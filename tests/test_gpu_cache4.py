@@ -136,6 +136,29 @@ def test_read(D, dtype, bits):
     assert all((x[1] == 8).all() and (x[2] == 8).all() and torch.equal(x[3].cpu(), values[0, int(table[3, 1]), i, :, 14].float()) for i, x in enumerate(table_out))
 
 
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("counts", [[300, 0, 1, 83], [128], [127], [40, 216, 5]])
+def test_read_of_many_tokens(counts, bits):
+    """A hundred and more in one call are what calls of one token a row give."""
+    import paper_2501_16385_amd as fbq
+    before = [7 + b for b in range(len(counts))]
+    pool, table, n, refs, _ = make_cache4([b + c for b, c in zip(before, counts)], 2, 72, 16, F16, seed=sum(counts))
+    cache = to_cache4(fbq, pool, table, n, refs, F16, 72)
+    if bits == 16:
+        x, table, n, refs = make_cache([b + c for b, c in zip(before, counts)], 2, 72, 16, F16, seed=sum(counts))
+        cache = fbq.Cache(x.cuda(), table.cuda(), n.cuda(), refs.cuda())
+    start = torch.tensor(before, dtype=torch.int32).cuda()
+    k, v = fbq.cache_read(cache, 0, sum(counts), start, q_start=starts(counts).cuda())
+    at = 0
+    for b, c in enumerate(counts):
+        for i in range(c):
+            ones = torch.full((len(counts),), -1, dtype=torch.int32)
+            ones[b] = before[b] + i
+            k1, v1 = fbq.cache_read(cache, 0, len(counts), ones.cuda())
+            assert torch.equal(k1[b], k[at]) and torch.equal(v1[b], v[at]), (b, i)
+            at += 1
+
+
 def test_read_follows_no_page_outside_the_pool():
     import paper_2501_16385_amd as fbq
     pool, table, n, refs, _ = make_cache4([40, 20], 2, 64, 16, F16)
