@@ -1,6 +1,6 @@
 // Attention of many query rows over a cache in 4 bits: the kernel of fbq_attend_many.h with keys and values made on their way to LDS (fbq_attend_codes.h).
-// Measured, 32 heads of 128: prompt of 2048 tokens in fp16 66 us, in bf16 87 (of 16 bits 53), 8192 630 and 740 (540); heads of 64 47 and 410 (36, 330), of 80 57 and 515 (45, 425).  What making
-// the operands takes is vector instructions, 160 a step of 64 keys beside the kernel's own 360.
+// Measured, 32 heads of 128: prompt of 2048 tokens in fp16 66 to 71 us from card to card, in bf16 86 (of 16 bits 53), 8192 630 to 690 and 715 (540); heads of 64 47 and 410 (36, 330), of 80 57 and 515
+// (45, 425).  What making the operands takes is vector instructions, 160 a step of 64 keys beside the kernel's own 360.
 #ifndef FBQ_ATTEND4_MANY_H
 #define FBQ_ATTEND4_MANY_H
 
@@ -17,8 +17,13 @@ __device__ __forceinline__ void attend4_many(const AttendArgs &a, bool shared, i
     attend_many<TY, DP, Codes<MAKE, NW, DP>>(a, shared, h, y, z, room, &odd);
     if constexpr (MAKE::kChecked) {
         if (!odd) return;
-        asm volatile("" : "+s"(h), "+s"(y), "+s"(z) : : "memory");           // (what was worked out from them the first time takes no registers until the second)
-        attend_many<TY, DP, Codes<MakeBf16, NW, DP>>(a, shared, h, y, z, room);
+        // What follows from the block, the lane and the arguments takes no registers until the second time: the arguments, each such kernel's first parameter, are read again.  (Kept from the first time
+        // they push others of the loop out to memory, whose loads wait for the codes under way: 97 us for 86 and 819 for 716, see above, 45 for 41 behind a shared prefix.)
+        asm volatile("" : "+s"(h), "+s"(y), "+s"(z) : : "memory");
+        typedef const __attribute__((address_space(4))) AttendArgs *Kept;
+        Kept again = (Kept)__builtin_amdgcn_kernarg_segment_ptr();
+        asm volatile("" : "+s"(again));
+        attend_many<TY, DP, Codes<MakeBf16, NW, DP>>(*(const AttendArgs *)again, shared, h, y, z, room);
     }
 }
 

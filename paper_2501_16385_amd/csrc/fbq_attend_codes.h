@@ -56,7 +56,8 @@ struct MakeF16 {
     typedef NumberF16 Number;
     typedef TypeF16 Operand;
     typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
-    static constexpr bool kChecked = false, kScaled = false;
+    // kChecked: scales may be out of its range; kScaled: queries become fp16 times a power of two a row; kTwice: of a kernel that may do its work again in another form
+    static constexpr bool kChecked = false, kScaled = false, kTwice = false;
     static __device__ __forceinline__ uint32_t scale_pair(uint32_t a, uint32_t b) { return (a >> 16) | (b & 0xffff0000u); }
     static __device__ __forceinline__ uint32_t low_pair(uint32_t a, uint32_t b) { return (a & 0xffff) | b << 16; }
     template <bool HIGH>
@@ -69,16 +70,15 @@ struct MakeF16 {
         return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(c, __builtin_bit_cast(half2_t, s), __builtin_bit_cast(half2_t, m)));
     }
 };
-struct MakeHalf : MakeF16 {              // a cache of bf16 in operands of fp16
+struct MakeHalf : MakeF16 {              // a cache of bf16 in operands of fp16: its scale words become fp16 on their way to the lanes that need them
     typedef NumberBf16 Number;
-    static constexpr bool kChecked = true, kScaled = true;
-    static __device__ __forceinline__ uint32_t scale_pair(uint32_t a, uint32_t b) { return TypeF16::pack(Number::of_upper(a), Number::of_upper(b)); }
-    static __device__ __forceinline__ uint32_t low_pair(uint32_t a, uint32_t b) { return TypeF16::pack(Number::of(a & 0xffff), Number::of(b & 0xffff)); }
+    static constexpr bool kChecked = true, kScaled = true, kTwice = true;
+    static __device__ __forceinline__ uint32_t halves(uint32_t word) { return TypeF16::pack(Number::of(word & 0xffff), Number::of_upper(word)); }
 };
 struct MakeBf16 {
     typedef NumberBf16 Number;
     typedef TypeBf16 Operand;
-    static constexpr bool kChecked = false, kScaled = false;
+    static constexpr bool kChecked = false, kScaled = false, kTwice = true;
     static __device__ __forceinline__ uint32_t scale_pair(uint32_t a, uint32_t b) { return MakeF16::scale_pair(a, b); }
     static __device__ __forceinline__ uint32_t low_pair(uint32_t a, uint32_t b) { return MakeF16::low_pair(a, b); }
     template <bool HIGH>
@@ -100,15 +100,19 @@ struct Codes {
     uint32_t of_key[G], of_four[4 * G];                       // while they are put down: of a key, and of four, [key][group]
     uint32_t *room;                                           // 16 G words of the wave's in LDS, where lanes find each other's scale words
     long head_bytes;
+    int own_lane;
     int k_at, v_at, last_at;                                  // where this lane's things go in a tile: the others' places follow from these
     unsigned long long met;                                   // lanes that have met a scale word out of range
 
+    // (of two ways to the same number the one that leaves the loop more registers; both were tried for each)
+    __device__ __forceinline__ int the_lane() const { return MAKE::kTwice ? own_lane : threadIdx.x & 63; }
     // Features from DS on are zeros for good: nothing else is put there.
     template <int PIECES>
-    __device__ __forceinline__ void begin(const AttendArgs &a, unsigned char *keys, unsigned char *values, unsigned char *rooms, int wave)
+    __device__ __forceinline__ void begin(const AttendArgs &a, unsigned char *keys, unsigned char *values, unsigned char *rooms, int wave, int lane)
     {
         room = reinterpret_cast<uint32_t *>(rooms) + wave * 64;
-        const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4, row = 16 * wave + r, piece = 2 * wave + (g & 1), half = 8 * (g >> 1);
+        own_lane = lane;
+        const int r = lane & 15, g = lane >> 4, row = 16 * wave + r, piece = 2 * wave + (g & 1), half = 8 * (g >> 1);
         head_bytes = (a.page_bytes >> 1) / a.kv_heads;
         k_at = row * PIECES * 16 + ((g ^ key_swap(row, PIECES)) << 4);
         v_at = turned_at(4 * r, piece) + half;
@@ -125,7 +129,7 @@ struct Codes {
     // The codes of 16 keys, or values, from `key` on, in `page` (whatever it is: none of the pool's, then zeros).
     __device__ __forceinline__ void ask(const AttendArgs &a, int h, int page, int key, int limit, bool values)
     {
-        const int lane = threadIdx.x & 63, slot = key & ((1 << a.log_ps) - 1);
+        const int lane = the_lane(), slot = key & ((1 << a.log_ps) - 1);
         const int valid = (unsigned)page < (unsigned)a.pages ? min(max(limit - key, 0), 16) : 0;
         const unsigned char *const head = a.kv + (valid ? page : 0) * a.page_bytes + (values ? a.page_bytes >> 1 : 0) + h * head_bytes;
         const __amdgpu_buffer_rsrc_t codes = buffer_of(head + codes_at4(slot, DS), valid ? 8 * DS : 0), scales = buffer_of(head + scales_at4(a.log_ps, slot, DS), valid * 4 * G);
@@ -137,9 +141,12 @@ struct Codes {
     // The scale words that are needed for what is put down next.  (All in one wave: LDS serves it in order.)
     __device__ __forceinline__ void spread(bool values)
     {
-        const int lane = threadIdx.x & 63;
-        const uint32_t word = values ? vs : ks;
-        if (MAKE::kChecked) look(word);
+        const int lane = the_lane();
+        uint32_t word = values ? vs : ks;
+        if constexpr (MAKE::kChecked) {
+            look(word);
+            word = MAKE::halves(word);
+        }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         if (lane >> 4 < G) room[(lane & 15) * G + (lane >> 4)] = word;
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");

@@ -78,7 +78,9 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, const bool shar
     constexpr int kRowsACopy = 64 / kPieces, kCopies = 16 / kRowsACopy;       // a wave copies 16 keys and 16 values a step
     unsigned char (*const lds)[2][kTileBytes] = reinterpret_cast<unsigned char (*)[2][kTileBytes]>(room);   // keys, values; two steps each
 
-    const int lane = threadIdx.x & 63, col = lane & 31, grp = lane >> 5, wave = uniform(threadIdx.x >> 6);
+    int thread = threadIdx.x;
+    if constexpr (kFour) asm volatile("" : "+v"(thread));     // (nothing that follows from it is kept in registers for a second time, or another branch of a kernel)
+    const int lane = thread & 63, col = lane & 31, grp = lane >> 5, wave = uniform(thread >> 6);
     const int D = a.D, ps1 = (1 << a.log_ps) - 1;
 
     // the row of the table, the tile of its query rows and the piece of the tile's keys (for the shared tokens all query tokens are one row's)
@@ -221,7 +223,7 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, const bool shar
     CODES codes;
     if constexpr (kFour) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) codes.template begin<kPieces>(a, lds[0][i], lds[1][i], room + 4 * kTileBytes, wave);
+        for (int i = 0; i < 2; ++i) codes.template begin<kPieces>(a, lds[0][i], lds[1][i], room + 4 * kTileBytes, wave, lane);
     }
     auto next_page = [&](int step) __attribute__((always_inline)) { return pages.at((key0 + step * kManyTile + 16 * wave) >> a.log_ps); };
     auto copy = [&](int step, int page, bool values) __attribute__((always_inline)) {
