@@ -264,3 +264,24 @@ def test_prompts_over_scales_that_fp16_operands_are_not_made_for(k_size, v_size)
     cache = to_cache4(fbq, pool, table, n, refs, BF16, D)
     got = fbq.attention(cache, 0, q.cuda(), q_start=starts(counts).cuda(), max_q=max(counts)).cpu().double()
     assert ((got - want).abs() <= bound).all()
+
+
+@pytest.mark.parametrize("D,kv_heads,rows", [(64, 8, 18), (80, 4, 30), (128, 4, 18)])
+@pytest.mark.parametrize("which,size", [(0, 1e-6), (1, 1e5), (1, 1e-20)])
+def test_shared_tokens_over_scales_that_fp16_operands_are_not_made_for(which, size, D, kv_heads, rows):
+    """bf16: pages of the shared tokens have such keys or values, the others ordinary ones; the rows' own tokens are in the same launch."""
+    import paper_2501_16385_amd as fbq
+    from cache4_cases import unpack
+    from cache_cases import make_cache
+    lengths = [8192 + 1 + 7 * b for b in range(rows)]
+    x, table, n, refs = make_cache(lengths, kv_heads, D, 64, BF16, shared_pages=128, seed=D)
+    for page in (3, 70, 127):
+        at = int(table[0, page])
+        x[0, at, which] = (x[0, at, which].double() * size).to(BF16)
+    pool = pack(x, 64)
+    values, counts = unpack(pool, BF16, D), [1] * rows
+    q = torch.randn(rows, kv_heads, D, generator=torch.Generator().manual_seed(9)).to(BF16)
+    want, _, bound, _ = attention4_64(values, table, n, 0, q, counts, D ** -0.5, False)
+    cache = to_cache4(fbq, pool, table, n, refs, BF16, D)
+    got = fbq.attention(cache, 0, q.cuda(), shared=table[0, :128].contiguous().cuda()).cpu().double()
+    assert ((got - want).abs() <= bound).all()
