@@ -430,6 +430,7 @@ fbq_status fbq_cache_compact(const fbq_cache *c, int32_t *table_out, int32_t *re
  * and lse = ln sum_j p_j.  A query token that sees nothing gets 0 and -infinity; what it does not see does not reach it, whatever lies there (an infinity that it does
  * see may make its result a NaN, where p_j rounds to 0).  Sums, maxima and exponentials are in fp32; p_j is rounded to the cache's type
  * as an operand of the matrix cores, out once at the end.
+ * The sum over j is divided at its end, and its p_j are up to 2^8 times what they are beside the largest: of bf16, values from about 2^120 / L on may take it beyond fp32.
  *   T query tokens in all; q_start device [rows + 1], ascending: row b's are q_start[b] .. q_start[b + 1] - 1; NULL: T == rows, one a row.  max_q: at least the most that a
  *            row has (1 with NULL; the result of a row with more is unspecified).  Tokens outside q_start[0] .. q_start[rows] - 1 are left alone
  *   q, out   device [T][heads][head_dim] of the cache's type, rows q_stride and out_stride elements apart (multiples of 8, at least heads * head_dim, at most 2^32)

@@ -2,11 +2,13 @@
 //
 // Codes go into the matrix cores as they are, fp16 numbers below the normal ones (fbq_cache4.h), and are multiplied exactly; scales come in afterwards, in 32 bits.
 //   scores   k = m + s c of a key's group:  q . k = sum over groups of  s (q . c) + m sum(q).  Queries are fp16 here, times a power of two for the row (which goes into its scale): the row's
-//            largest feature is near 2^15, and those of codes at high bits are divided by 16, so that only what is 2^-24 of the largest and less loses any.
+//            largest feature is near 2^15, and those of codes at high bits are divided by 16, so that only what is 2^-24 of the largest and less loses any.  Scores of
+//            bf16 are summed as 2^-24 of them: no number of the type takes such a sum beyond fp32.
 //   results  sum p v = sum (p s) (c - 8) + sum p (m + 8 s):  p s is operand B of the second product, a rounding to fp16 where fbq_attend_few.h rounds p; the 8 is a product of its own with the
 //            rounded numbers, and the second sum stays in 32 bits, in the lane.  (Without the 8 the rounding is that of numbers three times as large, which add up to the same: relative L2
 //            against 64 bits 5.4e-4 instead of 3e-4 for 1000 keys in fp16.)  p s has to be in fp16's range whatever the scales: p is relative to 2^e too, e the exponent of the largest 2^10 s
-//            so far, less 5, and follows when it is passed by 2^7.
+//            so far, less 5, and follows when it is passed by 2^7.  Of bf16, where that could be an exponent that p itself has no room for, e stays within -24 .. 34 - at 34 no sum of p m or
+//            p s over 2^24 tokens passes fp32's range - and what is beyond, x, is taken from the scales while they are spread.
 //   scales   A key's scale is wanted in all 16 lanes that have its row of a product.  The matrix cores, which have time, put it there: the scale words as operand A, [key][group] with m and s as
 //            neighbours, times constants as operand B are s, m + 8 s, and, with the sums of q in three parts of 16 bits each, m sum(q) - in 32 bits, exactly but for the last addition.
 //            (Vector instructions instead, neighbours' words by quad_perm: 350 a step, 100 of them for this, and 5.2 TB/s where it is now 5.9.)
@@ -41,8 +43,8 @@ struct Piece4 {
     int pages[kFew4Parts];                                    // of its first step
 };
 
-// The queries of a wave's 16 rows: operands for codes, of a group those at low bits and those at high bits; for scale words, what makes 2^10 s of a group and m sum(q) of all; and what scores
-// are to be multiplied by.
+// The queries of a wave's 16 rows: operands for codes, of a group those at low bits and those at high bits; for scale words, what makes s of a group and m sum(q) of all, 2^10 and 2^-14 of them,
+// or 1 and 2^-24; and what scores are to be multiplied by.
 template <class TY, class NT, int NW>
 struct Queries4 {
     static constexpr int G = groups4(32 * NW);
@@ -59,7 +61,8 @@ struct Queries4 {
 #pragma unroll
             for (int e = 0; e < 4; ++e) most = fmaxf(most, fmaxf(fabsf(NT::of(q[w][e] & 0xffff)), fabsf(NT::of_upper(q[w][e]))));
         const int up = __builtin_amdgcn_frexp_expf(larger_of_32(larger_of_16(most))) - 15;
-        unit = ldexpf(scale * 0x1p14f, up);
+        const int less = NT::kWide && up <= 96 ? 10 : 0;      // (above, with features of 2^110 and more, the unit itself would be beyond fp32)
+        unit = ldexpf(scale * 0x1p14f, up + less);
         word4_t h[NW];
 #pragma unroll
         for (int w = 0; w < NW; ++w)
@@ -78,8 +81,9 @@ struct Queries4 {
             at[y][1] = word4_t{a[2], a[3], b[2], b[3]};
             const float4_t s = TypeF16::mfma(sixteen, at[y][1], TypeF16::mfma(one, at[y][0], float4_t{0, 0, 0, 0}));
             sum = grp == y ? s[0] * 0x1p-14f : sum;
-            pick[y] = word2_t{grp == y ? NT::bits(1024.0f) << 16 : 0u, 0u};
+            pick[y] = word2_t{grp == y ? NT::bits(less ? 1.0f : 1024.0f) << 16 : 0u, 0u};
         }
+        sum = ldexpf(sum, -less);
         const uint32_t high = NT::bits(sum);
         const float rest = sum - NT::of(high);
         const uint32_t middle = NT::bits(rest);
@@ -87,7 +91,7 @@ struct Queries4 {
     }
 };
 
-// Of 16 keys, a lane's four (4 (l / 16) + i): 2^10 of their scales in a group.
+// Of 16 keys, a lane's four (4 (l / 16) + i): of their scale words in a group what `pick` makes.
 template <class TY>
 __device__ __forceinline__ float4_t scales_of(uint32_t words, word2_t pick) { return TY::mfma(word2_t{words, 0u}, pick, float4_t{0, 0, 0, 0}); }
 
@@ -172,12 +176,12 @@ __device__ __forceinline__ void attend4_few(const AttendArgs &a, int block, unsi
     };
 
     Queries4<TY, NT, NW> q;
-    word2_t eighths[G];                                       // what makes m + 8 s of a group's scale words
+    word2_t eighths[G], spread[G];                            // what makes (m + 8 s) / 2 (8 s may be beyond fp32), and 2^(10 - x) s, of a group's scale words
 #pragma unroll
-    for (int y = 0; y < G; ++y) eighths[y] = word2_t{grp == y ? NT::bits(8.0f) << 16 | NT::bits(1.0f) : 0u, 0u};
-    float4_t o[J], eights[G];                                 // eights: sums of 8 p s as it is rounded, times 2^-14 like those of p s c in o
-    float m, l, lows[G];                                      // lows: sum p (m + 8 s), of the lane's keys
-    int least, e;                                             // what every row of the piece sees; the exponent that p is relative to
+    for (int y = 0; y < G; ++y) eighths[y] = word2_t{grp == y ? NT::bits(4.0f) << 16 | NT::bits(0.5f) : 0u, 0u};
+    float4_t o[J], eights[G];                                 // eights: sums of 8 p s as it is rounded, times 2^(-14 - x) like those of p s c in o
+    float m, l, lows[G];                                      // lows: sum p (m + 8 s) / 2, of the lane's keys
+    int least, e, x_of;                                       // what every row of the piece sees; the exponent that p is relative to; x
     uint32_t most;                                            // the largest scale word that goes with e
     auto begin = [&]() __attribute__((always_inline)) {
         q.of(cur.q, a.scale);
@@ -187,10 +191,12 @@ __device__ __forceinline__ void attend4_few(const AttendArgs &a, int block, unsi
         for (int y = 0; y < G; ++y) {
             lows[y] = 0;
             eights[y] = float4_t{0, 0, 0, 0};
+            spread[y] = word2_t{grp == y ? NT::bits(1024.0f) << 16 : 0u, 0u};
         }
         m = kNoScore;
         l = 0;
         e = 0;
+        x_of = 0;
         most = 0;
         least = cur.t >= 0 ? cur.sees : cur.limit;
 #pragma unroll
@@ -220,23 +226,31 @@ __device__ __forceinline__ void attend4_few(const AttendArgs &a, int block, unsi
         top = larger_of_16(top);
         top = larger_of_32(top) * q.unit;
         if (__ballot(top > m - (float)e + kSlack || largest > most)) {
-            const int before = e;
+            const int before = e, x_before = x_of;
 #pragma unroll
             for (int w = 32; w; w >>= 1) largest = max(largest, (uint32_t)__shfl_xor((int)largest, w));
             largest = uniform(largest);
             if (largest > most) {
-                e = uniform(max(__builtin_amdgcn_frexp_expf(NT::of_upper(largest)) + 5, -90));
-                const uint32_t beyond = NT::bits(ldexpf(1.0f, e - 3));                    // (an infinity: no scale is)
+                const int all = uniform(__builtin_amdgcn_frexp_expf(NT::of_upper(largest)) + 5);
+                e = all;
+                if (NT::kWide) {
+                    e = min(max(all, -24), 34);
+                    x_of = max(all, -110) - e;                // (so that the factor is a number of the type)
+#pragma unroll
+                    for (int y = 0; y < G; ++y) spread[y][0] = grp == y ? NT::bits(ldexpf(1024.0f, -x_of)) << 16 : 0u;
+                }
+                const uint32_t beyond = NT::bits(ldexpf(1.0f, all - 3));                  // (an infinity: no scale is)
                 most = uniform((beyond << 16) - 1);
             }
             const float to = fmaxf(top, m - (float)before) + (float)e, by = __builtin_amdgcn_exp2f(m - to);
+            const float by_scaled = NT::kWide ? ldexpf(by, x_before - x_of) : by;
             l *= by;
 #pragma unroll
-            for (int j = 0; j < J; ++j) o[j] *= by;
+            for (int j = 0; j < J; ++j) o[j] *= by_scaled;
 #pragma unroll
             for (int y = 0; y < G; ++y) {
                 lows[y] *= by;
-                eights[y] *= by;
+                eights[y] *= by_scaled;
             }
             m = to;
         }
@@ -250,7 +264,7 @@ __device__ __forceinline__ void attend4_few(const AttendArgs &a, int block, unsi
             }
 #pragma unroll
             for (int y = 0; y < G; ++y) {
-                const float4_t s = scales_of<TY>(x.vs[part], q.pick[y]), low = scales_of<TY>(x.vs[part], eighths[y]);
+                const float4_t s = scales_of<TY>(x.vs[part], spread[y]), low = scales_of<TY>(x.vs[part], eighths[y]);
                 float of[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -279,11 +293,13 @@ __device__ __forceinline__ void attend4_few(const AttendArgs &a, int block, unsi
         for (int y = 0; y < G; ++y) {
             lows[y] += __shfl_xor(lows[y], 16);
             lows[y] += __shfl_xor(lows[y], 32);
+            lows[y] *= 2;
         }
+        const float back = NT::kWide ? ldexpf(0x1p14f, x_of) : 0x1p14f;
 #pragma unroll
         for (int j = 0; j < J; ++j)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) o[j][i] = __builtin_fmaf(j & 1 ? __builtin_fmaf(o[j][i], 0.0625f, -eights[j / 4][i]) : o[j][i] - eights[j / 4][i], 0x1p14f, lows[j / 4]);
+            for (int i = 0; i < 4; ++i) o[j][i] = __builtin_fmaf(j & 1 ? __builtin_fmaf(o[j][i], 0.0625f, -eights[j / 4][i]) : o[j][i] - eights[j / 4][i], back, lows[j / 4]);
         if (together) {                                       // the first wave joins the block's, as in attend_few_wave
             float *const at = reinterpret_cast<float *>(room) + lane;
             const int wave = uniform(threadIdx.x >> 6);

@@ -15,6 +15,7 @@ constexpr uint32_t kLowCodes = 0x000f000fu, kHighCodes = 0x00f000f0u;
 // Numbers of the cache's 16-bit type in 32 bits, and back (to nearest, ties to even).
 struct NumberF16 {
     static constexpr float kMost = 65504.0f;
+    static constexpr bool kWide = false;                      // has fp32's range
     static constexpr uint32_t kExponent = 0x7c00u, kNaN = 0x7e00u;
     static __device__ __forceinline__ float of(uint32_t bits) { return (float)__builtin_bit_cast(_Float16, (uint16_t)bits); }
     static __device__ __forceinline__ float of_upper(uint32_t word) { return (float)__builtin_bit_cast(_Float16, (uint16_t)(word >> 16)); }
@@ -22,6 +23,7 @@ struct NumberF16 {
 };
 struct NumberBf16 {
     static constexpr float kMost = 3.38953139e38f;
+    static constexpr bool kWide = true;
     static constexpr uint32_t kExponent = 0x7f80u, kNaN = 0x7fc0u;
     static __device__ __forceinline__ float of(uint32_t bits) { return __builtin_bit_cast(float, bits << 16); }
     static __device__ __forceinline__ float of_upper(uint32_t word) { return __builtin_bit_cast(float, word & 0xffff0000u); }

@@ -1,0 +1,89 @@
+"""Few query rows over a cache in 4 bits at both ends of its type's range: results and attention weights against the formula in 64 bits, element by element within the bounds of
+tests/cache4_cases.py, of which only what they grant to results near zero is less here."""
+import math
+
+import pytest
+import torch
+
+from cache4_cases import BF16, F16, attention4_64, pack, to_cache4, unpack
+from cache_cases import make_cache, starts
+
+pytestmark = pytest.mark.gpu
+
+LEAST = {F16: 2.0 ** -24, BF16: 2.0 ** -133}                  # the types' least numbers
+
+
+def sized(lengths, kv_heads, D, page, dtype, k_size, v_size, seed):
+    """(pool, table, lengths, refs, what the pool stands for): normal keys and values times their sizes, none beyond the type's largest."""
+    x, table, n, refs = make_cache(lengths, kv_heads, D, page, dtype, seed=seed)
+    most = torch.finfo(dtype).max
+    for i, size in ((0, k_size), (1, v_size)):
+        x[:, :, i] = (x[:, :, i].double() * size).clamp(-most, most).to(dtype)
+    pool = pack(x, page)
+    return pool, table, n, refs, unpack(pool, dtype, D)
+
+
+def check(lengths, counts, heads, kv_heads, D, dtype, k_size, v_size, seed=1):
+    import paper_2501_16385_amd as fbq
+    pool, table, n, refs, values = sized(lengths, kv_heads, D, 16, dtype, k_size, v_size, seed)
+    T = sum(counts)
+    q = (torch.randn(T, heads, D, generator=torch.Generator().manual_seed(seed + 1)).double() / k_size).to(dtype)
+    assert max(counts) * heads // kv_heads <= 16
+    # (results go with values' size: worked out at about 1, where the bound's 2^-24 for results near zero can be taken off)
+    size = 2.0 ** math.floor(math.log2(v_size))
+    values[:, :, 1] /= size
+    want, want_lse, bound, lse_bound = attention4_64(values, table, n, 0, q, counts, D ** -0.5, True)
+    want, bound = want * size, (bound - 2.0 ** -24) * size + LEAST[dtype]
+    lse = torch.empty(T, heads, device="cuda")
+    got = fbq.attention(to_cache4(fbq, pool, table, n, refs, dtype, D), 0, q.cuda(), q_start=starts(counts).cuda(), max_q=max(counts), lse=lse)
+    got, lse = got.cpu().double(), lse.cpu().double()
+    assert torch.isfinite(got).all() and torch.isfinite(lse).all()
+    off = (got - want).abs()
+    assert (off <= bound).all(), f"{float((off / bound).max()):.2f} times the bound"
+    assert ((lse - want_lse).abs() <= lse_bound).all()
+
+
+@pytest.mark.parametrize("size", [1e32, 5e36, 3e37, 3e38, 1e-29, 1e-33, 1e-36])
+@pytest.mark.parametrize("D", [64, 96, 128, 256])
+def test_values(D, size):
+    check([200, 77], [1, 1], 4, 2, D, BF16, 1.0, size)
+    check([200, 77], [4, 3], 4, 2, D, BF16, 1.0, size)
+
+
+@pytest.mark.parametrize("size", [1e32, 3e38, 1e-36])
+def test_values_of_rows_that_are_joined(size):
+    """Pieces of a block in LDS, and of many workers by the join kernel."""
+    check([900], [1], 2, 1, 64, BF16, 1.0, size)
+    check([9000, 33], [1, 1], 2, 1, 64, BF16, 1.0, size)
+
+
+@pytest.mark.parametrize("size", [1e32, 5e36, 3e38, 1e-30, 1e-35])
+@pytest.mark.parametrize("D", [64, 96, 128, 256])
+def test_keys(D, size):
+    """Queries so much smaller, or larger: with features of 2^110 and more, too."""
+    check([200, 77], [1, 1], 4, 2, D, BF16, size, 1.0)
+
+
+@pytest.mark.parametrize("size", [3e4, 1e-3])
+def test_values_and_keys_of_fp16(size):
+    check([200, 77], [4, 1], 4, 2, 128, F16, 1.0, size)
+    check([200, 77], [1, 1], 4, 2, 128, F16, size, 1.0)
+
+
+@pytest.mark.parametrize("counts,size", [([n, 1], size) for n in (1, 7) for size in (1e30, 5e36, 3e38, 1e-30)] + [([40, 20], size) for size in (1e30, 1e-30)])
+def test_weights(counts, size):
+    """Sums of what attention gave each key; beyond 16 query rows a head up to 1e30, where the queries are numbers that the matrix cores take as they are."""
+    import paper_2501_16385_amd as fbq
+    from test_gpu_eviction import weights64
+    D, dtype = 128, BF16
+    pool, table, n, refs, values = sized([200, 77], 2, D, 16, dtype, size, 1.0, 3)
+    T = sum(counts)
+    q = (torch.randn(T, 4, D, generator=torch.Generator().manual_seed(4)).double() / size).to(dtype)
+    cache, qs = to_cache4(fbq, pool, table, n, refs, dtype, D), starts(counts).cuda()
+    lse = torch.empty(T, 4, device="cuda")
+    fbq.attention(cache, 0, q.cuda(), q_start=qs, max_q=max(counts), lse=lse)
+    assert torch.isfinite(lse).all()
+    out = torch.zeros(2, 2, table.shape[1] * 16)
+    want, bound = weights64(values, table, n, 0, q, lse.cpu(), counts, D ** -0.5, None, 1.0, out)
+    got = fbq.attention_weights(cache, 0, q.cuda(), lse, None, q_start=qs, max_q=max(counts), out=out.cuda()).cpu().double()
+    assert ((got - want).abs() <= bound).all()
