@@ -14,7 +14,9 @@
 //            (Vector instructions instead, neighbours' words by quad_perm: 350 a step, 100 of them for this, and 5.2 TB/s where it is now 5.9.)
 // Bound by HBM in long rows: 16 rows of 16000 tokens, 32 heads of 128, 1.18 GB, 200 us (5.9 TB/s), 64 of 4096 with 64 heads to 8 62; in short ones by the time that begins and ends a piece, 9 us with one
 // step of 32 keys and nothing to join: 16 rows of about 1000 (74 MB) 24 us, one of 65537 with 8 heads (75 MB) 24.
-// A value that nobody sees has weight zero and finite scales, so nothing of it is added, whatever it is: no second look is needed.
+// A value that a row does not see has weight zero there and finite scales, so nothing of it is added.  But rows share e, and what some of them see and others do not may take bits of the others' p s:
+// where such scales are more than 2^4 times what all see, the wave does its work again, slowly, with an e and x for each row by the scales that it sees.  (4 tokens of 32 heads to 8 behind
+// 4000, the last one's values 10^4 times the others': 22 us, else 16.)
 #ifndef FBQ_ATTEND4_FEW_H
 #define FBQ_ATTEND4_FEW_H
 
@@ -113,12 +115,16 @@ __device__ __forceinline__ float4_t scores4(const uint32_t (&k)[NW], uint32_t ks
     return z;
 }
 
+// Bytes of LDS (aligned to 16) of a block of it: parts of waves 1 .., and a word a wave.
 template <int NW>
-constexpr int kFew4Room = (kFewWaves - 1) * (2 * 4 * NW + 2) * 256;
+constexpr int kFew4PartsRoom = (kFewWaves - 1) * (2 * 4 * NW + 2) * 256;
+template <int NW>
+constexpr int kFew4Room = kFew4PartsRoom<NW> + 4 * kFewWaves;
 
+// The work of the block's wave (see attend4_few), its results written; AGAIN: with exponents for each row.  Whether it has to be done so (for all waves of a block that join theirs the same answer).
 // TY: the type of queries and results; NT: its numbers.
-template <class TY, class NT, int NW>
-__device__ __forceinline__ void attend4_few(const AttendArgs &a, int block, unsigned char *room)
+template <class TY, class NT, int NW, bool AGAIN>
+__device__ __forceinline__ bool attend4_few_wave(const AttendArgs &a, int block, unsigned char *room)
 {
     constexpr int DS = 32 * NW, G = groups4(DS), J = 2 * NW;   // products of the results
     constexpr int kParts = kFew4Parts;
@@ -130,7 +136,7 @@ __device__ __forceinline__ void attend4_few(const AttendArgs &a, int block, unsi
 
     Piece4<NW> cur, behind;
     FewLine line;
-    if (!line.first(a, block, worker, cur)) return;
+    if (!line.first(a, block, worker, cur)) return false;
     const bool together = line.together;
     auto prepare = [&](Piece4<NW> &x) __attribute__((always_inline)) {
         few_sight(a, x, col);
@@ -181,8 +187,9 @@ __device__ __forceinline__ void attend4_few(const AttendArgs &a, int block, unsi
     for (int y = 0; y < G; ++y) eighths[y] = word2_t{grp == y ? NT::bits(4.0f) << 16 | NT::bits(0.5f) : 0u, 0u};
     float4_t o[J], eights[G];                                 // eights: sums of 8 p s as it is rounded, times 2^(-14 - x) like those of p s c in o
     float m, l, lows[G];                                      // lows: sum p (m + 8 s) / 2, of the lane's keys
-    int least, e, x_of;                                       // what every row of the piece sees; the exponent that p is relative to; x
-    uint32_t most;                                            // the largest scale word that goes with e
+    int least, e, x_of;                                       // what every row of the piece sees; the exponent that p is relative to, and x (AGAIN: of the lane's row; else the same in all lanes)
+    uint32_t most;                                            // the largest scale word that goes with them
+    bool again = false;
     auto begin = [&]() __attribute__((always_inline)) {
         q.of(cur.q, a.scale);
 #pragma unroll
@@ -225,13 +232,35 @@ __device__ __forceinline__ void attend4_few(const AttendArgs &a, int block, unsi
         }
         top = larger_of_16(top);
         top = larger_of_32(top) * q.unit;
+        const auto same = [](int v) { return AGAIN ? v : uniform(v); };
+        const bool apart = least < min(cur.limit, key + kFewTile);            // (rows see different tokens of the step)
+        if (AGAIN && apart) {                                 // of the lane's row
+            largest = 0;
+#pragma unroll 1
+            for (int k = 0; k < kFewTile; ++k)
+#pragma unroll
+                for (int y = 0; y < G; ++y) {
+                    const uint32_t word = __builtin_amdgcn_readlane((int)(k < 16 ? x.vs[0] : x.vs[1]), (k & 15) + 16 * y);
+                    if (k < cur.sees - key) largest = max(largest, word);
+                }
+        }
         if (__ballot(top > m - (float)e + kSlack || largest > most)) {
             const int before = e, x_before = x_of;
+            if (!AGAIN || !apart) {
 #pragma unroll
-            for (int w = 32; w; w >>= 1) largest = max(largest, (uint32_t)__shfl_xor((int)largest, w));
-            largest = uniform(largest);
+                for (int w = 32; w; w >>= 1) largest = max(largest, (uint32_t)__shfl_xor((int)largest, w));
+                largest = uniform(largest);
+            }
             if (largest > most) {
-                const int all = uniform(__builtin_amdgcn_frexp_expf(NT::of_upper(largest)) + 5);
+                const int all = same(__builtin_amdgcn_frexp_expf(NT::of_upper(largest)) + 5);
+                if (!AGAIN && apart) {                        // beside the largest that all see (who sees any of the piece sees its first key)
+                    const int seen = max(least - key, 1);
+                    uint32_t known = max(col < seen ? x.vs[0] : 0, 16 + col < seen ? x.vs[1] : 0);
+#pragma unroll 1
+                    for (int w = 32; w; w >>= 1) known = max(known, (uint32_t)__shfl_xor((int)known, w));
+                    const int beside = max(known >> 16 ? __builtin_amdgcn_frexp_expf(NT::of_upper(known)) + 5 : -1000, most ? e + x_of : -1000);
+                    again |= uniform(all > beside + 4) != 0;
+                }
                 e = all;
                 if (NT::kWide) {
                     e = min(max(all, -24), 34);
@@ -240,7 +269,7 @@ __device__ __forceinline__ void attend4_few(const AttendArgs &a, int block, unsi
                     for (int y = 0; y < G; ++y) spread[y][0] = grp == y ? NT::bits(ldexpf(1024.0f, -x_of)) << 16 : 0u;
                 }
                 const uint32_t beyond = NT::bits(ldexpf(1.0f, all - 3));                  // (an infinity: no scale is)
-                most = uniform((beyond << 16) - 1);
+                most = same((beyond << 16) - 1);
             }
             const float to = fmaxf(top, m - (float)before) + (float)e, by = __builtin_amdgcn_exp2f(m - to);
             const float by_scaled = NT::kWide ? ldexpf(by, x_before - x_of) : by;
@@ -269,7 +298,7 @@ __device__ __forceinline__ void attend4_few(const AttendArgs &a, int block, unsi
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     lows[y] = __builtin_fmaf(low[i], z[part][i], lows[y]);
-                    of[i] = s[i] * z[part][i];
+                    of[i] = (AGAIN && NT::kWide ? fminf(s[i], 0x1p127f) : s[i]) * z[part][i];        // (beyond fp32 it may be where the row does not see it, and p is 0)
                 }
                 ps[y][2 * part] = TypeF16::pack(of[0], of[1]);
                 ps[y][2 * part + 1] = TypeF16::pack(of[2], of[3]);
@@ -302,7 +331,10 @@ __device__ __forceinline__ void attend4_few(const AttendArgs &a, int block, unsi
             for (int i = 0; i < 4; ++i) o[j][i] = __builtin_fmaf(j & 1 ? __builtin_fmaf(o[j][i], 0.0625f, -eights[j / 4][i]) : o[j][i] - eights[j / 4][i], back, lows[j / 4]);
         if (together) {                                       // the first wave joins the block's, as in attend_few_wave
             float *const at = reinterpret_cast<float *>(room) + lane;
+            int *const flags = reinterpret_cast<int *>(room + kFew4PartsRoom<NW>);
             const int wave = uniform(threadIdx.x >> 6);
+            if (AGAIN) __syncthreads();                       // (the first one may still read what was joined before)
+            else if (lane == 0) flags[wave] = again;
             if (wave) {
                 float *const to = at + (wave - 1) * (4 * J + 2) * 64;
                 to[0] = m;
@@ -313,6 +345,10 @@ __device__ __forceinline__ void attend4_few(const AttendArgs &a, int block, unsi
                     for (int i = 0; i < 4; ++i) to[(2 + 4 * j + i) * 64] = o[j][i];
             }
             __syncthreads();
+            if (!AGAIN) {
+#pragma unroll
+                for (int w = 0; w < kFewWaves; ++w) again |= uniform(flags[w]) != 0;
+            }
             if (wave) return;
             float to = m;
 #pragma unroll
@@ -358,6 +394,22 @@ __device__ __forceinline__ void attend4_few(const AttendArgs &a, int block, unsi
         else if (a.lse) a.lse[(long)cur.t * a.heads + head] = l == 0 ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
     };
 
+    if constexpr (AGAIN) {                                    // (few registers before speed)
+        while (true) {
+            prepare(cur);
+            begin();
+            aim(cur, cur.n > 0);
+            for (int s = 0; s < cur.n; ++s) {
+                Step4<NW> x;
+                load(x);
+                compute(x, s);
+            }
+            finish();
+            if (!line.follow(a, cur, behind)) return false;
+            first = false;
+            cur = behind;
+        }
+    }
     // One copy of `finish` and of all that a new piece takes: the kernel is long, and where there is little to do it waits for its instructions.
     prepare(cur);
     behind = cur;                                             // (where there is none, something that is one)
@@ -381,12 +433,25 @@ __device__ __forceinline__ void attend4_few(const AttendArgs &a, int block, unsi
             }
         }
         finish();
-        if (!more) return;
+        if (!more) return again;
         first = false;
         cur = behind;
         more = line.follow(a, cur, behind);
         if (more) prepare(behind);
     }
+}
+
+// Block `block` of the few-row work, kFewWaves waves.
+template <class TY, class NT, int NW>
+__device__ __forceinline__ void attend4_few(const AttendArgs &a, int block, unsigned char *room)
+{
+    if (!attend4_few_wave<TY, NT, NW, false>(a, block, room)) return;
+    // What follows from the block and the arguments takes no registers until the second time: the arguments, each such kernel's first parameter, are read again (see fbq_attend4_many.h).
+    asm volatile("" : "+s"(block) : : "memory");
+    typedef const __attribute__((address_space(4))) AttendArgs *Kept;
+    Kept again = (Kept)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(again));
+    attend4_few_wave<TY, NT, NW, true>(*(const AttendArgs *)again, block, room);
 }
 
 }  // namespace fbq

@@ -70,6 +70,42 @@ def test_values_and_keys_of_fp16(size):
     check([200, 77], [1, 1], 4, 2, 128, F16, size, 1.0)
 
 
+def large_among_new(length, count, heads, D, dtype, size, back):
+    """A row's `count` new tokens, the one `back` from the last with values so much larger than the others'.  The tokens before it have the results, bit for bit, that they have without, all keep to the
+    formula's bounds.  With more than 16 query rows, where a block's operands of bf16 have the rounding that its largest scales leave them, all keep to that rounding's bounds."""
+    import paper_2501_16385_amd as fbq
+    kv_heads, few, place = 1, count * heads <= 16, length - 1 - back
+    x, table, n, refs = make_cache([length, 20], kv_heads, D, 16, dtype, seed=length)
+    q = torch.randn(count + 1, heads, D, generator=torch.Generator().manual_seed(7)).to(dtype)
+    results, at = [], (0, int(table[0, place // 16]), 1, 0, place % 16)
+    for times in (1.0, size):
+        y, most = x.clone(), torch.finfo(dtype).max
+        y[at] = (y[at].double() * times).clamp(-most, most).to(dtype)
+        pool = pack(y, 16)
+        lse = torch.empty(count + 1, heads, device="cuda")
+        out = fbq.attention(to_cache4(fbq, pool, table, n, refs, dtype, D), 0, q.cuda(), q_start=starts([count, 1]).cuda(), max_q=count, lse=lse)
+        results.append((out, lse))
+        want, _, bound, _ = attention4_64(unpack(pool, dtype, D), table, n, 0, q, [count, 1], D ** -0.5, few)
+        assert ((out.cpu().double() - want).abs() <= bound).all()
+    others = [t for t in range(count + 1) if t < count - 1 - back or t == count] if few else []
+    for one, other in zip(*results):
+        assert torch.equal(one[others], other[others])
+
+
+@pytest.mark.parametrize("dtype,size", [(F16, 3e4), (F16, 100.0), (BF16, 1e4), (BF16, 1e30), (BF16, 3e38)])
+@pytest.mark.parametrize("length,count,heads", [(90, 4, 4), (40, 8, 2), (600, 3, 10), (64, 16, 1), (33, 2, 4), (9000, 5, 2)])
+def test_large_values_that_a_token_does_not_see(length, count, heads, dtype, size):
+    large_among_new(length, count, heads, 128, dtype, size, 0)
+
+
+@pytest.mark.parametrize("dtype,size", [(F16, 1e4), (BF16, 1e4), (BF16, 1e36)])
+@pytest.mark.parametrize("D", [64, 96, 192, 256])
+def test_large_values_that_some_tokens_see(D, dtype, size):
+    large_among_new(70, 7, 2, D, dtype, size, 3)
+    large_among_new(2100, 16, 1, D, dtype, size, 15)
+    large_among_new(5, 4, 4, D, dtype, size, 1)
+
+
 @pytest.mark.parametrize("counts,size", [([n, 1], size) for n in (1, 7) for size in (1e30, 5e36, 3e38, 1e-30)] + [([40, 20], size) for size in (1e30, 1e-30)])
 def test_weights(counts, size):
     """Sums of what attention gave each key; beyond 16 query rows a head up to 1e30, where the queries are numbers that the matrix cores take as they are."""
