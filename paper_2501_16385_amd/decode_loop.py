@@ -78,7 +78,7 @@ class DecoderStack:
     nothing.  `lacking` [1]: the pages that the last step lacked, `most_lacking` [1] that any has; `lowest_start` [rows]: -1 where a step has left a row out.
 
     The cache may be one of 4 bits.  budget: a Budget; then every step adds up the attention weights in `weights` [layers, rows, kv_heads, tokens] and ends with the rows cut back
-    (a row that begins with another's tokens, as a forked one does, wants that one's weights copied there); `evicted` [2]: rows cut back by the last step, and rows that could not be.
+    (a row that begins with another's tokens, as a forked one does, wants that one's weights copied there; the weights of a row that a step leaves out, or has a `count` of 0 for, stay as they are); `evicted` [2]: rows cut back by the last step, and rows that could not be.
     """
 
     def __init__(self, layers, hidden: int, inter: int, keep_per_layer_buffers: bool = False, batch: int = 1,
@@ -128,6 +128,8 @@ class DecoderStack:
             self.weights = torch.zeros((cache.pool.shape[0], rows, cache.heads, width), dtype=torch.float32, device="cuda")
             self.keep, self.evicted = ints([self.budget.keep] * rows), ints([0, 0])
             self.evict_ws = kv.cache_evict_workspace(cache, self.weights)
+            self.added = torch.zeros_like(cache.lengths)        # the rows' lengths, 0 where a step has appended nothing: what `weights` counts
+            self.added_to = kv.Cache(cache.pool, cache.table, self.added, cache.refs, cache.dtype, cache.dim)
 
     def _attend(self, li, b, stream):
         """a = attention of this step's tokens over the cache, this layer's k and v in their pages first."""
@@ -138,7 +140,7 @@ class DecoderStack:
         q, lse = heads(b["q"], n), None if self.budget is None else self.lse
         kv.attention(c, li, q, q_start=self.q_start, max_q=self.max_q, shared=self.shared, out=heads(b["a"], n), lse=lse, workspace=self.attend_ws, stream=stream)
         if lse is not None:
-            kv.attention_weights(c, li, q, lse, self.weights[li], q_start=self.q_start, max_q=self.max_q, decay=self.budget.decay, stream=stream)
+            kv.attention_weights(self.added_to, li, q, lse, self.weights[li], q_start=self.q_start, max_q=self.max_q, decay=self.budget.decay, stream=stream)
         return b["a"]
 
     def _workspace(self, desc):
@@ -167,6 +169,9 @@ class DecoderStack:
             with fbq._on(stream):                       # (every step writes its own: these two stay, over the replays of a graph)
                 torch.minimum(self.lowest_start, self.start, out=self.lowest_start)
                 torch.maximum(self.most_lacking, self.lacking, out=self.most_lacking)
+                if self.budget is not None:             # (a last token held is no new one: its sums would begin anew, and a query that means nothing would count)
+                    torch.add(self.start, 1, out=self.added)
+                    torch.minimum(self.added, self.count, out=self.added).clamp_(0, 1).mul_(self.cache.lengths)
         for li in range(len(self.layers)):
             b = self.buf[li % len(self.buf)]
             if len(self.buf) > 1:
