@@ -58,15 +58,9 @@ class Budget:
     recent: int = 1
     decay: float = 1.0
 
-
-@dataclass(frozen=True)
-class Budget:
-    """What the rows of a cache may hold: at most `keep` tokens, the first `first` and the last `recent` ones among them, and those of the others that were attended to most; what a token
-    was given counts `decay` times as much a step later."""
-    keep: int
-    first: int = 0
-    recent: int = 1
-    decay: float = 1.0
+    def __post_init__(self):
+        if self.first < 0 or self.recent < 0 or self.first + self.recent > self.keep or not 0 <= self.decay <= 1:
+            raise ValueError("budget: first and recent tokens, 0 or more, within the ones to keep; decay 0 .. 1")      # (else no row would ever be cut back)
 
 
 class DecoderStack:
