@@ -72,7 +72,8 @@ class DecoderStack:
     nothing.  `lacking` [1]: the pages that the last step lacked, `most_lacking` [1] that any has; `lowest_start` [rows]: -1 where a step has left a row out.
 
     The cache may be one of 4 bits.  budget: a Budget; then every step adds up the attention weights in `weights` [layers, rows, kv_heads, tokens] and ends with the rows cut back
-    (a row that begins with another's tokens, as a forked one does, wants that one's weights copied there; the weights of a row that a step leaves out, or has a `count` of 0 for, stay as they are); `evicted` [2]: rows cut back by the last step, and rows that could not be.
+    (a row that begins with another's tokens, as a forked one does, wants that one's weights copied there; the weights of a row that a step leaves out, or has a `count` of 0 for, stay as they are); `evicted` [2]: rows cut back by the last step, and rows that could not be;
+    `most_skipped` [1]: the most of these that any step has had.
     """
 
     def __init__(self, layers, hidden: int, inter: int, keep_per_layer_buffers: bool = False, batch: int = 1,
@@ -120,7 +121,7 @@ class DecoderStack:
             width = cache.table.shape[1] * cache.page_size
             self.lse = torch.empty(q.shape[:2], dtype=torch.float32, device="cuda")
             self.weights = torch.zeros((cache.pool.shape[0], rows, cache.heads, width), dtype=torch.float32, device="cuda")
-            self.keep, self.evicted = ints([self.budget.keep] * rows), ints([0, 0])
+            self.keep, self.evicted, self.most_skipped = ints([self.budget.keep] * rows), ints([0, 0]), ints([0])
             self.evict_ws = kv.cache_evict_workspace(cache, self.weights)
             self.added = torch.zeros_like(cache.lengths)        # the rows' lengths, 0 where a step has appended nothing: what `weights` counts
             self.added_to = kv.Cache(cache.pool, cache.table, self.added, cache.refs, cache.dtype, cache.dim)
@@ -179,6 +180,8 @@ class DecoderStack:
             self._group(li, ("down",), [b["act"]], [b["down"]], sp, mix=(b["h"], x))         # x = (h + down) / 2
         if self.budget is not None:
             kv.cache_evict(self.cache, self.weights, self.keep, first=self.budget.first, recent=self.budget.recent, info=self.evicted, workspace=self.evict_ws, stream=stream)
+            with fbq._on(stream):
+                torch.maximum(self.most_skipped, self.evicted[1:], out=self.most_skipped)
         return x
 
     def capture(self):
