@@ -223,16 +223,22 @@ static int few_direct(long items, long tokens, bool four)
 // (50 MB) 40 / 35; 32 heads of 32, 32 rows of 20 behind 4096 97 / 195, of 64 210 / 220, of 128 410 / 303; 11 of 15, 16 heads of 96, behind 64 (5 MB) 23.6 / 8.9.  Few-row kernel: 8 of 4 behind 16384
 // 33 / 97, 2 of 4 23 / 35, 4 of 4 behind 4096 18 / 21; 64 rows of 2000 behind 512 (129 MB) 97 / 106, behind 64 (17 MB) 94.0 / 93.7, but of 600 behind 64 38 / 28: there a row is a block's
 // without a join.
-// In 4 bits what is not read again is less than a third, and the many-row kernel makes its operands first; fp16, bf16.  Many-row kernel for the shared tokens, single tokens: 16 rows behind 1024 (60 MB
-// as 16 bits) 19.3 / 18.7, 23 / 19, behind 4096 21.5 / 29, 25 / 29; 64 of 2000 behind 512 (126 MB) 58 / 48, 61 / 48, behind 2048 61 / 61, 63 / 61; 64 of 300 behind 1024 (252 MB) 26.5 / 22, 31 / 22.5,
-// behind 2048 35 / 43.5, 36.5 / 44.  8 tokens a row: 16 behind 2048 (120 MB) 50 / 40, 59 / 51, behind 4096 64 / 56, 75 / 73; 8 behind 16384 (448 MB) 76 / 86, 91 / 121.  Few-row kernel: 2 of 4 behind
-// 512 13.6 / 13.6, behind 2048 14.4 / 15.5, 4 of 4 behind 4096 16.4 / 18.4.
+// In 4 bits what is not read again is less than a third, and the many-row kernel makes its operands first; fp16, bf16, rows of 300 tokens of their own unless stated.  Many-row kernel for the shared tokens,
+// single tokens in the same launch (up to 128 features): what it costs is a launch's time and the queries', so it is the shared tokens that count, 2048 and more: 8 rows behind 1024 17.7 / 17.3, 20.3 / 18.2,
+// behind 2048 18.0 / 21.2, 20.4 / 21.2; 16 behind 1024 19.1 / 19.3, 21.7 / 20.2, behind 4096 (240 MiB as 16 bits) 20.7 / 29.6, 23.1 / 29.8; 64 behind 1024 (252 MiB) 27.5 / 22.6, 27.2 / 23.8, behind 2048
+// 36.0 / 43.7, 36.7 / 43.8; where they save something: 16 of 8 heads to 1 behind 4096 (30 MiB) 18.9 / 17.3, behind 8192 (60) 19.1 / 21.0, 5 behind 2048 (32) 17.6 / 17.4; and the rows' own are few beside
+// them: 16 of 2000 behind 2048 31.8 / 28.7, behind 4096 33.2 / 33.8, 35.5 / 33.6, but 64 of 2000 behind 2048 (504 MiB) 56.6 / 59.2.  Others by bytes: 4 tokens a row, 16 rows behind 4096 (240 MiB) 39.1 /
+// 32.9, behind 8192 39.1 / 42.7; 8 tokens, 16 behind 4096 63.6 / 56.3, behind 8192 72 / 87; 20 tokens, 32 heads of 32, 16 behind 1024 (240 MiB) 59 / 57, 67 / 71, behind 2048 67 / 89; 256 features, 16 behind
+// 2048 (240 MiB) 52 / 41, behind 4096 57 / 55, 54 / 55.  Few-row kernel: 2 of 4 behind 512 13.6 / 13.6, behind 2048 14.4 / 15.5, 4 of 4 behind 4096 16.4 / 18.4.
 static bool worth_sharing(const fbq_attention_call &c, bool few, long row_queries)
 {
     const fbq_cache_desc &d = c.cache.desc;
     const long tokens = (long)c.n_shared * d.page_size, saved = 4L * tokens * d.kv_heads * d.head_dim * (c.cache.rows - 1);
     if (saved == 0 || row_queries > 64) return false;
-    if (in_4_bits(d.type) && (long)c.T * (c.heads / d.kv_heads) > kFewRows) return saved >= 256L << 20;
+    if (in_4_bits(d.type) && (long)c.T * (c.heads / d.kv_heads) > kFewRows) {
+        const long own = (long)c.cache.max_pages * d.page_size - tokens;      // room for a row's own
+        return saved >= 256L << 20 || (few && row_queries == c.heads / d.kv_heads && d.head_dim <= 128 && tokens >= 2048 && tokens >= 4 * own && saved >= 48L << 20);
+    }
     if (!few) return saved >= (row_queries > 32 ? 96L : 32L) << 20;
     return saved >= (few_direct((long)c.cache.rows * d.kv_heads, (long)c.cache.max_pages * d.page_size, in_4_bits(d.type)) ? 24L : 2L) << 20;
 }
