@@ -124,6 +124,7 @@ class DecoderStack:
             self.keep, self.evicted, self.most_skipped = ints([self.budget.keep] * rows), ints([0, 0]), ints([0])
             self.evict_ws = kv.cache_evict_workspace(cache, self.weights)
             self.added = torch.zeros_like(cache.lengths)        # the rows' lengths, 0 where a step has appended nothing: what `weights` counts
+            self.appended = torch.zeros_like(cache.lengths, dtype=torch.bool)
             self.added_to = kv.Cache(cache.pool, cache.table, self.added, cache.refs, cache.dtype, cache.dim)
 
     def _attend(self, li, b, stream):
@@ -165,8 +166,9 @@ class DecoderStack:
                 torch.minimum(self.lowest_start, self.start, out=self.lowest_start)
                 torch.maximum(self.most_lacking, self.lacking, out=self.most_lacking)
                 if self.budget is not None:             # (a last token held is no new one: its sums would begin anew, and a query that means nothing would count)
-                    torch.add(self.start, 1, out=self.added)
-                    torch.minimum(self.added, self.count, out=self.added).clamp_(0, 1).mul_(self.cache.lengths)
+                    torch.bitwise_and(self.start, 0x7fffffff, out=self.added)                    # (-1: beyond every length)
+                    torch.lt(self.added, self.cache.lengths, out=self.appended)
+                    torch.mul(self.cache.lengths, self.appended, out=self.added)
         for li in range(len(self.layers)):
             b = self.buf[li % len(self.buf)]
             if len(self.buf) > 1:
