@@ -427,9 +427,11 @@ fbq_status fbq_cache_compact(const fbq_cache *c, int32_t *table_out, int32_t *re
 /*
  * fbq_attention - for query token i of the n_b that row b has in this call, head h, with the row's L = lengths[b] tokens (the new ones among them, appended before):
  *     out = sum_j p_j v_j / sum_j p_j,   p_j = exp(scale q . k_j),   over the tokens j < L - n_b + i + 1     (causal; k, v of head h / (heads / kv_heads))
- * and lse = ln sum_j p_j.  A query token that sees nothing gets 0 and -infinity; what it does not see does not reach it, whatever lies there, last bits aside where a
- * cache in 4 bits is read for many queries (an infinity that it does see may make its result a NaN, where p_j rounds to 0).  Sums, maxima and exponentials are in fp32; p_j is rounded to the cache's type
+ * and lse = ln sum_j p_j.  A query token that sees nothing gets 0 and -infinity; what it does not see does not reach it, whatever lies there, last bits aside over a
+ * cache in 4 bits (an infinity that it does see may make its result a NaN, where p_j rounds to 0).  Sums, maxima and exponentials are in fp32; p_j is rounded to the cache's type
  * as an operand of the matrix cores, out once at the end.
+ * (Over a cache in 4 bits it is p_j times the value's scale that is rounded, to fp16, for up to 16 query tokens times heads of a key/value head; for more m + s c of keys and values are rounded as well, to
+ * fp16, or bf16 where a bf16 cache's numbers are out of fp16's range.)
  * The sum over j is divided at its end, and its p_j are up to 2^8 times what they are beside the largest: of bf16, values from about 2^120 / L on may take it beyond fp32.
  *   T query tokens in all; q_start device [rows + 1], ascending: row b's are q_start[b] .. q_start[b + 1] - 1; NULL: T == rows, one a row.  max_q: at least the most that a
  *            row has (1 with NULL; the result of a row with more is unspecified).  Tokens outside q_start[0] .. q_start[rows] - 1 are left alone

@@ -1,5 +1,5 @@
 // A batch behind a shared prefix in one launch, over a cache in 4 bits: as in fbq_attend_both.hip, the shared tokens against the rows of all sequences, the first blocks, and every row's own tokens.
-// 24 rows of 64 heads (8 of keys) behind 8192 shared tokens, about 300 of their own each: 31 and 13 us one after the other, 38 this way (32 with the arguments read again, see fbq_attend4_many.h).
+// 24 rows of 64 heads (8 of keys) behind 8192 shared tokens, about 300 of their own each: 31 and 13 us one after the other, 30 this way, the join of 9 besides.
 #include "fbq_attend4_few.h"
 #include "fbq_attend4_many.h"
 

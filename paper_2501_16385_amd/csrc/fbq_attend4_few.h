@@ -12,8 +12,8 @@
 //   scales   A key's scale is wanted in all 16 lanes that have its row of a product.  The matrix cores, which have time, put it there: the scale words as operand A, [key][group] with m and s as
 //            neighbours, times constants as operand B are s, m + 8 s, and, with the sums of q in three parts of 16 bits each, m sum(q) - in 32 bits, exactly but for the last addition.
 //            (Vector instructions instead, neighbours' words by quad_perm: 350 a step, 100 of them for this, and 5.2 TB/s where it is now 5.9.)
-// Bound by HBM in long rows: 16 rows of 16000 tokens, 32 heads of 128, 1.18 GB, 200 us (5.9 TB/s), 64 of 4096 with 64 heads to 8 62; in short ones by the time that begins and ends a piece, 9 us with one
-// step of 32 keys and nothing to join: 16 rows of about 1000 (74 MB) 24 us, one of 65537 with 8 heads (75 MB) 24.
+// Bound by HBM in long rows: 16 rows of 16000 tokens, 32 heads of 128, 1.18 GB, 200 us (5.9 TB/s), 64 of 4096 with 64 heads to 8 62; in short ones by the time that begins and ends a piece, 8.5 us with one
+// step of 32 keys and nothing to join: 16 rows of about 1000 (74 MB) 25 us, one of 65537 with 8 heads (75 MB) 25.
 // A value that a row does not see has weight zero there and finite scales, so nothing of it is added.  But rows share e, and what some of them see and others do not may take bits of the others' p s:
 // where such scales are more than 2^4 times what all see, the wave does its work again, slowly, with an e and x for each row by the scales that it sees.  (4 tokens of 32 heads to 8 behind
 // 4000, the last one's values 10^4 times the others': 22 us, else 16.)

@@ -1,6 +1,8 @@
 // Attention of many query rows over a cache in 4 bits: the kernel of fbq_attend_many.h with keys and values made on their way to LDS (fbq_attend_codes.h).
-// Measured, 32 heads of 128: prompt of 2048 tokens in fp16 66 to 71 us from card to card, in bf16 86 (of 16 bits 53), 8192 630 to 690 and 715 (540); heads of 64 47 and 410 (36, 330), of 80 57 and 515
-// (45, 425).  What making the operands takes is vector instructions, 160 a step of 64 keys beside the kernel's own 360.
+// Measured, 32 heads of 128: prompt of 2048 tokens in fp16 66 to 71 us from card to card, in bf16 81 to 86 (of 16 bits 53), 8192 630 to 690 and 715 (540); fp16 heads of 64 46 and 410 to 430 (36, 330), of 80
+// 55 and 515 to 535 (45, 425), of 192 130 for 2048 (108), of 256 160 and 2053 (113, 1426).  What making the operands takes is vector instructions, 160 a step of 64 keys beside the kernel's own 360; heads
+// of 128 and 256 have 36 to 724 bytes a lane of scratch memory for it, what other loads wait for.  bf16, a token in sixteen with values 2^-20 times the others': 146 and 1422 for 81 and 716, heads of 256
+// 652 and 8587 for 141 and 1782: every block does its work twice, the second time in bf16.
 #ifndef FBQ_ATTEND4_MANY_H
 #define FBQ_ATTEND4_MANY_H
 

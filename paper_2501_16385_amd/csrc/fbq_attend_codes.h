@@ -4,7 +4,7 @@
 // off what they stand for there - and 254 us instead of 208 for 1000 tokens each behind 5000 of three rows, heads of 80.)
 // The operands are fp16 also for a cache of bf16 - queries too, times a power of two a row - since that is eight times as exact and takes half the instructions: relative L2 against 64 bits
 // 1.7e-3 instead of 4.2e-3, of which rounding the result is 1.6e-3.  That wants scales from 2^-13 to 2^11 and lowest values up to 2^15 (or groups of zeros); a block that meets others does
-// its work again with operands of bf16.
+// its work again with operands of bf16, at about twice the time (fbq_attend4_many.h).
 // A step's codes are made in shares, among the matrix products of the step before.  Values are put down turned, [feature][64 keys], since that is how their codes lie: 16 bytes are eight
 // keys of a feature in the order that the probabilities have.
 #ifndef FBQ_ATTEND_CODES_H

@@ -12,8 +12,9 @@ namespace fbq {
 // word's tokens are not of this call the rest of the word is kept.  Nobody else writes the word: a partial page has one holder.
 // Of a block of 16's new tokens the first is the one that it is done for.  A grid block looks at WINDOW tokens for such ones: at one where rows have few, and its keys and values are then on their
 // way before it knows where they go; at 16 where they have many (16 times as many blocks that find nothing: 62 us for 4267 tokens of 32 heads, 33 this way).  At one a wave has the keys or the
-// values alone: 16 tokens of 32 heads 5.0 us for 6.6, a chain of loads, minima and quotients that no size shortens.  At 16, 70 MB read and 20 written: 2.7 TB/s, bound by the instructions that
-// make codes.
+// values alone: 16 tokens of 32 heads 5.0 us for 6.6, a chain of loads, minima and quotients that no size shortens.  At 16, 70 MB read and 20 written in
+// 28 to 33 us from card to card.  Counters: vector instructions, 1364 a wave of a block of 16, keep the units busy 55 % of that; the waves, 2.5 a SIMD, wait for loads 36 % of theirs and as long for each other's
+// instructions: loads, codes, LDS and stores of a block follow each other, and the few waves hide only a part.
 template <class NT, int NW, int WINDOW>
 __global__ __launch_bounds__(256) void fbq_append4_kernel(CacheArgs c, long layer_offset, int T, const int32_t *__restrict__ q_start, const int32_t *__restrict__ start,
                                                           const uint16_t *__restrict__ k, long k_stride, const uint16_t *__restrict__ v, long v_stride)
@@ -195,8 +196,8 @@ hipError_t launch_append4(const CacheArgs &c, int type, long layer_offset, int T
                                 : launch_append<NumberBf16>(c, layer_offset, T, q_start, start, k, k_stride, v, v_stride, stream);
 }
 
-// Read: a block a token.  Four features a thread and step; what is written is seven times what is read, and bounds it (4267
-// tokens of 32 heads of 128, 140 MB written and 20 read: 32 us, 5.0 TB/s; a large copy moves 4.9).
+// Read: a block a token.  Four features a thread and step; what is written is seven times what is read (16 bits: twice), and bounds it (4270 tokens of 32 heads of 128, 140 MB written and 20 read:
+// 29 to 31 us, 5.0 TB/s and more; a large copy moves 4.9.  Of 16 bits, 70 MB read: 34.  16 single tokens 5.2 and 4.3).
 template <class NT, bool FOUR>
 __global__ __launch_bounds__(256) void fbq_cache_read_kernel(CacheArgs c, long layer_offset, const int32_t *__restrict__ q_start, const int32_t *__restrict__ start, float *__restrict__ k,
                                                              float *__restrict__ v)

@@ -3,12 +3,13 @@
 // The softmax's sums are known (lse), so a key's weights are exp(scale q . k - lse) and nothing runs along the keys.  S^T = K Q^T in v_mfma 16x16x32 as in fbq_attend_few.h; the exponentials are
 // added up in the lane and over its 16 columns at the end.
 //   few   up to 16 query rows of a key/value head (fbq_weigh_few_kernel): bound by reading the keys, half of what attention reads.  The waves of the grid share the steps of all rows and heads
-//         as attention's do (FewLine), a step's keys asked for a step ahead; there is nothing to join, since a key's sum is a wave's own.  16 rows of about 1000 tokens, 32 heads of 128 in 16
-//         bits, 136 MB: 28 us.  (Written as attention's loop, two steps at a time, the same.)
+//         as attention's do (FewLine), a step's keys asked for a step ahead; there is nothing to join, since a key's sum is a wave's own.  us from card to card, 16 rows
+//         of about 1000 tokens, 32 heads of 128: 28 to 32 in 16 bits (136 MB), 18.4 in 4 (41 MB); 64 of 4096, 64 heads to 8 of the keys': 119 (555 MB), 45 (169 MB); one of 65537: 35, 19.  (Written as
+//         attention's loop, two steps at a time, the same.)
 //   many  (fbq_weigh_many_kernel) bound by vector instructions and matrix products one behind the other in two waves a SIMD.  A wave keeps 64 keys as operands and goes through the query rows 16
-//         at a time, which come through LDS.  One, two or all four of a block's waves have the same 64 keys, and share the query tiles; their sums are added up in LDS in a fixed order.
-//         us, two rows of 4000 tokens, 512 of them queries, 32 heads of 128 to 8 of the keys': 63 in 4 bits, 45 in 16 (queries from memory as operands: 75 and 68; all four waves with
-//         the same keys, too: 78 and 72); 16000 tokens: 207 in 4 bits (252, 274).
+//         at a time, which come through LDS.  One, two or all four of a block's waves have the same 64 keys, and share the query tiles; their sums are added up in LDS in a fixed order.  Two
+//         rows of 4000 tokens, 512 of them queries, 32 heads of 128 to 8 of the keys', us from card to card: 45 to 50 in 16 bits, 55 to 59 in 4 of bf16, 65 in 4 of fp16 (a card that took 63 for bf16
+//         and 45 for 16 bits: queries from memory as operands 75 and 68, all four waves with the same keys, too, 78 and 72).  16000 tokens: 181 to 184, 208 and 226; heads of 256, 4000 tokens: 104, 151, 156.
 // Codes of 4 bits: few, as in fbq_attend4_few.h; many, as small whole numbers of the queries' type, exactly, and scales come in behind the product, in 32 bits: the matrix cores spread them over
 // the lanes once for 64 keys, and make m sum(q) of the sums of q over a group in parts of 16 bits, three of them (what bf16 leaves is 2^-24 of a sum), so that weights are as exact as lse is.
 #include <algorithm>
