@@ -190,6 +190,7 @@ __device__ __forceinline__ bool attend4_few_wave(const AttendArgs &a, int block,
     int least, e, x_of;                                       // what every row of the piece sees; the exponent that p is relative to, and x (AGAIN: of the lane's row; else the same in all lanes)
     uint32_t most;                                            // the largest scale word that goes with them
     bool again = false;
+    int beside;                                               // what e goes with of the scales that all rows see
     auto begin = [&]() __attribute__((always_inline)) {
         q.of(cur.q, a.scale);
 #pragma unroll
@@ -205,6 +206,7 @@ __device__ __forceinline__ bool attend4_few_wave(const AttendArgs &a, int block,
         e = 0;
         x_of = 0;
         most = 0;
+        beside = 1 << 20;
         least = cur.t >= 0 ? cur.sees : cur.limit;
 #pragma unroll
         for (int x = 8; x; x >>= 1) least = min(least, __shfl_xor(least, x));
@@ -251,15 +253,17 @@ __device__ __forceinline__ bool attend4_few_wave(const AttendArgs &a, int block,
                 for (int w = 32; w; w >>= 1) largest = max(largest, (uint32_t)__shfl_xor((int)largest, w));
                 largest = uniform(largest);
             }
+            // (AGAIN: a row's maximum follows as it did the first time, or with the row's own exponent)
+            const bool follows = !AGAIN || !apart || largest > most || __ballot(top > m - (float)e + kSlack);
             if (largest > most) {
                 const int all = same(__builtin_amdgcn_frexp_expf(NT::of_upper(largest)) + 5);
                 if (!AGAIN && apart) {                        // beside the largest that all see (who sees any of the piece sees its first key)
-                    const int seen = max(least - key, 1);
+                    const int seen = max(least - key, key == cur.key0 ? 1 : 0);
                     uint32_t known = max(col < seen ? x.vs[0] : 0, 16 + col < seen ? x.vs[1] : 0);
 #pragma unroll 1
                     for (int w = 32; w; w >>= 1) known = max(known, (uint32_t)__shfl_xor((int)known, w));
-                    const int beside = max(known >> 16 ? __builtin_amdgcn_frexp_expf(NT::of_upper(known)) + 5 : -1000, most ? e + x_of : -1000);
-                    again |= uniform(all > beside + 4) != 0;
+                    beside = min(beside, uniform(max(known >> 16 ? __builtin_amdgcn_frexp_expf(NT::of_upper(known)) + 5 : -1000, most ? e + x_of : -1000)));
+                    again |= all > beside + 4;
                 }
                 e = all;
                 if (NT::kWide) {
@@ -271,7 +275,7 @@ __device__ __forceinline__ bool attend4_few_wave(const AttendArgs &a, int block,
                 const uint32_t beyond = NT::bits(ldexpf(1.0f, all - 3));                  // (an infinity: no scale is)
                 most = same((beyond << 16) - 1);
             }
-            const float to = fmaxf(top, m - (float)before) + (float)e, by = __builtin_amdgcn_exp2f(m - to);
+            const float to = follows ? fmaxf(top, m - (float)before) + (float)e : m, by = __builtin_amdgcn_exp2f(m - to);
             const float by_scaled = NT::kWide ? ldexpf(by, x_before - x_of) : by;
             l *= by;
 #pragma unroll

@@ -106,6 +106,26 @@ def test_large_values_that_some_tokens_see(D, dtype, size):
     large_among_new(5, 4, 4, D, dtype, size, 1)
 
 
+@pytest.mark.parametrize("dtype,size", [(F16, 1e4), (BF16, 1e4), (BF16, 1e36)])
+@pytest.mark.parametrize("rows,length,count,kv_heads", [(32, 33, 2, 32), (32, 66, 5, 32), (1, 8996, 6, 16), (1, 8995, 6, 16)])
+def test_large_values_in_a_step_of_their_own(rows, length, count, kv_heads, dtype, size):
+    """New tokens on both sides of a step's end, in waves that have both steps: an item each, or pieces of several steps."""
+    import paper_2501_16385_amd as fbq
+    D = 64
+    x, table, n, refs = make_cache([length] * rows, kv_heads, D, 16, dtype, seed=length)
+    q, counts = torch.randn(rows * count, kv_heads, D, generator=torch.Generator().manual_seed(7)).to(dtype), [count] * rows
+    last, results = table[:, (length - 1) // 16].long(), []
+    for times in (1.0, size):
+        y, most = x.clone(), torch.finfo(dtype).max
+        y[0, last, 1, :, (length - 1) % 16] = (y[0, last, 1, :, (length - 1) % 16].double() * times).clamp(-most, most).to(dtype)
+        pool = pack(y, 16)
+        results.append(fbq.attention(to_cache4(fbq, pool, table, n, refs, dtype, D), 0, q.cuda(), q_start=starts(counts).cuda(), max_q=count).cpu())
+        want, _, bound, _ = attention4_64(unpack(pool, dtype, D), table, n, 0, q, counts, D ** -0.5, True)
+        assert ((results[-1].double() - want).abs() <= bound).all()
+    one, other = (r.view(rows, count, kv_heads, D)[:, :-1] for r in results)
+    assert torch.equal(one, other)
+
+
 @pytest.mark.parametrize("counts,size", [([n, 1], size) for n in (1, 7) for size in (1e30, 5e36, 3e38, 1e-30)] + [([40, 20], size) for size in (1e30, 1e-30)])
 def test_weights(counts, size):
     """Sums of what attention gave each key; beyond 16 query rows a head up to 1e30, where the queries are numbers that the matrix cores take as they are."""
