@@ -254,7 +254,7 @@ __device__ __forceinline__ bool attend4_few_wave(const AttendArgs &a, int block,
                 largest = uniform(largest);
             }
             // (AGAIN: a row's maximum follows as it did the first time, or with the row's own exponent)
-            const bool follows = !AGAIN || !apart || largest > most || __ballot(top > m - (float)e + kSlack);
+            const bool passed = AGAIN && __ballot(top > m - (float)e + kSlack) != 0, follows = !AGAIN || !apart || passed || largest > most;
             if (largest > most) {
                 const int all = same(__builtin_amdgcn_frexp_expf(NT::of_upper(largest)) + 5);
                 if (!AGAIN && apart) {                        // beside the largest that all see (who sees any of the piece sees its first key)
