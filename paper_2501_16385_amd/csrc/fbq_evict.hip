@@ -361,8 +361,11 @@ extern "C" fbq_status fbq_cache_evict(const fbq_cache *c, const float *weights, 
     if (!weights || !weights_out || !keep || !workspace) return FBQ_ERR_NULL;
     if (!aligned(weights, 4) || !aligned(weights_out, 4) || !aligned(keep, 4) || !aligned(info, 4) || !aligned(workspace, 16)) return FBQ_ERR_ALIGN;
     if (workspace_bytes < fbq_cache_evict_workspace_bytes(c, width)) return FBQ_ERR_WORKSPACE;
-    const uintptr_t all = ((uintptr_t)(c->desc.layers - 1) * layer_stride + of_layer * width) * 4, a = (uintptr_t)weights, b = (uintptr_t)weights_out;
-    if (a != b && a < b + all && b < a + all) return FBQ_ERR_UNSUPPORTED;                 // (one over a part of the other)
+    const uintptr_t a_layer = (uintptr_t)of_layer * width * 4, apart = (uintptr_t)layer_stride * 4, all = (c->desc.layers - 1) * apart + a_layer, a = (uintptr_t)weights, b = (uintptr_t)weights_out;
+    if (a != b && a < b + all && b < a + all) {               // one over a part of the other, unless each one's layers lie between the other's (rows of the same tensor)
+        const uintptr_t on = (a < b ? b - a : a - b) % apart;
+        if (on < a_layer || apart - on < a_layer) return FBQ_ERR_UNSUPPORTED;
+    }
     EvictArgs e{};
     e.c = cache_args(*c);
     e.weights = weights; e.weights_out = weights_out; e.layer_stride = layer_stride; e.keep = keep; e.width = width; e.first = first; e.recent = recent;
