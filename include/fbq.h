@@ -462,7 +462,8 @@ fbq_status fbq_attention(const fbq_attention_call *a, void *workspace, size_t wo
 /*
  * fbq_attention_weights - how much each key was attended to, added up for every key/value head over the call's query tokens i and the heads h that share it:
  *     out[b][hk][j] = decay * weights[b][hk][j] + sum_i sum_h exp(scale q_ih . k_j - lse_ih),   j < lengths[b] and j < width, i over the tokens that see j
- * where the row's new tokens (the last n_b of lengths[b]) begin without the first term, whatever lies there.  Places from lengths[b] on are left alone, and so are rows without query tokens.  The sums are in fp32, over the query
+ * where the row's new tokens (the last n_b of lengths[b]) begin without the first term, whatever lies there (a row that got no pages
+ * for its new tokens has none: with its own length its last ones would count as new; a cache whose lengths are 0 for such rows leaves them alone).  Places from lengths[b] on are left alone, and so are rows without query tokens.  The sums are in fp32, over the query
  * tokens in an order that the sizes alone decide.
  *   a        the call of fbq_attention that it follows: its cache, layer, heads, T, max_q, q_start, q, q_stride, scale, and lse as that wrote it (not NULL; a token that sees nothing
  *            counts nowhere); out and shared are not used

@@ -327,6 +327,7 @@ def attention_weights(cache: Cache, layer: int, q, lse, weights, q_start=None, m
 
     weights: float32 [rows, kv_heads, width], what earlier calls added up (times decay; the row's new tokens begin at 0), or None; out: the same shape, weights itself by default.
     Tokens from width on are not counted; places without a token, and rows without queries, are left alone.
+    A row that cache_reserve left out has no new tokens: it wants a Cache with a length of 0 for it here (decode_loop.py makes one), or the last ones that it holds count as new.
     """
     if out is None:
         out = weights
