@@ -126,6 +126,34 @@ def test_large_values_in_a_step_of_their_own(rows, length, count, kv_heads, dtyp
     assert torch.equal(one, other)
 
 
+@pytest.mark.parametrize("dtype,size", [(F16, 1e4), (BF16, 1e4), (BF16, 1e36)])
+@pytest.mark.parametrize("D,kv_heads", [(64, 8), (96, 6), (128, 4)])
+def test_large_values_behind_shared_tokens(D, kv_heads, dtype, size):
+    """The rows' own tokens in one launch with the shared ones, which 80 query rows a head read apart."""
+    import paper_2501_16385_amd as fbq
+    rows, shared, count, own = 20, 8192, 2, 40
+    assert 4 * shared * kv_heads * D * (rows - 1) >= 256 << 20
+    lengths, counts = [shared + own + b for b in range(rows)], [count] * rows
+    x, table, n, refs = make_cache(lengths, kv_heads, D, 64, dtype, shared_pages=shared // 64, seed=D)
+    q = torch.randn(rows * count, 2 * kv_heads, D, generator=torch.Generator().manual_seed(7)).to(dtype)
+    results = []
+    for times in (1.0, size):
+        y, most = x.clone(), torch.finfo(dtype).max
+        for b, length in enumerate(lengths):
+            at = (0, int(table[b, (length - 1) // 64]), 1, slice(None), (length - 1) % 64)
+            y[at] = (y[at].double() * times).clamp(-most, most).to(dtype)
+        pool = pack(y, 64)
+        cache = to_cache4(fbq, pool, table, n, refs, dtype, D)
+        results.append(fbq.attention(cache, 0, q.cuda(), q_start=starts(counts).cuda(), max_q=count, shared=table[0, :shared // 64].contiguous().cuda()).cpu())
+    # The result is sum p v over the shared tokens, rounded as many rows' are, and over the rows' own, rounded as few rows' are, in one quotient.  With o = o' + o'' each part is off by no more than its form's
+    # bound over all tokens, of which its own are a part: by both in all.  (Of the own ones that is a part of the largest value, also in features where the token that has it holds little: few rows round p s.)
+    values = unpack(pool, dtype, D)
+    (want, _, many, _), (_, _, few, _) = (attention4_64(values, table, n, 0, q, counts, D ** -0.5, which) for which in (False, True))
+    assert ((results[-1].double() - want).abs() <= many + few).all()
+    one, other = (r.view(rows, count, -1, D)[:, 0] for r in results)
+    assert torch.equal(one, other)
+
+
 @pytest.mark.parametrize("counts,size", [([n, 1], size) for n in (1, 7) for size in (1e30, 5e36, 3e38, 1e-30)] + [([40, 20], size) for size in (1e30, 1e-30)])
 def test_weights(counts, size):
     """Sums of what attention gave each key; beyond 16 query rows a head up to 1e30, where the queries are numbers that the matrix cores take as they are."""
